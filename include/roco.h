@@ -290,6 +290,112 @@ int roco_decode_step_gqa(const roco_params* params, int32_t group,
                          void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Speculative decoding on budgeted caches: a small model drafts several continuations of every request at once, a tree of
+ * tokens; one pass of the large model scores all of them (roco_tree_attend in every layer, the cache is not changed), and the
+ * longest path that it agrees with is taken over (roco_tree_commit).  A drafted chain is a tree too, and so is a single token.
+ *
+ * units = requests x heads with unit r * heads + h (heads: key/value heads, or layers x key/value heads), `group` query heads per
+ * unit; trees, paths and pages belong to requests.  A tree has `nodes` rows, of which the first n_nodes[r] exist; parent[r][i] < i
+ * is the node that node i continues, -1 (or anything that is not an earlier node) the last token of the cache.  Node i sees every
+ * cached token of its unit, the nodes above it and itself; its position is qpos0[u] + the number of nodes above it.
+ *
+ * Pages: requests of different budgets (section 5.1.5: B = prompt length x compression rate) in one call.  With `pages` NULL a cache
+ * is [units, B, d] as everywhere else.  Otherwise K_cache and V_cache are pools [n_pages, heads, page, d], slot j of the units of
+ * request r is row j % page of page table[r][j / page], and budget[r] slots are the request's (params->budget is the largest: the
+ * row length of stats and pos, which stay [units, 3, B] and [units, B]).  The scope of a request of fewer slots than params->scope is
+ * all of them.  Entries behind the pages that the slots in use need are not read.  What lies in a page outside [0, n_pages) is
+ * neither read nor written: such slots are not seen.
+ */
+typedef struct roco_pages {
+  const int32_t* table;   /* device [requests, max_pages]                                            */
+  const int32_t* budget;  /* device [requests], each 1 .. params->budget; NULL: params->budget for all */
+  int32_t max_pages;      /* max_pages * page >= params->budget                                      */
+  int32_t page;           /* slots per page: a power of two, 16 .. 1024                               */
+  int32_t n_pages;        /* pages of the pool; n_pages * heads * page < 2^31                        */
+} roco_pages;
+
+/* Bytes of scratch of the two calls for these shapes (0 on invalid ones): 1 <= nodes <= 64, 1 <= group <= 64. */
+size_t roco_tree_workspace_bytes(const roco_params* params, int32_t group, int32_t nodes);
+
+/*
+ * Attention of drafted trees (a matrix product over the cache for all nodes and heads at once: K and V are read once):
+ *   p_ih = softmax over the unit's n_used slots and the nodes that node i sees of scale q_ih . k + bias
+ *   out_ih = sum p_ih v,   lse_ih = ln of the sum of exponentials (roco_tree_commit wants it)
+ * Values of nodes that a row does not see do not reach it, infinite and NaN ones neither.
+ *
+ * q            in  [units, nodes, group, d] dtype
+ * k_new, v_new in  [units, nodes, d]        dtype
+ * parent       in  [requests, nodes] int32, or NULL: a chain (node i continues node i - 1)
+ * n_nodes      in  [requests] int32, 0 .. nodes, or NULL: nodes.  Rows of out and lse behind a tree's last node are left as they were.
+ * qpos0        in  [units]           int32 position of a node without a parent
+ * K_cache, V_cache, pos, n_used      in, as in roco_decode_step (pos is read where params->recency_window is in force)
+ * out          out [units, nodes, group, d] dtype
+ * lse          out [units, nodes, group]    fp32, or NULL
+ * params: scope, importance, scope_kind and sinks have no meaning here but have to be valid.
+ * Refused: units not a multiple of heads, nodes or heads or group < 1, a page size that is none (ROCO_EINVAL); nodes or group above 64
+ * (ROCO_EUNSUPPORTED).
+ */
+int roco_tree_attend(const roco_params* params, int32_t heads, int32_t group, int32_t nodes, const roco_pages* pages,
+                     const void* q, const void* k_new, const void* v_new, const int32_t* parent, const int32_t* n_nodes,
+                     const int32_t* qpos0, const void* K_cache, const void* V_cache, const int32_t* pos, const int32_t* n_used,
+                     void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Takes over the accepted path of every request: nodes path[r][0 .. a-1] in order, a = n_path[r] (0: nothing of the request's units
+ * changes), each the parent of the next.  Per unit with n = n_used slots and the request's budget B_r:
+ *   E = max(0, n + a - B_r) tokens are evicted by the statistics as they stand, as in roco_encode_block (the drafted tokens have still
+ *   seen them); the accepted tokens go, in order, to the ascending list of freed and still-empty slots, at positions qpos0 + k.
+ *   pbar_k = mean over the group's heads of exp(scale q_kh . K[j] + bias - lse_kh), the probabilities of roco_tree_attend, over the
+ *   remaining older slots and the accepted tokens 0 .. k: Acc += sum_k pbar_k, Acc2 += sum_k pbar_k^2, Count += 1 for every row that
+ *   attended the slot; accepted tokens start from 0.  (The other importance scores keep their second plane as they do elsewhere.)
+ * The same rows one after the other through roco_encode_block_gqa give the same statistics where nothing is evicted.
+ * next_slot is not kept: before a roco_decode_step, roco_select_victims has to refresh it.
+ *
+ * q, k_new, v_new, qpos0, heads, group, nodes, pages   as in roco_tree_attend
+ * lse          in  [units, nodes, group] fp32 of roco_tree_attend
+ * max_path         row length of path, 1 .. nodes
+ * path         in  [requests, max_path] int32; entries from n_path[r] on are not read
+ * n_path       in  [requests] int32, 0 .. min(max_path, B_r)
+ * K_cache, V_cache, stats, pos, n_used   in/out
+ * evicted_slot, evicted_pos  out [units, max_path] int32: the slot that token k took over from an evicted token and that token's
+ *              position, or -1 (either may be NULL)
+ */
+int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, int32_t nodes, const roco_pages* pages,
+                     const void* q, const void* k_new, const void* v_new, const float* lse, int32_t max_path, const int32_t* path,
+                     const int32_t* n_path, const int32_t* qpos0, void* K_cache, void* V_cache, float* stats, int32_t* pos,
+                     int32_t* n_used, int32_t* evicted_slot, int32_t* evicted_pos, void* workspace, size_t workspace_bytes,
+                     void* hip_stream);
+
+/*
+ * Block tables and slot maps from the requests' lengths, on the device: request r, which holds held[r] slots, is to have want[r].
+ * It takes the pages that it lacks, ceil(want / page) - ceil(held / page), from the list of free ones, the requests in order:
+ *   page_start[r]  = pages taken by the requests before r; page_start[requests] = all
+ *   row_start[r]   = new slots of the requests before r; row_start[requests] = all
+ *   table[r][i]    = free_pages[page_start[r] + i - ceil(held[r] / page)] for the new i; other entries are left as they were
+ *   slot map       : slot j of a request is pool slot table[r][j / page] * page + j % page.  packed (padded 0): map [rows], entry
+ *                    row_start[r] + i is the i-th new slot of request r; padded (1): map [requests, rows], entry r, i.  Entries without a
+ *                    slot are -1.
+ * Where the list is too short (page_start[requests] > n_free), the pages that it lacks are -1, in the table and in the map.
+ * held may be NULL (new requests); held is held inside [0, max_pages * page], want inside [held, max_pages * page].  The sums have
+ * 32 bits.  No workspace.
+ * page: a power of two, 16 .. 1024; n_free >= 0 (free_pages may be NULL with 0); 1 <= requests <= 65535; rows >= 1.
+ */
+int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const int32_t* held, const int32_t* want,
+                     const int32_t* free_pages, int32_t n_free, int32_t* table, int32_t* page_start, int32_t* row_start,
+                     int32_t* slot_map, int32_t rows, int32_t padded, void* hip_stream);
+
+/*
+ * Rows of K and V to their pool slots: the keys and values of new tokens straight from a projection, or compressed caches
+ * [units, B, d] into pages.  Entry (g, i) of the map [groups, rows] names the pool slot of row (g, i) of every head h, which lies
+ * group_stride g + row_stride i + head_stride h elements behind K_rows (V_rows); -1 (anything negative, or a page that the pool does
+ * not have): the row is not stored.  Two rows of the same slot: either.
+ * Pools [n_pages, heads, page, d], disjoint from the rows.  Strides are multiples of 16 bytes and not negative; n_pages * heads * page < 2^31.
+ */
+int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t groups, int32_t rows, const void* K_rows,
+                    const void* V_rows, int64_t group_stride, int64_t row_stride, int64_t head_stride, const int32_t* slot_map,
+                    void* K_pool, void* V_pool, int32_t n_pages, int32_t page, void* hip_stream);
+
+/*
  * Victim selection alone (section 4.3): for every full unit, next_slot[u] = the slot of lowest Acc/Count among
  * the s slots of lowest variance (or what params' policy ranks by); -1 for units that are not full.  Only needed
  * after the caller has edited stats / n_used itself.  stats in [units,3,B], pos in [units,B] (read only by
@@ -338,7 +444,9 @@ enum {
   ROCO_PROF_DECODE_SELECT = 0, ROCO_PROF_DECODE_ATTEND = 1, ROCO_PROF_DECODE_FINISH = 2,
   ROCO_PROF_PREFILL_ROWS = 3, ROCO_PROF_PREFILL_COLUMNS = 4, ROCO_PROF_PREFILL_SELECT = 5,
   ROCO_PROF_PREFILL_GATHER = 6, ROCO_PROF_READ_PROBE = 7, ROCO_PROF_BLOCK_PREPARE = 8,
-  ROCO_PROF_BLOCK_ATTEND = 9, ROCO_PROF_BLOCK_FINISH = 10, ROCO_PROF_MFMA_PROBE = 11, ROCO_PROF_KERNELS = 12
+  ROCO_PROF_BLOCK_ATTEND = 9, ROCO_PROF_BLOCK_FINISH = 10, ROCO_PROF_MFMA_PROBE = 11, ROCO_PROF_TREE_ATTEND = 12,
+  ROCO_PROF_TREE_JOIN = 13, ROCO_PROF_TREE_TAKE = 14, ROCO_PROF_TREE_STATISTICS = 15, ROCO_PROF_PAGE_TABLES = 16,
+  ROCO_PROF_PAGE_STORE = 17, ROCO_PROF_KERNELS = 18
 };
 int roco_profile_kernel(int which);
 int roco_profile_read(double* total_ms, int64_t* launches);

@@ -59,6 +59,25 @@ class RocoParams(ctypes.Structure):
                          int(recency_window), float(recency_bias), int(importance), int(scope_kind), int(sinks))
 
 
+class RocoPages(ctypes.Structure):
+    """Mirror of `roco_pages` (include/roco.h).  `table` [requests, max_pages] and `budget` [requests] or None are int32 device tensors
+    (or plain addresses, with `max_pages` given) and are kept alive with the structure."""
+
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("budget", ctypes.c_void_p),
+        ("max_pages", ctypes.c_int32),
+        ("page", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+    ]
+
+    def __init__(self, table, n_pages, page, budget=None, max_pages=None):
+        if max_pages is None:
+            max_pages = table.shape[-1]
+        super().__init__(_ptr(table), _ptr(budget), int(max_pages), int(page), int(n_pages))
+        self._held = (table, budget)
+
+
 def library_path() -> str:
     return os.path.join(_HERE, _LIB_NAME)
 
@@ -105,6 +124,17 @@ def load_library() -> ctypes.CDLL:
     lib.roco_encode_block_gqa.argtypes = [pp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.roco_decode_step_gqa.restype = ctypes.c_int
     lib.roco_decode_step_gqa.argtypes = [pp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    pg, i64 = ctypes.POINTER(RocoPages), ctypes.c_int64
+    lib.roco_tree_workspace_bytes.restype = sz
+    lib.roco_tree_workspace_bytes.argtypes = [pp, i32, i32]
+    lib.roco_tree_attend.restype = ctypes.c_int
+    lib.roco_tree_attend.argtypes = [pp, i32, i32, i32, pg, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.roco_tree_commit.restype = ctypes.c_int
+    lib.roco_tree_commit.argtypes = [pp, i32, i32, i32, pg, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.roco_page_tables.restype = ctypes.c_int
+    lib.roco_page_tables.argtypes = [i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp]
+    lib.roco_page_store.restype = ctypes.c_int
+    lib.roco_page_store.argtypes = [i32, i32, i32, i32, i32, vp, vp, i64, i64, i64, vp, vp, vp, i32, i32, vp]
     lib.roco_select_victims.restype = ctypes.c_int
     lib.roco_select_victims.argtypes = [pp, vp, vp, vp, vp, vp, sz, vp]
     lib.roco_select_retained.restype = ctypes.c_int
@@ -130,22 +160,42 @@ class _PlainCalls:
 
     # which of a function's arguments behind the parameters are integers; the others are tensors or addresses
     INTEGERS = {"prefill_compress": (4,), "prefill_compress_gqa": (0, 5), "prefill_compress_lse": (0, 5), "decode_step": (),
-                "decode_step_static": (), "encode_block": (0,), "encode_block_gqa": (0, 1), "decode_step_gqa": (0,)}
+                "decode_step_static": (), "encode_block": (0,), "encode_block_gqa": (0, 1), "decode_step_gqa": (0,),
+                "tree_attend": (0, 1, 2), "tree_commit": (0, 1, 2, 8)}
+    PAGES = {"tree_attend": 3, "tree_commit": 3}  # ... or a RocoPages
+    # the functions without parameters
+    PLAIN = {"page_tables": (0, 1, 2, 6, 11, 12), "page_store": (0, 1, 2, 3, 4, 7, 8, 9, 13, 14)}
 
     def __init__(self, lib):
         for name, integers in self.INTEGERS.items():
-            setattr(self, name, self._function(getattr(lib, "roco_" + name), integers, name != "decode_step_static"))
+            setattr(self, name, self._function(getattr(lib, "roco_" + name), integers, name != "decode_step_static", self.PAGES.get(name)))
+        for name, integers in self.PLAIN.items():
+            setattr(self, name, self._plain(getattr(lib, "roco_" + name), integers))
 
     @staticmethod
-    def _function(fn, integers, has_workspace):
+    def _function(fn, integers, has_workspace, pages):
         def call(params, *args):
             *args, stream = args
             size = ()
             if has_workspace:
                 *args, workspace_bytes = args
                 size = (int(args[-1].nbytes if workspace_bytes is None else workspace_bytes),)
-            return fn(ctypes.byref(params), *[int(a) if i in integers else _ptr(a) for i, a in enumerate(args)], *size, _stream(stream))
+            if pages is not None and args[pages] is not None and not isinstance(args[pages], RocoPages):
+                raise TypeError("roco: pages must be a RocoPages or None")
+            return fn(ctypes.byref(params), *[int(a) if i in integers else _pages(a) if i == pages else _ptr(a) for i, a in enumerate(args)],
+                      *size, _stream(stream))
         return call
+
+    @staticmethod
+    def _plain(fn, integers):
+        def call(*args):
+            *args, stream = args
+            return fn(*[int(a) if i in integers else _ptr(a) for i, a in enumerate(args)], _stream(stream))
+        return call
+
+
+def _pages(pages):
+    return None if pages is None else ctypes.byref(pages)
 
 
 def _bind_native(lib) -> None:
@@ -160,8 +210,9 @@ def _bind_native(lib) -> None:
     address = lambda fn: ctypes.cast(fn, ctypes.c_void_p).value
     native.bind(tuple(address(getattr(lib, name)) for name in (
         "roco_prefill_compress", "roco_prefill_compress_gqa", "roco_prefill_compress_lse", "roco_decode_step",
-        "roco_decode_step_static", "roco_encode_block", "roco_encode_block_gqa", "roco_decode_step_gqa")),
-        torch.Tensor, torch.nn.Parameter, RocoParams, _ptr, _stream)
+        "roco_decode_step_static", "roco_encode_block", "roco_encode_block_gqa", "roco_decode_step_gqa", "roco_tree_attend",
+        "roco_tree_commit", "roco_page_tables", "roco_page_store")),
+        torch.Tensor, torch.nn.Parameter, RocoParams, RocoPages, _ptr, _stream)
     if _native is None and hasattr(os, "register_at_fork"):
         os.register_at_fork(after_in_child=native.forget_gpu)  # a forked child is refused by torch, as before
     _native, _marshal, _native_lib = native, native, lib
@@ -192,7 +243,8 @@ def decode_workspace_bytes(params: RocoParams) -> int:
 
 PROF_KERNELS = {"decode_select": 0, "decode_attend": 1, "decode_finish": 2, "prefill_rows": 3,
                 "prefill_columns": 4, "prefill_select": 5, "prefill_gather": 6, "read_probe": 7,
-                "block_prepare": 8, "block_attend": 9, "block_finish": 10, "mfma_probe": 11}
+                "block_prepare": 8, "block_attend": 9, "block_finish": 10, "mfma_probe": 11, "tree_attend": 12, "tree_join": 13,
+                "tree_take": 14, "tree_statistics": 15, "page_tables": 16, "page_store": 17}
 
 
 def roco_profile_kernel(which: int) -> None:
@@ -337,6 +389,77 @@ def roco_decode_step_gqa(params: RocoParams, group: int, q, k_new, v_new, qpos, 
         raise RocoError(rc, "roco_decode_step_gqa")
 
 
+def tree_workspace_bytes(params: RocoParams, group: int, nodes: int) -> int:
+    return int(load_library().roco_tree_workspace_bytes(ctypes.byref(params), int(group), int(nodes)))
+
+
+def roco_tree_attend(params: RocoParams, heads: int, group: int, nodes: int, pages: Optional[RocoPages], q, k_new, v_new, parent, n_nodes,
+                     qpos0, K_cache, V_cache, pos, n_used, out, lse, workspace, workspace_bytes: Optional[int] = None, stream=None) -> None:
+    """See include/roco.h: attention of drafted trees over the budgeted cache, which is not changed.  `pages`, `parent`, `n_nodes` and
+    `lse` may be None."""
+    rc = _calls().tree_attend(params, heads, group, nodes, pages, q, k_new, v_new, parent, n_nodes, qpos0, K_cache, V_cache, pos, n_used,
+                              out, lse, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise RocoError(rc, "roco_tree_attend")
+
+
+def roco_tree_commit(params: RocoParams, heads: int, group: int, nodes: int, pages: Optional[RocoPages], q, k_new, v_new, lse, max_path: int,
+                     path, n_path, qpos0, K_cache, V_cache, stats, pos, n_used, evicted_slot, evicted_pos, workspace,
+                     workspace_bytes: Optional[int] = None, stream=None) -> None:
+    """See include/roco.h: takes over the accepted paths of drafted trees.  `pages`, `evicted_slot` and `evicted_pos` may be None."""
+    rc = _calls().tree_commit(params, heads, group, nodes, pages, q, k_new, v_new, lse, max_path, path, n_path, qpos0, K_cache, V_cache,
+                              stats, pos, n_used, evicted_slot, evicted_pos, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise RocoError(rc, "roco_tree_commit")
+
+
+def roco_page_tables(held, want, page: int, free_pages, table, page_start, row_start, slot_map, stream=None) -> None:
+    """See include/roco.h: block tables and slot maps from the requests' lengths.  `table` [requests, max_pages]; a `slot_map` of two
+    dimensions, [requests, rows], is a padded one; `held` may be None."""
+    requests, max_pages = table.shape
+    for t, n in ((held, requests), (want, requests), (page_start, requests + 1), (row_start, requests + 1)):
+        if t is not None and t.numel() != n:
+            raise ValueError("roco: held and want are [requests], page_start and row_start [requests + 1]")
+    padded = slot_map.dim() == 2
+    if padded and slot_map.shape[0] != requests:
+        raise ValueError("roco: a padded slot_map is [requests, rows]")
+    rc = _calls().page_tables(requests, page, max_pages, held, want, free_pages, free_pages.numel(), table, page_start, row_start, slot_map,
+                              slot_map.shape[-1], padded, stream)
+    if rc != 0:
+        raise RocoError(rc, "roco_page_tables")
+
+
+def roco_page_store(K_rows, V_rows, slot_map, K_pool, V_pool, stream=None) -> None:
+    """See include/roco.h: rows of K and V to their pool slots.  Rows [rows, heads, d] (of new tokens, with a map [rows]) or
+    [groups, heads, rows, d] (caches, with a map [groups, rows]) of any strides but the last dimension's; pools [n_pages, heads, page, d]."""
+    n_pages, heads, page, d = K_pool.shape
+    if K_rows.dim() == 3:
+        rows, groups = K_rows.shape[0], 1
+        row_stride, head_stride, last = K_rows.stride()
+        group_stride = 0
+        shape = (rows, heads, d)
+    else:
+        groups, _, rows, _ = K_rows.shape
+        group_stride, head_stride, row_stride, last = K_rows.stride()
+        shape = (groups, heads, rows, d)
+    if tuple(K_rows.shape) != shape or V_rows.shape != K_rows.shape or V_pool.shape != K_pool.shape or slot_map.numel() != groups * rows:
+        raise ValueError("roco: rows are [rows, heads, d] or [groups, heads, rows, d], the map has an entry for each, pools are [n_pages, heads, page, d]")
+    if last != 1 or V_rows.stride() != K_rows.stride():
+        raise ValueError("roco: a row's elements lie side by side, and the rows of V as those of K")
+    if not K_rows.dtype == V_rows.dtype == K_pool.dtype == V_pool.dtype:
+        raise ValueError("roco: rows and pools are of one type")
+    dtype = _dtype_code(K_pool.dtype)
+    rc = _calls().page_store(dtype, d, heads, groups, rows, K_rows.data_ptr(), V_rows.data_ptr(), group_stride, row_stride, head_stride,
+                             slot_map, K_pool, V_pool, n_pages, page, stream)
+    if rc != 0:
+        raise RocoError(rc, "roco_page_store")
+
+
+def _dtype_code(dtype) -> int:
+    import torch
+    return ROCO_BF16 if dtype == torch.bfloat16 else ROCO_F32 if dtype == torch.float32 else -1
+
+
 def roco_probe_cache_read(params: RocoParams, K_cache, V_cache, workspace, workspace_bytes: Optional[int] = None,
                           stream=None) -> None:
     """See include/roco.h: the loads of the decode attention kernel, and nothing else (benchmark aid)."""
@@ -396,7 +519,7 @@ def roco_select_retained(params: RocoParams, keep: int, stats, pos, n_used, mask
 class RocoCache:
     """Caller-owned device buffers of the budgeted cache (plain torch tensors, nothing else)."""
 
-    K: "object"  # [units, B, d]
+    K: "object"  # [units, B, d], or a pool [n_pages, heads, page, d]
     V: "object"
     stats: "object"  # [units, 3, B] fp32: Acc, Acc2, Count
     pos: "object"  # [units, B] int32
@@ -405,12 +528,21 @@ class RocoCache:
 
 
 def alloc_cache(params: RocoParams, device="cuda") -> RocoCache:
+    return _alloc(params, (params.units, params.budget, params.head_dim), device)
+
+
+def alloc_paged_cache(params: RocoParams, heads: int, n_pages: int, page: int, device="cuda") -> RocoCache:
+    """A cache whose K and V are pools of pages, [n_pages, heads, page, d] (see roco_pages in include/roco.h)."""
+    return _alloc(params, (int(n_pages), int(heads), int(page), params.head_dim), device)
+
+
+def _alloc(params, rows, device):
     import torch
     dt = torch.bfloat16 if params.dtype == ROCO_BF16 else torch.float32
-    U, B, d = params.units, params.budget, params.head_dim
+    U, B = params.units, params.budget
     return RocoCache(
-        torch.zeros((U, B, d), dtype=dt, device=device),
-        torch.zeros((U, B, d), dtype=dt, device=device),
+        torch.zeros(rows, dtype=dt, device=device),
+        torch.zeros(rows, dtype=dt, device=device),
         torch.zeros((U, 3, B), dtype=torch.float32, device=device),
         torch.full((U, B), -1, dtype=torch.int32, device=device),
         torch.zeros((U,), dtype=torch.int32, device=device),

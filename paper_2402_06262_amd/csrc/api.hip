@@ -102,6 +102,43 @@ int check_block(const roco_params* p, int32_t block) {
   return ROCO_OK;
 }
 
+// ---- drafted trees: heads, groups, nodes and pages; the paged rows are counted in 31 bits
+bool page_size_ok(int32_t page) { return page >= 16 && page <= 1024 && (page & (page - 1)) == 0; }
+int check_pages(int32_t n_pages, int32_t heads, int32_t page) {
+  if (n_pages < 1 || !page_size_ok(page)) return ROCO_EINVAL;
+  return static_cast<long long>(n_pages) * heads * page < (1ll << 31) ? ROCO_OK : ROCO_EUNSUPPORTED;
+}
+int check_tree(const roco_params* p, int32_t heads, int32_t group, int32_t nodes, const roco_pages* pages, CachePages& out) {
+  const int rc = check_params(p);
+  if (rc != ROCO_OK) return rc;
+  if (heads < 1 || group < 1 || nodes < 1 || p->units % heads != 0) return ROCO_EINVAL;
+  if (group > kMaxTreeGroup || nodes > kMaxTreeNodes) return ROCO_EUNSUPPORTED;
+  out = CachePages{nullptr, nullptr, 0, 0, 0};
+  if (pages == nullptr) return static_cast<long long>(p->units) * p->budget < (1ll << 32) ? ROCO_OK : ROCO_EUNSUPPORTED;
+  if (pages->table == nullptr || !aligned16(pages->table) || (pages->budget != nullptr && !aligned16(pages->budget))) return ROCO_EINVAL;
+  const int rc2 = check_pages(pages->n_pages, heads, pages->page);
+  if (rc2 != ROCO_OK) return rc2;
+  if (pages->max_pages < 1 || static_cast<long long>(pages->max_pages) * pages->page < p->budget) return ROCO_EINVAL;
+  out = CachePages{pages->table, pages->budget, pages->max_pages, __builtin_ctz(static_cast<unsigned>(pages->page)), pages->n_pages};
+  return ROCO_OK;
+}
+
+// ---- workspace of the trees: tree_attend's part_m | part_l | part_o, or tree_commit's taken | keys
+struct TreeLayout { size_t part_l, part_o, keys, total; int splits; };
+TreeLayout tree_layout(const roco_params* p, int32_t group, int32_t nodes) {
+  TreeLayout l;
+  const size_t U = p->units, B = p->budget, rows = static_cast<size_t>(group) * nodes;
+  l.splits = tree_attend_splits(p->units, group * nodes, p->budget);
+  const size_t plane = l.splits == 1 ? 0 : align_up(U * l.splits * rows * sizeof(float));
+  l.part_l = plane;
+  l.part_o = 2 * plane;
+  const size_t attend = 2 * plane + plane * p->head_dim;
+  l.keys = align_up(U * kTakenWords * sizeof(int32_t));
+  const size_t commit = l.keys + (p->budget > kMaxDecodeBudgetLds ? align_up(U * 2 * B * sizeof(uint32_t)) : 0);
+  l.total = std::max(attend, commit);
+  return l;
+}
+
 int env_int(const char* name, int dflt) {
   const char* v = getenv(name);
   return (v && *v) ? atoi(v) : dflt;
@@ -468,6 +505,108 @@ int roco_decode_step_gqa(const roco_params* params, int32_t group, const void* q
                          int32_t* evicted_pos, void* workspace, size_t workspace_bytes, void* hip_stream) {
   return run_block(params, 1, group, q, k_new, v_new, qpos, K_cache, V_cache, stats, pos, n_used, next_slot, out,
                    evicted_slot, evicted_pos, workspace, workspace_bytes, hip_stream);
+}
+
+size_t roco_tree_workspace_bytes(const roco_params* params, int32_t group, int32_t nodes) {
+  CachePages pages;
+  if (check_tree(params, 1, group, nodes, nullptr, pages) != ROCO_OK) return 0;
+  return tree_layout(params, group, nodes).total;
+}
+
+int roco_tree_attend(const roco_params* params, int32_t heads, int32_t group, int32_t nodes, const roco_pages* pages, const void* q,
+                     const void* k_new, const void* v_new, const int32_t* parent, const int32_t* n_nodes, const int32_t* qpos0,
+                     const void* K_cache, const void* V_cache, const int32_t* pos, const int32_t* n_used, void* out, float* lse,
+                     void* workspace, size_t workspace_bytes, void* hip_stream) {
+  TreeArgs a;
+  const int rc = check_tree(params, heads, group, nodes, pages, a.pages);
+  if (rc != ROCO_OK) return rc;
+  const void* need[] = {q, k_new, v_new, qpos0, K_cache, V_cache, pos, n_used, out, workspace};
+  for (const void* ptr : need)
+    if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
+  for (const void* ptr : {static_cast<const void*>(parent), static_cast<const void*>(n_nodes), static_cast<const void*>(lse)})
+    if (ptr != nullptr && !aligned16(ptr)) return ROCO_EINVAL;
+  const TreeLayout lay = tree_layout(params, group, nodes);
+  if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
+  a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
+  a.splits = lay.splits;
+  a.row_tiles = tree_attend_row_tiles(group * nodes);
+  a.scale_log2 = scale_log2(params);
+  a.recency_window = params->recency_window;
+  a.recency_bias_log2 = params->recency_bias * 1.4426950408889634f;
+  a.q = q; a.k_new = k_new; a.v_new = v_new; a.parent = parent; a.n_nodes = n_nodes; a.qpos0 = qpos0;
+  a.K = K_cache; a.V = V_cache; a.pos = pos; a.n_used = n_used; a.out = out; a.lse = lse;
+  char* ws = static_cast<char*>(workspace);
+  a.part_m = reinterpret_cast<float*>(ws);
+  a.part_l = reinterpret_cast<float*>(ws + lay.part_l);
+  a.part_o = reinterpret_cast<float*>(ws + lay.part_o);
+  return launch_tree_attend(params->dtype, params->head_dim, a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
+}
+
+int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, int32_t nodes, const roco_pages* pages, const void* q,
+                     const void* k_new, const void* v_new, const float* lse, int32_t max_path, const int32_t* path, const int32_t* n_path,
+                     const int32_t* qpos0, void* K_cache, void* V_cache, float* stats, int32_t* pos, int32_t* n_used,
+                     int32_t* evicted_slot, int32_t* evicted_pos, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  CommitArgs a;
+  const int rc = check_tree(params, heads, group, nodes, pages, a.pages);
+  if (rc != ROCO_OK) return rc;
+  if (max_path < 1 || max_path > nodes) return ROCO_EINVAL;
+  const void* need[] = {q, k_new, v_new, lse, path, n_path, qpos0, K_cache, V_cache, stats, pos, n_used, workspace};
+  for (const void* ptr : need)
+    if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
+  for (const void* ptr : {static_cast<const void*>(evicted_slot), static_cast<const void*>(evicted_pos)})
+    if (ptr != nullptr && !aligned16(ptr)) return ROCO_EINVAL;
+  const TreeLayout lay = tree_layout(params, group, nodes);
+  if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
+  a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
+  a.scope = params->scope; a.max_path = max_path;
+  a.splits = (params->budget + kTreeChunk - 1) / kTreeChunk;
+  a.pol = policy_of(params);
+  a.scale_log2 = scale_log2(params);
+  a.recency_window = params->recency_window;
+  a.recency_bias_log2 = params->recency_bias * 1.4426950408889634f;
+  a.q = q; a.k_new = k_new; a.v_new = v_new; a.lse = lse; a.path = path; a.n_path = n_path; a.qpos0 = qpos0;
+  a.K = K_cache; a.V = V_cache; a.stats = stats; a.pos = pos; a.n_used = n_used;
+  a.evicted_slot = evicted_slot; a.evicted_pos = evicted_pos;
+  char* ws = static_cast<char*>(workspace);
+  a.taken = reinterpret_cast<int32_t*>(ws);
+  a.keys = reinterpret_cast<uint32_t*>(ws + lay.keys);
+  return launch_tree_commit(params->dtype, params->head_dim, a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
+}
+
+int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const int32_t* held, const int32_t* want,
+                     const int32_t* free_pages, int32_t n_free, int32_t* table, int32_t* page_start, int32_t* row_start,
+                     int32_t* slot_map, int32_t rows, int32_t padded, void* hip_stream) {
+  if (requests < 1 || max_pages < 1 || n_free < 0 || rows < 1 || !page_size_ok(page)) return ROCO_EINVAL;
+  if (requests > 65535 || static_cast<long long>(max_pages) * page >= (1ll << 31)) return ROCO_EUNSUPPORTED;
+  if (padded && static_cast<long long>(requests) * rows >= (1ll << 40)) return ROCO_EUNSUPPORTED;
+  const void* need[] = {want, table, page_start, row_start, slot_map};
+  for (const void* ptr : need)
+    if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
+  if ((held != nullptr && !aligned16(held)) || !aligned16(free_pages) || (free_pages == nullptr && n_free > 0)) return ROCO_EINVAL;
+  const PageTableArgs a = {requests, __builtin_ctz(static_cast<unsigned>(page)), max_pages, n_free, rows, padded != 0, held, want,
+                           free_pages, table, page_start, row_start, slot_map};
+  return launch_page_tables(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
+}
+
+int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t groups, int32_t rows, const void* K_rows, const void* V_rows,
+                    int64_t group_stride, int64_t row_stride, int64_t head_stride, const int32_t* slot_map, void* K_pool, void* V_pool,
+                    int32_t n_pages, int32_t page, void* hip_stream) {
+  if (dtype != ROCO_F32 && dtype != ROCO_BF16) return ROCO_EUNSUPPORTED;
+  if (head_dim != 64 && head_dim != 128) return ROCO_EUNSUPPORTED;
+  if (heads < 1 || groups < 1 || rows < 1) return ROCO_EINVAL;
+  const int rc = check_pages(n_pages, heads, page);
+  if (rc != ROCO_OK) return rc;
+  const int64_t element = dtype == ROCO_BF16 ? 2 : 4;
+  for (const int64_t stride : {group_stride, row_stride, head_stride})
+    if (stride < 0 || stride > (1ll << 60) || stride * element % 16 != 0) return ROCO_EINVAL;
+  const void* need[] = {K_rows, V_rows, slot_map, K_pool, V_pool};
+  for (const void* ptr : need)
+    if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
+  // (a lane per 16 bytes, counted by the grid: at most 2^31 workgroups of 256)
+  if (static_cast<double>(groups) * heads * rows * head_dim * element / 16 / 256 >= 2147483647.0) return ROCO_EUNSUPPORTED;
+  const PageStoreArgs a = {heads, groups, rows, n_pages, __builtin_ctz(static_cast<unsigned>(page)), static_cast<int>(head_dim * element),
+                           K_rows, V_rows, group_stride * element, row_stride * element, head_stride * element, slot_map, K_pool, V_pool};
+  return launch_page_store(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
 }
 
 int roco_select_retained(const roco_params* params, int32_t keep, const float* stats, const int32_t* pos,

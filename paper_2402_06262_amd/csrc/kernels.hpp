@@ -166,6 +166,79 @@ hipError_t launch_block(int dtype, int head_dim, const BlockArgs& a, hipStream_t
 // The step of bf16 in one or two kernels, if that is the quicker way (BlockArgs::single is set); else false and nothing is launched.
 bool launch_block_fused(int head_dim, const BlockArgs& a, hipStream_t s, hipError_t& e);
 
+// ---------------------------------------------------------------- drafted trees, paged caches
+constexpr int kMaxTreeNodes = 64;     // nodes of a tree: a bit each in a 64-bit mask
+constexpr int kMaxTreeGroup = 64;     // query heads per unit
+constexpr int kMaxTreeSplits = 64;    // workgroups that share a unit's slots: a lane each in the kernel that joins them
+constexpr int kTreeChunk = 1024;      // most slots of a workgroup of tree_statistics
+
+// Where K and V rows lie: [units][B] without a table, else pages of 1 << page_log2 slots, [n_pages][heads][page].
+struct CachePages {
+  const int32_t* table;   // [requests][max_pages], or null
+  const int32_t* budget;  // [requests], or null: B
+  int max_pages, page_log2, n_pages;
+};
+
+struct TreeArgs {
+  int units, heads, group, nodes, B;
+  int splits;             // workgroups along a unit's slots
+  int row_tiles;          // ... and along its query rows
+  float scale_log2;
+  int recency_window;
+  float recency_bias_log2;
+  const void *q, *k_new, *v_new;              // [units][nodes][group][d], [units][nodes][d]
+  const int32_t *parent, *n_nodes, *qpos0;    // [requests][nodes] or null: a chain, [requests] or null: all, [units]
+  const void *K, *V;
+  const int32_t *pos, *n_used;                // [units][B], [units]
+  CachePages pages;
+  void* out;
+  float* lse;                                 // [units][nodes][group], may be null
+  // workspace: a split's share of every query row; only the rows that exist are written
+  float *part_m, *part_l;                     // [units][splits][nodes * group]
+  float* part_o;                              // [units][splits][nodes * group][d], not yet divided
+};
+hipError_t launch_tree_attend(int dtype, int head_dim, const TreeArgs& a, hipStream_t s);
+int tree_attend_row_tiles(int rows);
+int tree_attend_splits(int units, int rows, int B);
+
+struct CommitArgs {
+  int units, heads, group, nodes, B, scope, max_path;
+  int splits;             // workgroups along a unit's slots, of at most kTreeChunk each
+  Policy pol;
+  float scale_log2;
+  int recency_window;
+  float recency_bias_log2;
+  const void *q, *k_new, *v_new;
+  const float* lse;                           // [units][nodes][group]
+  const int32_t *path, *n_path, *qpos0;       // [requests][max_path], [requests], [units]
+  void *K, *V;
+  float* stats;
+  int32_t *pos, *n_used;
+  CachePages pages;
+  int32_t *evicted_slot, *evicted_pos;        // [units][max_path], may be null
+  // workspace
+  int32_t* taken;                             // [units][kTakenWords]: slots held before, tokens taken over, their slots in order
+  uint32_t* keys;                             // [units][2][B] when B is too large for LDS
+};
+constexpr int kTakenWords = 4 + kMaxTreeNodes;
+hipError_t launch_tree_commit(int dtype, int head_dim, const CommitArgs& a, hipStream_t s);
+
+struct PageTableArgs {
+  int requests, page_log2, max_pages, n_free, rows, padded;
+  const int32_t *held, *want, *free_pages;    // held may be null
+  int32_t *table, *page_start, *row_start, *map;
+};
+hipError_t launch_page_tables(const PageTableArgs& a, hipStream_t s);
+
+struct PageStoreArgs {
+  int heads, groups, rows, n_pages, page_log2, row_bytes;
+  const void *K_rows, *V_rows;
+  int64_t group_stride, row_stride, head_stride;  // bytes
+  const int32_t* map;
+  void *K, *V;
+};
+hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s);
+
 // dtype: 0 = f32, 1 = bf16; head_dim: 64 or 128.  Each returns hipGetLastError() of its launches.
 hipError_t launch_decode(int dtype, int head_dim, const DecodeArgs& a, hipStream_t s);
 int decode_rows_per_pass(int dtype, int head_dim, int unroll);  // granularity of DecodeArgs::rows_per_split

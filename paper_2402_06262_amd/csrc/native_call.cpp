@@ -17,6 +17,7 @@ namespace {
 // ------------------------------------------------------------------ what binding.py hands over once
 PyObject* g_tensor_types[2];  // torch.Tensor, torch.nn.Parameter: exactly these are read without a call
 PyObject* g_params_type;      // binding.RocoParams
+PyObject* g_pages_type;       // binding.RocoPages
 PyObject* g_pointer;          // binding._ptr: everything else
 PyObject* g_current_stream;   // binding._stream: anything but an address, and the current stream before it is known how to ask
 PyObject* g_raw_stream;       // torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice: set once the GPU is in use
@@ -31,6 +32,10 @@ struct Functions {
   decltype(&roco_encode_block) block;
   decltype(&roco_encode_block_gqa) block_gqa;
   decltype(&roco_decode_step_gqa) decode_gqa;
+  decltype(&roco_tree_attend) tree_attend;
+  decltype(&roco_tree_commit) tree_commit;
+  decltype(&roco_page_tables) page_tables;
+  decltype(&roco_page_store) page_store;
 } g_fn;
 
 // ------------------------------------------------------------------ arguments
@@ -113,13 +118,13 @@ void* stream_of(PyObject* o) {
   return s;
 }
 
-// The parameters' structure, a ctypes object of binding.py's class (or one derived from it), read through the buffer it exports and
-// copied: its first 44 bytes.
-roco_params params_of(PyObject* o) {
-  roco_params p;
+// A structure, a ctypes object of binding.py's class (or one derived from it), read through the buffer it exports and copied: its first
+// bytes (44 of the parameters).
+template <class S> S structure_of(PyObject* o, PyObject* type, const char* what) {
+  S p;
   Py_buffer view;
-  if (!PyObject_TypeCheck(o, reinterpret_cast<PyTypeObject*>(g_params_type))) {
-    PyErr_SetString(PyExc_TypeError, "roco: params must be a RocoParams");
+  if (!PyObject_TypeCheck(o, reinterpret_cast<PyTypeObject*>(type))) {
+    PyErr_SetString(PyExc_TypeError, what);
     throw Failed{};
   }
   if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Failed{};
@@ -127,6 +132,16 @@ roco_params params_of(PyObject* o) {
   PyBuffer_Release(&view);
   return p;
 }
+roco_params params_of(PyObject* o) { return structure_of<roco_params>(o, g_params_type, "roco: params must be a RocoParams"); }
+struct Pages {  // or none
+  roco_pages pages;
+  const roco_pages* p = nullptr;
+  explicit Pages(PyObject* o) {
+    if (o == Py_None) return;
+    pages = structure_of<roco_pages>(o, g_pages_type, "roco: pages must be a RocoPages or None");
+    p = &pages;
+  }
+};
 
 template <class Call> PyObject* guarded(Py_ssize_t n, Py_ssize_t expected, Call call) {
   if (n != expected) {
@@ -251,12 +266,77 @@ PyObject* prefill_compress_lse(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// bind(addresses, tensor, parameter, RocoParams, _ptr, _stream); use_gpu(getCurrentRawStream, getDevice)
+// (params, heads, group, nodes, pages, 13 pointers, workspace_bytes, stream)
+PyObject* tree_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 20, [&] {
+    const roco_params p = params_of(a[0]);
+    const int32_t heads = int32_of(a[1]), group = int32_of(a[2]), nodes = int32_of(a[3]);
+    const Pages pages(a[4]);
+    void* t[13];
+    for (int i = 0; i < 13; ++i) t[i] = pointer(a[5 + i]);
+    const size_t ws = bytes(a[18], a[17]);
+    void* const s = stream_of(a[19]);
+    NoGil g;
+    return g_fn.tree_attend(&p, heads, group, nodes, pages.p, t[0], t[1], t[2], static_cast<int32_t*>(t[3]), static_cast<int32_t*>(t[4]),
+                            static_cast<int32_t*>(t[5]), t[6], t[7], static_cast<int32_t*>(t[8]), static_cast<int32_t*>(t[9]), t[10],
+                            static_cast<float*>(t[11]), t[12], ws, s);
+  });
+}
+PyObject* tree_commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 23, [&] {
+    const roco_params p = params_of(a[0]);
+    const int32_t heads = int32_of(a[1]), group = int32_of(a[2]), nodes = int32_of(a[3]);
+    const Pages pages(a[4]);
+    void *in[4], *t[11];
+    for (int i = 0; i < 4; ++i) in[i] = pointer(a[5 + i]);
+    const int32_t max_path = int32_of(a[9]);
+    for (int i = 0; i < 11; ++i) t[i] = pointer(a[10 + i]);
+    const size_t ws = bytes(a[21], a[20]);
+    void* const s = stream_of(a[22]);
+    NoGil g;
+    return g_fn.tree_commit(&p, heads, group, nodes, pages.p, in[0], in[1], in[2], static_cast<float*>(in[3]), max_path,
+                            static_cast<int32_t*>(t[0]), static_cast<int32_t*>(t[1]), static_cast<int32_t*>(t[2]), t[3], t[4],
+                            static_cast<float*>(t[5]), static_cast<int32_t*>(t[6]), static_cast<int32_t*>(t[7]),
+                            static_cast<int32_t*>(t[8]), static_cast<int32_t*>(t[9]), t[10], ws, s);
+  });
+}
+PyObject* page_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 14, [&] {
+    const int32_t requests = int32_of(a[0]), page = int32_of(a[1]), max_pages = int32_of(a[2]);
+    int32_t* t[7];
+    for (int i = 0; i < 3; ++i) t[i] = static_cast<int32_t*>(pointer(a[3 + i]));
+    const int32_t n_free = int32_of(a[6]);
+    for (int i = 3; i < 7; ++i) t[i] = static_cast<int32_t*>(pointer(a[4 + i]));
+    const int32_t rows = int32_of(a[11]), padded = int32_of(a[12]);
+    void* const s = stream_of(a[13]);
+    NoGil g;
+    return g_fn.page_tables(requests, page, max_pages, t[0], t[1], t[2], n_free, t[3], t[4], t[5], t[6], rows, padded, s);
+  });
+}
+// (dtype, head_dim, heads, groups, rows, K_rows, V_rows, three strides, map, two pools, n_pages, page, stream)
+PyObject* page_store(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&] {
+    int32_t size[5];
+    for (int i = 0; i < 5; ++i) size[i] = int32_of(a[i]);
+    void *k = pointer(a[5]), *v = pointer(a[6]);
+    int64_t stride[3];
+    for (int i = 0; i < 3; ++i) stride[i] = static_cast<int64_t>(integer(a[7 + i]));
+    void* const map = pointer(a[10]);
+    void *k_pool = pointer(a[11]), *v_pool = pointer(a[12]);
+    const int32_t n_pages = int32_of(a[13]), page = int32_of(a[14]);
+    void* const s = stream_of(a[15]);
+    NoGil g;
+    return g_fn.page_store(size[0], size[1], size[2], size[3], size[4], k, v, stride[0], stride[1], stride[2], static_cast<int32_t*>(map),
+                           k_pool, v_pool, n_pages, page, s);
+  });
+}
+
+// bind(addresses, tensor, parameter, RocoParams, RocoPages, _ptr, _stream); use_gpu(getCurrentRawStream, getDevice)
 PyObject* bind(PyObject*, PyObject* args) {
-  unsigned long long f[8];
-  PyObject *tensor, *parameter, *params, *ptr, *stream;
-  if (!PyArg_ParseTuple(args, "(KKKKKKKK)OOO!OO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &tensor, &parameter,
-                        &PyType_Type, &params, &ptr, &stream))
+  unsigned long long f[12];
+  PyObject *tensor, *parameter, *params, *pages, *ptr, *stream;
+  if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKK)OOO!O!OO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9], &f[10],
+                        &f[11], &tensor, &parameter, &PyType_Type, &params, &PyType_Type, &pages, &ptr, &stream))
     return nullptr;
   g_fn.prefill = reinterpret_cast<decltype(g_fn.prefill)>(f[0]);
   g_fn.prefill_gqa = reinterpret_cast<decltype(g_fn.prefill_gqa)>(f[1]);
@@ -266,10 +346,15 @@ PyObject* bind(PyObject*, PyObject* args) {
   g_fn.block = reinterpret_cast<decltype(g_fn.block)>(f[5]);
   g_fn.block_gqa = reinterpret_cast<decltype(g_fn.block_gqa)>(f[6]);
   g_fn.decode_gqa = reinterpret_cast<decltype(g_fn.decode_gqa)>(f[7]);
-  Py_INCREF(tensor); Py_INCREF(parameter); Py_INCREF(params); Py_INCREF(ptr); Py_INCREF(stream);
+  g_fn.tree_attend = reinterpret_cast<decltype(g_fn.tree_attend)>(f[8]);
+  g_fn.tree_commit = reinterpret_cast<decltype(g_fn.tree_commit)>(f[9]);
+  g_fn.page_tables = reinterpret_cast<decltype(g_fn.page_tables)>(f[10]);
+  g_fn.page_store = reinterpret_cast<decltype(g_fn.page_store)>(f[11]);
+  Py_INCREF(tensor); Py_INCREF(parameter); Py_INCREF(params); Py_INCREF(pages); Py_INCREF(ptr); Py_INCREF(stream);
   Py_XSETREF(g_tensor_types[0], tensor);
   Py_XSETREF(g_tensor_types[1], parameter);
   Py_XSETREF(g_params_type, params);
+  Py_XSETREF(g_pages_type, pages);
   Py_XSETREF(g_pointer, ptr);
   Py_XSETREF(g_current_stream, stream);
   Py_RETURN_NONE;
@@ -292,7 +377,8 @@ PyObject* forget_gpu(PyObject*, PyObject*) {  // in a forked child
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     FAST(decode_step), FAST(decode_step_static), FAST(decode_step_gqa), FAST(encode_block), FAST(encode_block_gqa),
-    FAST(prefill_compress), FAST(prefill_compress_gqa), FAST(prefill_compress_lse),
+    FAST(prefill_compress), FAST(prefill_compress_gqa), FAST(prefill_compress_lse), FAST(tree_attend), FAST(tree_commit),
+    FAST(page_tables), FAST(page_store),
     {"bind", bind, METH_VARARGS, nullptr}, {"use_gpu", use_gpu, METH_VARARGS, nullptr},
     {"forget_gpu", forget_gpu, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef FAST

@@ -1,0 +1,233 @@
+"""Block tables and slot maps, rows stored by slot map (roco_page_tables, roco_page_store), and a speculative loop from prompts of
+different lengths on: every step against the oracle."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_06262_amd as roco
+from inputs import round_to_bf16
+from oracle import roco_oracle as orc
+from oracle import trees
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.int32).cuda()
+
+
+def tables(held, want, page, free, table, rows, padded):
+    R = len(want)
+    t = ints(table)
+    page_start, row_start = ints(np.full(R + 1, -9)), ints(np.full(R + 1, -9))
+    slots = ints(np.full((R, rows) if padded else rows, -9))
+    roco.roco_page_tables(None if held is None else ints(held), ints(want), page, ints(free), t, page_start, row_start, slots)
+    torch.cuda.synchronize()
+    return [x.cpu().numpy() for x in (t, page_start, row_start, slots)]
+
+
+def check(held, want, page, free, table, rows, padded):
+    got = tables(held, want, page, free, table, rows, padded)
+    expected = trees.page_tables(np.zeros(len(want), int) if held is None else held, want, page, free, table, rows, padded)
+    for g, e, name in zip(got, expected, ("table", "page_start", "row_start", "map")):
+        assert np.array_equal(g, e), name
+
+
+@pytest.mark.parametrize("padded", [False, True])
+@pytest.mark.parametrize("R,page,most,grow", [(1, 16, 5, None), (3, 16, 100, None), (64, 64, 700, 9), (70, 32, 300, 1), (1023, 16, 60, None),
+                                              (1025, 16, 90, 40), (2500, 128, 400, 3), (5, 1024, 9000, None)])
+def test_tables_and_maps(R, page, most, grow, padded):
+    rng = np.random.default_rng(R + page)
+    M = -(-most // page)
+    if grow is None:
+        held, want = None, rng.integers(0, most + 1, R)
+        table = np.full((R, M), -5)
+    else:
+        held = rng.integers(0, most + 1, R)
+        want = np.minimum(most, held + rng.integers(0, grow + 1, R))
+        table = rng.integers(0, 9999, (R, M))
+    h = np.zeros(R, int) if held is None else held
+    need = int((-(-want // page) - -(-h // page)).sum())
+    rows = max(1, int((want - h).max()) if padded else int((want - h).sum()))
+    free = rng.permutation(need + 7)
+    check(held, want, page, free, table, rows, padded)
+    check(held, want, page, free, table, rows + 5, padded)            # entries without a slot
+    if rows > 2:
+        check(held, want, page, free, table, rows - 2, padded)        # a map that ends early
+    if need > 2:
+        check(held, want, page, free[:need // 2], table, rows, padded)  # pages that lack
+    check(held, want, page, free[:0], table, rows, padded)
+
+
+def test_lengths_outside_the_tables():
+    """Lengths below what is held, above what a row of the table takes, negative ones; entries of the table that are no pages."""
+    check([10, 0, -4, 40, 99], [5, 99, 20, 40, 3], 16, np.arange(20) * 3, [[8, -1], [9, 9], [9, 9], [-1, 6], [2, 1]], 60, False)
+    check([10, 0, -4, 40, 99], [5, 99, 20, 40, 3], 16, np.arange(20) * 3, [[8, -1], [9, 9], [9, 9], [-1, 6], [2, 1]], 33, True)
+
+
+def test_tables_captured_and_replayed():
+    """The requests grow with every replay (and take the list's first pages again); eager calls between them."""
+    rng = np.random.default_rng(1)
+    R, page, M = 20, 16, 12
+    held, want = ints(rng.integers(0, 30, R)), ints(np.zeros(R))
+    want.copy_(held + 3)
+    table, free = ints(rng.permutation(R * M).reshape(R, M)), ints(R * M + rng.permutation(300))
+    starts, rows, slots = ints(np.zeros(R + 1)), ints(np.zeros(R + 1)), ints(np.zeros(R * 3))
+    call = lambda: roco.roco_page_tables(held, want, page, free, table, starts, rows, slots)  # noqa: E731
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        call()
+    for i in range(4):
+        before, h = table.cpu().numpy(), held.cpu().numpy()
+        graph.replay() if i % 2 == 0 else call()
+        torch.cuda.synchronize()
+        e = trees.page_tables(h, h + 3, page, free.cpu().numpy(), before, R * 3, False)
+        for g, x in zip((table, starts, rows, slots), e):
+            assert np.array_equal(g.cpu().numpy(), x)
+        held.add_(3)
+        want.add_(3)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,rows,page", [(1, 1, 16), (3, 7, 16), (8, 100, 64), (5, 33, 1024)])
+def test_new_tokens_and_caches_into_pages(dtype, d, heads, rows, page):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    n_pages = -(-4 * rows // page) + 3
+    order = torch.randperm((n_pages - 1) * page, generator=g, device="cuda").to(torch.int32)  # slots, each once; the last page stays
+    pools = [torch.full((n_pages, heads, page, d), 9.0, dtype=dtype, device="cuda") for _ in range(2)]
+
+    def expected(rows_of, slots):
+        want = torch.full((n_pages, heads, page, d), 9.0, dtype=dtype, device="cuda")
+        flat = want.permute(0, 2, 1, 3).reshape(-1, heads, d)
+        ok = (slots >= 0) & (slots < n_pages * page)
+        flat[slots[ok].long()] = rows_of[ok]
+        return flat.view(n_pages, page, heads, d).permute(0, 2, 1, 3)
+
+    # keys and values side by side in a fused projection, with some tokens that are not stored
+    qkv = torch.randn((rows, 4 * heads, d), generator=g, device="cuda").to(dtype)
+    slots = order[:rows].clone()
+    slots[::5] = -1
+    slots[2::9] = n_pages * page + 3
+    roco.roco_page_store(qkv[:, heads:2 * heads], qkv[:, 3 * heads:], slots, *pools)
+    torch.cuda.synchronize()
+    assert torch.equal(pools[0], expected(qkv[:, heads:2 * heads], slots)) and torch.equal(pools[1], expected(qkv[:, 3 * heads:], slots))
+    # caches of two requests, of different fills, contiguous and not
+    for store in (torch.empty((2, heads, rows, d), dtype=dtype, device="cuda"), torch.empty((rows, 2, heads, d), dtype=dtype, device="cuda").permute(1, 2, 0, 3)):
+        k, v = store.copy_(torch.randn((2, heads, rows, d), generator=g, device="cuda")), torch.empty_like(store).copy_(torch.randn((2, heads, rows, d), generator=g, device="cuda"))
+        if v.stride() != k.stride():
+            v = v.clone(memory_format=torch.preserve_format)
+        slots = order[rows:3 * rows].view(2, rows).clone()
+        slots[1, rows // 2:] = -1
+        for pool in pools:
+            pool.fill_(9.0)
+        roco.roco_page_store(k, v, slots, *pools)
+        torch.cuda.synchronize()
+        for pool, x in zip(pools, (k, v)):
+            assert torch.equal(pool, expected(x.transpose(1, 2).reshape(-1, heads, d), slots.view(-1)))
+
+
+def test_store_beyond_32_bits():
+    """Rows at the end of pools of 5 GiB, from rows that lie as far apart."""
+    n_pages, heads, page, d = 40960, 8, 64, 128
+    pools = [torch.zeros((n_pages, heads, page, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    far = torch.zeros((2, (5 << 30) // (2 * heads * d), heads, d), dtype=torch.bfloat16, device="cuda")[:, ::(4 << 30) // (2 * heads * d)].permute(0, 2, 1, 3)
+    assert far.shape[2] == 2
+    far.copy_(torch.randn(far.shape, device="cuda"))
+    slots = ints([[n_pages * page - 1, 5], [n_pages * page - 70, -1]])
+    roco.roco_page_store(far, far, slots, *pools)
+    torch.cuda.synchronize()
+    for pool in pools:
+        assert torch.equal(pool[-1, :, -1], far[0, :, 0]) and torch.equal(pool[0, :, 5], far[0, :, 1]) and torch.equal(pool[-2, :, -6], far[1, :, 0])
+        assert int((pool != 0).any(-1).sum()) == 3 * heads
+
+
+@pytest.mark.parametrize("dtype,d,group", [("bf16", 128, 2), ("f32", 64, 1), ("bf16", 64, 4)])
+def test_a_speculative_loop_on_paged_caches_of_prompts_of_different_lengths(dtype, d, group):
+    """Prompts compressed to half their length each, into pages; then steps of drafted trees, each attended and its accepted path taken
+    over.  The states of the oracle start from the library's compressed prompts (which have tests of their own)."""
+    rng = np.random.default_rng(d + group)
+    R, H, T, A, page, scope = 3, 2, 7, 4, 16, 12
+    lengths = [90, 41, 150]
+    budgets = [n // 2 for n in lengths]
+    B, U, sc = max(budgets), R * H, 1 / math.sqrt(d)
+    rnd = round_to_bf16 if dtype == "bf16" else (lambda x: x)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    draw = lambda *s: torch.from_numpy(rnd(rng.standard_normal(s).astype(np.float32))).cuda().to(dt)  # noqa: E731
+    p = roco.RocoParams(U, d, B, scope, roco.ROCO_BF16 if dtype == "bf16" else roco.ROCO_F32)
+    M = -(-B // page)
+    n_pages = sum(-(-b // page) for b in budgets) + 2
+    cache = roco.alloc_paged_cache(p, H, n_pages, page)
+    # prompts of one request at a time, each to a cache of its budget; the rows go to the pages, the rest to its place
+    table, starts, rows_at = ints(np.full((R, M), -1)), ints(np.zeros(R + 1)), ints(np.zeros(R + 1))
+    slots = ints(np.zeros(sum(budgets)))
+    roco.roco_page_tables(None, ints(budgets), page, ints(rng.permutation(n_pages)), table, starts, rows_at, slots)
+    for r, (n, b) in enumerate(zip(lengths, budgets)):
+        one = roco.RocoParams(H, d, b, min(scope, b), p.dtype)
+        c = roco.alloc_cache(one)
+        Q, K, V = draw(H, group, n, d), draw(H, n, d), draw(H, n, d)
+        ws = torch.empty(roco.prefill_gqa_workspace_bytes(one, group, n), dtype=torch.uint8, device="cuda")
+        roco.roco_prefill_compress_gqa(one, group, Q, K, V, ints([n] * H), n, c.K, c.V, c.stats, c.pos, c.n_used, c.next_slot, None, ws)
+        first = sum(budgets[:r])
+        mine = slots[first:first + b].clone().view(1, b)
+        roco.roco_page_store(c.K.view(1, H, b, d), c.V.view(1, H, b, d), mine, cache.K, cache.V)
+        mine = slice(r * H, r * H + H)
+        cache.stats[mine, :, :b], cache.pos[mine, :b], cache.n_used[mine] = c.stats, c.pos, c.n_used
+    host_table = table.cpu().numpy()
+
+    def rows_of(pool, u, n):
+        pool = pool.float().cpu().numpy()
+        return np.stack([pool[host_table[u // H, j // page], u % H, j % page] for j in range(n)])
+
+    states = []
+    for u in range(U):
+        n = int(cache.n_used[u])
+        assert n == budgets[u // H]
+        st = orc.CacheState(np.zeros((B, d)), np.zeros((B, d)), *cache.stats[u].cpu().numpy().astype(np.float64), cache.pos[u].cpu().numpy().astype(np.int64), n)
+        st.K[:n], st.V[:n] = rows_of(cache.K, u, n), rows_of(cache.V, u, n)
+        states.append(st)
+    pages = roco.RocoPages(table, n_pages, page, ints(budgets))
+    ws = torch.empty(roco.tree_workspace_bytes(p, group, T), dtype=torch.uint8, device="cuda")
+    at = list(lengths)
+    for step in range(4):
+        q, k, v = draw(U, T, group, d), draw(U, T, d), draw(U, T, d)
+        parent = [[-1 if i == 0 else int(rng.integers(-1, i)) for i in range(T)] for _ in range(R)]
+        nodes = [int(rng.integers(1, T + 1)) for _ in range(R)]
+        qpos0 = np.repeat(at, H)
+        out = torch.zeros((U, T, group, d), dtype=dt, device="cuda")
+        lse = torch.zeros((U, T, group), device="cuda")
+        roco.roco_tree_attend(p, H, group, T, pages, q, k, v, ints(parent), ints(nodes), ints(qpos0), cache.K, cache.V, cache.pos, cache.n_used, out, lse, ws)
+        paths = []
+        for r in range(R):
+            i, path = nodes[r] - 1, []
+            while i >= 0:
+                path.insert(0, i)
+                i = parent[r][i]
+            paths.append(path[:A])
+        path = np.array([x + [0] * (A - len(x)) for x in paths])
+        ev_slot, ev_pos = ints(np.zeros((U, A))), ints(np.zeros((U, A)))
+        roco.roco_tree_commit(p, H, group, T, pages, q, k, v, lse, A, ints(path), ints([len(x) for x in paths]), ints(qpos0), cache.K, cache.V, cache.stats,
+                              cache.pos, cache.n_used, ev_slot, ev_pos, ws)
+        torch.cuda.synchronize()
+        hq, hk, hv, ho, hl = (x.float().cpu().numpy() for x in (q, k, v, out, lse))
+        for u, st in enumerate(states):
+            r = u // H
+            t, n = nodes[r], st.n_used
+            w = trees.tree_attend(st.K[:n], st.V[:n], st.pos, hq[u, :t], hk[u, :t], hv[u, :t], parent[r], at[r], sc)
+            assert np.abs(hl[u, :t] - w.lse).max() < 2e-5
+            assert np.abs(ho[u, :t] - w.out).max() < (2.0 ** -7 if dtype == "bf16" else 2e-5) * np.abs(w.out).max()
+            # (the oracle ranks by the statistics that the library has left, which are fp32: see the end of this loop)
+            c = trees.tree_commit(st, budgets[r], hq[u], hk[u], hv[u], hl[u], paths[r], at[r], scope, sc)
+            a = len(paths[r])
+            assert ev_slot[u, :a].tolist() == c.evicted_slot.tolist() and ev_pos[u, :a].tolist() == c.evicted_pos.tolist(), (step, u)
+            got = cache.stats[u].cpu().numpy().astype(np.float64)
+            m = st.n_used
+            assert np.array_equal(got[2, :m], st.count[:m])
+            assert np.allclose(got[0, :m], st.acc[:m], rtol=1e-4, atol=1e-6) and np.allclose(got[1, :m], st.acc2[:m], rtol=1e-4, atol=1e-6)
+            st.acc[:], st.acc2[:] = got[0], got[1]
+            assert np.array_equal(rows_of(cache.K, u, m), st.K[:m]) and np.array_equal(rows_of(cache.V, u, m), st.V[:m])
+            assert np.array_equal(cache.pos[u].cpu().numpy(), st.pos)
+        at = [n + len(x) for n, x in zip(at, paths)]
