@@ -124,12 +124,12 @@ int check_tree(const roco_params* p, int32_t heads, int32_t group, int32_t nodes
 }
 
 // ---- workspace of the trees: tree_attend's part_m | part_l | part_o, or tree_commit's taken | keys
-struct TreeLayout { size_t part_l, part_o, keys, total; int splits; };
+struct TreeLayout { size_t part_l, part_o, keys, total; TreeSplits split; };
 TreeLayout tree_layout(const roco_params* p, int32_t group, int32_t nodes) {
   TreeLayout l;
   const size_t U = p->units, B = p->budget, rows = static_cast<size_t>(group) * nodes;
-  l.splits = tree_attend_splits(p->units, group * nodes, p->budget);
-  const size_t plane = l.splits == 1 ? 0 : align_up(U * l.splits * rows * sizeof(float));
+  l.split = tree_attend_splits(p->units, group * nodes, p->budget);
+  const size_t plane = l.split.splits == 1 ? 0 : align_up(U * l.split.splits * rows * sizeof(float));
   l.part_l = plane;
   l.part_o = 2 * plane;
   const size_t attend = 2 * plane + plane * p->head_dim;
@@ -528,8 +528,10 @@ int roco_tree_attend(const roco_params* params, int32_t heads, int32_t group, in
   const TreeLayout lay = tree_layout(params, group, nodes);
   if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
   a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
-  a.splits = lay.splits;
+  a.splits = lay.split.splits;
+  a.chunk = lay.split.chunk;
   a.row_tiles = tree_attend_row_tiles(group * nodes);
+  a.streaming = a.row_tiles == 1 && streaming_loads(params) ? 1 : 0;  // (several row tiles find the rows in their die's L2)
   a.scale_log2 = scale_log2(params);
   a.recency_window = params->recency_window;
   a.recency_bias_log2 = params->recency_bias * 1.4426950408889634f;
@@ -560,6 +562,7 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
   a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
   a.scope = params->scope; a.max_path = max_path;
   a.splits = (params->budget + kTreeChunk - 1) / kTreeChunk;
+  a.streaming = streaming_loads(params) ? 1 : 0;
   a.pol = policy_of(params);
   a.scale_log2 = scale_log2(params);
   a.recency_window = params->recency_window;

@@ -181,8 +181,10 @@ struct CachePages {
 
 struct TreeArgs {
   int units, heads, group, nodes, B;
-  int splits;             // workgroups along a unit's slots
+  int splits;             // most workgroups along a unit's slots
+  int chunk;              // ... of so many slots each, a multiple of 64
   int row_tiles;          // ... and along its query rows
+  int streaming;          // as DecodeArgs::streaming
   float scale_log2;
   int recency_window;
   float recency_bias_log2;
@@ -199,11 +201,13 @@ struct TreeArgs {
 };
 hipError_t launch_tree_attend(int dtype, int head_dim, const TreeArgs& a, hipStream_t s);
 int tree_attend_row_tiles(int rows);
-int tree_attend_splits(int units, int rows, int B);
+struct TreeSplits { int splits, chunk; };
+TreeSplits tree_attend_splits(int units, int rows, int B);
 
 struct CommitArgs {
   int units, heads, group, nodes, B, scope, max_path;
   int splits;             // workgroups along a unit's slots, of at most kTreeChunk each
+  int streaming;          // as DecodeArgs::streaming
   Policy pol;
   float scale_log2;
   int recency_window;

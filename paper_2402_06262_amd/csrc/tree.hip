@@ -1,4 +1,6 @@
 // Drafted trees: the joining of the splits' shares, and which form of tree_attend a call takes.
+#include <stdlib.h>
+
 #include <algorithm>
 
 #include "profile.hpp"
@@ -26,9 +28,11 @@ template <int DT, int HD> __global__ __launch_bounds__(kJoinThreads) void tree_j
   const int request = u / a.heads;
   const int nodes = a.n_nodes != nullptr ? min(max(a.n_nodes[request], 0), a.nodes) : a.nodes;
   if (row >= nodes * a.group) return;
+  const int splits = tree::splits_used(min(max(a.n_used[u], 0), tree::budget_of(a.pages, a.B, request)), a.chunk);
+  if (splits == 1) return;  // has written its rows
   const size_t first = static_cast<size_t>(u) * a.splits * all + row;  // of split 0; the others `all` further each
   float m = -INFINITY, l = 0.0f;
-  if (lane < a.splits) {
+  if (lane < splits) {
     m = a.part_m[first + static_cast<size_t>(lane) * all];
     l = a.part_l[first + static_cast<size_t>(lane) * all];
   }
@@ -38,18 +42,18 @@ template <int DT, int HD> __global__ __launch_bounds__(kJoinThreads) void tree_j
   float o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.0f;
-  for (int i0 = 0; i0 < a.splits; i0 += 4) {  // four at a time: behind the last split its outputs again, with nothing of them
+  for (int i0 = 0; i0 < splits; i0 += 4) {  // four at a time: behind the last split its outputs again, with nothing of them
     float v[4][E];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float* const p = a.part_o + (first + static_cast<size_t>(min(i0 + k, a.splits - 1)) * all) * HD + lane * E;
+      const float* const p = a.part_o + (first + static_cast<size_t>(min(i0 + k, splits - 1)) * all) * HD + lane * E;
 #pragma unroll
       for (int e = 0; e < E; ++e) v[k][e] = p[e];
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float wk = __shfl(w, min(i0 + k, kWave - 1), kWave);
-      if (i0 + k >= a.splits) break;
+      if (i0 + k >= splits) break;
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = fmaf(wk, v[k][e], o[e]);
     }
@@ -73,11 +77,19 @@ template <int DT, int HD> hipError_t launch_join(const TreeArgs& a, hipStream_t 
 
 int tree_attend_row_tiles(int rows) { return rows <= 64 ? 1 : (rows + 63) / 64; }
 
-// Two workgroups of two waves on every compute unit, while each has 256 slots.
-int tree_attend_splits(int units, int rows, int B) {
-  const long long groups = static_cast<long long>(units) * tree_attend_row_tiles(rows);
-  const int want = static_cast<int>(std::min<long long>(kMaxTreeSplits, (512 + groups - 1) / groups));
-  return std::max(1, std::min(want, B / 256));
+// Two workgroups of two waves on every compute unit, while each has 64 slots.
+TreeSplits tree_attend_splits(int units, int rows, int B) {
+  const char* const asked = getenv("ROCO_TREE_SPLITS");
+  int want = asked != nullptr ? atoi(asked) : 0;
+  if (want <= 0) {
+    const long long groups = static_cast<long long>(units) * tree_attend_row_tiles(rows);
+    want = static_cast<int>((512 + groups - 1) / groups);
+  }
+  want = std::max(1, std::min({want, kMaxTreeSplits, (B + 63) / 64}));
+  TreeSplits s;
+  s.chunk = ((B + want - 1) / want + 63) / 64 * 64;
+  s.splits = (B + s.chunk - 1) / s.chunk;
+  return s;
 }
 
 hipError_t launch_tree_attend(int dtype, int head_dim, const TreeArgs& a, hipStream_t s) {

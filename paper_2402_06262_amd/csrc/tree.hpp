@@ -6,6 +6,9 @@
 namespace roco {
 namespace tree {
 
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+
 using fused::f32x4;
 using mfma::lds_address;
 using mfma::lds_read_transposed;
@@ -48,12 +51,11 @@ template <int DT> __device__ __forceinline__ f32x4 score_step(const uint4& a, co
   }
 }
 
-// The nodes that node `lane` of a tree sees, a bit each: itself and those above it.  Twice as far up with every step.  A parent that is
-// not an earlier node is none.
-__device__ __forceinline__ uint64_t seen_nodes(const int32_t* parent, int nodes, int lane) {
-  int up = lane - 1;
-  if (parent != nullptr) up = lane < nodes ? parent[lane] : -1;
-  if (up >= lane || up < 0) up = -1;
+// The nodes that node `lane` of a tree sees, a bit each: itself and those above it, from its parent.  Twice as far up with every step.  A
+// parent that is not an earlier node is none.
+__device__ __forceinline__ uint64_t seen_nodes(int parent, int nodes, int lane) {
+  int up = parent;
+  if (up >= lane || up < 0 || lane >= nodes) up = -1;
   uint32_t lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);
 #pragma unroll
   for (int i = 0; i < 6; ++i) {
@@ -77,6 +79,9 @@ __device__ __forceinline__ uint64_t from_lane(uint64_t v, int lane) {
 __device__ __forceinline__ int budget_of(const CachePages& pages, int B, int request) {
   return pages.budget != nullptr ? min(max(pages.budget[request], 0), B) : B;
 }
+
+// Workgroups that a unit of n slots needs along its slots.
+__device__ __forceinline__ int splits_used(int n, int chunk) { return max((n + chunk - 1) / chunk, 1); }
 
 // A wave's tiles of the slots [row0, row1) of a unit: every W-th one, from a start that differs between workgroups so that they do not
 // walk the memory channels in lock step; behind the cache's tiles come `node_tiles` of a tree's nodes.  The tile numbers `t` are the
@@ -170,17 +175,19 @@ template <int DT, int HD, bool VALUES> __device__ __forceinline__ void load_offs
   }
 }
 
-// Requests a tile: eight loads.
-template <int DT, int HD, int G>
+// Requests a tile: eight loads.  STREAMING: of a cache that is far larger than the chip's last-level cache, with the non-temporal hint.
+template <int DT, int HD, bool STREAMING, int G>
 __device__ __forceinline__ void request_tile(const void* rows, const uint32_t (&row)[G], uint32_t there, uint32_t lds, const int* off) {
   using T = Tile<DT, HD>;
 #pragma unroll
   for (int i = 0; i < G; ++i) {
     const v4i32 buf = make_buffer(static_cast<const char*>(rows) + static_cast<size_t>(row[i]) * T::kBytes, ((there >> (8 * i)) & 0xffu) * T::kBytes);
 #pragma unroll
-    for (int j = 0; j < T::kGroupLoads; ++j) load16_to_lds(buf, lds + (i * T::kGroupLoads + j) * 1024, off[j], 0);
+    for (int j = 0; j < T::kGroupLoads; ++j) mfma::load16_to_lds_hint<STREAMING>(buf, lds + (i * T::kGroupLoads + j) * 1024, off[j], 0);
   }
 }
+
+#pragma clang diagnostic pop
 
 }  // namespace tree
 }  // namespace roco

@@ -33,34 +33,56 @@ template <int DT> __device__ __forceinline__ void store4(void* base, size_t idx,
   }
 }
 
+// Whether 16 bytes of values hold an infinite one or NaN.
+template <int DT> __device__ __forceinline__ bool holds_special(const uint4& v) {
+  // (the exponent's bits set: adding one to them carries)
+  const auto one = [](uint32_t x) {
+    if (DT == kBF16) return ((x & 0x7f800000u) + 0x00800000u) | (((x & 0x7f80u) + 0x80u) << 16);
+    return (x & 0x7f800000u) + 0x00800000u;
+  };
+  return ((one(v.x) | one(v.y) | one(v.z) | one(v.w)) & 0x80000000u) != 0;
+}
+template <int DT> __device__ __forceinline__ float load_elem(const void* base, size_t idx) {
+  if constexpr (DT == kBF16) return bf16_to_f32(static_cast<const uint16_t*>(base)[idx]);
+  else return static_cast<const float*>(base)[idx];
+}
+
 // NQ tiles of 16 query rows; a row is a node and a head of the group.  WINDOW: a recency bias is in force.
-template <int DT, int HD, int NQ, bool WINDOW>
+// A launch begins with a cold instruction cache, a third of a microsecond per KiB, so that nothing is unrolled that need not be: the
+// loop over the tiles begins two tiles early, with the requests alone, and what is rare loops over rows.
+template <int DT, int HD, int NQ, bool STREAMING, bool WINDOW>
 __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
   using T = Tile<DT, HD>;
   constexpr int W = kAttendWaves, G = T::kGroups, QR = 16 * NQ;
-  constexpr int kTileBytes = 8192, kWaveBytes = 4 * kTileBytes;  // K, K, V, V
+  constexpr int kTileBytes = 8192, kWaveBytes = 4 * kTileBytes;  // K, V, K, V
   constexpr int kSide = WINDOW ? 1 : 0;                          // the positions of a K tile's slots come along
+  // the queries come through the place of the second V tile, or of the second tiles, or before any tile
+  constexpr int kQueryBytes = QR * T::kBytes;
+  constexpr bool kBehindK = kQueryBytes <= kTileBytes, kBeforeK = !kBehindK && kQueryBytes <= 2 * kTileBytes;
   extern __shared__ __attribute__((aligned(1024))) char lds[];   // the waves' tiles; then a wave's outputs
   __shared__ __attribute__((aligned(256))) int32_t pos_s[WINDOW ? W : 1][2][kWave];
   __shared__ float merge_m[QR], merge_l[QR];
+  __shared__ uint64_t special_s[W];
   // the row tiles of a split go to one die: eight dies take the workgroups in turn
   const int per = 8 * a.row_tiles, id = blockIdx.x;
   const int us = id / per * 8 + id % 8, row_tile = id % per / 8;
   if (us >= a.units * a.splits) return;
   const int u = us / a.splits, split = us % a.splits;
   const int request = u / a.heads;
-  const int nodes = __builtin_amdgcn_readfirstlane(a.n_nodes != nullptr ? min(max(a.n_nodes[request], 0), a.nodes) : a.nodes);
-  const int rows = nodes * a.group, first_row = row_tile * QR;
-  if (first_row >= rows) return;
-  const int n = __builtin_amdgcn_readfirstlane(min(max(a.n_used[u], 0), budget_of(a.pages, a.B, request)));
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int qi = lane & 15, g = lane >> 4;
-
-  constexpr int kStep = T::kSlots * W;
-  const int chunk = ((n + a.splits - 1) / a.splits + kStep - 1) / kStep * kStep;
-  const int row0 = min(n, split * chunk), row1 = min(n, row0 + chunk);
+  // (what has to come from memory before anything else is asked for together)
+  int parent = lane - 1;
+  if (a.parent != nullptr) parent = a.parent[static_cast<size_t>(request) * a.nodes + min(lane, a.nodes - 1)];
+  const int asked_nodes = a.n_nodes != nullptr ? a.n_nodes[request] : a.nodes, held = a.n_used[u], budget = budget_of(a.pages, a.B, request);
+  const int nodes = __builtin_amdgcn_readfirstlane(min(max(asked_nodes, 0), a.nodes));
+  const int n = __builtin_amdgcn_readfirstlane(min(max(held, 0), budget));
+  const int rows = nodes * a.group, first_row = row_tile * QR;
+  const int used = splits_used(n, a.chunk);  // the last of them takes the nodes too
+  if (first_row >= rows || split >= used) return;
+  const int row0 = split * a.chunk, row1 = min(n, row0 + a.chunk);
   Walk<DT, HD, W> walk;
-  walk.init(a.pages, a.B, a.heads, u, request, row0, row1, split == a.splits - 1 ? nodes : 0, wave, static_cast<unsigned>(u) * 5u + static_cast<unsigned>(split) * 3u);
+  walk.init(a.pages, a.B, a.heads, u, request, row0, row1, split == used - 1 ? nodes : 0, wave, static_cast<unsigned>(u) * 5u + static_cast<unsigned>(split) * 3u);
   const int mine = walk.mine;
 
   char* const tiles = lds + wave * kWaveBytes;
@@ -68,52 +90,41 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
   int koff[T::kGroupLoads], voff[T::kGroupLoads];
   load_offsets<DT, HD, false>(koff);
   load_offsets<DT, HD, true>(voff);
-  const v4i32 pbuf = make_buffer(a.pos + static_cast<size_t>(u) * a.B, WINDOW ? static_cast<uint32_t>(a.B) * 4u : 0u);
-  const char* const new_k = static_cast<const char*>(a.k_new) + static_cast<size_t>(u) * a.nodes * T::kBytes;
-  const char* const new_v = static_cast<const char*>(a.v_new) + static_cast<size_t>(u) * a.nodes * T::kBytes;
-  typedef typename Walk<DT, HD, W>::Place Place;
-  auto request_k = [&](int t, const Place& p) {
-    const bool of_nodes = walk.is_nodes(t);
-    request_tile<DT, HD>(of_nodes ? new_k : static_cast<const char*>(a.K), p.row, p.there, tiles_addr + (t & 1) * kTileBytes, koff);
-    // (a wave-wide load of 64 words, whatever the tile; behind the unit's last slot, and for nodes, zeros)
-    if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + (t & 1) * (kWave * 4), of_nodes ? 0x7ffffffc : (walk.first_slot(t) + lane) * 4, 0);
-  };
-  auto request_v = [&](int t, const Place& p) {
-    request_tile<DT, HD>(walk.is_nodes(t) ? new_v : static_cast<const char*>(a.V), p.row, p.there, tiles_addr + (2 + (t & 1)) * kTileBytes, voff);
-  };
-
-  // B operand: the queries (lanes behind the last row repeat it; their results are dropped)
+  // B operand: the queries, a load's 16 rows of a tile as those of K (rows behind the last are zeros; their results are dropped)
+  const size_t row_base = static_cast<size_t>(u) * a.nodes * a.group;
+  const int kfrag = qi * T::kBytes + ((g ^ T::swizzle_k(qi)) << 4);
   uint4 own[NQ][T::kSteps];
-  int token[NQ];
+  constexpr int kQueryPlace = kBehindK ? 3 * kTileBytes : kBeforeK ? 2 * kTileBytes : 0;
 #pragma unroll
   for (int t2 = 0; t2 < NQ; ++t2) {
-    const int row = min(first_row + 16 * t2 + qi, rows - 1);
-    token[t2] = row / a.group;
-    const char* const q = static_cast<const char*>(a.q) + (static_cast<size_t>(u) * a.nodes * a.group + row) * T::kBytes;
+    const int row = first_row + 16 * t2;
+    const v4i32 buf = make_buffer(static_cast<const char*>(a.q) + (row_base + row) * T::kBytes, static_cast<uint32_t>(min(max(rows - row, 0), 16)) * T::kBytes);
 #pragma unroll
-    for (int kk = 0; kk < T::kSteps; ++kk) own[t2][kk] = load16(q + kk * 64 + g * 16);
+    for (int j = 0; j < T::kGroupLoads; ++j) load16_to_lds(buf, tiles_addr + kQueryPlace + (t2 * T::kGroupLoads + j) * 1024, koff[j], 0);
   }
-  uint32_t there[3] = {0, 0, 0};  // of this tile and the two behind it
-  if (mine > 0) {
-    const Place p = walk.place(0);
-    there[0] = p.there;
-    request_k(0, p);
-    request_v(0, p);
+  auto read_queries = [&]() {
+#pragma unroll
+    for (int t2 = 0; t2 < NQ; ++t2)
+#pragma unroll
+      for (int kk = 0; kk < T::kSteps; ++kk)
+        own[t2][kk] = *reinterpret_cast<const uint4*>(tiles + kQueryPlace + t2 * 16 * T::kBytes + (kfrag ^ (kk << 6)));
+    reads_done();
+  };
+  if (!kBehindK && !kBeforeK) {
+    wait_loads<0>();
+    read_queries();
   }
-  if (mine > 1) {
-    const Place p = walk.place(1);
-    there[1] = p.there;
-    request_k(1, p);
-    request_v(1, p);
-  }
+
   const float sc = a.scale_log2, rb = a.recency_bias_log2;
   const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
+  const auto token_of = [&](int t2) { return min(first_row + 16 * t2 + qi, rows - 1) / a.group; };
+  const auto see = [&]() { return seen_nodes(parent, nodes, lane); };
+  uint64_t seen = 0, special = 0;  // by node `lane`; nodes whose values are not finite
   int qp[NQ];
-  uint64_t seen = 0;  // by node `lane`
   if (WINDOW) {
-    seen = seen_nodes(a.parent != nullptr ? a.parent + static_cast<size_t>(request) * a.nodes : nullptr, nodes, lane);
+    seen = see();
 #pragma unroll
-    for (int t2 = 0; t2 < NQ; ++t2) qp[t2] = qp0 + __shfl(__builtin_popcountll(seen), token[t2], kWave) - 1;
+    for (int t2 = 0; t2 < NQ; ++t2) qp[t2] = qp0 + __shfl(__builtin_popcountll(seen), token_of(t2), kWave) - 1;
   }
   float m[NQ], l[NQ];
   f32x4 o[NQ][T::kBlocks];
@@ -124,191 +135,192 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
 #pragma unroll
     for (int db = 0; db < T::kBlocks; ++db) o[t2][db] = f32x4{0};
   }
-  const int kfrag = qi * T::kBytes + ((g ^ T::swizzle_k(qi)) << 4);
+  const v4i32 pbuf = make_buffer(a.pos + static_cast<size_t>(u) * a.B, WINDOW ? static_cast<uint32_t>(a.B) * 4u : 0u);
+  const size_t new_rows = static_cast<size_t>(u) * a.nodes * T::kBytes;
   // bf16: V^T of dimensions 0..15, rows 4 g + lane / 4 % 4, 8 bytes from column 4 (lane % 4) on; fp32: row 4 g, column lane % 16
   const int vrow = DT == kBF16 ? 4 * g + (qi >> 2) : 4 * g;
-  const int vfrag = DT == kBF16 ? vrow * T::kBytes + (T::swizzle_v(vrow) << 4) + (qi & 3) * 8 : vrow * T::kBytes + (T::swizzle_v(vrow) << 4) + qi * 4;
+  const int vfrag = vrow * T::kBytes + (T::swizzle_v(vrow) << 4) + (DT == kBF16 ? (qi & 3) * 8 : qi * 4);
 
+  uint32_t there0 = 0, there1 = 0, there2 = 0;  // of this tile and the two behind it
 #pragma unroll 1
-  for (int t = 0; t < mine; ++t) {
-    const char* const tileK = tiles + (t & 1) * kTileBytes;
-    char* const tileV = tiles + (2 + (t & 1)) * kTileBytes;
-    const bool of_nodes = walk.is_nodes(t);
-    if (t + 1 < mine) wait_loads<3 * T::kLoads + kSide>();
-    else wait_loads<T::kLoads>();
+  for (int t = -2; t < mine; ++t) {
+    char* const tileK = tiles + (t & 1) * 2 * kTileBytes;
+    char* const tileV = tileK + kTileBytes;
     f32x4 s[NQ][G];
-#pragma unroll
-    for (int kk = 0; kk < T::kSteps; ++kk) {
-#pragma unroll
-      for (int i = 0; i < G; ++i) {
-        const uint4 kf = *reinterpret_cast<const uint4*>(tileK + i * 16 * T::kBytes + (kfrag ^ (kk << 6)));
-#pragma unroll
-        for (int t2 = 0; t2 < NQ; ++t2) s[t2][i] = score_step<DT>(kf, own[t2][kk], kk == 0 ? f32x4{0} : s[t2][i]);
-      }
-    }
     int ps[G][4];
-    if (WINDOW) {
+    if (t >= 0) {
+      // K(t) has landed; V(t), and K and V of the next tile, may still be on their way
+      if (t + 1 < mine) wait_loads<3 * T::kLoads + kSide>();
+      else wait_loads<T::kLoads>();
 #pragma unroll
-      for (int i = 0; i < G; ++i) {
-        const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? wave : 0][t & 1][16 * i + 4 * g]);
-        ps[i][0] = p4.x; ps[i][1] = p4.y; ps[i][2] = p4.z; ps[i][3] = p4.w;
+      for (int kk = 0; kk < T::kSteps; ++kk) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const uint4 kf = *reinterpret_cast<const uint4*>(tileK + i * 16 * T::kBytes + (kfrag ^ (kk << 6)));
+#pragma unroll
+          for (int t2 = 0; t2 < NQ; ++t2) s[t2][i] = score_step<DT>(kf, own[t2][kk], kk == 0 ? f32x4{0} : s[t2][i]);
+        }
       }
+      if (WINDOW) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? wave : 0][t & 1][16 * i + 4 * g]);
+          ps[i][0] = p4.x; ps[i][1] = p4.y; ps[i][2] = p4.z; ps[i][3] = p4.w;
+        }
+      }
+      reads_done();
+    } else if (kBeforeK && t == -1) {
+      if (mine > 0) wait_loads<2 * T::kLoads + kSide>();
+      else wait_loads<0>();
+      read_queries();
     }
-    reads_done();
-    Place next;
+    typename Walk<DT, HD, W>::Place next;
+    bool next_nodes = false;
     if (t + 2 < mine) {
       next = walk.place(t + 2);
-      there[2] = next.there;
-      request_k(t + 2, next);
+      there2 = next.there;
+      next_nodes = walk.is_nodes(t + 2);
+      request_tile<DT, HD, STREAMING>(next_nodes ? static_cast<const char*>(a.k_new) + new_rows : static_cast<const char*>(a.K), next.row, next.there, lds_address(tileK), koff);
+      // (a wave-wide load of 64 words, whatever the tile; behind the unit's last slot, and for nodes, zeros)
+      if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + (t & 1) * (kWave * 4), next_nodes ? 0x7ffffffc : (walk.first_slot(t + 2) + lane) * 4, 0);
     }
-    // ---- base-2 logits; what a row does not see, or is not there, is -inf
-    if (of_nodes) {
-      if (!WINDOW) seen = seen_nodes(a.parent != nullptr ? a.parent + static_cast<size_t>(request) * a.nodes : nullptr, nodes, lane);
-      const int j0 = walk.first_node(t);
-#pragma unroll
-      for (int i = 0; i < G; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (WINDOW) ps[i][e] = qp0 + __shfl(__builtin_popcountll(seen), min(j0 + 16 * i + 4 * g + e, kWave - 1), kWave) - 1;
-        }
-    }
-    constexpr uint32_t kWhole = G == 1 ? 0x10u : G == 2 ? 0x1010u : 0x10101010u;
-    const bool whole = there[0] == kWhole && !of_nodes;
-#pragma unroll
-    for (int t2 = 0; t2 < NQ; ++t2) {
-      uint64_t sees = ~0ull;
-      if (of_nodes) sees = from_lane(seen, token[t2]);
-      float most = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < G; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x = s[t2][i][e] * sc;
-          if (WINDOW) {
-            const int away = qp[t2] - ps[i][e];
-            if (away >= 0 && away < w) x += rb;
-          }
-          if (!whole) {
-            const int at = 4 * g + e;
-            const bool visible = at < static_cast<int>((there[0] >> (8 * i)) & 0xffu) &&
-                                 (!of_nodes || ((sees >> (walk.first_node(t) + 16 * i + at)) & 1) != 0);
-            x = visible ? x : -INFINITY;
-          }
-          s[t2][i][e] = x;
-          most = fmaxf(most, x);
-        }
-      if (__any(most > m[t2] + kSlack)) {
-        most = fmaxf(most, __shfl_xor(most, 16, kWave));
-        most = fmaxf(most, __shfl_xor(most, 32, kWave));
-        const float m_new = most > m[t2] + kSlack ? most : m[t2];  // (a row's bits do not depend on the rows beside it)
-        const float alpha = m[t2] > -INFINITY ? fast_exp2(m[t2] - m_new) : 0.0f;
-        l[t2] *= alpha;
-#pragma unroll
-        for (int db = 0; db < T::kBlocks; ++db) o[t2][db] *= alpha;
-        m[t2] = m_new;
-      }
-      const float ref = m[t2] > -INFINITY ? m[t2] : 0.0f;  // nothing seen yet: every term is 2^-inf = 0
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < G; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[t2][i][e] = fast_exp2(s[t2][i][e] - ref);
-          sum += s[t2][i][e];
-        }
-      l[t2] += sum;
-    }
-    // ---- O^T += V^T . P^T
-    if (t + 2 < mine) wait_loads<3 * T::kLoads + 2 * kSide>();
-    else if (t + 1 < mine) wait_loads<2 * T::kLoads + kSide>();
-    else wait_loads<0>();
-    if (of_nodes) {
-      // A node's value that is infinite or NaN must not reach the rows that do not see the node, and 0 times it would: such rows are
-      // added by themselves, to the rows that see them, and zero for the products.
-      const auto special = [](const uint4& v) {
-        const auto one = [](uint32_t x) {
-          return (x & 0x7f800000u) == 0x7f800000u || (DT == kBF16 && (x & 0x7f80u) == 0x7f80u);
-        };
-        return one(v.x) || one(v.y) || one(v.z) || one(v.w);
-      };
-      bool any = false;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) any = any || special(*reinterpret_cast<const uint4*>(tileV + i * 1024 + lane * 16));
-      if (__any(any)) {
+    if (t >= 0) {
+      const bool of_nodes = walk.is_nodes(t);
+      constexpr uint32_t kWhole = G == 1 ? 0x10u : G == 2 ? 0x1010u : 0x10101010u;
+      if (of_nodes) {
+        if (!WINDOW) seen = see();
         const int j0 = walk.first_node(t);
-#pragma unroll 1
-        for (int j = 0; j < min(T::kSlots, nodes - j0); ++j) {
-          uint4* const row = reinterpret_cast<uint4*>(tileV + j * T::kBytes);
-          if (!__any(special(row[lane % T::kChunks]))) continue;
 #pragma unroll
-          for (int t2 = 0; t2 < NQ; ++t2) {
-            float p = 0.0f;
+        for (int i = 0; i < G; ++i) {
+          if (WINDOW) {
 #pragma unroll
-            for (int i = 0; i < G; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (j >> 4 == i && (j & 3) == e) p = s[t2][i][e];
-            p = __shfl(p, ((j >> 2) & 3) * 16 + qi, kWave);
-            const bool visible = ((from_lane(seen, token[t2]) >> (j0 + j)) & 1) != 0;
-#pragma unroll
-            for (int db = 0; db < T::kBlocks; ++db) {
-              f32x4 v;
-              if constexpr (DT == kBF16) {
-                const uint2 b = *reinterpret_cast<const uint2*>(tileV + j * T::kBytes + (((2 * db + (g >> 1)) ^ T::swizzle_v(j)) << 4) + (g & 1) * 8);
-                v = f32x4{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xffff0000u)};
-              } else {
-                v = *reinterpret_cast<const f32x4*>(tileV + j * T::kBytes + (((4 * db + g) ^ T::swizzle_v(j)) << 4));
-              }
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[t2][db][e] = visible ? fmaf(p, v[e], o[t2][db][e]) : o[t2][db][e];
-            }
+            for (int e = 0; e < 4; ++e) ps[i][e] = qp0 + __shfl(__builtin_popcountll(seen), min(j0 + 16 * i + 4 * g + e, kWave - 1), kWave) - 1;
           }
-          reads_done();
-          if (lane < T::kChunks) row[lane] = make_uint4(0u, 0u, 0u, 0u);
-          reads_done();
         }
-      }
-    }
-    if constexpr (DT == kBF16) {
-      // The probabilities as sums of two bf16 numbers: rounded to one they would make as much of the output's error as its own rounding
-      // (2.4e-3 against 1.7e-3 of its norm); the matrix cores have the time.
-#pragma unroll
-      for (int i = 0; i < G; i += 2) {
-        uint4 p[NQ][2];
 #pragma unroll
         for (int t2 = 0; t2 < NQ; ++t2) {
-          const f32x4 pair[2] = {s[t2][i], s[t2][i + 1]};
-          fused::split_positive(pair, p[t2]);
+          const uint64_t sees = from_lane(seen, token_of(t2)) >> j0;
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t2][i][e] = (sees >> (16 * i + 4 * g + e)) & 1 ? s[t2][i][e] : -INFINITY;
         }
+      } else if (there0 != kWhole) {
 #pragma unroll
-        for (int db = 0; db < T::kBlocks; ++db) {
-          const char* const vt = tileV + i * 16 * T::kBytes + (vfrag ^ (db << 5));
-          const uint2 lo = lds_read_transposed(vt), hi = lds_read_transposed(vt + 16 * T::kBytes);
-          const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
-#pragma unroll
-          for (int k = 1; k >= 0; --k)
-#pragma unroll
-            for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(vf, p[t2][k], o[t2][db]);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < G; ++i)
-#pragma unroll
-        for (int db = 0; db < T::kBlocks; ++db) {
-          const char* const vt = tileV + i * 16 * T::kBytes + (vfrag ^ (db << 6));
+        for (int i = 0; i < G; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = *reinterpret_cast<const float*>(vt + e * T::kBytes);
+            const bool visible = 4 * g + e < static_cast<int>((there0 >> (8 * i)) & 0xffu);
 #pragma unroll
-            for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[t2][i][e], o[t2][db], 0, 0, 0);
+            for (int t2 = 0; t2 < NQ; ++t2) s[t2][i][e] = visible ? s[t2][i][e] : -INFINITY;
+          }
+      }
+      // ---- base-2 logits and probabilities; what a row does not see is -inf
+#pragma unroll
+      for (int t2 = 0; t2 < NQ; ++t2) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = s[t2][i][e] * sc;
+            if (WINDOW) {
+              const int away = qp[t2] - ps[i][e];
+              if (away >= 0 && away < w) x += rb;
+            }
+            s[t2][i][e] = x;
+            most = fmaxf(most, x);
+          }
+        if (__any(most > m[t2] + kSlack)) {
+          most = fmaxf(most, __shfl_xor(most, 16, kWave));
+          most = fmaxf(most, __shfl_xor(most, 32, kWave));
+          const float m_new = most > m[t2] + kSlack ? most : m[t2];  // (a row's bits do not depend on the rows beside it)
+          const float alpha = m[t2] > -INFINITY ? fast_exp2(m[t2] - m_new) : 0.0f;
+          l[t2] *= alpha;
+#pragma unroll
+          for (int db = 0; db < T::kBlocks; ++db) o[t2][db] *= alpha;
+          m[t2] = m_new;
+        }
+        const float ref = m[t2] > -INFINITY ? m[t2] : 0.0f;  // nothing seen yet: every term is 2^-inf = 0
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[t2][i][e] = fast_exp2(s[t2][i][e] - ref);
+            sum += s[t2][i][e];
+          }
+        l[t2] += sum;
+      }
+      // ---- O^T += V^T . P^T
+      if (t + 2 < mine) wait_loads<3 * T::kLoads + 2 * kSide>();
+      else if (t + 1 < mine) wait_loads<2 * T::kLoads + kSide>();
+      else wait_loads<0>();
+      if (of_nodes) {
+        // A node's value that is infinite or NaN must not reach the rows that do not see the node, and 0 times it would: such nodes
+        // are zero in the products, and added in the end to the rows that see them.
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + lane * 16));
+        if (__any(any)) {
+          const int j0 = walk.first_node(t);
+#pragma unroll 1
+          for (int j = 0; j < min(T::kSlots, nodes - j0); ++j) {
+            uint4* const row = reinterpret_cast<uint4*>(tileV + j * T::kBytes) + lane % T::kChunks;
+            if (!__any(holds_special<DT>(*row))) continue;
+            special |= 1ull << (j0 + j);
+            *row = make_uint4(0u, 0u, 0u, 0u);
           }
         }
+        reads_done();
+      }
+      if constexpr (DT == kBF16) {
+        // The probabilities as sums of two bf16 numbers: rounded to one they would make as much of the output's error as its own
+        // rounding (2.4e-3 against 1.7e-3 of its norm); the matrix cores have the time.
+#pragma unroll
+        for (int i = 0; i < G; i += 2) {
+          uint4 p[NQ][2];
+#pragma unroll
+          for (int t2 = 0; t2 < NQ; ++t2) {
+            const f32x4 pair[2] = {s[t2][i], s[t2][i + 1]};
+            fused::split_positive(pair, p[t2]);
+          }
+#pragma unroll
+          for (int db = 0; db < T::kBlocks; ++db) {
+            const char* const vt = tileV + i * 16 * T::kBytes + (vfrag ^ (db << 5));
+            const uint2 lo = lds_read_transposed(vt), hi = lds_read_transposed(vt + 16 * T::kBytes);
+            const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
+#pragma unroll
+            for (int k = 1; k >= 0; --k)
+#pragma unroll
+              for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(vf, p[t2][k], o[t2][db]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int db = 0; db < T::kBlocks; ++db) {
+            const char* const vt = tileV + i * 16 * T::kBytes + (vfrag ^ (db << 6));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = *reinterpret_cast<const float*>(vt + e * T::kBytes);
+#pragma unroll
+              for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[t2][i][e], o[t2][db], 0, 0, 0);
+            }
+          }
+      }
+      reads_done();
     }
-    reads_done();
-    if (t + 2 < mine) request_v(t + 2, next);
-    there[0] = there[1];
-    there[1] = there[2];
+    if (kBehindK && t == -1) {
+      if (mine > 1) wait_loads<3 * T::kLoads + 2 * kSide>();
+      else if (mine > 0) wait_loads<2 * T::kLoads + kSide>();
+      else wait_loads<0>();
+      read_queries();
+    }
+    if (t + 2 < mine) request_tile<DT, HD, STREAMING>(next_nodes ? static_cast<const char*>(a.v_new) + new_rows : static_cast<const char*>(a.V), next.row, next.there, lds_address(tileV), voff);
+    there0 = there1;
+    there1 = there2;
   }
 #pragma unroll
   for (int t2 = 0; t2 < NQ; ++t2) {  // the lane groups have summed different slots
@@ -320,6 +332,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
   constexpr int kOut = HD + 4;
   __syncthreads();
   float* const outs = reinterpret_cast<float*>(lds);
+  if (lane == 0) special_s[wave] = special;
   if (wave == 1) {
 #pragma unroll
     for (int t2 = 0; t2 < NQ; ++t2) {
@@ -331,55 +344,90 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
   }
   __syncthreads();
   if (wave != 0) return;
+  special = special_s[0] | special_s[1];
+  const bool any_special = special != 0;
+  const size_t part_base = (static_cast<size_t>(u) * a.splits + split) * a.nodes * a.group;
 #pragma unroll
   for (int t2 = 0; t2 < NQ; ++t2) {
     const int q = 16 * t2 + qi, row = first_row + q;
-    if (row >= rows) continue;
     const float m1 = merge_m[q], l1 = merge_l[q];
     // (a maximum is -inf where a wave has seen nothing, or nothing but logits of -inf or NaN: NaN sums stay)
     const float M = fmaxf(m[t2], m1);
     const float w0 = m[t2] > -INFINITY ? fast_exp2(m[t2] - M) : 1.0f, w1 = m1 > -INFINITY ? fast_exp2(m1 - M) : 1.0f;
     const float sum = l[t2] * w0 + l1 * w1;
-    const size_t at = static_cast<size_t>(u) * a.nodes * a.group + row;
-    const size_t part = (static_cast<size_t>(u) * a.splits + split) * a.nodes * a.group + row;
-    const float scale = a.splits == 1 ? 1.0f / sum : 1.0f;
-    if (g == 0) {
-      if (a.splits == 1) {
-        if (a.lse != nullptr) a.lse[at] = kLn2 * (M + __log2f(sum));
+    const float scale = used == 1 ? 1.0f / sum : 1.0f;
+    if (g == 0 && row < rows) {
+      if (used == 1) {
+        if (a.lse != nullptr) a.lse[row_base + row] = kLn2 * (M + __log2f(sum));
       } else {
-        a.part_m[part] = M;
-        a.part_l[part] = sum;
+        a.part_m[part_base + row] = M;
+        a.part_l[part_base + row] = sum;
       }
+      merge_m[q] = M;
+      merge_l[q] = scale;
     }
 #pragma unroll
     for (int db = 0; db < T::kBlocks; ++db) {
-      const f32x4 other = *reinterpret_cast<const f32x4*>(outs + q * kOut + 16 * db + 4 * g);
-      const f32x4 v = (o[t2][db] * w0 + other * w1) * scale;
-      if (a.splits == 1) store4<DT>(a.out, at * HD + 16 * db + 4 * g, v);
-      else *reinterpret_cast<f32x4*>(a.part_o + part * HD + 16 * db + 4 * g) = v;
+      float* const at = outs + q * kOut + 16 * db + 4 * g;
+      const f32x4 v = (o[t2][db] * w0 + *reinterpret_cast<const f32x4*>(at) * w1) * scale;
+      if (any_special) *reinterpret_cast<f32x4*>(at) = v;
+      else if (row < rows && used == 1) store4<DT>(a.out, (row_base + row) * HD + 16 * db + 4 * g, v);
+      else if (row < rows) *reinterpret_cast<f32x4*>(a.part_o + (part_base + row) * HD + 16 * db + 4 * g) = v;
+    }
+  }
+  if (!any_special) return;
+  seen = see();
+  // a row at a time, HD / 64 of its elements per lane: what the nodes add that were left out
+  constexpr int E = HD / kWave;
+#pragma unroll 1
+  for (int q = 0; q < min(QR, rows - first_row); ++q) {
+    const int row = first_row + q, token = row / a.group;
+    const uint64_t sees = from_lane(seen, token);
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = outs[q * kOut + lane * E + e];
+#pragma unroll 1
+    for (uint64_t left = sees & special; left != 0; left &= left - 1) {
+      const int j = __builtin_ctzll(left);
+      const size_t node = (static_cast<size_t>(u) * a.nodes + j) * HD + lane * E;
+      float dot = 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) dot = fmaf(load_elem<DT>(a.q, (row_base + row) * HD + lane * E + e), load_elem<DT>(a.k_new, node + e), dot);
+      float x = group_sum<kWave>(dot) * sc;
+      if (WINDOW && __builtin_popcountll(sees) - __builtin_popcountll(from_lane(seen, j)) < w) x += rb;
+      const float p = fast_exp2(x - (merge_m[q] > -INFINITY ? merge_m[q] : 0.0f)) * merge_l[q];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = fmaf(p, load_elem<DT>(a.v_new, node + e), v[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (used == 1) store_elem<DT>(a.out, (row_base + row) * HD + lane * E + e, v[e]);
+      else a.part_o[(part_base + row) * HD + lane * E + e] = v[e];
     }
   }
 }
 
 #pragma clang diagnostic pop
 
-template <int DT, int HD, int NQ, bool WINDOW> hipError_t launch_attend(const TreeArgs& a, hipStream_t s) {
+template <int DT, int HD, int NQ, bool STREAMING, bool WINDOW> hipError_t launch_attend(const TreeArgs& a, hipStream_t s) {
   constexpr int kLds = kAttendWaves * 4 * 8192;
   static_assert(16 * NQ * (HD + 4) * 4 <= kLds, "a wave's outputs take the tiles' place");
-  const void* const fn = reinterpret_cast<const void*>(tree_attend<DT, HD, NQ, WINDOW>);
+  const void* const fn = reinterpret_cast<const void*>(tree_attend<DT, HD, NQ, STREAMING, WINDOW>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) return hipErrorInvalidValue;
   const int per = 8 * a.row_tiles;
   const unsigned blocks = static_cast<unsigned>((static_cast<long long>(a.units) * a.splits + 7) / 8 * per);
-  hipLaunchKernelGGL((tree_attend<DT, HD, NQ, WINDOW>), dim3(blocks), dim3(kAttendThreads), kLds, s, a);
+  hipLaunchKernelGGL((tree_attend<DT, HD, NQ, STREAMING, WINDOW>), dim3(blocks), dim3(kAttendThreads), kLds, s, a);
   return hipGetLastError();
 }
 
+template <int DT, int HD, int NQ> hipError_t launch_attend_form(const TreeArgs& a, hipStream_t s) {
+  if (a.recency_window > 0) return a.streaming ? launch_attend<DT, HD, NQ, true, true>(a, s) : launch_attend<DT, HD, NQ, false, true>(a, s);
+  return a.streaming ? launch_attend<DT, HD, NQ, true, false>(a, s) : launch_attend<DT, HD, NQ, false, false>(a, s);
+}
 // Query rows of a workgroup: up to 64, in tiles of 16.
 template <int DT, int HD> hipError_t launch_attend_rows(const TreeArgs& a, hipStream_t s) {
   const int rows = a.nodes * a.group;
-  if (a.recency_window > 0)
-    return rows <= 16 ? launch_attend<DT, HD, 1, true>(a, s) : rows <= 32 ? launch_attend<DT, HD, 2, true>(a, s) : launch_attend<DT, HD, 4, true>(a, s);
-  return rows <= 16 ? launch_attend<DT, HD, 1, false>(a, s) : rows <= 32 ? launch_attend<DT, HD, 2, false>(a, s) : launch_attend<DT, HD, 4, false>(a, s);
+  return rows <= 16 ? launch_attend_form<DT, HD, 1>(a, s) : rows <= 32 ? launch_attend_form<DT, HD, 2>(a, s) : launch_attend_form<DT, HD, 4>(a, s);
 }
 
 }  // namespace tree

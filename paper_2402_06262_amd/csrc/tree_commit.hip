@@ -121,7 +121,7 @@ constexpr size_t kMostQueryLds = 40960;  // bytes of accepted query rows that ar
 // The accepted rows in tiles of 16 tokens of one head.  A head's probabilities are formed a tile at a time and added up over the heads
 // in registers: Q is the A operand here, so that a lane holds four tokens of one slot and the sum over the tokens is over its registers
 // and two exchanges.  STAGED: the query rows are in LDS (they fit), else read where they are.
-template <int DT, int HD, bool WINDOW, bool STAGED>
+template <int DT, int HD, bool STREAMING, bool WINDOW, bool STAGED>
 __global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a) {
   using T = Tile<DT, HD>;
   constexpr int W = kStatWaves, G = T::kGroups, kTileBytes = 8192;
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a)
   uint32_t there[3] = {0, 0, 0};
   auto request_k = [&](int t) {
     const Place p = walk.place(t);
-    request_tile<DT, HD>(a.K, p.row, p.there, tiles_addr + (t & 1) * kTileBytes, koff);
+    request_tile<DT, HD, STREAMING>(a.K, p.row, p.there, tiles_addr + (t & 1) * kTileBytes, koff);
     return p.there;
   };
   if (mine > 0) there[0] = request_k(0);
@@ -285,12 +285,18 @@ __global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a)
 
 #pragma clang diagnostic pop
 
-template <int DT, int HD, bool WINDOW, bool STAGED> hipError_t launch_statistics(const CommitArgs& a, size_t lds, hipStream_t s) {
+template <int DT, int HD, bool STREAMING, bool WINDOW, bool STAGED> hipError_t launch_statistics(const CommitArgs& a, size_t lds, hipStream_t s) {
   constexpr int kMost = kStatWaves * 2 * 8192 + static_cast<int>(kMostQueryLds) + kMaxTreeNodes * kMaxTreeGroup * 4;
-  const void* const fn = reinterpret_cast<const void*>(tree_statistics<DT, HD, WINDOW, STAGED>);
+  const void* const fn = reinterpret_cast<const void*>(tree_statistics<DT, HD, STREAMING, WINDOW, STAGED>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kMost) != hipSuccess) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((tree_statistics<DT, HD, WINDOW, STAGED>), dim3(static_cast<unsigned>(a.units) * a.splits), dim3(kStatThreads), lds, s, a);
+  hipLaunchKernelGGL((tree_statistics<DT, HD, STREAMING, WINDOW, STAGED>), dim3(static_cast<unsigned>(a.units) * a.splits), dim3(kStatThreads), lds, s, a);
   return hipGetLastError();
+}
+
+template <int DT, int HD, bool STREAMING> hipError_t launch_statistics_form(const CommitArgs& a, bool staged, size_t lds, hipStream_t s) {
+  if (a.recency_window > 0)
+    return staged ? launch_statistics<DT, HD, STREAMING, true, true>(a, lds, s) : launch_statistics<DT, HD, STREAMING, true, false>(a, lds, s);
+  return staged ? launch_statistics<DT, HD, STREAMING, false, true>(a, lds, s) : launch_statistics<DT, HD, STREAMING, false, false>(a, lds, s);
 }
 
 template <int DT, int HD> hipError_t launch_commit(const CommitArgs& a, hipStream_t s) {
@@ -311,8 +317,7 @@ template <int DT, int HD> hipError_t launch_commit(const CommitArgs& a, hipStrea
   const size_t rows = static_cast<size_t>(a.group) * ((a.max_path + 15) / 16 * 16);
   const bool staged = rows * kRowBytes <= kMostQueryLds;
   const size_t lds = kStatWaves * 2 * 8192 + (staged ? rows * kRowBytes : 0) + rows * 4;
-  if (a.recency_window > 0) return staged ? launch_statistics<DT, HD, true, true>(a, lds, s) : launch_statistics<DT, HD, true, false>(a, lds, s);
-  return staged ? launch_statistics<DT, HD, false, true>(a, lds, s) : launch_statistics<DT, HD, false, false>(a, lds, s);
+  return a.streaming ? launch_statistics_form<DT, HD, true>(a, staged, lds, s) : launch_statistics_form<DT, HD, false>(a, staged, lds, s);
 }
 
 }  // namespace
