@@ -128,7 +128,7 @@ struct TreeLayout { size_t part_l, part_o, keys, total; TreeSplits split; };
 TreeLayout tree_layout(const roco_params* p, int32_t group, int32_t nodes) {
   TreeLayout l;
   const size_t U = p->units, B = p->budget, rows = static_cast<size_t>(group) * nodes;
-  l.split = tree_attend_splits(p->units, group * nodes, p->budget);
+  l.split = tree_attend_splits(p->dtype, p->units, group * nodes, p->budget, p->recency_window > 0);
   const size_t plane = l.split.splits == 1 ? 0 : align_up(U * l.split.splits * rows * sizeof(float));
   l.part_l = plane;
   l.part_o = 2 * plane;
@@ -530,7 +530,7 @@ int roco_tree_attend(const roco_params* params, int32_t heads, int32_t group, in
   a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
   a.splits = lay.split.splits;
   a.chunk = lay.split.chunk;
-  a.row_tiles = tree_attend_row_tiles(group * nodes);
+  a.row_tiles = tree_attend_row_tiles(params->dtype, group * nodes, params->recency_window > 0);
   a.streaming = a.row_tiles == 1 && streaming_loads(params) ? 1 : 0;  // (several row tiles find the rows in their die's L2)
   a.scale_log2 = scale_log2(params);
   a.recency_window = params->recency_window;

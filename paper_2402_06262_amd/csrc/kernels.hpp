@@ -200,9 +200,9 @@ struct TreeArgs {
   float* part_o;                              // [units][splits][nodes * group][d], not yet divided
 };
 hipError_t launch_tree_attend(int dtype, int head_dim, const TreeArgs& a, hipStream_t s);
-int tree_attend_row_tiles(int rows);
+int tree_attend_row_tiles(int dtype, int rows, bool window);
 struct TreeSplits { int splits, chunk; };
-TreeSplits tree_attend_splits(int units, int rows, int B);
+TreeSplits tree_attend_splits(int dtype, int units, int rows, int B, bool window);
 
 struct CommitArgs {
   int units, heads, group, nodes, B, scope, max_path;

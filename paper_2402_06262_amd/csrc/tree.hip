@@ -75,15 +75,22 @@ template <int DT, int HD> hipError_t launch_join(const TreeArgs& a, hipStream_t 
 
 }  // namespace
 
-int tree_attend_row_tiles(int rows) { return rows <= 64 ? 1 : (rows + 63) / 64; }
+// Query rows of a workgroup: 64, or of bf16 192 (128 with a recency window, whose code has no registers for the third tile of a wave).
+int tree_attend_row_tiles(int dtype, int rows, bool window) {
+  const int most = dtype != kBF16 || rows <= 64 ? 64 : window ? 128 : 192;
+  return (rows + most - 1) / most;
+}
 
-// Two workgroups of two waves on every compute unit, while each has 64 slots.
-TreeSplits tree_attend_splits(int units, int rows, int B) {
+// Two workgroups on every compute unit, while each has 64 slots (256 and more rows: while it has 256, and four of them, since they take
+// turns).
+TreeSplits tree_attend_splits(int dtype, int units, int rows, int B, bool window) {
   const char* const asked = getenv("ROCO_TREE_SPLITS");
   int want = asked != nullptr ? atoi(asked) : 0;
+  const bool wide = dtype == kBF16 && rows > 64;
   if (want <= 0) {
-    const long long groups = static_cast<long long>(units) * tree_attend_row_tiles(rows);
-    want = static_cast<int>((512 + groups - 1) / groups);
+    const long long groups = static_cast<long long>(units) * tree_attend_row_tiles(dtype, rows, window);
+    want = static_cast<int>(((wide ? 1024 : 512) + groups - 1) / groups);
+    if (wide) want = std::min(want, (B + 255) / 256);
   }
   want = std::max(1, std::min({want, kMaxTreeSplits, (B + 63) / 64}));
   TreeSplits s;

@@ -89,13 +89,13 @@ __device__ __forceinline__ int splits_used(int n, int chunk) { return max((n + c
 template <int DT, int HD, int W> struct Walk {
   using T = Tile<DT, HD>;
   static constexpr int G = T::kGroups;
-  static constexpr int kAhead = kWave / G;  // tiles whose pages a register holds
+  typedef const __attribute__((address_space(4))) int32_t* Table;  // (constant: read by scalar loads, which the tiles' loads do not wait for)
   int row0, row1, cache_tiles, mine, rot, wave, nodes;
   uint32_t first_row;     // without a table: row of the unit's slot 0
   int head, heads, page_log2, n_pages;
-  const int32_t* table;   // the request's, or null
-  int entries[2];         // lane i: page of group i % G of tile kAhead b + i / G, b even or odd
-  int loaded;             // blocks of entries so far
+  bool paged;
+  Table table;            // the request's
+  int ahead[G];           // pages of the groups of the tile that is asked for next
 
   __device__ __forceinline__ void init(const CachePages& pages, int B, int heads_, int unit, int request, int row0_, int row1_, int nodes_, int wave_, unsigned start) {
     row0 = row0_; row1 = row1_; nodes = nodes_; wave = wave_;
@@ -108,9 +108,9 @@ template <int DT, int HD, int W> struct Walk {
     head = unit - request * heads;
     page_log2 = pages.page_log2;
     n_pages = pages.n_pages;
-    table = pages.table != nullptr ? pages.table + static_cast<size_t>(request) * pages.max_pages : nullptr;
-    entries[0] = entries[1] = -1;
-    loaded = 0;
+    paged = pages.table != nullptr;
+    table = (Table)(pages.table + static_cast<size_t>(request) * pages.max_pages);
+    look_ahead(0);
   }
   __device__ __forceinline__ int index(int t) const {  // among the workgroup's tiles
     int i = t + rot;
@@ -120,49 +120,46 @@ template <int DT, int HD, int W> struct Walk {
   __device__ __forceinline__ bool is_nodes(int t) const { return index(t) >= cache_tiles; }
   __device__ __forceinline__ int first_slot(int t) const { return row0 + index(t) * T::kSlots; }
   __device__ __forceinline__ int first_node(int t) const { return (index(t) - cache_tiles) * T::kSlots; }
+  __device__ __forceinline__ void look_ahead(int t) {
+    if (!paged || cache_tiles == 0) return;
+#pragma unroll
+    for (int i = 0; i < G; ++i) ahead[i] = table[min(first_slot(t) + 16 * i, row1 - 1) >> page_log2];
+  }
 
   // Rows of the groups of tile t in their array, and how many of each are there (a byte each).
   struct Place { uint32_t row[G]; uint32_t there; };
   __device__ __forceinline__ Place place(int t) {
     Place p;
     p.there = 0;
-    if (is_nodes(t)) {
-      const int j = first_node(t);
-#pragma unroll
-      for (int i = 0; i < G; ++i) {
-        p.row[i] = static_cast<uint32_t>(j + 16 * i);
-        p.there |= static_cast<uint32_t>(min(max(nodes - j - 16 * i, 0), 16)) << (8 * i);
-      }
-      return p;
-    }
-    if (table != nullptr && t / kAhead >= loaded) {
-      const int lane = threadIdx.x & (kWave - 1);
-      const int mt = loaded * kAhead + lane / G;
-      const int slot = first_slot(min(mt, mine - 1)) + 16 * (lane % G);
-      int e = -1;
-      if (mt < mine && !is_nodes(mt) && slot < row1) e = table[slot >> page_log2];
-      if (loaded & 1) entries[1] = e;
-      else entries[0] = e;
-      ++loaded;
-    }
-    const int slot0 = first_slot(t);
+    const bool of_nodes = is_nodes(t);
+    const int first = of_nodes ? first_node(t) : first_slot(t), end = of_nodes ? nodes : row1;
 #pragma unroll
     for (int i = 0; i < G; ++i) {
-      const int slot = slot0 + 16 * i;
-      int there = min(max(row1 - slot, 0), 16);
-      uint32_t row = first_row + static_cast<uint32_t>(slot);
-      if (table != nullptr) {
-        const int at = (t % kAhead) * G + i;
-        const int page = __builtin_amdgcn_readlane((t / kAhead) & 1 ? entries[1] : entries[0], at);
+      const int slot = first + 16 * i;
+      int there = min(max(end - slot, 0), 16);
+      uint32_t row = (of_nodes ? 0u : first_row) + static_cast<uint32_t>(slot);
+      if (paged && !of_nodes) {
+        const int page = ahead[i];
         if (page < 0 || page >= n_pages) there = 0;  // such a page is not touched, and what it would hold is not seen
-        row = (static_cast<uint32_t>(max(page, 0) * heads + head) << page_log2) + static_cast<uint32_t>(slot & ((1 << page_log2) - 1));
+        row = (static_cast<uint32_t>(page * heads + head) << page_log2) + static_cast<uint32_t>(slot & ((1 << page_log2) - 1));
       }
       p.row[i] = there > 0 ? row : 0u;
       p.there |= static_cast<uint32_t>(there) << (8 * i);
     }
+    if (t + 1 < mine) look_ahead(t + 1);
     return p;
   }
 };
+
+// 16 bytes at an LDS address.
+__device__ __forceinline__ uint4 lds_read16(uint32_t addr) {
+  typedef const __attribute__((address_space(3))) mfma::v4i32 lds_v4i32;
+  return __builtin_bit_cast(uint4, *(lds_v4i32*)(static_cast<uintptr_t>(addr)));
+}
+__device__ __forceinline__ uint2 lds_read_transposed_at(uint32_t addr) {
+  const mfma::v4i16 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mfma::lds_v4i16*)(static_cast<uintptr_t>(addr)));
+  return __builtin_bit_cast(uint2, v);
+}
 
 // Byte offsets inside a group's rows of the chunks that this lane fetches with the group's loads.
 template <int DT, int HD, bool VALUES> __device__ __forceinline__ void load_offsets(int* off) {

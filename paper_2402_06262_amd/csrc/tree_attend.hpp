@@ -42,9 +42,56 @@ template <int DT> __device__ __forceinline__ bool holds_special(const uint4& v) 
   };
   return ((one(v.x) | one(v.y) | one(v.z) | one(v.w)) & 0x80000000u) != 0;
 }
+// What is derived from these is computed where it is used, not kept in registers through the loop: for what only some tiles need.
+struct LateLane {
+  int lane, qi, g;
+  __device__ __forceinline__ LateLane() : lane(late_thread_id() & (kWave - 1)), qi(lane & 15), g(lane >> 4) {}
+};
+__device__ __forceinline__ int late(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
+
 template <int DT> __device__ __forceinline__ float load_elem(const void* base, size_t idx) {
   if constexpr (DT == kBF16) return bf16_to_f32(static_cast<const uint16_t*>(base)[idx]);
   else return static_cast<const float*>(base)[idx];
+}
+
+// The nodes whose values are not finite, added to the rows that see them: `count` rows from `first` on, which the wave has written without
+// them, a row at a time, HD / 64 of its elements per lane.  max_s, scale_s: the rows' maxima, and what they were multiplied by.  (Final rows
+// of bf16 are rounded twice where they see such a node.)
+template <int DT, int HD, bool WINDOW>
+__device__ __forceinline__ void add_special_nodes(const TreeArgs& a, int u, size_t out_row, size_t part_row, int first, int count, int used, uint64_t seen,
+                                                  uint64_t special, const float* max_s, const float* scale_s) {
+  constexpr int E = HD / kWave;
+  __threadfence_block();
+  const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll 1
+  for (int q = 0; q < count; ++q) {
+    const uint64_t sees = from_lane(seen, (first + q) / a.group);
+    if ((sees & special) == 0) continue;
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = used == 1 ? load_elem<DT>(a.out, (out_row + q) * HD + lane * E + e) : a.part_o[(part_row + q) * HD + lane * E + e];
+#pragma unroll 1
+    for (uint64_t left = sees & special; left != 0; left &= left - 1) {
+      const int j = __builtin_ctzll(left);
+      const size_t node = (static_cast<size_t>(u) * a.nodes + j) * HD + lane * E;
+      float dot = 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) dot = fmaf(load_elem<DT>(a.q, (out_row + q) * HD + lane * E + e), load_elem<DT>(a.k_new, node + e), dot);
+      float x = group_sum<kWave>(dot) * a.scale_log2;
+      if (WINDOW && __builtin_popcountll(sees) - __builtin_popcountll(from_lane(seen, j)) < a.recency_window) x += a.recency_bias_log2;
+      const float p = fast_exp2(x - (max_s[q] > -INFINITY ? max_s[q] : 0.0f)) * scale_s[q];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = fmaf(p, load_elem<DT>(a.v_new, node + e), v[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (used == 1) store_elem<DT>(a.out, (out_row + q) * HD + lane * E + e, v[e]);
+      else a.part_o[(part_row + q) * HD + lane * E + e] = v[e];
+    }
+  }
 }
 
 // NQ tiles of 16 query rows; a row is a node and a head of the group.  WINDOW: a recency bias is in force.
@@ -115,16 +162,16 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
     read_queries();
   }
 
-  const float sc = a.scale_log2, rb = a.recency_bias_log2;
+  const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 / sc : 0.0f;  // (the products are multiplied by sc where they become exponents)
   const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
-  const auto token_of = [&](int t2) { return min(first_row + 16 * t2 + qi, rows - 1) / a.group; };
-  const auto see = [&]() { return seen_nodes(parent, nodes, lane); };
+  const auto token_of = [&](int t2, int q) { return min(first_row + 16 * t2 + q, rows - 1) / late(a.group); };
+  const auto see = [&]() { return seen_nodes(parent, nodes, LateLane().lane); };
   uint64_t seen = 0, special = 0;  // by node `lane`; nodes whose values are not finite
   int qp[NQ];
   if (WINDOW) {
     seen = see();
 #pragma unroll
-    for (int t2 = 0; t2 < NQ; ++t2) qp[t2] = qp0 + __shfl(__builtin_popcountll(seen), token_of(t2), kWave) - 1;
+    for (int t2 = 0; t2 < NQ; ++t2) qp[t2] = qp0 + __shfl(__builtin_popcountll(seen), token_of(t2, qi), kWave) - 1;
   }
   float m[NQ], l[NQ];
   f32x4 o[NQ][T::kBlocks];
@@ -190,32 +237,34 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
       if (of_nodes) {
         if (!WINDOW) seen = see();
         const int j0 = walk.first_node(t);
+        const LateLane L;
 #pragma unroll
         for (int i = 0; i < G; ++i) {
           if (WINDOW) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ps[i][e] = qp0 + __shfl(__builtin_popcountll(seen), min(j0 + 16 * i + 4 * g + e, kWave - 1), kWave) - 1;
+            for (int e = 0; e < 4; ++e) ps[i][e] = qp0 + __shfl(__builtin_popcountll(seen), min(j0 + 16 * i + 4 * L.g + e, kWave - 1), kWave) - 1;
           }
         }
 #pragma unroll
         for (int t2 = 0; t2 < NQ; ++t2) {
-          const uint64_t sees = from_lane(seen, token_of(t2)) >> j0;
+          const uint64_t sees = from_lane(seen, token_of(t2, L.qi)) >> (j0 + 4 * L.g);
 #pragma unroll
           for (int i = 0; i < G; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t2][i][e] = (sees >> (16 * i + 4 * g + e)) & 1 ? s[t2][i][e] : -INFINITY;
+            for (int e = 0; e < 4; ++e) s[t2][i][e] = (sees >> (16 * i + e)) & 1 ? s[t2][i][e] : -INFINITY;
         }
       } else if (there0 != kWhole) {
+        const LateLane L;
 #pragma unroll
         for (int i = 0; i < G; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool visible = 4 * g + e < static_cast<int>((there0 >> (8 * i)) & 0xffu);
+            const bool visible = 4 * L.g + e < static_cast<int>((there0 >> (8 * i)) & 0xffu);
 #pragma unroll
             for (int t2 = 0; t2 < NQ; ++t2) s[t2][i][e] = visible ? s[t2][i][e] : -INFINITY;
           }
       }
-      // ---- base-2 logits and probabilities; what a row does not see is -inf
+      // ---- probabilities; what a row does not see is -inf
 #pragma unroll
       for (int t2 = 0; t2 < NQ; ++t2) {
         float most = -INFINITY;
@@ -223,14 +272,13 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
         for (int i = 0; i < G; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            float x = s[t2][i][e] * sc;
             if (WINDOW) {
               const int away = qp[t2] - ps[i][e];
-              if (away >= 0 && away < w) x += rb;
+              s[t2][i][e] += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
             }
-            s[t2][i][e] = x;
-            most = fmaxf(most, x);
+            most = fmaxf(most, s[t2][i][e]);
           }
+        most *= sc;
         if (__any(most > m[t2] + kSlack)) {
           most = fmaxf(most, __shfl_xor(most, 16, kWave));
           most = fmaxf(most, __shfl_xor(most, 32, kWave));
@@ -247,7 +295,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
         for (int i = 0; i < G; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[t2][i][e] = fast_exp2(s[t2][i][e] - ref);
+            s[t2][i][e] = fast_exp2(fmaf(s[t2][i][e], sc, -ref));
             sum += s[t2][i][e];
           }
         l[t2] += sum;
@@ -260,13 +308,14 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
         // A node's value that is infinite or NaN must not reach the rows that do not see the node, and 0 times it would: such nodes
         // are zero in the products, and added in the end to the rows that see them.
         bool any = false;
+        const LateLane L;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + lane * 16));
+        for (int i = 0; i < 8; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + L.lane * 16));
         if (__any(any)) {
           const int j0 = walk.first_node(t);
 #pragma unroll 1
           for (int j = 0; j < min(T::kSlots, nodes - j0); ++j) {
-            uint4* const row = reinterpret_cast<uint4*>(tileV + j * T::kBytes) + lane % T::kChunks;
+            uint4* const row = reinterpret_cast<uint4*>(tileV + j * T::kBytes) + L.lane % T::kChunks;
             if (!__any(holds_special<DT>(*row))) continue;
             special |= 1ull << (j0 + j);
             *row = make_uint4(0u, 0u, 0u, 0u);
@@ -345,7 +394,6 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
   __syncthreads();
   if (wave != 0) return;
   special = special_s[0] | special_s[1];
-  const bool any_special = special != 0;
   const size_t part_base = (static_cast<size_t>(u) * a.splits + split) * a.nodes * a.group;
 #pragma unroll
   for (int t2 = 0; t2 < NQ; ++t2) {
@@ -368,43 +416,312 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
     }
 #pragma unroll
     for (int db = 0; db < T::kBlocks; ++db) {
-      float* const at = outs + q * kOut + 16 * db + 4 * g;
-      const f32x4 v = (o[t2][db] * w0 + *reinterpret_cast<const f32x4*>(at) * w1) * scale;
-      if (any_special) *reinterpret_cast<f32x4*>(at) = v;
-      else if (row < rows && used == 1) store4<DT>(a.out, (row_base + row) * HD + 16 * db + 4 * g, v);
+      const f32x4 v = (o[t2][db] * w0 + *reinterpret_cast<const f32x4*>(outs + q * kOut + 16 * db + 4 * g) * w1) * scale;
+      if (row < rows && used == 1) store4<DT>(a.out, (row_base + row) * HD + 16 * db + 4 * g, v);
       else if (row < rows) *reinterpret_cast<f32x4*>(a.part_o + (part_base + row) * HD + 16 * db + 4 * g) = v;
     }
   }
-  if (!any_special) return;
-  seen = see();
-  // a row at a time, HD / 64 of its elements per lane: what the nodes add that were left out
-  constexpr int E = HD / kWave;
+  if (special != 0)
+    add_special_nodes<DT, HD, WINDOW>(a, u, row_base + first_row, part_base + first_row, first_row, min(QR, rows - first_row), used, see(), special, merge_m, merge_l);
+}
+
+// More than 64 query rows of bf16: four waves with 16 NQ rows each share the tiles, which come in a ring of three, a quarter of each by every
+// wave; one barrier per tile.  Two workgroups on a compute unit, so that one wave's exponentials run beside another's products: with 64
+// rows to a workgroup and the rest in others, every row tile fetched K and V again, and a wave had its matrix cores to itself.
+// Here the matrix cores are what the step waits for, so that probabilities are rounded to one bf16 number each (2^-9 of each; the
+// outputs, sums over many, are 2.4e-3 of their norm off instead of 1.7e-3, their own rounding): the second number would be a third more
+// products and as much vector work again.
+constexpr int kWideWaves = 4;
+constexpr int kWideThreads = kWideWaves * kWave;
+constexpr int kWideStages = 3;
+
+template <int HD, int NQ, bool WINDOW>
+__global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) {
+  constexpr int DT = kBF16;
+  using T = Tile<DT, HD>;
+  constexpr int W = kWideWaves, G = T::kGroups, QR = 16 * NQ;  // query rows of a wave
+  constexpr int kTileBytes = 8192, kStageBytes = 2 * kTileBytes;
+  constexpr int kMyLoads = T::kLoads / W;                      // of an operand's tile
+  constexpr int kSide = WINDOW ? 1 : 0;
+  static_assert(kMyLoads <= T::kGroupLoads, "a wave's loads lie in one group");
+  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the ring
+  __shared__ __attribute__((aligned(256))) int32_t pos_s[WINDOW ? W : 1][kWideStages][kWave];
+  __shared__ float max_s[W][QR], scale_s[W][QR];
+  const int per = 8 * a.row_tiles, id = blockIdx.x;
+  const int us = id / per * 8 + id % 8, row_tile = id % per / 8;
+  if (us >= a.units * a.splits) return;
+  const int u = us / a.splits, split = us % a.splits;
+  const int request = u / a.heads;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int qi = lane & 15, g = lane >> 4;
+  const int asked_nodes = a.n_nodes != nullptr ? a.n_nodes[request] : a.nodes, held = a.n_used[u], budget = budget_of(a.pages, a.B, request);
+  const int nodes = __builtin_amdgcn_readfirstlane(min(max(asked_nodes, 0), a.nodes));
+  const int n = __builtin_amdgcn_readfirstlane(min(max(held, 0), budget));
+  const int rows = nodes * a.group, first_row = row_tile * W * QR + wave * QR;
+  const int used = splits_used(n, a.chunk);
+  if (row_tile * W * QR >= rows || split >= used) return;
+  const int row0 = split * a.chunk, row1 = min(n, row0 + a.chunk);
+  Walk<DT, HD, 1> walk;
+  walk.init(a.pages, a.B, a.heads, u, request, row0, row1, split == used - 1 ? nodes : 0, 0, static_cast<unsigned>(u) * 5u + static_cast<unsigned>(split) * 3u);
+  const int tiles = walk.mine;
+
+  int koff[T::kGroupLoads];
+  load_offsets<DT, HD, false>(koff);
+  const size_t row_base = static_cast<size_t>(u) * a.nodes * a.group;
+  const int kfrag = qi * T::kBytes + ((g ^ T::swizzle_k(qi)) << 4);
+  // the wave's queries come through its share of the ring (12 KiB, 16 rows of up to 4 KiB at a time), before any tile
+  uint4 own[NQ][T::kSteps];
+  {
+    static_assert(QR * T::kBytes <= kWideStages * kStageBytes / W, "the wave's share of the ring");
+    char* const place = lds + wave * (kWideStages * kStageBytes / W);
+#pragma unroll
+    for (int t2 = 0; t2 < NQ; ++t2) {
+      const int row = first_row + 16 * t2;
+      const v4i32 buf = make_buffer(static_cast<const char*>(a.q) + (row_base + min(row, rows - 1)) * T::kBytes, static_cast<uint32_t>(min(max(rows - row, 0), 16)) * T::kBytes);
+#pragma unroll
+      for (int j = 0; j < T::kGroupLoads; ++j) load16_to_lds(buf, lds_address(place) + (t2 * T::kGroupLoads + j) * 1024, koff[j], 0);
+    }
+    wait_loads<0>();
+#pragma unroll
+    for (int t2 = 0; t2 < NQ; ++t2)
+#pragma unroll
+      for (int kk = 0; kk < T::kSteps; ++kk) own[t2][kk] = *reinterpret_cast<const uint4*>(place + t2 * 16 * T::kBytes + (kfrag ^ (kk << 6)));
+    reads_done();
+    __syncthreads();
+  }
+  const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 / sc : 0.0f;
+  const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
+  const auto token_of = [&](int t2, int q) { return min(first_row + 16 * t2 + q, rows - 1) / late(a.group); };
+  uint64_t seen = 0, special = 0;
+  const auto see = [&]() {
+    const int node = LateLane().lane;
+    return seen_nodes(a.parent != nullptr ? a.parent[static_cast<size_t>(request) * a.nodes + min(node, a.nodes - 1)] : node - 1, nodes, node);
+  };
+  int qp[NQ];
+  if (WINDOW) {
+    seen = see();
+#pragma unroll
+    for (int t2 = 0; t2 < NQ; ++t2) qp[t2] = qp0 + __shfl(__builtin_popcountll(seen), token_of(t2, qi), kWave) - 1;
+  }
+  float m[NQ], l[NQ];
+  f32x4 o[NQ][T::kBlocks];
+#pragma unroll
+  for (int t2 = 0; t2 < NQ; ++t2) {
+    m[t2] = -INFINITY;
+    l[t2] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < T::kBlocks; ++db) o[t2][db] = f32x4{0};
+  }
+  const v4i32 pbuf = make_buffer(a.pos + static_cast<size_t>(u) * a.B, WINDOW ? static_cast<uint32_t>(a.B) * 4u : 0u);
+  const uint32_t pos_addr = lds_address(&pos_s[WINDOW ? wave : 0][0][0]), ring_addr = lds_address(lds);
+  const size_t new_rows = static_cast<size_t>(u) * a.nodes * T::kBytes;
+  const int my_group = wave * kMyLoads / T::kGroupLoads, my_first = wave * kMyLoads % T::kGroupLoads;  // of a tile's loads
+
+  uint32_t there0 = 0, there1 = 0, there2 = 0;
 #pragma unroll 1
-  for (int q = 0; q < min(QR, rows - first_row); ++q) {
-    const int row = first_row + q, token = row / a.group;
-    const uint64_t sees = from_lane(seen, token);
-    float v[E];
+  for (int t = -2; t < tiles; ++t) {
+    if (t >= 0) {  // this tile has landed, and nobody reads the one before it any more
+      if (t + 1 < tiles) wait_loads<2 * kMyLoads + kSide>();
+      else wait_loads<0>();
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    if (t + 2 < tiles) {
+      const typename Walk<DT, HD, 1>::Place next = walk.place(t + 2);
+      const bool next_nodes = walk.is_nodes(t + 2);
+      there2 = next.there;
+      uint32_t row = next.row[0];
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = outs[q * kOut + lane * E + e];
+      for (int i = 1; i < G; ++i) row = my_group == i ? next.row[i] : row;
+      const uint32_t bytes = ((next.there >> (8 * my_group)) & 0xffu) * T::kBytes;
+      const size_t at = next_nodes ? new_rows + static_cast<size_t>(row) * T::kBytes : static_cast<size_t>(row) * T::kBytes;
+      const v4i32 kbuf = make_buffer(static_cast<const char*>(next_nodes ? a.k_new : a.K) + at, bytes);
+      const v4i32 vbuf = make_buffer(static_cast<const char*>(next_nodes ? a.v_new : a.V) + at, bytes);
+      const uint32_t stage = ring_addr + static_cast<uint32_t>((t + 2) % kWideStages) * kStageBytes + wave * kMyLoads * 1024;
+      const int lane2 = LateLane().lane;
+#pragma unroll
+      for (int j = 0; j < kMyLoads; ++j) {
+        const int r = T::kPerLoad * (my_first + j) + lane2 / T::kChunks, c = lane2 % T::kChunks;
+        load16_to_lds(kbuf, stage + j * 1024, r * T::kBytes + ((c ^ T::swizzle_k(r)) << 4), 0);
+        load16_to_lds(vbuf, stage + kTileBytes + j * 1024, r * T::kBytes + ((c ^ T::swizzle_v(r)) << 4), 0);
+      }
+      if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + ((t + 2) % kWideStages) * (kWave * 4), next_nodes ? 0x7ffffffc : (walk.first_slot(t + 2) + lane) * 4, 0);
+    }
+    if (t >= 0) {
+      char* const tileV = lds + t % kWideStages * kStageBytes + kTileBytes;
+      // (the tiles lie at multiples of 1 KiB: the chunk's exclusive or can be taken of the address)
+      const LateLane F;
+      const int vrow = 4 * F.g + (F.qi >> 2);
+      const uint32_t stage = ring_addr + static_cast<uint32_t>(t % kWideStages) * kStageBytes;
+      const uint32_t k_at = stage + F.qi * T::kBytes + ((F.g ^ T::swizzle_k(F.qi)) << 4);
+      const uint32_t v_at = stage + kTileBytes + vrow * T::kBytes + (T::swizzle_v(vrow) << 4) + (F.qi & 3) * 8;
+      // (fragments are read a step ahead and no further: the scheduler would take all registers for them, and more)
+      f32x4 s[NQ][G];
+      uint4 kf[2][G];
+      const auto read_k = [&](int kk) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) kf[kk & 1][i] = lds_read16((k_at ^ (kk << 6)) + i * 16 * T::kBytes);
+      };
+      read_k(0);
+#pragma unroll
+      for (int kk = 0; kk < T::kSteps; ++kk) {
+        if (kk + 1 < T::kSteps) read_k(kk + 1);
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int t2 = 0; t2 < NQ; ++t2) s[t2][i] = score_step<DT>(kf[kk & 1][i], own[t2][kk], kk == 0 ? f32x4{0} : s[t2][i]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const bool of_nodes = walk.is_nodes(t);
+      constexpr uint32_t kWhole = G == 1 ? 0x10u : G == 2 ? 0x1010u : 0x10101010u;
+      if (of_nodes) {
+        const LateLane L;
+        if (!WINDOW) seen = see();
+        const int j0 = walk.first_node(t);
+#pragma unroll
+        for (int t2 = 0; t2 < NQ; ++t2) {
+          const uint64_t sees = from_lane(seen, token_of(t2, L.qi)) >> (j0 + 4 * L.g);
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if (WINDOW) {
+                const int away = qp[t2] - qp0 + 1 - __shfl(__builtin_popcountll(seen), min(j0 + 16 * i + 4 * L.g + e, kWave - 1), kWave);
+                s[t2][i][e] += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
+              }
+              s[t2][i][e] = (sees >> (16 * i + e)) & 1 ? s[t2][i][e] : -INFINITY;
+            }
+        }
+        // (see tree_attend; the rows are everybody's)
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + L.lane * 16));
+        if (__any(any)) {
 #pragma unroll 1
-    for (uint64_t left = sees & special; left != 0; left &= left - 1) {
-      const int j = __builtin_ctzll(left);
-      const size_t node = (static_cast<size_t>(u) * a.nodes + j) * HD + lane * E;
-      float dot = 0.0f;
+          for (int j = 0; j < min(T::kSlots, nodes - j0); ++j)
+            if (__any(holds_special<DT>(*(reinterpret_cast<const uint4*>(tileV + j * T::kBytes) + L.lane % T::kChunks)))) special |= 1ull << (j0 + j);
+          __syncthreads();
+          if (wave == 0) {
+#pragma unroll 1
+            for (int j = 0; j < min(T::kSlots, nodes - j0); ++j)
+              if ((special >> (j0 + j)) & 1) reinterpret_cast<uint4*>(tileV + j * T::kBytes)[L.lane % T::kChunks] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          __syncthreads();
+        }
+      } else {
+        if (WINDOW) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) dot = fmaf(load_elem<DT>(a.q, (row_base + row) * HD + lane * E + e), load_elem<DT>(a.k_new, node + e), dot);
-      float x = group_sum<kWave>(dot) * sc;
-      if (WINDOW && __builtin_popcountll(sees) - __builtin_popcountll(from_lane(seen, j)) < w) x += rb;
-      const float p = fast_exp2(x - (merge_m[q] > -INFINITY ? merge_m[q] : 0.0f)) * merge_l[q];
+          for (int i = 0; i < G; ++i) {
+            const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? wave : 0][t % kWideStages][16 * i + 4 * g]);
+            const int ps[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = fmaf(p, load_elem<DT>(a.v_new, node + e), v[e]);
+            for (int t2 = 0; t2 < NQ; ++t2)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int away = qp[t2] - ps[e];
+                s[t2][i][e] += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
+              }
+          }
+        }
+        if (there0 != kWhole) {
+          const LateLane L;
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool visible = 4 * L.g + e < static_cast<int>((there0 >> (8 * i)) & 0xffu);
+#pragma unroll
+              for (int t2 = 0; t2 < NQ; ++t2) s[t2][i][e] = visible ? s[t2][i][e] : -INFINITY;
+            }
+        }
+      }
+#pragma unroll
+      for (int t2 = 0; t2 < NQ; ++t2) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most = fmaxf(most, s[t2][i][e]);
+        most *= sc;
+        if (__any(most > m[t2] + kSlack)) {
+          most = fmaxf(most, __shfl_xor(most, 16, kWave));
+          most = fmaxf(most, __shfl_xor(most, 32, kWave));
+          const float m_new = most > m[t2] + kSlack ? most : m[t2];
+          const float alpha = m[t2] > -INFINITY ? fast_exp2(m[t2] - m_new) : 0.0f;
+          l[t2] *= alpha;
+#pragma unroll
+          for (int db = 0; db < T::kBlocks; ++db) o[t2][db] *= alpha;
+          m[t2] = m_new;
+        }
+        const float ref = m[t2] > -INFINITY ? m[t2] : 0.0f;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[t2][i][e] = fast_exp2(fmaf(s[t2][i][e], sc, -ref));
+            sum += s[t2][i][e];
+          }
+        l[t2] += sum;
+      }
+#pragma unroll
+      for (int i = 0; i < G; i += 2) {
+        uint4 p[NQ];
+#pragma unroll
+        for (int t2 = 0; t2 < NQ; ++t2) {
+          mfma::bf16x8 r;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) r[e] = static_cast<__bf16>(s[t2][i + (e >> 2)][e & 3]);
+          p[t2] = __builtin_bit_cast(uint4, r);
+        }
+        uint4 vf[2];
+        const auto read_v = [&](int db) {
+          const uint32_t vt = (v_at ^ (db << 5)) + i * 16 * T::kBytes;
+          const uint2 lo = lds_read_transposed_at(vt), hi = lds_read_transposed_at(vt + 16 * T::kBytes);
+          vf[db & 1] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        };
+        read_v(0);
+#pragma unroll
+        for (int db = 0; db < T::kBlocks; ++db) {
+          if (db + 1 < T::kBlocks) read_v(db + 1);
+#pragma unroll
+          for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(vf[db & 1], p[t2], o[t2][db]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    there0 = there1;
+    there1 = there2;
+  }
+  const LateLane L;
+  const size_t part_base = (static_cast<size_t>(u) * a.splits + split) * a.nodes * a.group;
+#pragma unroll
+  for (int t2 = 0; t2 < NQ; ++t2) {
+    const int row = first_row + 16 * t2 + L.qi;
+    float sum = l[t2];
+    sum += __shfl_xor(sum, 16, kWave);
+    sum += __shfl_xor(sum, 32, kWave);
+    const float scale = used == 1 ? 1.0f / sum : 1.0f;
+    if (L.g == 0) {
+      if (row < rows) {
+        if (used == 1) {
+          if (a.lse != nullptr) a.lse[row_base + row] = kLn2 * (m[t2] + __log2f(sum));
+        } else {
+          a.part_m[part_base + row] = m[t2];
+          a.part_l[part_base + row] = sum;
+        }
+      }
+      max_s[wave][16 * t2 + L.qi] = m[t2];
+      scale_s[wave][16 * t2 + L.qi] = scale;
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (used == 1) store_elem<DT>(a.out, (row_base + row) * HD + lane * E + e, v[e]);
-      else a.part_o[(part_base + row) * HD + lane * E + e] = v[e];
+    for (int db = 0; db < T::kBlocks; ++db) {
+      const f32x4 v = o[t2][db] * scale;
+      if (row < rows && used == 1) store4<DT>(a.out, (row_base + row) * HD + 16 * db + 4 * L.g, v);
+      else if (row < rows) *reinterpret_cast<f32x4*>(a.part_o + (part_base + row) * HD + 16 * db + 4 * L.g) = v;
     }
   }
+  if (special != 0)
+    add_special_nodes<DT, HD, WINDOW>(a, u, row_base + first_row, part_base + first_row, first_row, min(QR, rows - first_row), used, see(), special, max_s[wave], scale_s[wave]);
 }
 
 #pragma clang diagnostic pop
@@ -420,13 +737,30 @@ template <int DT, int HD, int NQ, bool STREAMING, bool WINDOW> hipError_t launch
   return hipGetLastError();
 }
 
+template <int HD, int NQ, bool WINDOW> hipError_t launch_attend_wide(const TreeArgs& a, hipStream_t s) {
+  constexpr int kLds = kWideStages * 2 * 8192;
+  const void* const fn = reinterpret_cast<const void*>(tree_attend_wide<HD, NQ, WINDOW>);
+  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) return hipErrorInvalidValue;
+  const int per = 8 * a.row_tiles;
+  const unsigned blocks = static_cast<unsigned>((static_cast<long long>(a.units) * a.splits + 7) / 8 * per);
+  hipLaunchKernelGGL((tree_attend_wide<HD, NQ, WINDOW>), dim3(blocks), dim3(kWideThreads), kLds, s, a);
+  return hipGetLastError();
+}
+
 template <int DT, int HD, int NQ> hipError_t launch_attend_form(const TreeArgs& a, hipStream_t s) {
   if (a.recency_window > 0) return a.streaming ? launch_attend<DT, HD, NQ, true, true>(a, s) : launch_attend<DT, HD, NQ, false, true>(a, s);
   return a.streaming ? launch_attend<DT, HD, NQ, true, false>(a, s) : launch_attend<DT, HD, NQ, false, false>(a, s);
 }
-// Query rows of a workgroup: up to 64, in tiles of 16.
+// Query rows of a workgroup: up to 64, in tiles of 16; bf16 with more: up to 192.
 template <int DT, int HD> hipError_t launch_attend_rows(const TreeArgs& a, hipStream_t s) {
   const int rows = a.nodes * a.group;
+  if constexpr (DT == kBF16) {
+    if (rows > 64) {
+      const bool three = (rows + a.row_tiles - 1) / a.row_tiles > 128;
+      if (a.recency_window > 0) return launch_attend_wide<HD, 2, true>(a, s);
+      return three ? launch_attend_wide<HD, 3, false>(a, s) : launch_attend_wide<HD, 2, false>(a, s);
+    }
+  }
   return rows <= 16 ? launch_attend_form<DT, HD, 1>(a, s) : rows <= 32 ? launch_attend_form<DT, HD, 2>(a, s) : launch_attend_form<DT, HD, 4>(a, s);
 }
 

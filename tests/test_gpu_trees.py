@@ -3,7 +3,9 @@
 Tolerances, from the roundings of the two storage types and of fp32 (u = 2^-24):
   logits   a product of d terms in fp32, scaled: within x = (d + 8) u L, L the row's largest scale sum |q k|; 2^x then moves a probability by a
            factor of x (natural logarithm), the exponential's and the sum's own roundings by (8 + sqrt of the number of terms) u
-  outputs  rel = 2 x + (8 + 2 sqrt n) u of sum p |v|; probabilities as two bf16 numbers 2^-16 of it more; half a step of the type
+  outputs  rel = 2 x + (8 + 2 sqrt n) u of sum p |v|; probabilities as two bf16 numbers 2^-16 of it more; half a step of the type.  With more
+           than 64 query rows of bf16 they are one bf16 number each: p (1 + e) with |e| <= 2^-8, half a step, so that sum p v is off by at most
+           2^-8 sum p |v|, and their sum, which divides, is that of the unrounded ones: 2^-8 of sum p |v| in all
   lse      x + (8 + sqrt n) u + 2^-22 |lse|
   Acc      what a step adds: 2 x + 2^-21 of it, and half a step of the sum; Acc2 twice that
 """
@@ -135,7 +137,7 @@ class Step:
             w = self.want(u)
             n = self.used[u // self.heads] + t
             x = (self.d + 8) * U * w.logit
-            rel = 2 * x + (8 + 2 * math.sqrt(n)) * U + (2.0 ** -16 if self.dtype == "bf16" else 0)
+            rel = 2 * x + (8 + 2 * math.sqrt(n)) * U + (0 if self.dtype == "f32" else 2.0 ** -16 if self.T * self.group <= 64 else 2.0 ** -8)
             half = 2.0 ** -8 if self.dtype == "bf16" else U
             err = np.abs(out[u, :t] - w.out)
             tol = rel * w.mass + half * np.abs(w.out) + 1e-30
