@@ -81,16 +81,14 @@ int tree_attend_row_tiles(int dtype, int rows, bool window) {
   return (rows + most - 1) / most;
 }
 
-// Two workgroups on every compute unit, while each has 64 slots (256 and more rows: while it has 256, and four of them, since they take
-// turns).
+// Two workgroups on every compute unit, while each has 64 slots (with more than 64 rows of bf16 192: its share of the outputs is larger).
 TreeSplits tree_attend_splits(int dtype, int units, int rows, int B, bool window) {
   const char* const asked = getenv("ROCO_TREE_SPLITS");
   int want = asked != nullptr ? atoi(asked) : 0;
-  const bool wide = dtype == kBF16 && rows > 64;
   if (want <= 0) {
     const long long groups = static_cast<long long>(units) * tree_attend_row_tiles(dtype, rows, window);
-    want = static_cast<int>(((wide ? 1024 : 512) + groups - 1) / groups);
-    if (wide) want = std::min(want, (B + 255) / 256);
+    want = static_cast<int>((512 + groups - 1) / groups);
+    if (dtype == kBF16 && rows > 64) want = std::min(want, (B + 191) / 192);
   }
   want = std::max(1, std::min({want, kMaxTreeSplits, (B + 63) / 64}));
   TreeSplits s;

@@ -75,6 +75,18 @@ __device__ __forceinline__ uint64_t from_lane(uint64_t v, int lane) {
   return lo | static_cast<uint64_t>(hi) << 32;
 }
 
+// Minimum and maximum of values that are the same for all lanes: the compiler forms a clamp on the vector ALU.
+__device__ __forceinline__ int uniform_min(int a, int b) {
+  int r;
+  asm("s_min_i32 %0, %1, %2" : "=s"(r) : "s"(a), "s"(b) : "scc");
+  return r;
+}
+__device__ __forceinline__ int uniform_max(int a, int b) {
+  int r;
+  asm("s_max_i32 %0, %1, %2" : "=s"(r) : "s"(a), "s"(b) : "scc");
+  return r;
+}
+
 // Slots of a request's units, and how many of them a unit uses.
 __device__ __forceinline__ int budget_of(const CachePages& pages, int B, int request) {
   return pages.budget != nullptr ? min(max(pages.budget[request], 0), B) : B;
@@ -123,7 +135,7 @@ template <int DT, int HD, int W> struct Walk {
   __device__ __forceinline__ void look_ahead(int t) {
     if (!paged || cache_tiles == 0) return;
 #pragma unroll
-    for (int i = 0; i < G; ++i) ahead[i] = table[min(first_slot(t) + 16 * i, row1 - 1) >> page_log2];
+    for (int i = 0; i < G; ++i) ahead[i] = table[uniform_min(first_slot(t) + 16 * i, row1 - 1) >> page_log2];
   }
 
   // Rows of the groups of tile t in their array, and how many of each are there (a byte each).
@@ -136,7 +148,7 @@ template <int DT, int HD, int W> struct Walk {
 #pragma unroll
     for (int i = 0; i < G; ++i) {
       const int slot = first + 16 * i;
-      int there = min(max(end - slot, 0), 16);
+      int there = uniform_min(uniform_max(end - slot, 0), 16);
       uint32_t row = (of_nodes ? 0u : first_row) + static_cast<uint32_t>(slot);
       if (paged && !of_nodes) {
         const int page = ahead[i];

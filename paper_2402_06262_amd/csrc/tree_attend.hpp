@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
   const int per = 8 * a.row_tiles, id = blockIdx.x;
   const int us = id / per * 8 + id % 8, row_tile = id % per / 8;
   if (us >= a.units * a.splits) return;
-  const int u = us / a.splits, split = us % a.splits;
+  const int u = us % a.units, split = us / a.units;  // (the later splits, which not every unit needs, come last and to all dies)
   const int request = u / a.heads;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int qi = lane & 15, g = lane >> 4;
@@ -425,32 +425,31 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
     add_special_nodes<DT, HD, WINDOW>(a, u, row_base + first_row, part_base + first_row, first_row, min(QR, rows - first_row), used, see(), special, merge_m, merge_l);
 }
 
-// More than 64 query rows of bf16: four waves with 16 NQ rows each share the tiles, which come in a ring of three, a quarter of each by every
-// wave; one barrier per tile.  Two workgroups on a compute unit, so that one wave's exponentials run beside another's products: with 64
+// More than 64 query rows of bf16: four waves with 16 NQ rows each share the tiles, which come two at a time, a quarter of each by every
+// wave, while the two before them are used; one barrier for two tiles.  Two workgroups on a compute unit, so that one wave's exponentials run beside another's products: with 64
 // rows to a workgroup and the rest in others, every row tile fetched K and V again, and a wave had its matrix cores to itself.
 // Here the matrix cores are what the step waits for, so that probabilities are rounded to one bf16 number each (2^-9 of each; the
 // outputs, sums over many, are 2.4e-3 of their norm off instead of 1.7e-3, their own rounding): the second number would be a third more
 // products and as much vector work again.
 constexpr int kWideWaves = 4;
 constexpr int kWideThreads = kWideWaves * kWave;
-constexpr int kWideStages = 3;
 
 template <int HD, int NQ, bool WINDOW>
 __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) {
   constexpr int DT = kBF16;
   using T = Tile<DT, HD>;
   constexpr int W = kWideWaves, G = T::kGroups, QR = 16 * NQ;  // query rows of a wave
-  constexpr int kTileBytes = 8192, kStageBytes = 2 * kTileBytes;
+  constexpr int kTileBytes = 8192, kPairBytes = 2 * kTileBytes;  // a tile of K and one of V
   constexpr int kMyLoads = T::kLoads / W;                      // of an operand's tile
   constexpr int kSide = WINDOW ? 1 : 0;
   static_assert(kMyLoads <= T::kGroupLoads, "a wave's loads lie in one group");
-  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the ring
-  __shared__ __attribute__((aligned(256))) int32_t pos_s[WINDOW ? W : 1][kWideStages][kWave];
+  extern __shared__ __attribute__((aligned(1024))) char lds[];  // four pairs of tiles: two in use, two on their way
+  __shared__ __attribute__((aligned(256))) int32_t pos_s[WINDOW ? W : 1][4][kWave];
   __shared__ float max_s[W][QR], scale_s[W][QR];
   const int per = 8 * a.row_tiles, id = blockIdx.x;
   const int us = id / per * 8 + id % 8, row_tile = id % per / 8;
   if (us >= a.units * a.splits) return;
-  const int u = us / a.splits, split = us % a.splits;
+  const int u = us % a.units, split = us / a.units;  // (the later splits, which not every unit needs, come last and to all dies)
   const int request = u / a.heads;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int qi = lane & 15, g = lane >> 4;
@@ -469,11 +468,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
   load_offsets<DT, HD, false>(koff);
   const size_t row_base = static_cast<size_t>(u) * a.nodes * a.group;
   const int kfrag = qi * T::kBytes + ((g ^ T::swizzle_k(qi)) << 4);
-  // the wave's queries come through its share of the ring (12 KiB, 16 rows of up to 4 KiB at a time), before any tile
+  // the wave's queries come through a pair's place, before any tile
   uint4 own[NQ][T::kSteps];
   {
-    static_assert(QR * T::kBytes <= kWideStages * kStageBytes / W, "the wave's share of the ring");
-    char* const place = lds + wave * (kWideStages * kStageBytes / W);
+    static_assert(QR * T::kBytes <= kPairBytes, "a pair's place");
+    char* const place = lds + wave * kPairBytes;
 #pragma unroll
     for (int t2 = 0; t2 < NQ; ++t2) {
       const int row = first_row + 16 * t2;
@@ -517,43 +516,49 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
   const size_t new_rows = static_cast<size_t>(u) * a.nodes * T::kBytes;
   const int my_group = wave * kMyLoads / T::kGroupLoads, my_first = wave * kMyLoads % T::kGroupLoads;  // of a tile's loads
 
-  uint32_t there0 = 0, there1 = 0, there2 = 0;
+  uint32_t there[2] = {0, 0}, there_next[2] = {0, 0};
 #pragma unroll 1
-  for (int t = -2; t < tiles; ++t) {
-    if (t >= 0) {  // this tile has landed, and nobody reads the one before it any more
-      if (t + 1 < tiles) wait_loads<2 * kMyLoads + kSide>();
-      else wait_loads<0>();
+  for (int t0 = -2; t0 < tiles; t0 += 2) {
+    if (t0 >= 0) {  // these tiles have landed, and nobody reads those before them any more
+      wait_loads<0>();
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
-    if (t + 2 < tiles) {
-      const typename Walk<DT, HD, 1>::Place next = walk.place(t + 2);
-      const bool next_nodes = walk.is_nodes(t + 2);
-      there2 = next.there;
+#pragma unroll 1
+    for (int sub = 0; sub < 2; ++sub) {
+      const int t = t0 + 2 + sub;
+      if (t >= tiles) break;
+      const typename Walk<DT, HD, 1>::Place next = walk.place(t);
+      const bool next_nodes = walk.is_nodes(t);
+      if (sub == 0) there_next[0] = next.there;
+      else there_next[1] = next.there;
       uint32_t row = next.row[0];
 #pragma unroll
       for (int i = 1; i < G; ++i) row = my_group == i ? next.row[i] : row;
       const uint32_t bytes = ((next.there >> (8 * my_group)) & 0xffu) * T::kBytes;
-      const size_t at = next_nodes ? new_rows + static_cast<size_t>(row) * T::kBytes : static_cast<size_t>(row) * T::kBytes;
+      const size_t at = (next_nodes ? new_rows : 0) + static_cast<size_t>(row) * T::kBytes;
       const v4i32 kbuf = make_buffer(static_cast<const char*>(next_nodes ? a.k_new : a.K) + at, bytes);
       const v4i32 vbuf = make_buffer(static_cast<const char*>(next_nodes ? a.v_new : a.V) + at, bytes);
-      const uint32_t stage = ring_addr + static_cast<uint32_t>((t + 2) % kWideStages) * kStageBytes + wave * kMyLoads * 1024;
+      const uint32_t pair = ring_addr + static_cast<uint32_t>(t & 3) * kPairBytes + wave * kMyLoads * 1024;
       const int lane2 = LateLane().lane;
 #pragma unroll
       for (int j = 0; j < kMyLoads; ++j) {
         const int r = T::kPerLoad * (my_first + j) + lane2 / T::kChunks, c = lane2 % T::kChunks;
-        load16_to_lds(kbuf, stage + j * 1024, r * T::kBytes + ((c ^ T::swizzle_k(r)) << 4), 0);
-        load16_to_lds(vbuf, stage + kTileBytes + j * 1024, r * T::kBytes + ((c ^ T::swizzle_v(r)) << 4), 0);
+        load16_to_lds(kbuf, pair + j * 1024, r * T::kBytes + ((c ^ T::swizzle_k(r)) << 4), 0);
+        load16_to_lds(vbuf, pair + kTileBytes + j * 1024, r * T::kBytes + ((c ^ T::swizzle_v(r)) << 4), 0);
       }
-      if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + ((t + 2) % kWideStages) * (kWave * 4), next_nodes ? 0x7ffffffc : (walk.first_slot(t + 2) + lane) * 4, 0);
+      if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + (t & 3) * (kWave * 4), next_nodes ? 0x7ffffffc : (walk.first_slot(t) + lane) * 4, 0);
     }
-    if (t >= 0) {
-      char* const tileV = lds + t % kWideStages * kStageBytes + kTileBytes;
+#pragma unroll 1
+    for (int sub = 0; sub < 2; ++sub) {
+      const int t = t0 + sub;
+      if (t < 0 || t >= tiles) break;
+      char* const tileV = lds + (t & 3) * kPairBytes + kTileBytes;
       // (the tiles lie at multiples of 1 KiB: the chunk's exclusive or can be taken of the address)
       const LateLane F;
       const int vrow = 4 * F.g + (F.qi >> 2);
-      const uint32_t stage = ring_addr + static_cast<uint32_t>(t % kWideStages) * kStageBytes;
-      const uint32_t k_at = stage + F.qi * T::kBytes + ((F.g ^ T::swizzle_k(F.qi)) << 4);
-      const uint32_t v_at = stage + kTileBytes + vrow * T::kBytes + (T::swizzle_v(vrow) << 4) + (F.qi & 3) * 8;
+      const uint32_t pair = ring_addr + static_cast<uint32_t>(t & 3) * kPairBytes;
+      const uint32_t k_at = pair + F.qi * T::kBytes + ((F.g ^ T::swizzle_k(F.qi)) << 4);
+      const uint32_t v_at = pair + kTileBytes + vrow * T::kBytes + (T::swizzle_v(vrow) << 4) + (F.qi & 3) * 8;
       // (fragments are read a step ahead and no further: the scheduler would take all registers for them, and more)
       f32x4 s[NQ][G];
       uint4 kf[2][G];
@@ -573,65 +578,55 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
       }
       const bool of_nodes = walk.is_nodes(t);
       constexpr uint32_t kWhole = G == 1 ? 0x10u : G == 2 ? 0x1010u : 0x10101010u;
-      if (of_nodes) {
+      const uint32_t here = sub == 0 ? there[0] : there[1];
+      if (WINDOW) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? wave : 0][t & 3][16 * i + 4 * g]);
+          int ps[4] = {p4.x, p4.y, p4.z, p4.w};
+          if (of_nodes) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ps[e] = qp0 - 1 + __shfl(__builtin_popcountll(seen), min(walk.first_node(t) + 16 * i + 4 * g + e, kWave - 1), kWave);
+          }
+#pragma unroll
+          for (int t2 = 0; t2 < NQ; ++t2)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t2][i][e] += static_cast<unsigned>(qp[t2] - ps[e]) < static_cast<unsigned>(w) ? bias : 0.0f;
+        }
+      }
+      if (of_nodes || here != kWhole) {
         const LateLane L;
-        if (!WINDOW) seen = see();
         const int j0 = walk.first_node(t);
+        if (of_nodes && !WINDOW) seen = see();
+        uint64_t there4 = 0;  // bit 16 i + e: slot 4 g + e of group i is there
+#pragma unroll
+        for (int i = 0; i < G; ++i) there4 |= static_cast<uint64_t>(0xffffu >> (16 - ((here >> (8 * i)) & 0xffu))) << (16 * i);
+        there4 >>= 4 * L.g;
 #pragma unroll
         for (int t2 = 0; t2 < NQ; ++t2) {
-          const uint64_t sees = from_lane(seen, token_of(t2, L.qi)) >> (j0 + 4 * L.g);
+          uint64_t visible = there4;
+          if (of_nodes) visible &= from_lane(seen, token_of(t2, L.qi)) >> (j0 + 4 * L.g);
 #pragma unroll
           for (int i = 0; i < G; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (WINDOW) {
-                const int away = qp[t2] - qp0 + 1 - __shfl(__builtin_popcountll(seen), min(j0 + 16 * i + 4 * L.g + e, kWave - 1), kWave);
-                s[t2][i][e] += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
-              }
-              s[t2][i][e] = (sees >> (16 * i + e)) & 1 ? s[t2][i][e] : -INFINITY;
-            }
+            for (int e = 0; e < 4; ++e) s[t2][i][e] = (visible >> (16 * i + e)) & 1 ? s[t2][i][e] : -INFINITY;
         }
-        // (see tree_attend; the rows are everybody's)
-        bool any = false;
+        if (of_nodes) {  // (see tree_attend; the rows are everybody's)
+          bool any = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + L.lane * 16));
-        if (__any(any)) {
-#pragma unroll 1
-          for (int j = 0; j < min(T::kSlots, nodes - j0); ++j)
-            if (__any(holds_special<DT>(*(reinterpret_cast<const uint4*>(tileV + j * T::kBytes) + L.lane % T::kChunks)))) special |= 1ull << (j0 + j);
-          __syncthreads();
-          if (wave == 0) {
+          for (int i = 0; i < 8; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + L.lane * 16));
+          if (__any(any)) {
 #pragma unroll 1
             for (int j = 0; j < min(T::kSlots, nodes - j0); ++j)
-              if ((special >> (j0 + j)) & 1) reinterpret_cast<uint4*>(tileV + j * T::kBytes)[L.lane % T::kChunks] = make_uint4(0u, 0u, 0u, 0u);
-          }
-          __syncthreads();
-        }
-      } else {
-        if (WINDOW) {
-#pragma unroll
-          for (int i = 0; i < G; ++i) {
-            const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? wave : 0][t % kWideStages][16 * i + 4 * g]);
-            const int ps[4] = {p4.x, p4.y, p4.z, p4.w};
-#pragma unroll
-            for (int t2 = 0; t2 < NQ; ++t2)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int away = qp[t2] - ps[e];
-                s[t2][i][e] += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
-              }
-          }
-        }
-        if (there0 != kWhole) {
-          const LateLane L;
-#pragma unroll
-          for (int i = 0; i < G; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const bool visible = 4 * L.g + e < static_cast<int>((there0 >> (8 * i)) & 0xffu);
-#pragma unroll
-              for (int t2 = 0; t2 < NQ; ++t2) s[t2][i][e] = visible ? s[t2][i][e] : -INFINITY;
+              if (__any(holds_special<DT>(*(reinterpret_cast<const uint4*>(tileV + j * T::kBytes) + L.lane % T::kChunks)))) special |= 1ull << (j0 + j);
+            __syncthreads();
+            if (wave == 0) {
+#pragma unroll 1
+              for (int j = 0; j < min(T::kSlots, nodes - j0); ++j)
+                if ((special >> (j0 + j)) & 1) reinterpret_cast<uint4*>(tileV + j * T::kBytes)[L.lane % T::kChunks] = make_uint4(0u, 0u, 0u, 0u);
             }
+            __syncthreads();
+          }
         }
       }
 #pragma unroll
@@ -689,8 +684,8 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
         }
       }
     }
-    there0 = there1;
-    there1 = there2;
+    there[0] = there_next[0];
+    there[1] = there_next[1];
   }
   const LateLane L;
   const size_t part_base = (static_cast<size_t>(u) * a.splits + split) * a.nodes * a.group;
@@ -738,7 +733,7 @@ template <int DT, int HD, int NQ, bool STREAMING, bool WINDOW> hipError_t launch
 }
 
 template <int HD, int NQ, bool WINDOW> hipError_t launch_attend_wide(const TreeArgs& a, hipStream_t s) {
-  constexpr int kLds = kWideStages * 2 * 8192;
+  constexpr int kLds = 4 * 2 * 8192;
   const void* const fn = reinterpret_cast<const void*>(tree_attend_wide<HD, NQ, WINDOW>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) return hipErrorInvalidValue;
   const int per = 8 * a.row_tiles;
