@@ -16,61 +16,82 @@ hipError_t launch_tree_attend_f32_64(const TreeArgs& a, hipStream_t s);
 namespace {
 
 constexpr int kJoinThreads = 256;
+constexpr int kJoinAhead = 4;  // of a lane's loads
 
-// A wave per query row: its splits' maxima and sums, a lane each, then their outputs, weighted, in the order of the splits.
-template <int DT, int HD> __global__ __launch_bounds__(kJoinThreads) void tree_join(TreeArgs a) {
-  constexpr int E = HD / kWave;
+// WAVES waves per query row: its splits' maxima and sums, a lane each, then their outputs, weighted.  HD / 4 lanes take a split's 16 bytes at a
+// time, so that a wave has 2 or 4 splits in hand; the sums over the lanes and the waves have a fixed order.  What bounds it is the
+// latency of its loads: one wave per row with two of a split's elements per lane took 14 us for 1024 rows of 32 splits.
+template <int DT, int HD, int WAVES> __global__ __launch_bounds__(kJoinThreads) void tree_join(TreeArgs a) {
+  constexpr int LANES = HD / 4, PER = kWave / LANES, STEP = PER * WAVES * kJoinAhead;
+  constexpr int ROWS = kJoinThreads / kWave / WAVES;  // of a workgroup
+  __shared__ __attribute__((aligned(16))) float other_s[WAVES > 1 ? ROWS * WAVES : 1][WAVES > 1 ? HD : 1];
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  const int part = wave % WAVES;
   const int all = a.nodes * a.group;
-  const long long id = static_cast<long long>(blockIdx.x) * (kJoinThreads / kWave) + wave;
+  const long long id = static_cast<long long>(blockIdx.x) * ROWS + wave / WAVES;
   const int u = static_cast<int>(id / all), row = static_cast<int>(id % all);
-  if (u >= a.units) return;
+  if (u >= a.units) return;  // (a row's waves go together: with several of them a workgroup has one row)
   const int request = u / a.heads;
   const int nodes = a.n_nodes != nullptr ? min(max(a.n_nodes[request], 0), a.nodes) : a.nodes;
-  if (row >= nodes * a.group) return;
   const int splits = tree::splits_used(min(max(a.n_used[u], 0), tree::budget_of(a.pages, a.B, request)), a.chunk);
-  if (splits == 1) return;  // has written its rows
+  if (row >= nodes * a.group || splits == 1) return;  // (the only split has written its rows)
   const size_t first = static_cast<size_t>(u) * a.splits * all + row;  // of split 0; the others `all` further each
   float m = -INFINITY, l = 0.0f;
   if (lane < splits) {
     m = a.part_m[first + static_cast<size_t>(lane) * all];
     l = a.part_l[first + static_cast<size_t>(lane) * all];
   }
-  const float M = group_max<kWave>(m);
-  const float w = m > -INFINITY ? fast_exp2(m - M) : 1.0f;  // (a split of no maximum has a sum of zero, or NaN)
-  const float sum = group_sum<kWave>(l * w);
-  float o[E];
+  const int col = lane % LANES * 4, mine = lane / LANES * WAVES + part;  // this lane's splits: mine, mine + PER * WAVES, ...
+  tree::f32x4 o = tree::f32x4{0};
+  float M = 0.0f, w = 0.0f;
+#pragma unroll 1
+  for (int i0 = 0; i0 < splits; i0 += STEP) {
+    tree::f32x4 v[kJoinAhead];
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.0f;
-  for (int i0 = 0; i0 < splits; i0 += 4) {  // four at a time: behind the last split its outputs again, with nothing of them
-    float v[4][E];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float* const p = a.part_o + (first + static_cast<size_t>(min(i0 + k, splits - 1)) * all) * HD + lane * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = p[e];
+    for (int k = 0; k < kJoinAhead; ++k) {
+      const int i = min(i0 + mine + k * PER * WAVES, splits - 1);
+      v[k] = *reinterpret_cast<const tree::f32x4*>(a.part_o + (first + static_cast<size_t>(i) * all) * HD + col);
+    }
+    if (i0 == 0) {
+      M = group_max<kWave>(m);
+      w = m > -INFINITY ? fast_exp2(m - M) : 1.0f;  // (a split of no maximum has a sum of zero, or NaN)
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float wk = __shfl(w, min(i0 + k, kWave - 1), kWave);
-      if (i0 + k >= splits) break;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = fmaf(wk, v[k][e], o[e]);
+    for (int k = 0; k < kJoinAhead; ++k) {
+      const int i = i0 + mine + k * PER * WAVES;
+      const float wk = __shfl(w, min(i, kWave - 1), kWave);
+      if (i < splits) o += v[k] * wk;
     }
   }
-  const float scale = 1.0f / sum;
-  const size_t at = static_cast<size_t>(u) * all + row;
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_elem<DT>(a.out, at * HD + lane * E + e, o[e] * scale);
+  for (int step = LANES; step < kWave; step *= 2) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], step, kWave);
+  }
+  if (WAVES > 1) {
+    if (lane < LANES) *reinterpret_cast<tree::f32x4*>(&other_s[wave][WAVES > 1 ? col : 0]) = o;
+    __syncthreads();
+    if (part != 0) return;
+    o = tree::f32x4{0};
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) o += *reinterpret_cast<const tree::f32x4*>(&other_s[WAVES > 1 ? wave + k : 0][WAVES > 1 ? col : 0]);
+  }
+  const float sum = group_sum<kWave>(l * w);
+  const size_t at = static_cast<size_t>(u) * all + row;
+  if (lane < LANES) tree::store4<DT>(a.out, at * HD + col, o * (1.0f / sum));
   if (a.lse != nullptr && lane == 0) a.lse[at] = 0.6931471805599453f * (M + __log2f(sum));
 }
 
+template <int DT, int HD, int WAVES> hipError_t launch_join_waves(const TreeArgs& a, hipStream_t s) {
+  constexpr int kRows = kJoinThreads / kWave / WAVES;
+  const long long rows = static_cast<long long>(a.units) * a.nodes * a.group;
+  hipLaunchKernelGGL((tree_join<DT, HD, WAVES>), dim3(static_cast<unsigned>((rows + kRows - 1) / kRows)), dim3(kJoinThreads), 0, s, a);
+  return hipGetLastError();
+}
+// Four waves per row where the splits are many: then the rows are few.
 template <int DT, int HD> hipError_t launch_join(const TreeArgs& a, hipStream_t s) {
   ProfScope ps(kProfTreeJoin, s);
-  const long long rows = static_cast<long long>(a.units) * a.nodes * a.group;
-  const unsigned blocks = static_cast<unsigned>((rows + kJoinThreads / kWave - 1) / (kJoinThreads / kWave));
-  hipLaunchKernelGGL((tree_join<DT, HD>), dim3(blocks), dim3(kJoinThreads), 0, s, a);
-  return hipGetLastError();
+  return a.splits > 8 ? launch_join_waves<DT, HD, 4>(a, s) : launch_join_waves<DT, HD, 1>(a, s);
 }
 
 }  // namespace

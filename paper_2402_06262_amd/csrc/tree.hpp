@@ -51,6 +51,18 @@ template <int DT> __device__ __forceinline__ f32x4 score_step(const uint4& a, co
   }
 }
 
+// Four consecutive elements, rounded to the storage type.
+template <int DT> __device__ __forceinline__ void store4(void* base, size_t idx, const f32x4& v) {
+  if constexpr (DT == kBF16) {
+    uint2 r;
+    r.x = f32_to_bf16(v.x) | static_cast<uint32_t>(f32_to_bf16(v.y)) << 16;
+    r.y = f32_to_bf16(v.z) | static_cast<uint32_t>(f32_to_bf16(v.w)) << 16;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + idx) = r;
+  } else {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(base) + idx) = v;
+  }
+}
+
 // The nodes that node `lane` of a tree sees, a bit each: itself and those above it, from its parent.  Twice as far up with every step.  A
 // parent that is not an earlier node is none.
 __device__ __forceinline__ uint64_t seen_nodes(int parent, int nodes, int lane) {

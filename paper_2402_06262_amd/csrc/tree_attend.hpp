@@ -22,17 +22,6 @@ constexpr int kAttendThreads = kAttendWaves * kWave;
 constexpr float kSlack = 8.0f;  // base-2 logits that a tile may lie above the running maximum
 constexpr float kLn2 = 0.6931471805599453f;
 
-template <int DT> __device__ __forceinline__ void store4(void* base, size_t idx, const f32x4& v) {
-  if constexpr (DT == kBF16) {
-    uint2 r;
-    r.x = f32_to_bf16(v.x) | static_cast<uint32_t>(f32_to_bf16(v.y)) << 16;
-    r.y = f32_to_bf16(v.z) | static_cast<uint32_t>(f32_to_bf16(v.w)) << 16;
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + idx) = r;
-  } else {
-    *reinterpret_cast<f32x4*>(static_cast<float*>(base) + idx) = v;
-  }
-}
-
 // Whether 16 bytes of values hold an infinite one or NaN.
 template <int DT> __device__ __forceinline__ bool holds_special(const uint4& v) {
   // (the exponent's bits set: adding one to them carries)
