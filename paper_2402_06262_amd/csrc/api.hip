@@ -561,7 +561,11 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
   if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
   a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
   a.scope = params->scope; a.max_path = max_path;
-  a.splits = (params->budget + kTreeChunk - 1) / kTreeChunk;
+  {  // chunks of whole tiles of every wave, smaller ones while that gives a workgroup to compute units that have none
+    const int want = (params->budget + 255) / 256 < 512 / params->units ? (params->budget + 255) / 256 : std::max(1, 512 / params->units);
+    a.chunk = std::min(kTreeChunk, ((params->budget + want - 1) / want + 255) / 256 * 256);
+    a.splits = (params->budget + a.chunk - 1) / a.chunk;
+  }
   a.streaming = streaming_loads(params) ? 1 : 0;
   a.pol = policy_of(params);
   a.scale_log2 = scale_log2(params);

@@ -116,32 +116,45 @@ template <int NT, bool LDS> __global__ __launch_bounds__(NT, 8) void tree_take(C
 
 constexpr int kStatWaves = 4;
 constexpr int kStatThreads = kStatWaves * kWave;
-constexpr size_t kMostQueryLds = 40960;  // bytes of accepted query rows that are kept in LDS
+constexpr int kMostQueryLds = 40960;  // bytes of accepted query rows in LDS at a time: 64 heads of fp32 / 128 take 32 KiB for a token
 
-// The accepted rows in tiles of 16 tokens of one head.  A head's probabilities are formed a tile at a time and added up over the heads
-// in registers: Q is the A operand here, so that a lane holds four tokens of one slot and the sum over the tokens is over its registers
-// and two exchanges.  STAGED: the query rows are in LDS (they fit), else read where they are.
-template <int DT, int HD, bool STREAMING, bool WINDOW, bool STAGED>
-__global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a) {
+// How the accepted rows lie in matrix tiles of 16: a token's heads side by side, filled up to a power of two, so that as few tiles as
+// can be are formed (a row of no head, or of no token, has a normaliser of infinity and no probability), and the mean over the heads is a sum
+// over registers (up to four heads), lane groups (up to 16) and tiles.
+struct RowPlan {
+  int heads_log2;  // of a token, filled up
+  int per_pass;    // tokens whose rows are in LDS at a time, whole tiles of them
+  __host__ __device__ int rows(int tokens) const { return ((tokens << heads_log2) + 15) / 16 * 16; }
+};
+inline RowPlan row_plan(int group, int max_path, int row_bytes) {
+  RowPlan p;
+  p.heads_log2 = 0;
+  while ((1 << p.heads_log2) < group) ++p.heads_log2;
+  const int tokens_per_tile = std::max(1, 16 >> p.heads_log2), most = kMostQueryLds / row_bytes >> p.heads_log2;
+  p.per_pass = std::min((max_path + tokens_per_tile - 1) / tokens_per_tile * tokens_per_tile, most / tokens_per_tile * tokens_per_tile);
+  return p;
+}
+
+// Q is the A operand here, so that a lane holds four rows of one slot.  The accepted tokens' K rows have been written to their slots: a slot of
+// token m is one that the rows before m do not see.  More rows than the LDS takes: another pass over K (which the L2 mostly has).
+template <int DT, int HD, bool STREAMING, bool WINDOW>
+__global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a, RowPlan plan) {
   using T = Tile<DT, HD>;
   constexpr int W = kStatWaves, G = T::kGroups, kTileBytes = 8192;
-  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the waves' tiles, two each; then the query rows
+  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the waves' tiles, two each; then the query rows and their normalisers
   __shared__ float sum_s[kTreeChunk], sum2_s[kTreeChunk];
   __shared__ signed char token_s[kTreeChunk];  // accepted token that a slot has taken, or -1
   __shared__ int32_t pos_s[WINDOW ? kTreeChunk : 1];
-  __shared__ int node_s[kMaxTreeNodes];
-  const int u = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+  const int u = blockIdx.x % a.units, split = blockIdx.x / a.units;
   const int request = u / a.heads;
-  const int32_t* const taken = a.taken + static_cast<size_t>(u) * kTakenWords;
-  const int n = __builtin_amdgcn_readfirstlane(taken[0]), len = __builtin_amdgcn_readfirstlane(taken[1]), n_new = __builtin_amdgcn_readfirstlane(taken[2]);
-  if (len == 0) return;
-  constexpr int kStep = T::kSlots * W;
-  static_assert(kTreeChunk % kStep == 0, "a chunk of whole tiles");
-  const int chunk = ((n_new + a.splits - 1) / a.splits + kStep - 1) / kStep * kStep;
-  const int row0 = min(n_new, split * chunk), row1 = min(n_new, row0 + chunk);
-  if (row0 >= row1) return;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int qi = lane & 15, g = lane >> 4;
+  const int32_t* const taken = a.taken + static_cast<size_t>(u) * kTakenWords;
+  // (what has to come from memory before anything else is asked for together)
+  const int my_slot = taken[4 + lane], my_node = path_node(a, request, min(lane, a.max_path - 1));
+  const int n = __builtin_amdgcn_readfirstlane(taken[0]), len = __builtin_amdgcn_readfirstlane(taken[1]), n_new = __builtin_amdgcn_readfirstlane(taken[2]);
+  const int row0 = split * a.chunk, row1 = min(n_new, row0 + a.chunk);
+  if (len == 0 || row0 >= row1) return;
 
   Walk<DT, HD, W> walk;
   walk.init(a.pages, a.B, a.heads, u, request, row0, row1, 0, wave, static_cast<unsigned>(u) * 5u + static_cast<unsigned>(split) * 3u);
@@ -150,124 +163,136 @@ __global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a)
   const uint32_t tiles_addr = lds_address(tiles);
   int koff[T::kGroupLoads];
   load_offsets<DT, HD, false>(koff);
-  typedef typename Walk<DT, HD, W>::Place Place;
-  uint32_t there[3] = {0, 0, 0};
   auto request_k = [&](int t) {
-    const Place p = walk.place(t);
+    const typename Walk<DT, HD, W>::Place p = walk.place(t);
     request_tile<DT, HD, STREAMING>(a.K, p.row, p.there, tiles_addr + (t & 1) * kTileBytes, koff);
     return p.there;
   };
-  if (mine > 0) there[0] = request_k(0);
-  if (mine > 1) there[1] = request_k(1);
-
-  // ---- the accepted rows
-  const int token_tiles = (len + 15) / 16, padded = token_tiles * 16;
-  char* const q_s = lds + W * 2 * kTileBytes;
-  float* const lse_s = reinterpret_cast<float*>(q_s + (STAGED ? static_cast<size_t>(a.group) * padded * T::kBytes : 0));  // [group][padded], base 2
-  if (tid < len) node_s[tid] = path_node(a, request, tid);
-  for (int j = tid; j < kTreeChunk; j += kStatThreads) {
+  for (int j = tid; j < row1 - row0; j += kStatThreads) {
     token_s[j] = -1;
-    if (WINDOW && row0 + j < row1) pos_s[WINDOW ? j : 0] = a.pos[static_cast<size_t>(u) * a.B + row0 + j];
+    sum_s[j] = sum2_s[j] = 0.0f;
+    if (WINDOW) pos_s[WINDOW ? j : 0] = a.pos[static_cast<size_t>(u) * a.B + row0 + j];
   }
   __syncthreads();
-  if (tid < len) {
-    const int j = taken[4 + tid] - row0;
-    if (j >= 0 && j < row1 - row0) token_s[j] = static_cast<signed char>(tid);
-  }
-  for (int i = tid; i < a.group * padded; i += kStatThreads) {
-    const int h = i / padded, k = i % padded;
-    lse_s[i] = k < len ? a.lse[(static_cast<size_t>(u) * a.nodes + node_s[k]) * a.group + h] * kLog2e : 0.0f;
-  }
-  if (STAGED) {
-    for (int i = tid; i < a.group * padded * T::kChunks; i += kStatThreads) {
-      const int row = i / T::kChunks, c = i % T::kChunks, h = row / padded, k = row % padded;
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (k < len) v = load16(static_cast<const char*>(a.q) + ((static_cast<size_t>(u) * a.nodes + node_s[k]) * a.group + h) * T::kBytes + c * 16);
-      *reinterpret_cast<uint4*>(q_s + row * T::kBytes + ((c ^ T::swizzle_k(row & 15)) << 4)) = v;
-    }
-  }
-  __syncthreads();
+  if (tid < len && my_slot >= row0 && my_slot < row1) token_s[my_slot - row0] = static_cast<signed char>(tid);
 
-  const float sc = a.scale_log2, rb = a.recency_bias_log2, share = 1.0f / static_cast<float>(a.group);
+  const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 : 0.0f, share = 1.0f / static_cast<float>(a.group);
   const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
   const int frag = qi * T::kBytes + ((g ^ T::swizzle_k(qi)) << 4);
+  // of the lane's four rows of a tile, those whose register holds a token's sum over its heads in the end
+  const int heads_log2 = plan.heads_log2, in_tile = min(heads_log2, 4);
+  const int slices = 1 << (heads_log2 - in_tile);  // tiles of a token
+  const bool filled_up = (1 << heads_log2) != a.group;
+  const int stride = 1 << min(in_tile, 2);
+  const bool holds = in_tile < 3 || (g & ((1 << (in_tile - 2)) - 1)) == 0;
+  char* const q_s = lds + W * 2 * kTileBytes;
+  float* const lse_s = reinterpret_cast<float*>(q_s + static_cast<size_t>(plan.rows(plan.per_pass)) * T::kBytes);  // base 2
 #pragma unroll 1
-  for (int t = 0; t < mine; ++t) {
-    const char* const tile = tiles + (t & 1) * kTileBytes;
-    if (t + 1 < mine) wait_loads<T::kLoads>();
-    else wait_loads<0>();
-    uint4 kf[G][T::kSteps];
-#pragma unroll
-    for (int i = 0; i < G; ++i)
-#pragma unroll
-      for (int kk = 0; kk < T::kSteps; ++kk) kf[i][kk] = *reinterpret_cast<const uint4*>(tile + i * 16 * T::kBytes + (frag ^ (kk << 6)));
-    reads_done();
-    if (t + 2 < mine) there[2] = request_k(t + 2);
-    const int j0 = walk.first_slot(t) - row0;
-    float sum[G], sum2[G];
-    int own[G], at[G];
-#pragma unroll
-    for (int i = 0; i < G; ++i) {
-      sum[i] = sum2[i] = 0.0f;
-      own[i] = token_s[j0 + 16 * i + qi];
-      at[i] = WINDOW ? pos_s[WINDOW ? j0 + 16 * i + qi : 0] : 0;
+  for (int first = 0; first < len; first += plan.per_pass) {
+    const int tokens = min(plan.per_pass, len - first), rows = plan.rows(tokens);
+    __syncthreads();  // nobody reads the rows of the pass before
+    uint32_t there0 = 0, there1 = 0;
+    if (first > 0) walk.look_ahead(0);
+    if (mine > 0) there0 = request_k(0);
+    if (mine > 1) there1 = request_k(1);
+    // row i: token first + i >> heads_log2, with its heads beyond 16 in tiles of their own
+#pragma unroll 1
+    for (int i = tid; i < rows * T::kChunks; i += kStatThreads) {
+      const int row = i / T::kChunks, c = i % T::kChunks;
+      const int k = row >> heads_log2, h = row & ((1 << heads_log2) - 1);
+      const bool real = k < tokens && h < a.group;
+      const size_t at = (static_cast<size_t>(u) * a.nodes + __shfl(my_node, min(first + k, kWave - 1), kWave)) * a.group + h;
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (real) v = load16(static_cast<const char*>(a.q) + at * T::kBytes + c * 16);
+      *reinterpret_cast<uint4*>(q_s + row * T::kBytes + ((c ^ T::swizzle_k(row & 15)) << 4)) = v;
+      if (c == 0) lse_s[row] = real ? a.lse[at] * kLog2e : INFINITY;
     }
+    __syncthreads();
 #pragma unroll 1
-    for (int tt = 0; tt < token_tiles; ++tt) {
-      f32x4 p[G];
-#pragma unroll
-      for (int i = 0; i < G; ++i) p[i] = f32x4{0};
-#pragma unroll 1
-      for (int h = 0; h < a.group; ++h) {
-        const int row = h * padded + 16 * tt;
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(lse_s + row + 4 * g);
-        const char* const q = STAGED ? q_s + row * T::kBytes
-                                     : static_cast<const char*>(a.q) + ((static_cast<size_t>(u) * a.nodes + node_s[min(16 * tt + qi, len - 1)]) * a.group + h) * T::kBytes;
-        f32x4 s[G];
-#pragma unroll
-        for (int kk = 0; kk < T::kSteps; ++kk) {
-          const uint4 qf = STAGED ? *reinterpret_cast<const uint4*>(q + (frag ^ (kk << 6))) : load16(q + kk * 64 + g * 16);
-#pragma unroll
-          for (int i = 0; i < G; ++i) s[i] = score_step<DT>(qf, kf[i][kk], kk == 0 ? f32x4{0} : s[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = fmaf(s[i][e], sc, -lse[e]);
-            if (WINDOW) {
-              const int away = qp0 + 16 * tt + 4 * g + e - at[i];
-              if (away >= 0 && away < w) x += rb;
-            }
-            p[i][e] += fast_exp2(x);
-          }
-      }
+    for (int t = 0; t < mine; ++t) {
+      const char* const tile = tiles + (t & 1) * kTileBytes;
+      if (t + 1 < mine) wait_loads<T::kLoads>();
+      else wait_loads<0>();
+      uint4 kf[G][T::kSteps];
 #pragma unroll
       for (int i = 0; i < G; ++i)
 #pragma unroll
+        for (int kk = 0; kk < T::kSteps; ++kk) kf[i][kk] = *reinterpret_cast<const uint4*>(tile + i * 16 * T::kBytes + (frag ^ (kk << 6)));
+      reads_done();
+      uint32_t there2 = 0;
+      if (t + 2 < mine) there2 = request_k(t + 2);
+      const int j0 = walk.first_slot(t) - row0;
+      float sum[G], sum2[G];
+      int own[G], at[G];
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        sum[i] = sum2[i] = 0.0f;
+        const int j = min(j0 + 16 * i + qi, row1 - row0 - 1);
+        own[i] = token_s[j];
+        at[i] = WINDOW ? pos_s[WINDOW ? j : 0] : 0;
+      }
+#pragma unroll 1
+      for (int tile0 = 0; tile0 < rows; tile0 += 16 * slices) {
+        const int token0 = first + (tile0 >> heads_log2);
+        f32x4 p[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) p[i] = f32x4{0};
+#pragma unroll 1
+        for (int row = tile0; row < tile0 + 16 * slices; row += 16) {
+          const f32x4 lse = *reinterpret_cast<const f32x4*>(lse_s + row + 4 * g);
+          const char* const q = q_s + row * T::kBytes;
+          f32x4 s[G];
+#pragma unroll
+          for (int kk = 0; kk < T::kSteps; ++kk) {
+            const uint4 qf = *reinterpret_cast<const uint4*>(q + (frag ^ (kk << 6)));
+#pragma unroll
+            for (int i = 0; i < G; ++i) s[i] = score_step<DT>(qf, kf[i][kk], kk == 0 ? f32x4{0} : s[i]);
+          }
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float x = fmaf(s[i][e], sc, -lse[e]);
+              if (WINDOW) x += static_cast<unsigned>(qp0 + token0 + ((4 * g + e) >> in_tile) - at[i]) < static_cast<unsigned>(w) ? bias : 0.0f;
+              const float v = fast_exp2(x);
+              p[i][e] += filled_up && lse[e] == INFINITY ? 0.0f : v;  // (0 times an infinite key is NaN)
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          if (in_tile >= 1) { p[i][0] += p[i][1]; p[i][2] += p[i][3]; }
+          if (in_tile >= 2) p[i][0] += p[i][2];
+          if (in_tile >= 3) p[i][0] += __shfl_xor(p[i][0], 16, kWave);
+          if (in_tile >= 4) p[i][0] += __shfl_xor(p[i][0], 32, kWave);
+        }
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int k = 16 * tt + 4 * g + e;  // sees the tokens before it, and itself
-          const float v = p[i][e] * share;
-          if (k < len && k >= own[i]) {
-            sum[i] += v;
-            sum2[i] += a.pol.keeps_last_score() ? (k == len - 1 ? v : 0.0f) : a.pol.second_statistic(0.0f, v, static_cast<float>(n + k + 1));
+          if ((e & (stride - 1)) != 0) continue;
+          const int k = token0 + ((4 * g + e) >> in_tile);  // sees the tokens before it, and itself
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            const float v = p[i][e] * share;
+            const bool counts = holds && k < len && k >= own[i];
+            const float second = a.pol.keeps_last_score() ? (k == len - 1 ? v : 0.0f) : a.pol.second_statistic(0.0f, v, static_cast<float>(n + k + 1));
+            sum[i] += counts ? v : 0.0f;
+            sum2[i] += counts ? second : 0.0f;
           }
         }
-    }
-#pragma unroll
-    for (int i = 0; i < G; ++i) {
-      sum[i] += __shfl_xor(sum[i], 16, kWave);
-      sum[i] += __shfl_xor(sum[i], 32, kWave);
-      sum2[i] += __shfl_xor(sum2[i], 16, kWave);
-      sum2[i] += __shfl_xor(sum2[i], 32, kWave);
-      const bool real = qi < static_cast<int>((there[0] >> (8 * i)) & 0xffu);  // slots of no page have received nothing
-      if (g == 0) {
-        sum_s[j0 + 16 * i + qi] = real ? sum[i] : 0.0f;
-        sum2_s[j0 + 16 * i + qi] = real ? sum2[i] : 0.0f;
       }
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        sum[i] += __shfl_xor(sum[i], 16, kWave);
+        sum[i] += __shfl_xor(sum[i], 32, kWave);
+        sum2[i] += __shfl_xor(sum2[i], 16, kWave);
+        sum2[i] += __shfl_xor(sum2[i], 32, kWave);
+        if (g == 0 && qi < static_cast<int>((there0 >> (8 * i)) & 0xffu)) {  // (slots of no page have received nothing)
+          sum_s[j0 + 16 * i + qi] += sum[i];
+          sum2_s[j0 + 16 * i + qi] += sum2[i];
+        }
+      }
+      there0 = there1;
+      there1 = there2;
     }
-    there[0] = there[1];
-    there[1] = there[2];
   }
   __syncthreads();
   // ---- the slots' statistics: added to those of older tokens, the first ones of the accepted
@@ -285,18 +310,14 @@ __global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a)
 
 #pragma clang diagnostic pop
 
-template <int DT, int HD, bool STREAMING, bool WINDOW, bool STAGED> hipError_t launch_statistics(const CommitArgs& a, size_t lds, hipStream_t s) {
-  constexpr int kMost = kStatWaves * 2 * 8192 + static_cast<int>(kMostQueryLds) + kMaxTreeNodes * kMaxTreeGroup * 4;
-  const void* const fn = reinterpret_cast<const void*>(tree_statistics<DT, HD, STREAMING, WINDOW, STAGED>);
+template <int DT, int HD, bool STREAMING, bool WINDOW> hipError_t launch_statistics(const CommitArgs& a, hipStream_t s) {
+  constexpr int kRowBytes = Tile<DT, HD>::kBytes, kTiles = kStatWaves * 2 * 8192, kMost = kTiles + kMostQueryLds / kRowBytes * (kRowBytes + 4);
+  const RowPlan plan = row_plan(a.group, a.max_path, kRowBytes);
+  const void* const fn = reinterpret_cast<const void*>(tree_statistics<DT, HD, STREAMING, WINDOW>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kMost) != hipSuccess) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((tree_statistics<DT, HD, STREAMING, WINDOW, STAGED>), dim3(static_cast<unsigned>(a.units) * a.splits), dim3(kStatThreads), lds, s, a);
+  const size_t lds = kTiles + static_cast<size_t>(plan.rows(plan.per_pass)) * (kRowBytes + 4);
+  hipLaunchKernelGGL((tree_statistics<DT, HD, STREAMING, WINDOW>), dim3(static_cast<unsigned>(a.units) * a.splits), dim3(kStatThreads), lds, s, a, plan);
   return hipGetLastError();
-}
-
-template <int DT, int HD, bool STREAMING> hipError_t launch_statistics_form(const CommitArgs& a, bool staged, size_t lds, hipStream_t s) {
-  if (a.recency_window > 0)
-    return staged ? launch_statistics<DT, HD, STREAMING, true, true>(a, lds, s) : launch_statistics<DT, HD, STREAMING, true, false>(a, lds, s);
-  return staged ? launch_statistics<DT, HD, STREAMING, false, true>(a, lds, s) : launch_statistics<DT, HD, STREAMING, false, false>(a, lds, s);
 }
 
 template <int DT, int HD> hipError_t launch_commit(const CommitArgs& a, hipStream_t s) {
@@ -314,10 +335,8 @@ template <int DT, int HD> hipError_t launch_commit(const CommitArgs& a, hipStrea
     if (e != hipSuccess) return e;
   }
   ProfScope ps(kProfTreeStatistics, s);
-  const size_t rows = static_cast<size_t>(a.group) * ((a.max_path + 15) / 16 * 16);
-  const bool staged = rows * kRowBytes <= kMostQueryLds;
-  const size_t lds = kStatWaves * 2 * 8192 + (staged ? rows * kRowBytes : 0) + rows * 4;
-  return a.streaming ? launch_statistics_form<DT, HD, true>(a, staged, lds, s) : launch_statistics_form<DT, HD, false>(a, staged, lds, s);
+  if (a.recency_window > 0) return a.streaming ? launch_statistics<DT, HD, true, true>(a, s) : launch_statistics<DT, HD, false, true>(a, s);
+  return a.streaming ? launch_statistics<DT, HD, true, false>(a, s) : launch_statistics<DT, HD, false, false>(a, s);
 }
 
 }  // namespace
