@@ -561,9 +561,9 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
   if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
   a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
   a.scope = params->scope; a.max_path = max_path;
-  {  // chunks of whole tiles of every wave, smaller ones while that gives a workgroup to compute units that have none
-    const int want = (params->budget + 255) / 256 < 512 / params->units ? (params->budget + 255) / 256 : std::max(1, 512 / params->units);
-    a.chunk = std::min(kTreeChunk, ((params->budget + want - 1) / want + 255) / 256 * 256);
+  {  // chunks of whole tiles of every wave, smaller ones while that gives compute units a workgroup that have none
+    const int want = std::max(1, 512 / params->units);
+    a.chunk = std::min(kTreeChunk, ((params->budget + want - 1) / want + 127) / 128 * 128);
     a.splits = (params->budget + a.chunk - 1) / a.chunk;
   }
   a.streaming = streaming_loads(params) ? 1 : 0;

@@ -206,7 +206,7 @@ TreeSplits tree_attend_splits(int dtype, int units, int rows, int B, bool window
 
 struct CommitArgs {
   int units, heads, group, nodes, B, scope, max_path;
-  int splits, chunk;      // workgroups along a unit's slots, of `chunk` each, a multiple of 256 and kTreeChunk at most
+  int splits, chunk;      // workgroups along a unit's slots, of `chunk` each, a multiple of 128 and kTreeChunk at most
   int streaming;          // as DecodeArgs::streaming
   Policy pol;
   float scale_log2;

@@ -7,8 +7,10 @@
 namespace roco {
 namespace {
 
-constexpr int kTableThreads = 1024;
-constexpr int kMapPerBlock = 4096;   // entries of the map that a workgroup of the fill writes
+constexpr int kSumThreads = 1024;
+constexpr int kFillThreads = 256;
+constexpr int kFillEntries = 4;      // of the map, side by side, per thread and step
+constexpr int kSelfSummed = 2048;    // most requests whose sums every workgroup of the fill forms itself
 
 struct Need { int first, last, held, want; };  // pages [first, last) are to be taken, slots [held, want) are new
 __device__ __forceinline__ Need need_of(const PageTableArgs& a, int r) {
@@ -22,18 +24,18 @@ __device__ __forceinline__ Need need_of(const PageTableArgs& a, int r) {
   return x;
 }
 
-// One workgroup: the prefix sums of pages and of new slots over the requests, and the new pages into the table.
-__global__ __launch_bounds__(kTableThreads) void page_sums(PageTableArgs a) {
-  __shared__ uint32_t sh[kTableThreads / kWave + 1];
+// One workgroup: the prefix sums of pages and of new slots over the requests.
+__global__ __launch_bounds__(kSumThreads) void page_sums(PageTableArgs a) {
+  __shared__ uint32_t sh[kSumThreads / kWave + 1];
   uint32_t pages = 0, rows = 0;
 #pragma unroll 1
-  for (int r0 = 0; r0 < a.requests; r0 += kTableThreads) {
+  for (int r0 = 0; r0 < a.requests; r0 += kSumThreads) {
     const int r = r0 + threadIdx.x;
     Need x = {0, 0, 0, 0};
     if (r < a.requests) x = need_of(a, r);
     uint32_t more_pages, more_rows;
-    const uint32_t p = pages + block_exclusive_scan<kTableThreads>(static_cast<uint32_t>(x.last - x.first), sh, more_pages);
-    const uint32_t s = rows + block_exclusive_scan<kTableThreads>(static_cast<uint32_t>(x.want - x.held), sh, more_rows);
+    const uint32_t p = pages + block_exclusive_scan<kSumThreads>(static_cast<uint32_t>(x.last - x.first), sh, more_pages);
+    const uint32_t s = rows + block_exclusive_scan<kSumThreads>(static_cast<uint32_t>(x.want - x.held), sh, more_rows);
     if (r < a.requests) {
       a.page_start[r] = static_cast<int32_t>(p);
       a.row_start[r] = static_cast<int32_t>(s);
@@ -47,54 +49,143 @@ __global__ __launch_bounds__(kTableThreads) void page_sums(PageTableArgs a) {
   }
 }
 
-// Page number `i` of request r: one of those it takes now, or one that its table holds.
-__device__ __forceinline__ int page_of(const PageTableArgs& a, int r, const Need& x, int start, int i) {
-  if (i < x.first) return a.table[static_cast<size_t>(r) * a.max_pages + i];
-  const int at = start + i - x.first;
-  return at < a.n_free ? a.free_pages[at] : -1;
-}
-
-// The map, kMapPerBlock entries a workgroup, then (blocks from map_blocks on) the table, a workgroup per request.
-__global__ __launch_bounds__(256) void page_fill(PageTableArgs a, int map_blocks) {
-  if (static_cast<int>(blockIdx.x) >= map_blocks) {
-    const int r = blockIdx.x - map_blocks;
-    const Need x = need_of(a, r);
-    const int start = a.page_start[r];
-    for (int i = x.first + threadIdx.x; i < x.last; i += 256) a.table[static_cast<size_t>(r) * a.max_pages + i] = page_of(a, r, x, start, i);
-    return;
+// The map, kFillEntries entries per thread at a time, and the table, a wave per request.  SELF: every workgroup forms the requests' sums in its
+// LDS, from lengths that the L2 has, instead of waiting for a launch that does: a step of 64 requests 7.7 -> 5.9 us.  A page number is asked
+// for once for entries of the same page; a division and a search per entry took 19.6 us for 1024 requests of up to 8192 slots.
+template <bool SELF> __global__ __launch_bounds__(kFillThreads) void page_fill(PageTableArgs a) {
+  __shared__ uint32_t sh[kFillThreads / kWave + 1];
+  extern __shared__ int32_t sums_s[];  // SELF: pages before a request, new slots before it, slots that it holds
+  int32_t *const page_s = sums_s, *const row_s = page_s + a.requests + 1, *const held_s = row_s + a.requests + 1;
+  const int tid = threadIdx.x;
+  if (SELF) {
+    constexpr int kEach = kSelfSummed / kFillThreads;
+    const int each = (a.requests + kFillThreads - 1) / kFillThreads, r0 = tid * each;
+    uint32_t pages[kEach], rows[kEach], all_pages = 0, all_rows = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      pages[i] = rows[i] = 0;
+      if (i < each && r0 + i < a.requests) {
+        const Need x = need_of(a, r0 + i);
+        pages[i] = static_cast<uint32_t>(x.last - x.first);
+        rows[i] = static_cast<uint32_t>(x.want - x.held);
+        held_s[r0 + i] = x.held;
+      }
+      all_pages += pages[i];
+      all_rows += rows[i];
+    }
+    uint32_t page_total, row_total;
+    uint32_t p = block_exclusive_scan<kFillThreads>(all_pages, sh, page_total), s = block_exclusive_scan<kFillThreads>(all_rows, sh, row_total);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (i < each && r0 + i < a.requests) {
+        page_s[r0 + i] = static_cast<int32_t>(p);
+        row_s[r0 + i] = static_cast<int32_t>(s);
+      }
+      p += pages[i];
+      s += rows[i];
+    }
+    if (tid == 0) {
+      page_s[a.requests] = static_cast<int32_t>(page_total);
+      row_s[a.requests] = static_cast<int32_t>(row_total);
+    }
+    __syncthreads();
+    if (blockIdx.x == 0) {
+      for (int r = tid; r <= a.requests; r += kFillThreads) {
+        a.page_start[r] = page_s[r];
+        a.row_start[r] = row_s[r];
+      }
+    }
+  }
+  const int32_t* const page_start = SELF ? page_s : a.page_start;
+  const int32_t* const row_start = SELF ? row_s : a.row_start;
+  auto lengths_of = [&](int r) {
+    if (!SELF) return need_of(a, r);
+    Need x;
+    x.held = held_s[r];
+    x.want = x.held + row_s[r + 1] - row_s[r];
+    x.first = (x.held + (1 << a.page_log2) - 1) >> a.page_log2;
+    x.last = x.first + page_s[r + 1] - page_s[r];
+    return x;
+  };
+  // Page number i of request r: one of those it takes now, or one that its table holds.
+  auto page_of = [&](int r, const Need& x, int i) {
+    if (i < x.first) return a.table[static_cast<size_t>(r) * a.max_pages + i];
+    const int at = page_start[r] + i - x.first;
+    return at < a.n_free ? a.free_pages[at] : -1;
+  };
+  const int waves = kFillThreads / kWave * gridDim.x;
+  for (int r = blockIdx.x * (kFillThreads / kWave) + tid / kWave; r < a.requests; r += waves) {
+    const Need x = lengths_of(r);
+    for (int i = x.first + tid % kWave; i < x.last; i += kWave) a.table[static_cast<size_t>(r) * a.max_pages + i] = page_of(r, x, i);
   }
   const long long total = a.padded ? static_cast<long long>(a.requests) * a.rows : a.rows;
-  const long long first = static_cast<long long>(blockIdx.x) * kMapPerBlock;
-  const long long end = min(total, first + kMapPerBlock);
+  const long long step = static_cast<long long>(gridDim.x) * kFillThreads * kFillEntries;
   const int low = (1 << a.page_log2) - 1;
-  for (long long i = first + threadIdx.x; i < end; i += 256) {
-    int r, k;
+  for (long long i0 = (static_cast<long long>(blockIdx.x) * kFillThreads + tid) * kFillEntries; i0 < total; i0 += step) {
+    int r, k;  // request and new slot of the entry
     if (a.padded) {
-      r = static_cast<int>(i / a.rows);
-      k = static_cast<int>(i % a.rows);
+      if (total <= 0x7fffffff) {
+        r = static_cast<int>(static_cast<uint32_t>(i0) / static_cast<uint32_t>(a.rows));
+        k = static_cast<int>(static_cast<uint32_t>(i0) - static_cast<uint32_t>(r) * static_cast<uint32_t>(a.rows));
+      } else {
+        r = static_cast<int>(i0 / a.rows);
+        k = static_cast<int>(i0 % a.rows);
+      }
     } else {
-      int lo = 0, hi = a.requests;  // the last request that starts at i or before it
+      int lo = 0, hi = a.requests;  // the last request that starts at i0 or before it
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (a.row_start[mid] <= i) lo = mid;
+        if (row_start[mid] <= i0) lo = mid;
         else hi = mid;
       }
       r = lo;
-      k = static_cast<int>(i - a.row_start[r]);
+      k = static_cast<int>(i0 - row_start[r]);
     }
-    const Need x = need_of(a, r);
-    const int slot = x.held + k;
-    int entry = -1;
-    if (slot < x.want) {
-      const int page = page_of(a, r, x, a.page_start[r], slot >> a.page_log2);
-      if (page >= 0) entry = (page << a.page_log2) + (slot & low);
+    Need x = lengths_of(r);
+    int at = -1, page = -1;  // page `at` of the request
+    int4 entries;
+    int* const e = &entries.x;
+    const int last = x.held + k + kFillEntries - 1;  // slot of the last entry, if they are all of this request
+    if (a.padded && k + kFillEntries <= a.rows && x.held + k >= x.want) {
+      entries = make_int4(-1, -1, -1, -1);
+    } else if (k + kFillEntries <= (a.padded ? a.rows : x.want - x.held) && last < x.want && (last & low) >= kFillEntries - 1) {  // of one page
+      page = page_of(r, x, last >> a.page_log2);
+      const int entry = (page << a.page_log2) + (last & low) - (kFillEntries - 1);
+      entries = page < 0 ? make_int4(-1, -1, -1, -1) : make_int4(entry, entry + 1, entry + 2, entry + 3);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kFillEntries; ++j) {
+        // the next request: behind the end of its row of a padded map, or of its new slots in a packed one
+        while (r + 1 < a.requests && k >= (a.padded ? a.rows : x.want - x.held)) {
+          k = a.padded ? 0 : k - (x.want - x.held);
+          x = lengths_of(++r);
+          at = -1;
+        }
+        const int slot = x.held + k;
+        e[j] = -1;
+        if (slot < x.want && k >= 0) {
+          if (slot >> a.page_log2 != at) {
+            at = slot >> a.page_log2;
+            page = page_of(r, x, at);
+          }
+          if (page >= 0) e[j] = (page << a.page_log2) + (slot & low);
+        }
+        ++k;
+      }
     }
-    a.map[i] = entry;
+    if (i0 + kFillEntries <= total) {
+      *reinterpret_cast<int4*>(a.map + i0) = entries;
+    } else {
+#pragma unroll
+      for (int j = 0; j < kFillEntries; ++j)
+        if (i0 + j < total) a.map[i0 + j] = e[j];
+    }
   }
 }
 
-// 16 bytes of a row of K and of V per lane; a row's lanes lie side by side.
-__global__ __launch_bounds__(256) void page_store(PageStoreArgs a, int lanes_log2) {
+// 16 bytes of a row of K and of V per lane; a row's lanes lie side by side.  Bound by the bytes.  STREAMING: rows that are more than the chip's
+// last-level cache takes, with the non-temporal hint both ways (16 caches x 32 heads x 2048 rows of 256 bytes, twice: 151 -> 143 us, 5.6 TB/s).
+template <bool STREAMING> __global__ __launch_bounds__(256) void page_store(PageStoreArgs a, int lanes_log2) {
   const int lanes = 1 << lanes_log2;
   const long long id = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
   const long long row = id >> lanes_log2;  // (group, head, row), rows side by side
@@ -108,19 +199,33 @@ __global__ __launch_bounds__(256) void page_store(PageStoreArgs a, int lanes_log
   if (slot < 0 || page >= a.n_pages) return;
   const size_t src = static_cast<size_t>(group * a.group_stride + i * a.row_stride + h * a.head_stride) + col;
   const size_t dst = (((static_cast<size_t>(page) * a.heads + h) << a.page_log2) + (slot & ((1 << a.page_log2) - 1))) * a.row_bytes + col;
-  const uint4 k = load16(static_cast<const char*>(a.K_rows) + src), v = load16(static_cast<const char*>(a.V_rows) + src);
-  *reinterpret_cast<uint4*>(static_cast<char*>(a.K) + dst) = k;
-  *reinterpret_cast<uint4*>(static_cast<char*>(a.V) + dst) = v;
+  const char *const k_row = static_cast<const char*>(a.K_rows) + src, *const v_row = static_cast<const char*>(a.V_rows) + src;
+  const uint4 k = STREAMING ? load16_streaming(k_row) : load16(k_row), v = STREAMING ? load16_streaming(v_row) : load16(v_row);
+  uint4_vec *const k_at = reinterpret_cast<uint4_vec*>(static_cast<char*>(a.K) + dst), *const v_at = reinterpret_cast<uint4_vec*>(static_cast<char*>(a.V) + dst);
+  if (STREAMING) {
+    __builtin_nontemporal_store(__builtin_bit_cast(uint4_vec, k), k_at);
+    __builtin_nontemporal_store(__builtin_bit_cast(uint4_vec, v), v_at);
+  } else {
+    *k_at = __builtin_bit_cast(uint4_vec, k);
+    *v_at = __builtin_bit_cast(uint4_vec, v);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_page_tables(const PageTableArgs& a, hipStream_t s) {
   ProfScope ps(kProfPageTables, s);
-  hipLaunchKernelGGL(page_sums, dim3(1), dim3(kTableThreads), 0, s, a);
   const long long total = a.padded ? static_cast<long long>(a.requests) * a.rows : a.rows;
-  const int map_blocks = static_cast<int>((total + kMapPerBlock - 1) / kMapPerBlock);
-  hipLaunchKernelGGL(page_fill, dim3(map_blocks + a.requests), dim3(256), 0, s, a, map_blocks);
+  // a step of every thread, as far as that gives no more than six workgroups per compute unit (1024 prompts of up to 8192 slots: 512 of them
+  // 16.6 us, 1024 12.9, 1536 12.6, 2048 13.5)
+  const long long want = std::max<long long>((total + kFillThreads * kFillEntries - 1) / (kFillThreads * kFillEntries), (a.requests + 3) / 4);
+  const dim3 grid(static_cast<unsigned>(std::min<long long>(want, 1536)));
+  if (a.requests <= kSelfSummed) {
+    hipLaunchKernelGGL((page_fill<true>), grid, dim3(kFillThreads), (3 * a.requests + 2) * sizeof(int32_t), s, a);
+  } else {
+    hipLaunchKernelGGL(page_sums, dim3(1), dim3(kSumThreads), 0, s, a);
+    hipLaunchKernelGGL((page_fill<false>), grid, dim3(kFillThreads), 0, s, a);
+  }
   return hipGetLastError();
 }
 
@@ -128,7 +233,9 @@ hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s) {
   ProfScope ps(kProfPageStore, s);
   const int lanes_log2 = __builtin_ctz(a.row_bytes) - 4;
   const long long lanes = (static_cast<long long>(a.groups) * a.heads * a.rows) << lanes_log2;
-  hipLaunchKernelGGL(page_store, dim3(static_cast<unsigned>((lanes + 255) / 256)), dim3(256), 0, s, a, lanes_log2);
+  const dim3 grid(static_cast<unsigned>((lanes + 255) / 256));
+  if (lanes * 32 > (192ll << 20)) hipLaunchKernelGGL((page_store<true>), grid, dim3(256), 0, s, a, lanes_log2);
+  else hipLaunchKernelGGL((page_store<false>), grid, dim3(256), 0, s, a, lanes_log2);
   return hipGetLastError();
 }
 

@@ -18,17 +18,17 @@ using mfma::reads_done;
 using mfma::v4i32;
 using mfma::wait_loads;
 
-// Tiles of 8 KiB, one wave's, in groups of 16 slots: a page holds whole groups, and what a group's load finds behind its last row
+// Tiles of BYTES, one wave's, in groups of 16 slots: a page holds whole groups, and what a group's load finds behind its last row
 // comes back as zeros (the group has a buffer descriptor of its own, of as many rows as are there).
 // Chunk c (16 bytes) of a row r of K lies in slot c ^ swizzle_k(r), of V in slot c ^ swizzle_v(r), so that what the lanes read together
 // falls on distinct banks: 16 rows of one chunk of K; of V 32 bytes of 8 rows (bf16, transposed) or 64 bytes of every fourth row (fp32).
-template <int DT, int HD> struct Tile {
+template <int DT, int HD, int BYTES = 8192> struct Tile {
   static constexpr int kBytes = HD * (DT == kBF16 ? 2 : 4);   // of a row
   static constexpr int kChunks = kBytes / 16;
   static constexpr int kPerLoad = kWave / kChunks;            // rows of a wave-wide load
-  static constexpr int kSlots = 8192 / kBytes;
+  static constexpr int kSlots = BYTES / kBytes;
   static constexpr int kGroups = kSlots / 16;
-  static constexpr int kLoads = 8, kGroupLoads = kLoads / kGroups;
+  static constexpr int kLoads = BYTES / 1024, kGroupLoads = kLoads / kGroups;
   static constexpr int kSteps = kChunks / 4;                  // of a score: four lane groups with a chunk each
   static constexpr int kBlocks = HD / 16;                     // of 16 output dimensions
   static __device__ __forceinline__ int swizzle_k(int r) { return kBytes == 128 ? (r >> 1) & 7 : r & 15; }
@@ -110,8 +110,8 @@ __device__ __forceinline__ int splits_used(int n, int chunk) { return max((n + c
 // A wave's tiles of the slots [row0, row1) of a unit: every W-th one, from a start that differs between workgroups so that they do not
 // walk the memory channels in lock step; behind the cache's tiles come `node_tiles` of a tree's nodes.  The tile numbers `t` are the
 // wave's own; they are asked for in order.
-template <int DT, int HD, int W> struct Walk {
-  using T = Tile<DT, HD>;
+template <int DT, int HD, int W, int BYTES = 8192> struct Walk {
+  using T = Tile<DT, HD, BYTES>;
   static constexpr int G = T::kGroups;
   typedef const __attribute__((address_space(4))) int32_t* Table;  // (constant: read by scalar loads, which the tiles' loads do not wait for)
   int row0, row1, cache_tiles, mine, rot, wave, nodes;
@@ -196,7 +196,7 @@ template <int DT, int HD, bool VALUES> __device__ __forceinline__ void load_offs
   }
 }
 
-// Requests a tile: eight loads.  STREAMING: of a cache that is far larger than the chip's last-level cache, with the non-temporal hint.
+// Requests a tile.  STREAMING: of a cache that is far larger than the chip's last-level cache, with the non-temporal hint.
 template <int DT, int HD, bool STREAMING, int G>
 __device__ __forceinline__ void request_tile(const void* rows, const uint32_t (&row)[G], uint32_t there, uint32_t lds, const int* off) {
   using T = Tile<DT, HD>;

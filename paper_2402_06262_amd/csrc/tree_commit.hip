@@ -116,6 +116,10 @@ template <int NT, bool LDS> __global__ __launch_bounds__(NT, 8) void tree_take(C
 
 constexpr int kStatWaves = 4;
 constexpr int kStatThreads = kStatWaves * kWave;
+// Bytes of a wave's tile: small ones, so that four workgroups are on a compute unit and one's sums over its rows, or its way to the first tile,
+// go beside the others' streams (8 KiB and two workgroups: 512 units x 2048 slots of bf16 / 128 75.1 us against 70.3, 192 x 4096 of
+// bf16 / 64 51.1 / 46.6).  16 slots are the least.
+template <int DT, int HD> constexpr int kStatTile = DT == kF32 && HD == 128 ? 8192 : 4096;
 constexpr int kMostQueryLds = 40960;  // bytes of accepted query rows in LDS at a time: 64 heads of fp32 / 128 take 32 KiB for a token
 
 // How the accepted rows lie in matrix tiles of 16: a token's heads side by side, filled up to a power of two, so that as few tiles as
@@ -138,9 +142,10 @@ inline RowPlan row_plan(int group, int max_path, int row_bytes) {
 // Q is the A operand here, so that a lane holds four rows of one slot.  The accepted tokens' K rows have been written to their slots: a slot of
 // token m is one that the rows before m do not see.  More rows than the LDS takes: another pass over K (which the L2 mostly has).
 template <int DT, int HD, bool STREAMING, bool WINDOW>
-__global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a, RowPlan plan) {
-  using T = Tile<DT, HD>;
-  constexpr int W = kStatWaves, G = T::kGroups, kTileBytes = 8192;
+__global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a, RowPlan plan) {
+  constexpr int kTileBytes = kStatTile<DT, HD>;
+  using T = Tile<DT, HD, kTileBytes>;
+  constexpr int W = kStatWaves, G = T::kGroups;
   extern __shared__ __attribute__((aligned(1024))) char lds[];  // the waves' tiles, two each; then the query rows and their normalisers
   __shared__ float sum_s[kTreeChunk], sum2_s[kTreeChunk];
   __shared__ signed char token_s[kTreeChunk];  // accepted token that a slot has taken, or -1
@@ -156,7 +161,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a,
   const int row0 = split * a.chunk, row1 = min(n_new, row0 + a.chunk);
   if (len == 0 || row0 >= row1) return;
 
-  Walk<DT, HD, W> walk;
+  Walk<DT, HD, W, kTileBytes> walk;
   walk.init(a.pages, a.B, a.heads, u, request, row0, row1, 0, wave, static_cast<unsigned>(u) * 5u + static_cast<unsigned>(split) * 3u);
   const int mine = walk.mine;
   char* const tiles = lds + wave * 2 * kTileBytes;
@@ -164,7 +169,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a,
   int koff[T::kGroupLoads];
   load_offsets<DT, HD, false>(koff);
   auto request_k = [&](int t) {
-    const typename Walk<DT, HD, W>::Place p = walk.place(t);
+    const typename Walk<DT, HD, W, kTileBytes>::Place p = walk.place(t);
     request_tile<DT, HD, STREAMING>(a.K, p.row, p.there, tiles_addr + (t & 1) * kTileBytes, koff);
     return p.there;
   };
@@ -311,7 +316,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void tree_statistics(CommitArgs a,
 #pragma clang diagnostic pop
 
 template <int DT, int HD, bool STREAMING, bool WINDOW> hipError_t launch_statistics(const CommitArgs& a, hipStream_t s) {
-  constexpr int kRowBytes = Tile<DT, HD>::kBytes, kTiles = kStatWaves * 2 * 8192, kMost = kTiles + kMostQueryLds / kRowBytes * (kRowBytes + 4);
+  constexpr int kRowBytes = Tile<DT, HD>::kBytes, kTiles = kStatWaves * 2 * kStatTile<DT, HD>, kMost = kTiles + kMostQueryLds / kRowBytes * (kRowBytes + 4);
   const RowPlan plan = row_plan(a.group, a.max_path, kRowBytes);
   const void* const fn = reinterpret_cast<const void*>(tree_statistics<DT, HD, STREAMING, WINDOW>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kMost) != hipSuccess) return hipErrorInvalidValue;
