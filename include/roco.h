@@ -445,8 +445,8 @@ enum {
   ROCO_PROF_PREFILL_ROWS = 3, ROCO_PROF_PREFILL_COLUMNS = 4, ROCO_PROF_PREFILL_SELECT = 5,
   ROCO_PROF_PREFILL_GATHER = 6, ROCO_PROF_READ_PROBE = 7, ROCO_PROF_BLOCK_PREPARE = 8,
   ROCO_PROF_BLOCK_ATTEND = 9, ROCO_PROF_BLOCK_FINISH = 10, ROCO_PROF_MFMA_PROBE = 11, ROCO_PROF_TREE_ATTEND = 12,
-  ROCO_PROF_TREE_JOIN = 13, ROCO_PROF_TREE_TAKE = 14, ROCO_PROF_TREE_STATISTICS = 15, ROCO_PROF_PAGE_TABLES = 16,
-  ROCO_PROF_PAGE_STORE = 17, ROCO_PROF_KERNELS = 18
+  ROCO_PROF_TREE_JOIN = 13, ROCO_PROF_TREE_CHOOSE = 14, ROCO_PROF_TREE_STATISTICS = 15, ROCO_PROF_TREE_APPLY = 16,
+  ROCO_PROF_PAGE_TABLES = 17, ROCO_PROF_PAGE_STORE = 18, ROCO_PROF_KERNELS = 19
 };
 int roco_profile_kernel(int which);
 int roco_profile_read(double* total_ms, int64_t* launches);

@@ -244,7 +244,7 @@ def decode_workspace_bytes(params: RocoParams) -> int:
 PROF_KERNELS = {"decode_select": 0, "decode_attend": 1, "decode_finish": 2, "prefill_rows": 3,
                 "prefill_columns": 4, "prefill_select": 5, "prefill_gather": 6, "read_probe": 7,
                 "block_prepare": 8, "block_attend": 9, "block_finish": 10, "mfma_probe": 11, "tree_attend": 12, "tree_join": 13,
-                "tree_take": 14, "tree_statistics": 15, "page_tables": 16, "page_store": 17}
+                "tree_choose": 14, "tree_statistics": 15, "tree_apply": 16, "page_tables": 17, "page_store": 18}
 
 
 def roco_profile_kernel(which: int) -> None:

@@ -123,8 +123,8 @@ int check_tree(const roco_params* p, int32_t heads, int32_t group, int32_t nodes
   return ROCO_OK;
 }
 
-// ---- workspace of the trees: tree_attend's part_m | part_l | part_o, or tree_commit's taken | keys
-struct TreeLayout { size_t part_l, part_o, keys, total; TreeSplits split; };
+// ---- workspace of the trees: tree_attend's part_m | part_l | part_o, or tree_commit's taken | sums | fresh | keys
+struct TreeLayout { size_t part_l, part_o, sums, fresh, keys, total; TreeSplits split; };
 TreeLayout tree_layout(const roco_params* p, int32_t group, int32_t nodes) {
   TreeLayout l;
   const size_t U = p->units, B = p->budget, rows = static_cast<size_t>(group) * nodes;
@@ -133,7 +133,9 @@ TreeLayout tree_layout(const roco_params* p, int32_t group, int32_t nodes) {
   l.part_l = plane;
   l.part_o = 2 * plane;
   const size_t attend = 2 * plane + plane * p->head_dim;
-  l.keys = align_up(U * kTakenWords * sizeof(int32_t));
+  l.sums = align_up(U * kTakenWords * sizeof(int32_t));
+  l.fresh = l.sums + align_up(U * 2 * B * sizeof(float));
+  l.keys = l.fresh + align_up(U * 2 * kMaxTreeNodes * sizeof(float));
   const size_t commit = l.keys + (p->budget > kMaxDecodeBudgetLds ? align_up(U * 2 * B * sizeof(uint32_t)) : 0);
   l.total = std::max(attend, commit);
   return l;
@@ -576,6 +578,8 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
   a.evicted_slot = evicted_slot; a.evicted_pos = evicted_pos;
   char* ws = static_cast<char*>(workspace);
   a.taken = reinterpret_cast<int32_t*>(ws);
+  a.sums = reinterpret_cast<float*>(ws + lay.sums);
+  a.fresh = reinterpret_cast<float*>(ws + lay.fresh);
   a.keys = reinterpret_cast<uint32_t*>(ws + lay.keys);
   return launch_tree_commit(params->dtype, params->head_dim, a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
 }

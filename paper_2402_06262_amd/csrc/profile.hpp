@@ -9,8 +9,8 @@ enum ProfKernel : int {
   kProfPrefillRows = 3, kProfPrefillColumns = 4, kProfPrefillSelect = 5, kProfPrefillGather = 6, kProfReadProbe = 7,
   kProfBlockPrepare = 8, kProfBlockAttend = 9, kProfBlockFinish = 10,
   kProfMfmaProbe = 11,
-  kProfTreeAttend = 12, kProfTreeJoin = 13, kProfTreeTake = 14, kProfTreeStatistics = 15, kProfPageTables = 16, kProfPageStore = 17,
-  kProfKernels = 18
+  kProfTreeAttend = 12, kProfTreeJoin = 13, kProfTreeChoose = 14, kProfTreeStatistics = 15, kProfTreeApply = 16, kProfPageTables = 17, kProfPageStore = 18,
+  kProfKernels = 19
 };
 
 extern int g_prof_which;  // -1 = off

@@ -1,10 +1,15 @@
-// A drafted tree's accepted path taken over into the budgeted cache.
+// A drafted tree's accepted path taken over into the budgeted cache, in two launches.
 //
-//   tree_take       : one workgroup per unit.  E = max(0, n + a - budget) victims by the statistics as they stand (two exact searches, as
-//                     in block_prepare), the accepted tokens to the freed and the empty slots in order, their K / V rows into the cache.
-//   tree_statistics : up to 1024 slots per workgroup.  The accepted rows' probabilities are formed again, exp(logit - lse), from one pass
-//                     over K alone: half of what the attention has read, where probabilities left behind by the attention would be 4 bytes
-//                     per slot, head and node, of which the accepted ones are known only now.
+//   tree_statistics : up to 1024 slots per workgroup.  The accepted rows' probabilities are formed again, exp(logit - lse), from one pass over K
+//                     alone: half of what the attention has read, where probabilities left behind by the attention would be 4 bytes per
+//                     slot, head and node, of which the accepted ones are known only now.  Their sums go to the workspace.  Beside these
+//                     workgroups, and before them, one per unit chooses the victims, E = max(0, n + a - budget) of them by the statistics
+//                     as they stand (two exact searches, as in block_prepare), and the slots that the accepted tokens take.  Neither changes
+//                     what the other reads.
+//   tree_apply      : the sums added to the statistics, the accepted tokens' rows, positions and statistics to their slots.
+//
+// (One after the other, choice and sums took 14 + 45 us on 512 units x 2048 slots and 9 + 7 on 16 x 500.  The search of a large budget
+// needs more threads and LDS than the sums leave it: above kMostChosenBeside slots it is a launch of its own.)
 #include <algorithm>
 
 #include "profile.hpp"
@@ -18,6 +23,8 @@ namespace {
 
 using namespace tree;
 
+constexpr int kMostChosenBeside = 4096;
+
 __device__ __forceinline__ int path_length(const CommitArgs& a, int request, int budget) {
   return min(max(a.n_path[request], 0), min(a.max_path, budget));
 }
@@ -25,13 +32,10 @@ __device__ __forceinline__ int path_node(const CommitArgs& a, int request, int k
   return min(max(a.path[static_cast<size_t>(request) * a.max_path + k], 0), a.nodes - 1);
 }
 
-// LDS: the ranking keys are in LDS (B <= kMaxDecodeBudgetLds).
-template <int NT, bool LDS> __global__ __launch_bounds__(NT, 8) void tree_take(CommitArgs a, int row_bytes) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t lds_keys[];  // [2][B]
-  __shared__ __attribute__((aligned(16))) uint32_t sel_sh[SelectLds<1>::kWords];
-  __shared__ uint32_t scan_sh[NT / kWave + 1];
-  __shared__ int slot_of[kMaxTreeNodes];
-  const int u = blockIdx.x, tid = threadIdx.x, B = a.B;
+// The victims and the slots of the accepted tokens: CommitArgs::taken and the records of what is evicted.  All threads of the workgroup.
+// sel_sh: SelectLds<1>::kWords words; keys: [2][B].
+template <int NT> __device__ __forceinline__ void choose_slots(const CommitArgs& a, int u, uint32_t* sel_sh, uint32_t* scan_sh, uint32_t* keys) {
+  const int tid = threadIdx.x, B = a.B;
   const int request = u / a.heads;
   const int budget = budget_of(a.pages, B, request);
   const int n = min(max(a.n_used[u], 0), budget);
@@ -51,18 +55,17 @@ template <int NT, bool LDS> __global__ __launch_bounds__(NT, 8) void tree_take(C
   const float* const acc = a.stats + static_cast<size_t>(u) * 3 * B;
   const float* const acc2 = acc + B;
   const float* const cnt = acc2 + B;
-  int32_t* const pos = a.pos + static_cast<size_t>(u) * B;
-  uint32_t* const var_key = LDS ? lds_keys : a.keys + static_cast<size_t>(u) * 2 * B;
-  uint32_t* const mas_key = var_key + B;
+  const int32_t* const pos = a.pos + static_cast<size_t>(u) * B;
+  uint32_t *const var_key = keys, *const mas_key = keys + B;
   KSmallest scope = {0u, 0u}, out = {0u, 0u};
   if (E > 0) {
-#pragma unroll 1
+#pragma unroll 4
     for (int i = tid; i < n; i += NT) ranking_keys(acc[i], acc2[i], cnt[i], pos[i], a.pol, mas_key[i], var_key[i]);
     __syncthreads();
     const uint32_t m = min(static_cast<uint32_t>(n), static_cast<uint32_t>(a.pol.scope_size(min(a.scope, budget), n)) + static_cast<uint32_t>(E) - 1u);
 #pragma unroll 1
     for (int phase = 0; phase < 2; ++phase) {
-      const KSmallest r = select_k_smallest<NT, 1, 1>(
+      const KSmallest r = select_k_smallest<NT, 1, NT <= 256 ? 4 : 1>(
           [&](int i) -> uint32_t {
             const uint32_t vk = var_key[i];
             return phase == 0 ? vk : scope.has(vk, i) ? mas_key[i] : 0xffffffffu;
@@ -85,33 +88,25 @@ template <int NT, bool LDS> __global__ __launch_bounds__(NT, 8) void tree_take(C
   for (int j = lo; j < hi; ++j) mine += is_target(j) ? 1u : 0u;
   uint32_t total;
   uint32_t rank = block_exclusive_scan<NT>(mine, scan_sh, total);
+  if (mine == 0) return;
 #pragma unroll 1
   for (int j = lo; j < hi; ++j) {
     if (!is_target(j) || rank >= static_cast<uint32_t>(len)) continue;
     const int k = static_cast<int>(rank++);
-    slot_of[k] = j;
     taken[4 + k] = j;
     const bool held = j < n;  // by a token that is now evicted
     if (a.evicted_slot != nullptr) a.evicted_slot[static_cast<size_t>(u) * a.max_path + k] = held ? j : -1;
     if (a.evicted_pos != nullptr) a.evicted_pos[static_cast<size_t>(u) * a.max_path + k] = held ? pos[j] : -1;
-    pos[j] = a.qpos0[u] + k;
   }
-  __syncthreads();
-  if (tid == 0) a.n_used[u] = n_new;
-  const int lanes = row_bytes / 16;
-#pragma unroll 1
-  for (int i = tid; i < len * lanes; i += NT) {
-    const int k = i / lanes, col = i % lanes * 16, slot = slot_of[k];
-    const size_t src = (static_cast<size_t>(u) * a.nodes + path_node(a, request, k)) * row_bytes + col;
-    size_t row = static_cast<size_t>(u) * B + slot;
-    if (a.pages.table != nullptr) {
-      const int page = a.pages.table[static_cast<size_t>(request) * a.pages.max_pages + (slot >> a.pages.page_log2)];
-      if (page < 0 || page >= a.pages.n_pages) continue;
-      row = ((static_cast<size_t>(page) * a.heads + (u - request * a.heads)) << a.pages.page_log2) + (slot & ((1 << a.pages.page_log2) - 1));
-    }
-    *reinterpret_cast<uint4*>(static_cast<char*>(a.K) + row * row_bytes + col) = load16(static_cast<const char*>(a.k_new) + src);
-    *reinterpret_cast<uint4*>(static_cast<char*>(a.V) + row * row_bytes + col) = load16(static_cast<const char*>(a.v_new) + src);
-  }
+}
+
+// LDS: the ranking keys are in LDS (B <= kMaxDecodeBudgetLds).
+constexpr int kChooseThreads = 1024;
+template <bool LDS> __global__ __launch_bounds__(kChooseThreads, 8) void tree_choose(CommitArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds_keys[];  // [2][B]
+  __shared__ __attribute__((aligned(16))) uint32_t sel_sh[SelectLds<1>::kWords];
+  __shared__ uint32_t scan_sh[kChooseThreads / kWave + 1];
+  choose_slots<kChooseThreads>(a, blockIdx.x, sel_sh, scan_sh, LDS ? lds_keys : a.keys + static_cast<size_t>(blockIdx.x) * 2 * a.B);
 }
 
 constexpr int kStatWaves = 4;
@@ -139,30 +134,38 @@ inline RowPlan row_plan(int group, int max_path, int row_bytes) {
   return p;
 }
 
-// Q is the A operand here, so that a lane holds four rows of one slot.  The accepted tokens' K rows have been written to their slots: a slot of
-// token m is one that the rows before m do not see.  More rows than the LDS takes: another pass over K (which the L2 mostly has).
+// Q is the A operand here, so that a lane holds four rows of one slot.  The accepted tokens themselves are tiles of the last workgroup, gathered
+// from k_new; token m is not seen by the rows before m.  More rows than the LDS takes: another pass over K (which the L2 mostly has).
+// choosers: the first workgroups, one per unit, that choose its slots (0: they have been chosen).
 template <int DT, int HD, bool STREAMING, bool WINDOW>
-__global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a, RowPlan plan) {
+__global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a, RowPlan plan, int choosers) {
   constexpr int kTileBytes = kStatTile<DT, HD>;
   using T = Tile<DT, HD, kTileBytes>;
   constexpr int W = kStatWaves, G = T::kGroups;
-  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the waves' tiles, two each; then the query rows and their normalisers
-  __shared__ float sum_s[kTreeChunk], sum2_s[kTreeChunk];
-  __shared__ signed char token_s[kTreeChunk];  // accepted token that a slot has taken, or -1
+  extern __shared__ __attribute__((aligned(1024))) char lds[];  // the waves' tiles, two each, then the query rows and their normalisers; or a choice's keys
+  __shared__ float sum_s[kTreeChunk], sum2_s[kTreeChunk], fresh_s[2][kMaxTreeNodes];
   __shared__ int32_t pos_s[WINDOW ? kTreeChunk : 1];
-  const int u = blockIdx.x % a.units, split = blockIdx.x / a.units;
+  if (static_cast<int>(blockIdx.x) < choosers) {
+    uint32_t* const words = reinterpret_cast<uint32_t*>(lds);
+    choose_slots<kStatThreads>(a, blockIdx.x, words, reinterpret_cast<uint32_t*>(fresh_s[0]), words + (SelectLds<1>::kWords + 3) / 4 * 4);
+    return;
+  }
+  const int id = blockIdx.x - choosers, u = id % a.units, split = id / a.units;
   const int request = u / a.heads;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int qi = lane & 15, g = lane >> 4;
-  const int32_t* const taken = a.taken + static_cast<size_t>(u) * kTakenWords;
   // (what has to come from memory before anything else is asked for together)
-  const int my_slot = taken[4 + lane], my_node = path_node(a, request, min(lane, a.max_path - 1));
-  const int n = __builtin_amdgcn_readfirstlane(taken[0]), len = __builtin_amdgcn_readfirstlane(taken[1]), n_new = __builtin_amdgcn_readfirstlane(taken[2]);
-  const int row0 = split * a.chunk, row1 = min(n_new, row0 + a.chunk);
-  if (len == 0 || row0 >= row1) return;
+  const int my_node = path_node(a, request, min(lane, a.max_path - 1));
+  const int budget = budget_of(a.pages, a.B, request), asked_len = a.n_path[request], held = a.n_used[u];
+  const int n = __builtin_amdgcn_readfirstlane(min(max(held, 0), budget));
+  const int len = __builtin_amdgcn_readfirstlane(min(max(asked_len, 0), min(a.max_path, budget)));
+  const int used = splits_used(n, a.chunk);  // the last of them takes the accepted tokens too
+  if (len == 0 || split >= used) return;
+  const int row0 = split * a.chunk, row1 = min(n, row0 + a.chunk);
+  const int fresh = split == used - 1 ? len : 0;
 
   Walk<DT, HD, W, kTileBytes> walk;
-  walk.init(a.pages, a.B, a.heads, u, request, row0, row1, 0, wave, static_cast<unsigned>(u) * 5u + static_cast<unsigned>(split) * 3u);
+  walk.init(a.pages, a.B, a.heads, u, request, row0, row1, fresh, wave, static_cast<unsigned>(u) * 5u + static_cast<unsigned>(split) * 3u);
   const int mine = walk.mine;
   char* const tiles = lds + wave * 2 * kTileBytes;
   const uint32_t tiles_addr = lds_address(tiles);
@@ -170,16 +173,27 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
   load_offsets<DT, HD, false>(koff);
   auto request_k = [&](int t) {
     const typename Walk<DT, HD, W, kTileBytes>::Place p = walk.place(t);
-    request_tile<DT, HD, STREAMING>(a.K, p.row, p.there, tiles_addr + (t & 1) * kTileBytes, koff);
+    const uint32_t dst = tiles_addr + (t & 1) * kTileBytes;
+    if (!walk.is_nodes(t)) {
+      request_tile<DT, HD, STREAMING>(a.K, p.row, p.there, dst, koff);
+      return p.there;
+    }
+    // the accepted tokens' rows, each from its node's (what lies behind the last token is out of range)
+    const v4i32 buf = make_buffer(static_cast<const char*>(a.k_new) + static_cast<size_t>(u) * a.nodes * T::kBytes, static_cast<uint32_t>(a.nodes) * T::kBytes);
+    const int lane2 = late_thread_id() & (kWave - 1);
+#pragma unroll
+    for (int j = 0; j < T::kLoads; ++j) {
+      const int r = T::kPerLoad * j + lane2 / T::kChunks, c = lane2 % T::kChunks, k = walk.first_node(t) + r;
+      const int node = __shfl(my_node, min(k, kWave - 1), kWave);
+      mfma::load16_to_lds(buf, dst + j * 1024, k < len ? node * T::kBytes + ((c ^ T::swizzle_k(r & 15)) << 4) : 0x7ffffff0, 0);
+    }
     return p.there;
   };
   for (int j = tid; j < row1 - row0; j += kStatThreads) {
-    token_s[j] = -1;
     sum_s[j] = sum2_s[j] = 0.0f;
     if (WINDOW) pos_s[WINDOW ? j : 0] = a.pos[static_cast<size_t>(u) * a.B + row0 + j];
   }
-  __syncthreads();
-  if (tid < len && my_slot >= row0 && my_slot < row1) token_s[my_slot - row0] = static_cast<signed char>(tid);
+  if (tid < 2 * kMaxTreeNodes) fresh_s[tid / kMaxTreeNodes][tid % kMaxTreeNodes] = 0.0f;
 
   const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 : 0.0f, share = 1.0f / static_cast<float>(a.group);
   const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
@@ -226,15 +240,16 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
       reads_done();
       uint32_t there2 = 0;
       if (t + 2 < mine) there2 = request_k(t + 2);
-      const int j0 = walk.first_slot(t) - row0;
+      const bool of_fresh = walk.is_nodes(t);
+      const int j0 = of_fresh ? walk.first_node(t) : walk.first_slot(t) - row0;
       float sum[G], sum2[G];
-      int own[G], at[G];
+      int own[G], at[G];  // the first row that sees the slot, or the token; its position
 #pragma unroll
       for (int i = 0; i < G; ++i) {
         sum[i] = sum2[i] = 0.0f;
-        const int j = min(j0 + 16 * i + qi, row1 - row0 - 1);
-        own[i] = token_s[j];
-        at[i] = WINDOW ? pos_s[WINDOW ? j : 0] : 0;
+        const int j = j0 + 16 * i + qi;
+        own[i] = of_fresh ? j : 0;
+        at[i] = !WINDOW ? 0 : of_fresh ? qp0 + j : pos_s[WINDOW ? min(j, kTreeChunk - 1) : 0];
       }
 #pragma unroll 1
       for (int tile0 = 0; tile0 < rows; tile0 += 16 * slices) {
@@ -291,8 +306,9 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
         sum2[i] += __shfl_xor(sum2[i], 16, kWave);
         sum2[i] += __shfl_xor(sum2[i], 32, kWave);
         if (g == 0 && qi < static_cast<int>((there0 >> (8 * i)) & 0xffu)) {  // (slots of no page have received nothing)
-          sum_s[j0 + 16 * i + qi] += sum[i];
-          sum2_s[j0 + 16 * i + qi] += sum2[i];
+          float *const first_sum = of_fresh ? fresh_s[0] : sum_s, *const second_sum = of_fresh ? fresh_s[1] : sum2_s;
+          first_sum[j0 + 16 * i + qi] += sum[i];
+          second_sum[j0 + 16 * i + qi] += sum2[i];
         }
       }
       there0 = there1;
@@ -300,48 +316,107 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
     }
   }
   __syncthreads();
-  // ---- the slots' statistics: added to those of older tokens, the first ones of the accepted
+  float* const sums = a.sums + static_cast<size_t>(u) * 2 * a.B + row0;
+  for (int j = tid; j < row1 - row0; j += kStatThreads) {
+    sums[j] = sum_s[j];
+    sums[a.B + j] = sum2_s[j];
+  }
+  if (tid < 2 * kMaxTreeNodes && tid % kMaxTreeNodes < fresh)
+    a.fresh[static_cast<size_t>(u) * 2 * kMaxTreeNodes + tid] = fresh_s[tid / kMaxTreeNodes][tid % kMaxTreeNodes];
+}
+
+// ------------------------------------------------------------------------------------------------
+constexpr int kApplyThreads = 256;
+// A workgroup has kTreeChunk slots of a unit.
+__global__ __launch_bounds__(kApplyThreads) void tree_apply(CommitArgs a, int row_bytes) {
+  __shared__ signed char token_s[kTreeChunk];  // accepted token that a slot takes, or -1
+  const int u = blockIdx.x % a.units, row0 = blockIdx.x / a.units * kTreeChunk;
+  const int request = u / a.heads;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int32_t* const taken = a.taken + static_cast<size_t>(u) * kTakenWords;
+  const int len = taken[1], n_new = taken[2];
+  const int my_slot = taken[4 + lane], my_node = path_node(a, request, min(lane, a.max_path - 1));
+  const int row1 = min(n_new, row0 + kTreeChunk);
+  if (len == 0 || row0 >= row1) return;
+  for (int j = tid; j < kTreeChunk; j += kApplyThreads) token_s[j] = -1;
+  __syncthreads();
+  if (tid < len && my_slot >= row0 && my_slot < row1) {
+    token_s[my_slot - row0] = static_cast<signed char>(tid);
+    a.pos[static_cast<size_t>(u) * a.B + my_slot] = a.qpos0[u] + tid;
+  }
+  if (tid == 0 && row0 == 0) a.n_used[u] = n_new;
+  __syncthreads();
   float* const acc = a.stats + static_cast<size_t>(u) * 3 * a.B + row0;
   float* const acc2 = acc + a.B;
   float* const cnt = acc2 + a.B;
-  for (int j = tid; j < row1 - row0; j += kStatThreads) {
+  const float* const sums = a.sums + static_cast<size_t>(u) * 2 * a.B + row0;
+  const float* const fresh = a.fresh + static_cast<size_t>(u) * 2 * kMaxTreeNodes;
+#pragma unroll 1
+  for (int j = tid; j < row1 - row0; j += kApplyThreads) {
     const int k = token_s[j];
-    const bool old = k < 0;
-    acc[j] = (old ? acc[j] : 0.0f) + sum_s[j];
-    acc2[j] = (old && !a.pol.keeps_last_score() ? acc2[j] : 0.0f) + sum2_s[j];
-    cnt[j] = old ? cnt[j] + static_cast<float>(len) : static_cast<float>(len - k);
+    if (k >= 0) {
+      acc[j] = fresh[k];
+      acc2[j] = fresh[kMaxTreeNodes + k];
+      cnt[j] = static_cast<float>(len - k);
+    } else {
+      acc[j] += sums[j];
+      acc2[j] = (a.pol.keeps_last_score() ? 0.0f : acc2[j]) + sums[a.B + j];
+      cnt[j] += static_cast<float>(len);
+    }
+  }
+  // the rows of the tokens whose slots are among these, a wave's token at a time
+#pragma unroll 1
+  for (int k = tid / kWave; k < len; k += kApplyThreads / kWave) {
+    const int slot = __shfl(my_slot, k, kWave), node = __shfl(my_node, k, kWave);
+    if (slot < row0 || slot >= row1) continue;
+    size_t row = static_cast<size_t>(u) * a.B + slot;
+    if (a.pages.table != nullptr) {
+      const int page = a.pages.table[static_cast<size_t>(request) * a.pages.max_pages + (slot >> a.pages.page_log2)];
+      if (page < 0 || page >= a.pages.n_pages) continue;
+      row = ((static_cast<size_t>(page) * a.heads + (u - request * a.heads)) << a.pages.page_log2) + (slot & ((1 << a.pages.page_log2) - 1));
+    }
+    const size_t src = (static_cast<size_t>(u) * a.nodes + node) * row_bytes, dst = row * row_bytes;
+    if (lane * 16 < row_bytes) {
+      *reinterpret_cast<uint4*>(static_cast<char*>(a.K) + dst + lane * 16) = load16(static_cast<const char*>(a.k_new) + src + lane * 16);
+      *reinterpret_cast<uint4*>(static_cast<char*>(a.V) + dst + lane * 16) = load16(static_cast<const char*>(a.v_new) + src + lane * 16);
+    }
   }
 }
 
 #pragma clang diagnostic pop
 
 template <int DT, int HD, bool STREAMING, bool WINDOW> hipError_t launch_statistics(const CommitArgs& a, hipStream_t s) {
-  constexpr int kRowBytes = Tile<DT, HD>::kBytes, kTiles = kStatWaves * 2 * kStatTile<DT, HD>, kMost = kTiles + kMostQueryLds / kRowBytes * (kRowBytes + 4);
+  ProfScope ps(kProfTreeStatistics, s);
+  constexpr int kRowBytes = Tile<DT, HD>::kBytes, kTiles = kStatWaves * 2 * kStatTile<DT, HD>;
+  constexpr int kMostStat = kTiles + kMostQueryLds / kRowBytes * (kRowBytes + 4), kMostChoice = (SelectLds<1>::kWords + 4 + 2 * kMostChosenBeside) * 4;
   const RowPlan plan = row_plan(a.group, a.max_path, kRowBytes);
+  const int choosers = a.B <= kMostChosenBeside ? a.units : 0;
   const void* const fn = reinterpret_cast<const void*>(tree_statistics<DT, HD, STREAMING, WINDOW>);
-  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kMost) != hipSuccess) return hipErrorInvalidValue;
-  const size_t lds = kTiles + static_cast<size_t>(plan.rows(plan.per_pass)) * (kRowBytes + 4);
-  hipLaunchKernelGGL((tree_statistics<DT, HD, STREAMING, WINDOW>), dim3(static_cast<unsigned>(a.units) * a.splits), dim3(kStatThreads), lds, s, a, plan);
+  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, std::max(kMostStat, kMostChoice)) != hipSuccess) return hipErrorInvalidValue;
+  const int stat = kTiles + plan.rows(plan.per_pass) * (kRowBytes + 4), choice = choosers > 0 ? (SelectLds<1>::kWords + 4 + 2 * a.B) * 4 : 0;
+  hipLaunchKernelGGL((tree_statistics<DT, HD, STREAMING, WINDOW>), dim3(static_cast<unsigned>(choosers) + static_cast<unsigned>(a.units) * a.splits), dim3(kStatThreads),
+                     std::max(stat, choice), s, a, plan, choosers);
   return hipGetLastError();
 }
 
 template <int DT, int HD> hipError_t launch_commit(const CommitArgs& a, hipStream_t s) {
-  constexpr int kRowBytes = Tile<DT, HD>::kBytes;
-  const size_t key_lds = key_lds_bytes(a.B);
-  if (!allow_key_lds(reinterpret_cast<const void*>(tree_take<512, true>), key_lds) ||
-      !allow_key_lds(reinterpret_cast<const void*>(tree_take<1024, true>), key_lds))
-    return hipErrorInvalidValue;
-  {
-    ProfScope ps(kProfTreeTake, s);
-    if (key_lds == 0) hipLaunchKernelGGL((tree_take<1024, false>), dim3(a.units), dim3(1024), 0, s, a, kRowBytes);
-    else if (a.units > 256) hipLaunchKernelGGL((tree_take<512, true>), dim3(a.units), dim3(512), key_lds, s, a, kRowBytes);
-    else hipLaunchKernelGGL((tree_take<1024, true>), dim3(a.units), dim3(1024), key_lds, s, a, kRowBytes);
-    const hipError_t e = hipGetLastError();
+  hipError_t e = hipSuccess;
+  if (a.B > kMostChosenBeside) {
+    ProfScope ps(kProfTreeChoose, s);
+    const size_t key_lds = key_lds_bytes(a.B);
+    if (!allow_key_lds(reinterpret_cast<const void*>(tree_choose<true>), key_lds)) return hipErrorInvalidValue;
+    if (key_lds == 0) hipLaunchKernelGGL((tree_choose<false>), dim3(a.units), dim3(kChooseThreads), 0, s, a);
+    else hipLaunchKernelGGL((tree_choose<true>), dim3(a.units), dim3(kChooseThreads), key_lds, s, a);
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  ProfScope ps(kProfTreeStatistics, s);
-  if (a.recency_window > 0) return a.streaming ? launch_statistics<DT, HD, true, true>(a, s) : launch_statistics<DT, HD, false, true>(a, s);
-  return a.streaming ? launch_statistics<DT, HD, true, false>(a, s) : launch_statistics<DT, HD, false, false>(a, s);
+  if (a.recency_window > 0) e = a.streaming ? launch_statistics<DT, HD, true, true>(a, s) : launch_statistics<DT, HD, false, true>(a, s);
+  else e = a.streaming ? launch_statistics<DT, HD, true, false>(a, s) : launch_statistics<DT, HD, false, false>(a, s);
+  if (e != hipSuccess) return e;
+  ProfScope ps(kProfTreeApply, s);
+  const unsigned chunks = static_cast<unsigned>((a.B + kTreeChunk - 1) / kTreeChunk);
+  hipLaunchKernelGGL(tree_apply, dim3(static_cast<unsigned>(a.units) * chunks), dim3(kApplyThreads), 0, s, a, Tile<DT, HD>::kBytes);
+  return hipGetLastError();
 }
 
 }  // namespace
