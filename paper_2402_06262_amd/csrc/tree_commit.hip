@@ -111,6 +111,8 @@ template <bool LDS> __global__ __launch_bounds__(kChooseThreads, 8) void tree_ch
 
 constexpr int kStatWaves = 4;
 constexpr int kStatThreads = kStatWaves * kWave;
+constexpr int kChoiceWords = 8 + (SelectLds<1>::kWords + 3) / 4 * 4;  // of a choice among the sums, before its keys
+static_assert(kStatThreads / kWave + 1 <= 8, "the scan's words");
 // Bytes of a wave's tile: small ones, so that four workgroups are on a compute unit and one's sums over its rows, or its way to the first tile,
 // go beside the others' streams (8 KiB and two workgroups: 512 units x 2048 slots of bf16 / 128 75.1 us against 70.3, 192 x 4096 of
 // bf16 / 64 51.1 / 46.6).  16 slots are the least.
@@ -143,11 +145,10 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
   using T = Tile<DT, HD, kTileBytes>;
   constexpr int W = kStatWaves, G = T::kGroups;
   extern __shared__ __attribute__((aligned(1024))) char lds[];  // the waves' tiles, two each, then the query rows and their normalisers; or a choice's keys
-  __shared__ float sum_s[kTreeChunk], sum2_s[kTreeChunk], fresh_s[2][kMaxTreeNodes];
   __shared__ int32_t pos_s[WINDOW ? kTreeChunk : 1];
   if (static_cast<int>(blockIdx.x) < choosers) {
     uint32_t* const words = reinterpret_cast<uint32_t*>(lds);
-    choose_slots<kStatThreads>(a, blockIdx.x, words, reinterpret_cast<uint32_t*>(fresh_s[0]), words + (SelectLds<1>::kWords + 3) / 4 * 4);
+    choose_slots<kStatThreads>(a, blockIdx.x, words + 8, words, words + kChoiceWords);
     return;
   }
   const int id = blockIdx.x - choosers, u = id % a.units, split = id / a.units;
@@ -189,11 +190,10 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
     }
     return p.there;
   };
-  for (int j = tid; j < row1 - row0; j += kStatThreads) {
-    sum_s[j] = sum2_s[j] = 0.0f;
-    if (WINDOW) pos_s[WINDOW ? j : 0] = a.pos[static_cast<size_t>(u) * a.B + row0 + j];
-  }
-  if (tid < 2 * kMaxTreeNodes) fresh_s[tid / kMaxTreeNodes][tid % kMaxTreeNodes] = 0.0f;
+  if (WINDOW)
+    for (int j = tid; j < row1 - row0; j += kStatThreads) pos_s[WINDOW ? j : 0] = a.pos[static_cast<size_t>(u) * a.B + row0 + j];
+  float* const sums = a.sums + static_cast<size_t>(u) * 2 * a.B + row0;
+  float* const fresh_sums = a.fresh + static_cast<size_t>(u) * 2 * kMaxTreeNodes;
 
   const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 : 0.0f, share = 1.0f / static_cast<float>(a.group);
   const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
@@ -230,8 +230,10 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
 #pragma unroll 1
     for (int t = 0; t < mine; ++t) {
       const char* const tile = tiles + (t & 1) * kTileBytes;
-      if (t + 1 < mine) wait_loads<T::kLoads>();
-      else wait_loads<0>();
+      // (newer than the tile's loads: those of the tile after it, and the stores of the two before)
+      if (t + 1 >= mine) wait_loads<0>();
+      else if (t == 0) wait_loads<T::kLoads>();
+      else wait_loads<T::kLoads + G>();
       uint4 kf[G][T::kSteps];
 #pragma unroll
       for (int i = 0; i < G; ++i)
@@ -305,24 +307,20 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
         sum[i] += __shfl_xor(sum[i], 32, kWave);
         sum2[i] += __shfl_xor(sum2[i], 16, kWave);
         sum2[i] += __shfl_xor(sum2[i], 32, kWave);
-        if (g == 0 && qi < static_cast<int>((there0 >> (8 * i)) & 0xffu)) {  // (slots of no page have received nothing)
-          float *const first_sum = of_fresh ? fresh_s[0] : sum_s, *const second_sum = of_fresh ? fresh_s[1] : sum2_s;
-          first_sum[j0 + 16 * i + qi] += sum[i];
-          second_sum[j0 + 16 * i + qi] += sum2[i];
-        }
+        // A slot's sums are its wave's alone: they go to memory at once (8 KiB of LDS for them would cost a workgroup per compute unit), as one
+        // store of a count that the waits rely on: the first 16 lanes' Acc, the next 16 lanes' Acc2, the others' out of range.
+        const int j = j0 + 16 * i + qi, step = of_fresh ? kMaxTreeNodes : a.B;
+        float* const to = of_fresh ? fresh_sums : sums;
+        float v = qi < static_cast<int>((there0 >> (8 * i)) & 0xffu) ? g == 0 ? sum[i] : sum2[i] : 0.0f;  // (slots of no page receive nothing)
+        const bool there = g < 2 && j < (of_fresh ? len : row1 - row0);
+        if (first > 0 && there) v += to[g * step + j];
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), __builtin_amdgcn_make_buffer_rsrc(to, 0, (step + (of_fresh ? len : row1 - row0)) * 4, 0x00020000),
+                                              there ? (g * step + j) * 4 : 0x7ffffff0, 0, 0);
       }
       there0 = there1;
       there1 = there2;
     }
   }
-  __syncthreads();
-  float* const sums = a.sums + static_cast<size_t>(u) * 2 * a.B + row0;
-  for (int j = tid; j < row1 - row0; j += kStatThreads) {
-    sums[j] = sum_s[j];
-    sums[a.B + j] = sum2_s[j];
-  }
-  if (tid < 2 * kMaxTreeNodes && tid % kMaxTreeNodes < fresh)
-    a.fresh[static_cast<size_t>(u) * 2 * kMaxTreeNodes + tid] = fresh_s[tid / kMaxTreeNodes][tid % kMaxTreeNodes];
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -388,12 +386,12 @@ __global__ __launch_bounds__(kApplyThreads) void tree_apply(CommitArgs a, int ro
 template <int DT, int HD, bool STREAMING, bool WINDOW> hipError_t launch_statistics(const CommitArgs& a, hipStream_t s) {
   ProfScope ps(kProfTreeStatistics, s);
   constexpr int kRowBytes = Tile<DT, HD>::kBytes, kTiles = kStatWaves * 2 * kStatTile<DT, HD>;
-  constexpr int kMostStat = kTiles + kMostQueryLds / kRowBytes * (kRowBytes + 4), kMostChoice = (SelectLds<1>::kWords + 4 + 2 * kMostChosenBeside) * 4;
+  constexpr int kMostStat = kTiles + kMostQueryLds / kRowBytes * (kRowBytes + 4), kMostChoice = (kChoiceWords + 2 * kMostChosenBeside) * 4;
   const RowPlan plan = row_plan(a.group, a.max_path, kRowBytes);
   const int choosers = a.B <= kMostChosenBeside ? a.units : 0;
   const void* const fn = reinterpret_cast<const void*>(tree_statistics<DT, HD, STREAMING, WINDOW>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, std::max(kMostStat, kMostChoice)) != hipSuccess) return hipErrorInvalidValue;
-  const int stat = kTiles + plan.rows(plan.per_pass) * (kRowBytes + 4), choice = choosers > 0 ? (SelectLds<1>::kWords + 4 + 2 * a.B) * 4 : 0;
+  const int stat = kTiles + plan.rows(plan.per_pass) * (kRowBytes + 4), choice = choosers > 0 ? (kChoiceWords + 2 * a.B) * 4 : 0;
   hipLaunchKernelGGL((tree_statistics<DT, HD, STREAMING, WINDOW>), dim3(static_cast<unsigned>(choosers) + static_cast<unsigned>(a.units) * a.splits), dim3(kStatThreads),
                      std::max(stat, choice), s, a, plan, choosers);
   return hipGetLastError();
