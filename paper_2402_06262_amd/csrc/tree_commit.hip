@@ -33,8 +33,9 @@ __device__ __forceinline__ int path_node(const CommitArgs& a, int request, int k
 }
 
 // The victims and the slots of the accepted tokens: CommitArgs::taken and the records of what is evicted.  All threads of the workgroup.
-// sel_sh: SelectLds<1>::kWords words; keys: [2][B].
-template <int NT> __device__ __forceinline__ void choose_slots(const CommitArgs& a, int u, uint32_t* sel_sh, uint32_t* scan_sh, uint32_t* keys) {
+// sel_sh: SelectLds<1>::kWords words; list_sh: kListWords; keys: [2][B].
+constexpr int kListWords = (1 + kMaxTreeNodes + 3) / 4 * 4;
+template <int NT> __device__ __forceinline__ void choose_slots(const CommitArgs& a, int u, uint32_t* sel_sh, uint32_t* list_sh, uint32_t* keys) {
   const int tid = threadIdx.x, B = a.B;
   const int request = u / a.heads;
   const int budget = budget_of(a.pages, B, request);
@@ -50,6 +51,7 @@ template <int NT> __device__ __forceinline__ void choose_slots(const CommitArgs&
     taken[0] = n;
     taken[1] = len;
     taken[2] = n_new;
+    list_sh[0] = 0u;
   }
   if (len == 0) return;
   const float* const acc = a.stats + static_cast<size_t>(u) * 3 * B;
@@ -58,8 +60,10 @@ template <int NT> __device__ __forceinline__ void choose_slots(const CommitArgs&
   const int32_t* const pos = a.pos + static_cast<size_t>(u) * B;
   uint32_t *const var_key = keys, *const mas_key = keys + B;
   KSmallest scope = {0u, 0u}, out = {0u, 0u};
-  if (E > 0) {
-#pragma unroll 4
+  if (E == 0) {
+    __syncthreads();
+  } else {
+#pragma unroll 8
     for (int i = tid; i < n; i += NT) ranking_keys(acc[i], acc2[i], cnt[i], pos[i], a.pol, mas_key[i], var_key[i]);
     __syncthreads();
     const uint32_t m = min(static_cast<uint32_t>(n), static_cast<uint32_t>(a.pol.scope_size(min(a.scope, budget), n)) + static_cast<uint32_t>(E) - 1u);
@@ -80,24 +84,23 @@ template <int NT> __device__ __forceinline__ void choose_slots(const CommitArgs&
     if (E == 0) return false;
     return out.has(scope.has(var_key[j], j) ? mas_key[j] : 0xffffffffu, j);
   };
-  // thread t owns the slots [t c, (t + 1) c); the i-th target takes the i-th token
-  const int c = (n_new + NT - 1) / NT;
-  const int lo = min(n_new, tid * c), hi = min(n_new, lo + c);
-  uint32_t mine = 0;
-#pragma unroll 1
-  for (int j = lo; j < hi; ++j) mine += is_target(j) ? 1u : 0u;
-  uint32_t total;
-  uint32_t rank = block_exclusive_scan<NT>(mine, scan_sh, total);
-  if (mine == 0) return;
-#pragma unroll 1
-  for (int j = lo; j < hi; ++j) {
-    if (!is_target(j) || rank >= static_cast<uint32_t>(len)) continue;
-    const int k = static_cast<int>(rank++);
-    taken[4 + k] = j;
-    const bool held = j < n;  // by a token that is now evicted
-    if (a.evicted_slot != nullptr) a.evicted_slot[static_cast<size_t>(u) * a.max_path + k] = held ? j : -1;
-    if (a.evicted_pos != nullptr) a.evicted_pos[static_cast<size_t>(u) * a.max_path + k] = held ? pos[j] : -1;
-  }
+  // The targets, `len` of them, in any order, then each by the number of those before it: the i-th takes the i-th token.
+  uint32_t* const found = list_sh + 1;
+#pragma unroll 4
+  for (int j = tid; j < n_new; j += NT)
+    if (is_target(j)) {
+      const uint32_t at = atomicAdd(&list_sh[0], 1u);
+      if (at < static_cast<uint32_t>(len)) found[at] = static_cast<uint32_t>(j);
+    }
+  __syncthreads();
+  if (tid >= len) return;
+  const int j = static_cast<int>(found[tid]);
+  int k = 0;
+  for (int i = 0; i < len; ++i) k += static_cast<int>(found[i]) < j ? 1 : 0;
+  taken[4 + k] = j;
+  const bool held = j < n;  // by a token that is now evicted
+  if (a.evicted_slot != nullptr) a.evicted_slot[static_cast<size_t>(u) * a.max_path + k] = held ? j : -1;
+  if (a.evicted_pos != nullptr) a.evicted_pos[static_cast<size_t>(u) * a.max_path + k] = held ? pos[j] : -1;
 }
 
 // LDS: the ranking keys are in LDS (B <= kMaxDecodeBudgetLds).
@@ -105,14 +108,13 @@ constexpr int kChooseThreads = 1024;
 template <bool LDS> __global__ __launch_bounds__(kChooseThreads, 8) void tree_choose(CommitArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint32_t lds_keys[];  // [2][B]
   __shared__ __attribute__((aligned(16))) uint32_t sel_sh[SelectLds<1>::kWords];
-  __shared__ uint32_t scan_sh[kChooseThreads / kWave + 1];
-  choose_slots<kChooseThreads>(a, blockIdx.x, sel_sh, scan_sh, LDS ? lds_keys : a.keys + static_cast<size_t>(blockIdx.x) * 2 * a.B);
+  __shared__ uint32_t list_sh[kListWords];
+  choose_slots<kChooseThreads>(a, blockIdx.x, sel_sh, list_sh, LDS ? lds_keys : a.keys + static_cast<size_t>(blockIdx.x) * 2 * a.B);
 }
 
 constexpr int kStatWaves = 4;
 constexpr int kStatThreads = kStatWaves * kWave;
-constexpr int kChoiceWords = 8 + (SelectLds<1>::kWords + 3) / 4 * 4;  // of a choice among the sums, before its keys
-static_assert(kStatThreads / kWave + 1 <= 8, "the scan's words");
+constexpr int kChoiceWords = kListWords + (SelectLds<1>::kWords + 3) / 4 * 4;  // of a choice among the sums, before its keys
 // Bytes of a wave's tile: small ones, so that four workgroups are on a compute unit and one's sums over its rows, or its way to the first tile,
 // go beside the others' streams (8 KiB and two workgroups: 512 units x 2048 slots of bf16 / 128 75.1 us against 70.3, 192 x 4096 of
 // bf16 / 64 51.1 / 46.6).  16 slots are the least.
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
   __shared__ int32_t pos_s[WINDOW ? kTreeChunk : 1];
   if (static_cast<int>(blockIdx.x) < choosers) {
     uint32_t* const words = reinterpret_cast<uint32_t*>(lds);
-    choose_slots<kStatThreads>(a, blockIdx.x, words + 8, words, words + kChoiceWords);
+    choose_slots<kStatThreads>(a, blockIdx.x, words + kListWords, words, words + kChoiceWords);
     return;
   }
   const int id = blockIdx.x - choosers, u = id % a.units, split = id / a.units;
@@ -325,59 +327,70 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
 
 // ------------------------------------------------------------------------------------------------
 constexpr int kApplyThreads = 256;
-// A workgroup has kTreeChunk slots of a unit.
+constexpr int kApplySlots = kTreeChunk;  // of a workgroup
 __global__ __launch_bounds__(kApplyThreads) void tree_apply(CommitArgs a, int row_bytes) {
-  __shared__ signed char token_s[kTreeChunk];  // accepted token that a slot takes, or -1
-  const int u = blockIdx.x % a.units, row0 = blockIdx.x / a.units * kTreeChunk;
+  constexpr int kEach = kApplySlots / kApplyThreads;
+  static_assert(kEach == 4, "a word of token_s per thread");
+  __shared__ uint32_t token_s[kApplyThreads];  // a byte per slot: the accepted token that it takes, or 255
+  const int u = blockIdx.x % a.units, row0 = blockIdx.x / a.units * kApplySlots;
   const int request = u / a.heads;
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int32_t* const taken = a.taken + static_cast<size_t>(u) * kTakenWords;
+  // (asked for together, a trip to memory: what lies behind the unit's last slot is the array's, and not used)
   const int len = taken[1], n_new = taken[2];
-  const int my_slot = taken[4 + lane], my_node = path_node(a, request, min(lane, a.max_path - 1));
-  const int row1 = min(n_new, row0 + kTreeChunk);
+  const int my_slot = taken[4 + lane], my_node = path_node(a, request, min(lane, a.max_path - 1)), position = a.qpos0[u];
+  float* const acc = a.stats + static_cast<size_t>(u) * 3 * a.B;
+  float* const acc2 = acc + a.B;
+  float* const cnt = acc2 + a.B;
+  const float* const sums = a.sums + static_cast<size_t>(u) * 2 * a.B;
+  const float* const fresh = a.fresh + static_cast<size_t>(u) * 2 * kMaxTreeNodes;
+  float first[kEach], second[kEach], count[kEach], more[kEach], more2[kEach];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int j = min(row0 + tid + e * kApplyThreads, a.B - 1);
+    first[e] = acc[j];
+    second[e] = acc2[j];
+    count[e] = cnt[j];
+    more[e] = sums[j];
+    more2[e] = sums[a.B + j];
+  }
+  const int row1 = min(n_new, row0 + kApplySlots);
   if (len == 0 || row0 >= row1) return;
-  for (int j = tid; j < kTreeChunk; j += kApplyThreads) token_s[j] = -1;
+  token_s[tid] = 0xffffffffu;
   __syncthreads();
   if (tid < len && my_slot >= row0 && my_slot < row1) {
-    token_s[my_slot - row0] = static_cast<signed char>(tid);
-    a.pos[static_cast<size_t>(u) * a.B + my_slot] = a.qpos0[u] + tid;
+    reinterpret_cast<uint8_t*>(token_s)[my_slot - row0] = static_cast<uint8_t>(tid);
+    a.pos[static_cast<size_t>(u) * a.B + my_slot] = position + tid;
   }
   if (tid == 0 && row0 == 0) a.n_used[u] = n_new;
   __syncthreads();
-  float* const acc = a.stats + static_cast<size_t>(u) * 3 * a.B + row0;
-  float* const acc2 = acc + a.B;
-  float* const cnt = acc2 + a.B;
-  const float* const sums = a.sums + static_cast<size_t>(u) * 2 * a.B + row0;
-  const float* const fresh = a.fresh + static_cast<size_t>(u) * 2 * kMaxTreeNodes;
+  // the rows of the tokens whose slots are among these, 16 bytes per thread
+  const int chunks = row_bytes / 16;
 #pragma unroll 1
-  for (int j = tid; j < row1 - row0; j += kApplyThreads) {
-    const int k = token_s[j];
-    if (k >= 0) {
-      acc[j] = fresh[k];
-      acc2[j] = fresh[kMaxTreeNodes + k];
-      cnt[j] = static_cast<float>(len - k);
-    } else {
-      acc[j] += sums[j];
-      acc2[j] = (a.pol.keeps_last_score() ? 0.0f : acc2[j]) + sums[a.B + j];
-      cnt[j] += static_cast<float>(len);
-    }
-  }
-  // the rows of the tokens whose slots are among these, a wave's token at a time
-#pragma unroll 1
-  for (int k = tid / kWave; k < len; k += kApplyThreads / kWave) {
-    const int slot = __shfl(my_slot, k, kWave), node = __shfl(my_node, k, kWave);
-    if (slot < row0 || slot >= row1) continue;
+  for (int i = 0; i < len * chunks; i += kApplyThreads) {
+    const int k = (i + tid) / chunks, c = (i + tid) - k * chunks;
+    const int slot = __shfl(my_slot, k & (kWave - 1), kWave), node = __shfl(my_node, k & (kWave - 1), kWave);
+    if (k >= len || slot < row0 || slot >= row1) continue;
     size_t row = static_cast<size_t>(u) * a.B + slot;
     if (a.pages.table != nullptr) {
       const int page = a.pages.table[static_cast<size_t>(request) * a.pages.max_pages + (slot >> a.pages.page_log2)];
       if (page < 0 || page >= a.pages.n_pages) continue;
       row = ((static_cast<size_t>(page) * a.heads + (u - request * a.heads)) << a.pages.page_log2) + (slot & ((1 << a.pages.page_log2) - 1));
     }
-    const size_t src = (static_cast<size_t>(u) * a.nodes + node) * row_bytes, dst = row * row_bytes;
-    if (lane * 16 < row_bytes) {
-      *reinterpret_cast<uint4*>(static_cast<char*>(a.K) + dst + lane * 16) = load16(static_cast<const char*>(a.k_new) + src + lane * 16);
-      *reinterpret_cast<uint4*>(static_cast<char*>(a.V) + dst + lane * 16) = load16(static_cast<const char*>(a.v_new) + src + lane * 16);
-    }
+    const size_t src = (static_cast<size_t>(u) * a.nodes + node) * row_bytes + c * 16, dst = row * row_bytes + c * 16;
+    const uint4 key = load16(static_cast<const char*>(a.k_new) + src), value = load16(static_cast<const char*>(a.v_new) + src);
+    *reinterpret_cast<uint4*>(static_cast<char*>(a.K) + dst) = key;
+    *reinterpret_cast<uint4*>(static_cast<char*>(a.V) + dst) = value;
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int j = tid + e * kApplyThreads;
+    if (row0 + j >= row1) break;
+    const int k = reinterpret_cast<const uint8_t*>(token_s)[j];
+    const bool taken_over = k < kMaxTreeNodes;
+    acc[row0 + j] = taken_over ? fresh[k] : first[e] + more[e];
+    acc2[row0 + j] = taken_over ? fresh[kMaxTreeNodes + k] : (a.pol.keeps_last_score() ? 0.0f : second[e]) + more2[e];
+    cnt[row0 + j] = taken_over ? static_cast<float>(len - k) : count[e] + static_cast<float>(len);
   }
 }
 
@@ -412,7 +425,7 @@ template <int DT, int HD> hipError_t launch_commit(const CommitArgs& a, hipStrea
   else e = a.streaming ? launch_statistics<DT, HD, true, false>(a, s) : launch_statistics<DT, HD, false, false>(a, s);
   if (e != hipSuccess) return e;
   ProfScope ps(kProfTreeApply, s);
-  const unsigned chunks = static_cast<unsigned>((a.B + kTreeChunk - 1) / kTreeChunk);
+  const unsigned chunks = static_cast<unsigned>((a.B + kApplySlots - 1) / kApplySlots);
   hipLaunchKernelGGL(tree_apply, dim3(static_cast<unsigned>(a.units) * chunks), dim3(kApplyThreads), 0, s, a, Tile<DT, HD>::kBytes);
   return hipGetLastError();
 }
