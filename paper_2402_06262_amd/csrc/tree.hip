@@ -82,16 +82,82 @@ template <int DT, int HD, int WAVES> __global__ __launch_bounds__(kJoinThreads) 
   if (a.lse != nullptr && lane == 0) a.lse[at] = 0.6931471805599453f * (M + __log2f(sum));
 }
 
+// Few splits of many rows: HD / 4 lanes and their 16 bytes have kJoinRows rows each, so that the loads of all of them are in flight (a wave per row
+// took 21 us for 65536 rows of two splits, 63 MB, and these 9.8; 1260 rows 4.8 and 6.2).  The sums over the splits are in their order.
+constexpr int kJoinRows = 4, kFewSplits = 8, kManyRows = 16384;
+template <int DT, int HD> __global__ __launch_bounds__(kJoinThreads) void tree_join_few(TreeArgs a, int groups) {
+  constexpr int LANES = HD / 4, STEP = kJoinThreads / LANES;
+  const int u = blockIdx.x / groups, row0 = blockIdx.x % groups * (STEP * kJoinRows);
+  const int request = u / a.heads, all = a.nodes * a.group;
+  const int nodes = a.n_nodes != nullptr ? min(max(a.n_nodes[request], 0), a.nodes) : a.nodes;
+  const int rows = nodes * a.group;
+  const int splits = tree::splits_used(min(max(a.n_used[u], 0), tree::budget_of(a.pages, a.B, request)), a.chunk);
+  if (row0 >= rows || splits == 1) return;  // (the only split has written its rows)
+  const int sub = threadIdx.x % LANES, col = sub * 4;
+  int row[kJoinRows];
+  size_t first[kJoinRows];
+  float m[kJoinRows], l[kJoinRows], M[kJoinRows], sum[kJoinRows];
+  tree::f32x4 o[kJoinRows];
+#pragma unroll
+  for (int r = 0; r < kJoinRows; ++r) {
+    row[r] = row0 + r * STEP + static_cast<int>(threadIdx.x) / LANES;
+    first[r] = static_cast<size_t>(u) * a.splits * all + min(row[r], rows - 1);
+    const size_t at = first[r] + static_cast<size_t>(min(sub, splits - 1)) * all;
+    m[r] = a.part_m[at];
+    l[r] = a.part_l[at];
+    o[r] = tree::f32x4{0};
+  }
+#pragma unroll 1
+  for (int i = 0; i < splits; i += 2) {
+    tree::f32x4 v[2][kJoinRows];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int r = 0; r < kJoinRows; ++r) v[k][r] = *reinterpret_cast<const tree::f32x4*>(a.part_o + (first[r] + static_cast<size_t>(min(i + k, splits - 1)) * all) * HD + col);
+    if (i == 0) {
+#pragma unroll
+      for (int r = 0; r < kJoinRows; ++r) {
+        M[r] = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kFewSplits; ++k) M[r] = fmaxf(M[r], __shfl(m[r], k, LANES));  // (lanes behind the last split have the last one's)
+        m[r] = m[r] > -INFINITY ? fast_exp2(m[r] - M[r]) : 1.0f;  // a split's weight (one of no maximum has a sum of zero, or NaN)
+        sum[r] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int r = 0; r < kJoinRows; ++r) {
+        const float w = __shfl(m[r], i + k, LANES), s = __shfl(l[r], i + k, LANES);
+        if (i + k >= splits) continue;
+        o[r] += v[k][r] * w;
+        sum[r] += s * w;
+      }
+  }
+#pragma unroll
+  for (int r = 0; r < kJoinRows; ++r) {
+    if (row[r] >= rows) continue;
+    const size_t at = static_cast<size_t>(u) * all + row[r];
+    tree::store4<DT>(a.out, at * HD + col, o[r] * (1.0f / sum[r]));
+    if (a.lse != nullptr && sub == 0) a.lse[at] = 0.6931471805599453f * (M[r] + __log2f(sum[r]));
+  }
+}
+
 template <int DT, int HD, int WAVES> hipError_t launch_join_waves(const TreeArgs& a, hipStream_t s) {
   constexpr int kRows = kJoinThreads / kWave / WAVES;
   const long long rows = static_cast<long long>(a.units) * a.nodes * a.group;
   hipLaunchKernelGGL((tree_join<DT, HD, WAVES>), dim3(static_cast<unsigned>((rows + kRows - 1) / kRows)), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
-// Four waves per row where the splits are many: then the rows are few.
+// A wave per row, or four where the splits are many: then the rows are few.
 template <int DT, int HD> hipError_t launch_join(const TreeArgs& a, hipStream_t s) {
   ProfScope ps(kProfTreeJoin, s);
-  return a.splits > 8 ? launch_join_waves<DT, HD, 4>(a, s) : launch_join_waves<DT, HD, 1>(a, s);
+  if (a.splits > kFewSplits) return launch_join_waves<DT, HD, 4>(a, s);
+  if (static_cast<long long>(a.units) * a.nodes * a.group < kManyRows) return launch_join_waves<DT, HD, 1>(a, s);
+  constexpr int kRows = kJoinThreads / (HD / 4) * kJoinRows;
+  const int groups = (a.nodes * a.group + kRows - 1) / kRows;
+  hipLaunchKernelGGL((tree_join_few<DT, HD>), dim3(static_cast<unsigned>(a.units) * groups), dim3(kJoinThreads), 0, s, a, groups);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -102,14 +168,26 @@ int tree_attend_row_tiles(int dtype, int rows, bool window) {
   return (rows + most - 1) / most;
 }
 
-// Two workgroups on every compute unit, while each has 64 slots (with more than 64 rows of bf16 192: its share of the outputs is larger).
+// Two workgroups on every compute unit, while each has 64 slots.  With more than 64 rows of bf16, where a workgroup's products bound it and not the
+// memory: the splits, of 192 slots at least, whose rounds of 512 workgroups are shortest, a workgroup being as long as its tiles of 32 and 8
+// more for its start and its share of the outputs (128 units x 4096 slots x 512 rows: four splits 231 us, two 227, three 243; with requests of
+// different lengths, which fewer splits leave waiting for the longest, 155, 161 and 164; 192 units x 2048 x 160 rows: two splits 53 us, three 62).
 TreeSplits tree_attend_splits(int dtype, int units, int rows, int B, bool window) {
   const char* const asked = getenv("ROCO_TREE_SPLITS");
   int want = asked != nullptr ? atoi(asked) : 0;
   if (want <= 0) {
     const long long groups = static_cast<long long>(units) * tree_attend_row_tiles(dtype, rows, window);
     want = static_cast<int>((512 + groups - 1) / groups);
-    if (dtype == kBF16 && rows > 64) want = std::min(want, (B + 191) / 192);
+    if (dtype == kBF16 && rows > 64) {
+      long long least = -1;
+      for (int splits = 1; splits <= std::max(1, std::min(kMaxTreeSplits, B / 192)); ++splits) {
+        const long long cost = (groups * splits + 511) / 512 * ((B + splits - 1) / splits + 8 * 32);
+        if (least < 0 || cost < least) {
+          least = cost;
+          want = splits;
+        }
+      }
+    }
   }
   want = std::max(1, std::min({want, kMaxTreeSplits, (B + 63) / 64}));
   TreeSplits s;

@@ -541,6 +541,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
     for (int sub = 0; sub < 2; ++sub) {
       const int t = t0 + sub;
       if (t < 0 || t >= tiles) break;
+      if (first_row >= rows && !walk.is_nodes(t)) continue;  // no rows of this wave's (a tile of nodes may have everybody wait)
       char* const tileV = lds + (t & 3) * kPairBytes + kTileBytes;
       // (the tiles lie at multiples of 1 KiB: the chunk's exclusive or can be taken of the address)
       const LateLane F;
