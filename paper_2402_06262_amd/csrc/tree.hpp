@@ -109,8 +109,8 @@ __device__ __forceinline__ int splits_used(int n, int chunk) { return max((n + c
 
 // A wave's tiles of the slots [row0, row1) of a unit: every W-th one, from a start that differs between workgroups so that they do not
 // walk the memory channels in lock step; behind the cache's tiles come `node_tiles` of a tree's nodes.  The tile numbers `t` are the
-// wave's own; they are asked for in order.
-template <int DT, int HD, int W, int BYTES = 8192> struct Walk {
+// wave's own; they are asked for in order, every STEP-th one.
+template <int DT, int HD, int W, int BYTES = 8192, int STEP = 1> struct Walk {
   using T = Tile<DT, HD, BYTES>;
   static constexpr int G = T::kGroups;
   typedef const __attribute__((address_space(4))) int32_t* Table;  // (constant: read by scalar loads, which the tiles' loads do not wait for)
@@ -170,7 +170,7 @@ template <int DT, int HD, int W, int BYTES = 8192> struct Walk {
       p.row[i] = there > 0 ? row : 0u;
       p.there |= static_cast<uint32_t>(there) << (8 * i);
     }
-    if (t + 1 < mine) look_ahead(t + 1);
+    if (t + STEP < mine) look_ahead(t + STEP);
     return p;
   }
 };

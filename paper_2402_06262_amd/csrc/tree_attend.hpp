@@ -8,6 +8,8 @@
 // The running maximum follows a tile's only when that is more than 2^8 above it: no rescaling, and no exchange between lanes, for most
 // tiles, and the sums stay far from the ends of fp32.
 #pragma once
+#include <type_traits>
+
 #include "tree.hpp"
 #include "profile.hpp"
 
@@ -414,7 +416,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
     add_special_nodes<DT, HD, WINDOW>(a, u, row_base + first_row, part_base + first_row, first_row, min(QR, rows - first_row), used, see(), special, merge_m, merge_l);
 }
 
-// More than 64 query rows of bf16: four waves with 16 NQ rows each share the tiles, which come two at a time, a quarter of each by every
+// More than 64 query rows of bf16: four waves with 16 NQ rows each share the tiles, which come two at a time, K or V of one by each
 // wave, while the two before them are used; one barrier for two tiles.  Two workgroups on a compute unit, so that one wave's exponentials run beside another's products: with 64
 // rows to a workgroup and the rest in others, every row tile fetched K and V again, and a wave had its matrix cores to itself.
 // Here the matrix cores are what the step waits for, so that probabilities are rounded to one bf16 number each (2^-9 of each; the
@@ -429,12 +431,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
   using T = Tile<DT, HD>;
   constexpr int W = kWideWaves, G = T::kGroups, QR = 16 * NQ;  // query rows of a wave
   constexpr int kTileBytes = 8192, kPairBytes = 2 * kTileBytes;  // a tile of K and one of V
-  constexpr int kMyLoads = T::kLoads / W;                      // of an operand's tile
-  constexpr int kSide = WINDOW ? 1 : 0;
-  static_assert(kMyLoads <= T::kGroupLoads, "a wave's loads lie in one group");
+  static_assert(W == 4, "two waves ask for K, two for V");
   extern __shared__ __attribute__((aligned(1024))) char lds[];  // four pairs of tiles: two in use, two on their way
-  __shared__ __attribute__((aligned(256))) int32_t pos_s[WINDOW ? W : 1][4][kWave];
+  __shared__ __attribute__((aligned(256))) int32_t pos_s[WINDOW ? 4 : 1][kWave];
   __shared__ float max_s[W][QR], scale_s[W][QR];
+  __shared__ uint32_t there_s[4];  // Place::there of the tiles
   const int per = 8 * a.row_tiles, id = blockIdx.x;
   const int us = id / per * 8 + id % 8, row_tile = id % per / 8;
   if (us >= a.units * a.splits) return;
@@ -449,9 +450,10 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
   const int used = splits_used(n, a.chunk);
   if (row_tile * W * QR >= rows || split >= used) return;
   const int row0 = split * a.chunk, row1 = min(n, row0 + a.chunk);
-  Walk<DT, HD, 1> walk;
+  Walk<DT, HD, 1, kTileBytes, 2> walk;
   walk.init(a.pages, a.B, a.heads, u, request, row0, row1, split == used - 1 ? nodes : 0, 0, static_cast<unsigned>(u) * 5u + static_cast<unsigned>(split) * 3u);
   const int tiles = walk.mine;
+  if ((wave >> 1) < tiles) walk.look_ahead(wave >> 1);
 
   int koff[T::kGroupLoads];
   load_offsets<DT, HD, false>(koff);
@@ -501,41 +503,44 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
     for (int db = 0; db < T::kBlocks; ++db) o[t2][db] = f32x4{0};
   }
   const v4i32 pbuf = make_buffer(a.pos + static_cast<size_t>(u) * a.B, WINDOW ? static_cast<uint32_t>(a.B) * 4u : 0u);
-  const uint32_t pos_addr = lds_address(&pos_s[WINDOW ? wave : 0][0][0]), ring_addr = lds_address(lds);
+  const uint32_t pos_addr = lds_address(&pos_s[0][0]), ring_addr = lds_address(lds);
   const size_t new_rows = static_cast<size_t>(u) * a.nodes * T::kBytes;
-  const int my_group = wave * kMyLoads / T::kGroupLoads, my_first = wave * kMyLoads % T::kGroupLoads;  // of a tile's loads
 
-  uint32_t there[2] = {0, 0}, there_next[2] = {0, 0};
+  // K (even waves) or V of a tile
+  const auto request_operand = [&](auto of_v, const typename Walk<DT, HD, 1, kTileBytes, 2>::Place& next, bool of_nodes, const void* cache, const void* fresh, uint32_t dst) {
+    constexpr bool kOfV = decltype(of_v)::value;
+    const int lane2 = LateLane().lane;
+    int off[T::kGroupLoads];
+#pragma unroll
+    for (int j = 0; j < T::kGroupLoads; ++j) {
+      const int r = T::kPerLoad * j + lane2 / T::kChunks, c = lane2 % T::kChunks;
+      off[j] = r * T::kBytes + ((c ^ (kOfV ? T::swizzle_v(r) : T::swizzle_k(r))) << 4);
+    }
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const size_t at = (of_nodes ? new_rows : 0) + static_cast<size_t>(next.row[i]) * T::kBytes;
+      const v4i32 buf = make_buffer(static_cast<const char*>(of_nodes ? fresh : cache) + at, ((next.there >> (8 * i)) & 0xffu) * T::kBytes);
+#pragma unroll
+      for (int j = 0; j < T::kGroupLoads; ++j) load16_to_lds(buf, dst + (i * T::kGroupLoads + j) * 1024, off[j], 0);
+    }
+  };
 #pragma unroll 1
   for (int t0 = -2; t0 < tiles; t0 += 2) {
     if (t0 >= 0) {  // these tiles have landed, and nobody reads those before them any more
       wait_loads<0>();
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
-#pragma unroll 1
-    for (int sub = 0; sub < 2; ++sub) {
-      const int t = t0 + 2 + sub;
-      if (t >= tiles) break;
-      const typename Walk<DT, HD, 1>::Place next = walk.place(t);
+    if (const int t = t0 + 2 + (wave >> 1); t < tiles) {
+      const typename Walk<DT, HD, 1, kTileBytes, 2>::Place next = walk.place(t);
       const bool next_nodes = walk.is_nodes(t);
-      if (sub == 0) there_next[0] = next.there;
-      else there_next[1] = next.there;
-      uint32_t row = next.row[0];
-#pragma unroll
-      for (int i = 1; i < G; ++i) row = my_group == i ? next.row[i] : row;
-      const uint32_t bytes = ((next.there >> (8 * my_group)) & 0xffu) * T::kBytes;
-      const size_t at = (next_nodes ? new_rows : 0) + static_cast<size_t>(row) * T::kBytes;
-      const v4i32 kbuf = make_buffer(static_cast<const char*>(next_nodes ? a.k_new : a.K) + at, bytes);
-      const v4i32 vbuf = make_buffer(static_cast<const char*>(next_nodes ? a.v_new : a.V) + at, bytes);
-      const uint32_t pair = ring_addr + static_cast<uint32_t>(t & 3) * kPairBytes + wave * kMyLoads * 1024;
-      const int lane2 = LateLane().lane;
-#pragma unroll
-      for (int j = 0; j < kMyLoads; ++j) {
-        const int r = T::kPerLoad * (my_first + j) + lane2 / T::kChunks, c = lane2 % T::kChunks;
-        load16_to_lds(kbuf, pair + j * 1024, r * T::kBytes + ((c ^ T::swizzle_k(r)) << 4), 0);
-        load16_to_lds(vbuf, pair + kTileBytes + j * 1024, r * T::kBytes + ((c ^ T::swizzle_v(r)) << 4), 0);
+      const uint32_t pair = ring_addr + static_cast<uint32_t>(t & 3) * kPairBytes;
+      if (wave & 1) {
+        request_operand(std::true_type(), next, next_nodes, a.V, a.v_new, pair + kTileBytes);
+      } else {
+        request_operand(std::false_type(), next, next_nodes, a.K, a.k_new, pair);
+        if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + (t & 3) * (kWave * 4), next_nodes ? 0x7ffffffc : (walk.first_slot(t) + lane) * 4, 0);
+        if (LateLane().lane == 0) there_s[t & 3] = next.there;
       }
-      if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + (t & 3) * (kWave * 4), next_nodes ? 0x7ffffffc : (walk.first_slot(t) + lane) * 4, 0);
     }
 #pragma unroll 1
     for (int sub = 0; sub < 2; ++sub) {
@@ -568,11 +573,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
       }
       const bool of_nodes = walk.is_nodes(t);
       constexpr uint32_t kWhole = G == 1 ? 0x10u : G == 2 ? 0x1010u : 0x10101010u;
-      const uint32_t here = sub == 0 ? there[0] : there[1];
+      const uint32_t here = __builtin_amdgcn_readfirstlane(there_s[t & 3]);
       if (WINDOW) {
 #pragma unroll
         for (int i = 0; i < G; ++i) {
-          const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? wave : 0][t & 3][16 * i + 4 * g]);
+          const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? t & 3 : 0][16 * i + 4 * g]);
           int ps[4] = {p4.x, p4.y, p4.z, p4.w};
           if (of_nodes) {
 #pragma unroll
@@ -674,8 +679,6 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
         }
       }
     }
-    there[0] = there_next[0];
-    there[1] = there_next[1];
   }
   const LateLane L;
   const size_t part_base = (static_cast<size_t>(u) * a.splits + split) * a.nodes * a.group;
