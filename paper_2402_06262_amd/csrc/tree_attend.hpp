@@ -93,6 +93,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
   using T = Tile<DT, HD>;
   constexpr int W = kAttendWaves, G = T::kGroups, QR = 16 * NQ;
   constexpr int kTileBytes = 8192, kWaveBytes = 4 * kTileBytes;  // K, V, K, V
+  constexpr int kAhead = 2;
   constexpr int kSide = WINDOW ? 1 : 0;                          // the positions of a K tile's slots come along
   // the queries come through the place of the second V tile, or of the second tiles, or before any tile
   constexpr int kQueryBytes = QR * T::kBytes;
@@ -190,14 +191,22 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
       // K(t) has landed; V(t), and K and V of the next tile, may still be on their way
       if (t + 1 < mine) wait_loads<3 * T::kLoads + kSide>();
       else wait_loads<T::kLoads>();
+      // (fragments are read kAhead steps ahead: left to itself the compiler reads each one right before its use, and waits for it)
+      uint4 kf[kAhead + 1][G];
+      const auto read_k = [&](int kk) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) kf[kk % (kAhead + 1)][i] = *reinterpret_cast<const uint4*>(tileK + i * 16 * T::kBytes + (kfrag ^ (kk << 6)));
+      };
+#pragma unroll
+      for (int kk = 0; kk < kAhead; ++kk) read_k(kk);
 #pragma unroll
       for (int kk = 0; kk < T::kSteps; ++kk) {
+        if (kk + kAhead < T::kSteps) read_k(kk + kAhead);
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-          const uint4 kf = *reinterpret_cast<const uint4*>(tileK + i * 16 * T::kBytes + (kfrag ^ (kk << 6)));
+        for (int i = 0; i < G; ++i)
 #pragma unroll
-          for (int t2 = 0; t2 < NQ; ++t2) s[t2][i] = score_step<DT>(kf, own[t2][kk], kk == 0 ? f32x4{0} : s[t2][i]);
-        }
+          for (int t2 = 0; t2 < NQ; ++t2) s[t2][i] = score_step<DT>(kf[kk % (kAhead + 1)][i], own[t2][kk], kk == 0 ? f32x4{0} : s[t2][i]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       if (WINDOW) {
 #pragma unroll
@@ -316,7 +325,15 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
       }
       if constexpr (DT == kBF16) {
         // The probabilities as sums of two bf16 numbers: rounded to one they would make as much of the output's error as its own
-        // rounding (2.4e-3 against 1.7e-3 of its norm); the matrix cores have the time.
+        // rounding (2.3e-3 against 1.7e-3 of its norm); the matrix cores have the time.
+        uint4 vf[kAhead + 1];
+        const auto read_v = [&](int at) {
+          const char* const vt = tileV + at / T::kBlocks * 2 * 16 * T::kBytes + (vfrag ^ (at % T::kBlocks << 5));
+          const uint2 lo = lds_read_transposed(vt), hi = lds_read_transposed(vt + 16 * T::kBytes);
+          vf[at % (kAhead + 1)] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        };
+#pragma unroll
+        for (int at = 0; at < kAhead; ++at) read_v(at);
 #pragma unroll
         for (int i = 0; i < G; i += 2) {
           uint4 p[NQ][2];
@@ -327,28 +344,35 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
           }
 #pragma unroll
           for (int db = 0; db < T::kBlocks; ++db) {
-            const char* const vt = tileV + i * 16 * T::kBytes + (vfrag ^ (db << 5));
-            const uint2 lo = lds_read_transposed(vt), hi = lds_read_transposed(vt + 16 * T::kBytes);
-            const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            const int at = i / 2 * T::kBlocks + db;
+            if (at + kAhead < G / 2 * T::kBlocks) read_v(at + kAhead);
+            const uint4 v = vf[at % (kAhead + 1)];
 #pragma unroll
             for (int k = 1; k >= 0; --k)
 #pragma unroll
-              for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(vf, p[t2][k], o[t2][db]);
+              for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(v, p[t2][k], o[t2][db]);
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
       } else {
+        float vf[kAhead + 1][4];
+        const auto read_v = [&](int at) {
+          const char* const vt = tileV + at / T::kBlocks * 16 * T::kBytes + (vfrag ^ (at % T::kBlocks << 6));
 #pragma unroll
-        for (int i = 0; i < G; ++i)
+          for (int e = 0; e < 4; ++e) vf[at % (kAhead + 1)][e] = *reinterpret_cast<const float*>(vt + e * T::kBytes);
+        };
 #pragma unroll
-          for (int db = 0; db < T::kBlocks; ++db) {
-            const char* const vt = tileV + i * 16 * T::kBytes + (vfrag ^ (db << 6));
+        for (int at = 0; at < kAhead; ++at) read_v(at);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float v = *reinterpret_cast<const float*>(vt + e * T::kBytes);
+        for (int at = 0; at < G * T::kBlocks; ++at) {
+          if (at + kAhead < G * T::kBlocks) read_v(at + kAhead);
+          const int i = at / T::kBlocks, db = at % T::kBlocks;
 #pragma unroll
-              for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[t2][i][e], o[t2][db], 0, 0, 0);
-            }
-          }
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[at % (kAhead + 1)][e], s[t2][i][e], o[t2][db], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
       reads_done();
     }
@@ -420,7 +444,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
 // wave, while the two before them are used; one barrier for two tiles.  Two workgroups on a compute unit, so that one wave's exponentials run beside another's products: with 64
 // rows to a workgroup and the rest in others, every row tile fetched K and V again, and a wave had its matrix cores to itself.
 // Here the matrix cores are what the step waits for, so that probabilities are rounded to one bf16 number each (2^-9 of each; the
-// outputs, sums over many, are 2.4e-3 of their norm off instead of 1.7e-3, their own rounding): the second number would be a third more
+// outputs, sums over many, are 2.3e-3 of their norm off instead of 1.7e-3, their own rounding): the second number would be a third more
 // products and as much vector work again.
 constexpr int kWideWaves = 4;
 constexpr int kWideThreads = kWideWaves * kWave;
