@@ -86,10 +86,12 @@ __device__ __forceinline__ void add_special_nodes(const TreeArgs& a, int u, size
 }
 
 // NQ tiles of 16 query rows; a row is a node and a head of the group.  WINDOW: a recency bias is in force.
-// A launch begins with a cold instruction cache, a third of a microsecond per KiB, so that nothing is unrolled that need not be: the
-// loop over the tiles begins two tiles early, with the requests alone, and what is rare loops over rows.
+// A launch begins with a cold instruction cache, a third of a microsecond per KiB, so that nothing is unrolled that need not be, and what is
+// rare loops over rows.
+// One wave on a SIMD (the registers are filled up to that): the two workgroups that LDS lets on a compute unit otherwise share two of its SIMDs,
+// and leave two idle (512 units x 2048 slots of bf16 92.2 us against 84.4, 60 units x 1501 of fp32 with 21 rows 40.5 / 31.1).
 template <int DT, int HD, int NQ, bool STREAMING, bool WINDOW>
-__global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
+__global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void tree_attend(TreeArgs a) {
   using T = Tile<DT, HD>;
   constexpr int W = kAttendWaves, G = T::kGroups, QR = 16 * NQ;
   constexpr int kTileBytes = 8192, kWaveBytes = 4 * kTileBytes;  // K, V, K, V
@@ -180,209 +182,230 @@ __global__ __launch_bounds__(kAttendThreads, 1) void tree_attend(TreeArgs a) {
   const int vrow = DT == kBF16 ? 4 * g + (qi >> 2) : 4 * g;
   const int vfrag = vrow * T::kBytes + (T::swizzle_v(vrow) << 4) + (DT == kBF16 ? (qi & 3) * 8 : qi * 4);
 
+  typedef typename Walk<DT, HD, W>::Place Place;
+  const auto request_k = [&](const Place& p, bool of_nodes, int t) {
+    request_tile<DT, HD, STREAMING>(of_nodes ? static_cast<const char*>(a.k_new) + new_rows : static_cast<const char*>(a.K), p.row, p.there, tiles_addr + (t & 1) * 2 * kTileBytes, koff);
+    // (a wave-wide load of 64 words, whatever the tile; behind the unit's last slot, and for nodes, zeros)
+    if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + (t & 1) * (kWave * 4), of_nodes ? 0x7ffffffc : (walk.first_slot(t) + lane) * 4, 0);
+  };
+  const auto request_v = [&](const Place& p, bool of_nodes, int t) {
+    request_tile<DT, HD, STREAMING>(of_nodes ? static_cast<const char*>(a.v_new) + new_rows : static_cast<const char*>(a.V), p.row, p.there, tiles_addr + (t & 1) * 2 * kTileBytes + kTileBytes, voff);
+  };
+  Place second;
+  bool second_nodes = false;
   uint32_t there0 = 0, there1 = 0, there2 = 0;  // of this tile and the two behind it
+  // (the first requests are not a part of the loop over the tiles, though that is code again: with the queries read inside it their registers were copied
+  // on its way round, 120 instructions per tile of fp32 / 128, and 32 rows took 43 us where they take 34)
 #pragma unroll 1
-  for (int t = -2; t < mine; ++t) {
-    char* const tileK = tiles + (t & 1) * 2 * kTileBytes;
-    char* const tileV = tileK + kTileBytes;
-    f32x4 s[NQ][G];
-    int ps[G][4];
-    if (t >= 0) {
-      // K(t) has landed; V(t), and K and V of the next tile, may still be on their way
-      if (t + 1 < mine) wait_loads<3 * T::kLoads + kSide>();
-      else wait_loads<T::kLoads>();
-      // (fragments are read kAhead steps ahead: left to itself the compiler reads each one right before its use, and waits for it)
-      uint4 kf[kAhead + 1][G];
-      const auto read_k = [&](int kk) {
-#pragma unroll
-        for (int i = 0; i < G; ++i) kf[kk % (kAhead + 1)][i] = *reinterpret_cast<const uint4*>(tileK + i * 16 * T::kBytes + (kfrag ^ (kk << 6)));
-      };
-#pragma unroll
-      for (int kk = 0; kk < kAhead; ++kk) read_k(kk);
-#pragma unroll
-      for (int kk = 0; kk < T::kSteps; ++kk) {
-        if (kk + kAhead < T::kSteps) read_k(kk + kAhead);
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-          for (int t2 = 0; t2 < NQ; ++t2) s[t2][i] = score_step<DT>(kf[kk % (kAhead + 1)][i], own[t2][kk], kk == 0 ? f32x4{0} : s[t2][i]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (WINDOW) {
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-          const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? wave : 0][t & 1][16 * i + 4 * g]);
-          ps[i][0] = p4.x; ps[i][1] = p4.y; ps[i][2] = p4.z; ps[i][3] = p4.w;
-        }
-      }
-      reads_done();
-    } else if (kBeforeK && t == -1) {
+  for (int t = 0; t < 2; ++t) {
+    if (kBeforeK && t == 1) {
       if (mine > 0) wait_loads<2 * T::kLoads + kSide>();
       else wait_loads<0>();
       read_queries();
     }
-    typename Walk<DT, HD, W>::Place next;
+    if (t < mine) {
+      const Place next = walk.place(t);
+      const bool next_nodes = walk.is_nodes(t);
+      if (t == 0) there0 = next.there;
+      else there1 = next.there;
+      request_k(next, next_nodes, t);
+      if (!kBehindK || t == 0) request_v(next, next_nodes, t);
+      else second = next, second_nodes = next_nodes;
+    }
+  }
+  if (kBehindK) {
+    if (mine > 1) wait_loads<3 * T::kLoads + 2 * kSide>();
+    else if (mine > 0) wait_loads<2 * T::kLoads + kSide>();
+    else wait_loads<0>();
+    read_queries();
+    if (mine > 1) request_v(second, second_nodes, 1);
+  }
+#pragma unroll 1
+  for (int t = 0; t < mine; ++t) {
+    char* const tileK = tiles + (t & 1) * 2 * kTileBytes;
+    char* const tileV = tileK + kTileBytes;
+    f32x4 s[NQ][G];
+    int ps[G][4];
+    // K(t) has landed; V(t), and K and V of the next tile, may still be on their way
+    if (t + 1 < mine) wait_loads<3 * T::kLoads + kSide>();
+    else wait_loads<T::kLoads>();
+    // (fragments are read kAhead steps ahead: left to itself the compiler reads each one right before its use, and waits for it)
+    uint4 kf[kAhead + 1][G];
+    const auto read_k = [&](int kk) {
+#pragma unroll
+      for (int i = 0; i < G; ++i) kf[kk % (kAhead + 1)][i] = *reinterpret_cast<const uint4*>(tileK + i * 16 * T::kBytes + (kfrag ^ (kk << 6)));
+    };
+#pragma unroll
+    for (int kk = 0; kk < kAhead; ++kk) read_k(kk);
+#pragma unroll
+    for (int kk = 0; kk < T::kSteps; ++kk) {
+      if (kk + kAhead < T::kSteps) read_k(kk + kAhead);
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int t2 = 0; t2 < NQ; ++t2) s[t2][i] = score_step<DT>(kf[kk % (kAhead + 1)][i], own[t2][kk], kk == 0 ? f32x4{0} : s[t2][i]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (WINDOW) {
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const int4 p4 = *reinterpret_cast<const int4*>(&pos_s[WINDOW ? wave : 0][t & 1][16 * i + 4 * g]);
+        ps[i][0] = p4.x; ps[i][1] = p4.y; ps[i][2] = p4.z; ps[i][3] = p4.w;
+      }
+    }
+    reads_done();
+    Place next;
     bool next_nodes = false;
     if (t + 2 < mine) {
       next = walk.place(t + 2);
       there2 = next.there;
       next_nodes = walk.is_nodes(t + 2);
-      request_tile<DT, HD, STREAMING>(next_nodes ? static_cast<const char*>(a.k_new) + new_rows : static_cast<const char*>(a.K), next.row, next.there, lds_address(tileK), koff);
-      // (a wave-wide load of 64 words, whatever the tile; behind the unit's last slot, and for nodes, zeros)
-      if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + (t & 1) * (kWave * 4), next_nodes ? 0x7ffffffc : (walk.first_slot(t + 2) + lane) * 4, 0);
+      request_k(next, next_nodes, t + 2);
     }
-    if (t >= 0) {
-      const bool of_nodes = walk.is_nodes(t);
-      constexpr uint32_t kWhole = G == 1 ? 0x10u : G == 2 ? 0x1010u : 0x10101010u;
-      if (of_nodes) {
-        if (!WINDOW) seen = see();
-        const int j0 = walk.first_node(t);
-        const LateLane L;
+    const bool of_nodes = walk.is_nodes(t);
+    constexpr uint32_t kWhole = G == 1 ? 0x10u : G == 2 ? 0x1010u : 0x10101010u;
+    if (of_nodes) {
+      if (!WINDOW) seen = see();
+      const int j0 = walk.first_node(t);
+      const LateLane L;
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-          if (WINDOW) {
+      for (int i = 0; i < G; ++i) {
+        if (WINDOW) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ps[i][e] = qp0 + __shfl(__builtin_popcountll(seen), min(j0 + 16 * i + 4 * L.g + e, kWave - 1), kWave) - 1;
-          }
+          for (int e = 0; e < 4; ++e) ps[i][e] = qp0 + __shfl(__builtin_popcountll(seen), min(j0 + 16 * i + 4 * L.g + e, kWave - 1), kWave) - 1;
         }
-#pragma unroll
-        for (int t2 = 0; t2 < NQ; ++t2) {
-          const uint64_t sees = from_lane(seen, token_of(t2, L.qi)) >> (j0 + 4 * L.g);
-#pragma unroll
-          for (int i = 0; i < G; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[t2][i][e] = (sees >> (16 * i + e)) & 1 ? s[t2][i][e] : -INFINITY;
-        }
-      } else if (there0 != kWhole) {
-        const LateLane L;
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool visible = 4 * L.g + e < static_cast<int>((there0 >> (8 * i)) & 0xffu);
-#pragma unroll
-            for (int t2 = 0; t2 < NQ; ++t2) s[t2][i][e] = visible ? s[t2][i][e] : -INFINITY;
-          }
       }
-      // ---- probabilities; what a row does not see is -inf
 #pragma unroll
       for (int t2 = 0; t2 < NQ; ++t2) {
-        float most = -INFINITY;
+        const uint64_t sees = from_lane(seen, token_of(t2, L.qi)) >> (j0 + 4 * L.g);
 #pragma unroll
         for (int i = 0; i < G; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (WINDOW) {
-              const int away = qp[t2] - ps[i][e];
-              s[t2][i][e] += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
-            }
-            most = fmaxf(most, s[t2][i][e]);
-          }
-        most *= sc;
-        if (__any(most > m[t2] + kSlack)) {
-          most = fmaxf(most, __shfl_xor(most, 16, kWave));
-          most = fmaxf(most, __shfl_xor(most, 32, kWave));
-          const float m_new = most > m[t2] + kSlack ? most : m[t2];  // (a row's bits do not depend on the rows beside it)
-          const float alpha = m[t2] > -INFINITY ? fast_exp2(m[t2] - m_new) : 0.0f;
-          l[t2] *= alpha;
-#pragma unroll
-          for (int db = 0; db < T::kBlocks; ++db) o[t2][db] *= alpha;
-          m[t2] = m_new;
-        }
-        const float ref = m[t2] > -INFINITY ? m[t2] : 0.0f;  // nothing seen yet: every term is 2^-inf = 0
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[t2][i][e] = fast_exp2(fmaf(s[t2][i][e], sc, -ref));
-            sum += s[t2][i][e];
-          }
-        l[t2] += sum;
+          for (int e = 0; e < 4; ++e) s[t2][i][e] = (sees >> (16 * i + e)) & 1 ? s[t2][i][e] : -INFINITY;
       }
-      // ---- O^T += V^T . P^T
-      if (t + 2 < mine) wait_loads<3 * T::kLoads + 2 * kSide>();
-      else if (t + 1 < mine) wait_loads<2 * T::kLoads + kSide>();
-      else wait_loads<0>();
-      if (of_nodes) {
-        // A node's value that is infinite or NaN must not reach the rows that do not see the node, and 0 times it would: such nodes
-        // are zero in the products, and added in the end to the rows that see them.
-        bool any = false;
-        const LateLane L;
+    } else if (there0 != kWhole) {
+      const LateLane L;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + L.lane * 16));
-        if (__any(any)) {
-          const int j0 = walk.first_node(t);
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool visible = 4 * L.g + e < static_cast<int>((there0 >> (8 * i)) & 0xffu);
+#pragma unroll
+          for (int t2 = 0; t2 < NQ; ++t2) s[t2][i][e] = visible ? s[t2][i][e] : -INFINITY;
+        }
+    }
+    // ---- probabilities; what a row does not see is -inf
+#pragma unroll
+    for (int t2 = 0; t2 < NQ; ++t2) {
+      float most = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (WINDOW) {
+            const int away = qp[t2] - ps[i][e];
+            s[t2][i][e] += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
+          }
+          most = fmaxf(most, s[t2][i][e]);
+        }
+      most *= sc;
+      if (__any(most > m[t2] + kSlack)) {
+        most = fmaxf(most, __shfl_xor(most, 16, kWave));
+        most = fmaxf(most, __shfl_xor(most, 32, kWave));
+        const float m_new = most > m[t2] + kSlack ? most : m[t2];  // (a row's bits do not depend on the rows beside it)
+        const float alpha = m[t2] > -INFINITY ? fast_exp2(m[t2] - m_new) : 0.0f;
+        l[t2] *= alpha;
+#pragma unroll
+        for (int db = 0; db < T::kBlocks; ++db) o[t2][db] *= alpha;
+        m[t2] = m_new;
+      }
+      const float ref = m[t2] > -INFINITY ? m[t2] : 0.0f;  // nothing seen yet: every term is 2^-inf = 0
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[t2][i][e] = fast_exp2(fmaf(s[t2][i][e], sc, -ref));
+          sum += s[t2][i][e];
+        }
+      l[t2] += sum;
+    }
+    // ---- O^T += V^T . P^T
+    if (t + 2 < mine) wait_loads<3 * T::kLoads + 2 * kSide>();
+    else if (t + 1 < mine) wait_loads<2 * T::kLoads + kSide>();
+    else wait_loads<0>();
+    if (of_nodes) {
+      // A node's value that is infinite or NaN must not reach the rows that do not see the node, and 0 times it would: such nodes
+      // are zero in the products, and added in the end to the rows that see them.
+      bool any = false;
+      const LateLane L;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + L.lane * 16));
+      if (__any(any)) {
+        const int j0 = walk.first_node(t);
 #pragma unroll 1
-          for (int j = 0; j < min(T::kSlots, nodes - j0); ++j) {
-            uint4* const row = reinterpret_cast<uint4*>(tileV + j * T::kBytes) + L.lane % T::kChunks;
-            if (!__any(holds_special<DT>(*row))) continue;
-            special |= 1ull << (j0 + j);
-            *row = make_uint4(0u, 0u, 0u, 0u);
-          }
-        }
-        reads_done();
-      }
-      if constexpr (DT == kBF16) {
-        // The probabilities as sums of two bf16 numbers: rounded to one they would make as much of the output's error as its own
-        // rounding (2.3e-3 against 1.7e-3 of its norm); the matrix cores have the time.
-        uint4 vf[kAhead + 1];
-        const auto read_v = [&](int at) {
-          const char* const vt = tileV + at / T::kBlocks * 2 * 16 * T::kBytes + (vfrag ^ (at % T::kBlocks << 5));
-          const uint2 lo = lds_read_transposed(vt), hi = lds_read_transposed(vt + 16 * T::kBytes);
-          vf[at % (kAhead + 1)] = make_uint4(lo.x, lo.y, hi.x, hi.y);
-        };
-#pragma unroll
-        for (int at = 0; at < kAhead; ++at) read_v(at);
-#pragma unroll
-        for (int i = 0; i < G; i += 2) {
-          uint4 p[NQ][2];
-#pragma unroll
-          for (int t2 = 0; t2 < NQ; ++t2) {
-            const f32x4 pair[2] = {s[t2][i], s[t2][i + 1]};
-            fused::split_positive(pair, p[t2]);
-          }
-#pragma unroll
-          for (int db = 0; db < T::kBlocks; ++db) {
-            const int at = i / 2 * T::kBlocks + db;
-            if (at + kAhead < G / 2 * T::kBlocks) read_v(at + kAhead);
-            const uint4 v = vf[at % (kAhead + 1)];
-#pragma unroll
-            for (int k = 1; k >= 0; --k)
-#pragma unroll
-              for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(v, p[t2][k], o[t2][db]);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-      } else {
-        float vf[kAhead + 1][4];
-        const auto read_v = [&](int at) {
-          const char* const vt = tileV + at / T::kBlocks * 16 * T::kBytes + (vfrag ^ (at % T::kBlocks << 6));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) vf[at % (kAhead + 1)][e] = *reinterpret_cast<const float*>(vt + e * T::kBytes);
-        };
-#pragma unroll
-        for (int at = 0; at < kAhead; ++at) read_v(at);
-#pragma unroll
-        for (int at = 0; at < G * T::kBlocks; ++at) {
-          if (at + kAhead < G * T::kBlocks) read_v(at + kAhead);
-          const int i = at / T::kBlocks, db = at % T::kBlocks;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[at % (kAhead + 1)][e], s[t2][i][e], o[t2][db], 0, 0, 0);
-          __builtin_amdgcn_sched_barrier(0);
+        for (int j = 0; j < min(T::kSlots, nodes - j0); ++j) {
+          uint4* const row = reinterpret_cast<uint4*>(tileV + j * T::kBytes) + L.lane % T::kChunks;
+          if (!__any(holds_special<DT>(*row))) continue;
+          special |= 1ull << (j0 + j);
+          *row = make_uint4(0u, 0u, 0u, 0u);
         }
       }
       reads_done();
     }
-    if (kBehindK && t == -1) {
-      if (mine > 1) wait_loads<3 * T::kLoads + 2 * kSide>();
-      else if (mine > 0) wait_loads<2 * T::kLoads + kSide>();
-      else wait_loads<0>();
-      read_queries();
+    if constexpr (DT == kBF16) {
+      // The probabilities as sums of two bf16 numbers: rounded to one they would make as much of the output's error as its own
+      // rounding (2.3e-3 against 1.7e-3 of its norm); the matrix cores have the time.
+      uint4 vf[kAhead + 1];
+      const auto read_v = [&](int at) {
+        const char* const vt = tileV + at / T::kBlocks * 2 * 16 * T::kBytes + (vfrag ^ (at % T::kBlocks << 5));
+        const uint2 lo = lds_read_transposed(vt), hi = lds_read_transposed(vt + 16 * T::kBytes);
+        vf[at % (kAhead + 1)] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      };
+#pragma unroll
+      for (int at = 0; at < kAhead; ++at) read_v(at);
+#pragma unroll
+      for (int i = 0; i < G; i += 2) {
+        uint4 p[NQ][2];
+#pragma unroll
+        for (int t2 = 0; t2 < NQ; ++t2) {
+          const f32x4 pair[2] = {s[t2][i], s[t2][i + 1]};
+          fused::split_positive(pair, p[t2]);
+        }
+#pragma unroll
+        for (int db = 0; db < T::kBlocks; ++db) {
+          const int at = i / 2 * T::kBlocks + db;
+          if (at + kAhead < G / 2 * T::kBlocks) read_v(at + kAhead);
+          const uint4 v = vf[at % (kAhead + 1)];
+#pragma unroll
+          for (int k = 1; k >= 0; --k)
+#pragma unroll
+            for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(v, p[t2][k], o[t2][db]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    } else {
+      float vf[kAhead + 1][4];
+      const auto read_v = [&](int at) {
+        const char* const vt = tileV + at / T::kBlocks * 16 * T::kBytes + (vfrag ^ (at % T::kBlocks << 6));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vf[at % (kAhead + 1)][e] = *reinterpret_cast<const float*>(vt + e * T::kBytes);
+      };
+#pragma unroll
+      for (int at = 0; at < kAhead; ++at) read_v(at);
+#pragma unroll
+      for (int at = 0; at < G * T::kBlocks; ++at) {
+        if (at + kAhead < G * T::kBlocks) read_v(at + kAhead);
+        const int i = at / T::kBlocks, db = at % T::kBlocks;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[at % (kAhead + 1)][e], s[t2][i][e], o[t2][db], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    if (t + 2 < mine) request_tile<DT, HD, STREAMING>(next_nodes ? static_cast<const char*>(a.v_new) + new_rows : static_cast<const char*>(a.V), next.row, next.there, lds_address(tileV), voff);
+    reads_done();
+    if (t + 2 < mine) request_v(next, next_nodes, t);
     there0 = there1;
     there1 = there2;
   }
