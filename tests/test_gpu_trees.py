@@ -304,6 +304,33 @@ def test_logits_far_apart(dtype, d):
     s.check_attend(*s.attend())
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("T,group,page", [(40, 3, 0), (64, 5, 16), (64, 5, 64)])
+def test_recency_window_over_many_rows(dtype, d, T, group, page):
+    s = Step(T + page, dtype, d, used=[0, 90, 310, 1000], B=1000, budgets=[30, 90, 400, 1000], T=T, group=group, window=70, page=page,
+             n_nodes=[T, T // 2, T, T - 1]).upload()
+    s.check_attend(*s.attend())
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("splits", [1, 2, 5, 8, 9, 64])
+def test_any_number_of_splits(monkeypatch, dtype, d, splits):
+    """Many rows, so that few splits of them are joined several rows at a time, and few; units that use one split, some or all."""
+    monkeypatch.setenv("ROCO_TREE_SPLITS", str(splits))
+    for T, group in ((64, 32), (5, 2)):
+        s = Step(splits, dtype, d, used=[0, 65, 700, 333], B=700, T=T, group=group, n_nodes=[T, T - 1, T // 2, T]).upload()
+        s.check_attend(*s.attend(), f"{T} nodes")
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_the_largest_trees(dtype, d):
+    s = Step(2, dtype, d, used=[130, 77], heads=1, B=140, T=64, group=64, chain=True, page=16, n_nodes=[64, 63]).upload()
+    s.check_attend(*s.attend())
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
 def test_pages_outside_the_pool_are_not_seen(dtype, d):
     """Pages behind the pool and before it: their slots count as not there.  (The host has checked the pool's size; the kernel every entry.)"""
@@ -413,6 +440,25 @@ def test_the_same_node_twice_and_no_records_of_the_evicted():
 
 def test_large_budgets_keep_their_keys_in_the_workspace():
     s = Step(7, "bf16", 64, used=[17000], heads=1, B=17000, T=5, chain=True, max_path=4).upload()
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+
+
+@pytest.mark.parametrize("B", [4095, 4096, 4097])
+def test_budgets_at_the_border_of_a_choice_beside_the_sums(B):
+    for dtype, d, used in (("bf16", 128, [B, B - 2, 700]), ("f32", 64, [B])):
+        s = Step(B, dtype, d, used=used, heads=1, T=5, chain=True, max_path=4, scope=B // 2).upload()
+        lse = s.exact_lse()
+        s.commit(lse)
+        s.check_commit(lse, dtype)
+
+
+@pytest.mark.parametrize("n", [70, 600, 2000])
+def test_equal_statistics_are_told_apart_by_their_slots(n):
+    s = Step(n, "bf16", 64, used=[n, n - 1], T=8, chain=True, max_path=8, scope=n)
+    s.stats[:, 0], s.stats[:, 1], s.stats[:, 2] = 0.5, 0.25, 2.0
+    s.upload()
     lse = s.exact_lse()
     s.commit(lse)
     s.check_commit(lse)
