@@ -378,7 +378,8 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
  * Where the list is too short (page_start[requests] > n_free), the pages that it lacks are -1, in the table and in the map.
  * held may be NULL (new requests); held is held inside [0, max_pages * page], want inside [held, max_pages * page].  The sums have
  * 32 bits.  No workspace.
- * page: a power of two, 16 .. 1024; n_free >= 0 (free_pages may be NULL with 0); 1 <= requests <= 65535; rows >= 1.
+ * page: a power of two, 16 .. 1024; n_free >= 0 (free_pages may be NULL with 0); 1 <= requests <= 65535; rows >= 1.  free_pages may be the
+ * rest of a list: it is aligned to 4 bytes.
  */
 int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const int32_t* held, const int32_t* want,
                      const int32_t* free_pages, int32_t n_free, int32_t* table, int32_t* page_start, int32_t* row_start,
@@ -389,7 +390,7 @@ int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const in
  * [units, B, d] into pages.  Entry (g, i) of the map [groups, rows] names the pool slot of row (g, i) of every head h, which lies
  * group_stride g + row_stride i + head_stride h elements behind K_rows (V_rows); -1 (anything negative, or a page that the pool does
  * not have): the row is not stored.  Two rows of the same slot: either.
- * Pools [n_pages, heads, page, d], disjoint from the rows.  Strides are multiples of 16 bytes and not negative; n_pages * heads * page < 2^31.
+ * Pools [n_pages, heads, page, d], disjoint from the rows.  The map may be a part of a packed one: it is aligned to 4 bytes.  Strides are multiples of 16 bytes and not negative; n_pages * heads * page < 2^31.
  */
 int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t groups, int32_t rows, const void* K_rows,
                     const void* V_rows, int64_t group_stride, int64_t row_stride, int64_t head_stride, const int32_t* slot_map,

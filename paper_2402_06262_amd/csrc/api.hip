@@ -26,6 +26,7 @@ constexpr int kStreamingAboveMiB = 192;
 constexpr int kMaxPrefillGroup = 64;  // query heads per key/value head in the grouped-query prefill
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 int check_params(const roco_params* p) {
   if (p == nullptr) return ROCO_EINVAL;
@@ -593,7 +594,7 @@ int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const in
   const void* need[] = {want, table, page_start, row_start, slot_map};
   for (const void* ptr : need)
     if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
-  if ((held != nullptr && !aligned16(held)) || !aligned16(free_pages) || (free_pages == nullptr && n_free > 0)) return ROCO_EINVAL;
+  if ((held != nullptr && !aligned16(held)) || !aligned4(free_pages) || (free_pages == nullptr && n_free > 0)) return ROCO_EINVAL;
   const PageTableArgs a = {requests, __builtin_ctz(static_cast<unsigned>(page)), max_pages, n_free, rows, padded != 0, held, want,
                            free_pages, table, page_start, row_start, slot_map};
   return launch_page_tables(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
@@ -610,9 +611,10 @@ int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t grou
   const int64_t element = dtype == ROCO_BF16 ? 2 : 4;
   for (const int64_t stride : {group_stride, row_stride, head_stride})
     if (stride < 0 || stride > (1ll << 60) || stride * element % 16 != 0) return ROCO_EINVAL;
-  const void* need[] = {K_rows, V_rows, slot_map, K_pool, V_pool};
+  const void* need[] = {K_rows, V_rows, K_pool, V_pool};
   for (const void* ptr : need)
     if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
+  if (slot_map == nullptr || !aligned4(slot_map)) return ROCO_EINVAL;
   // (a lane per 16 bytes, counted by the grid: at most 2^31 workgroups of 256)
   if (static_cast<double>(groups) * heads * rows * head_dim * element / 16 / 256 >= 2147483647.0) return ROCO_EUNSUPPORTED;
   const PageStoreArgs a = {heads, groups, rows, n_pages, __builtin_ctz(static_cast<unsigned>(page)), static_cast<int>(head_dim * element),

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kSumThreads) void page_sums(PageTableArgs a) {
 }
 
 // The map, kFillEntries entries per thread at a time, and the table, a wave per request.  SELF: every workgroup forms the requests' sums in its
-// LDS, from lengths that the L2 has, instead of waiting for a launch that does: a step of 64 requests 7.7 -> 5.9 us.  A page number is asked
+// LDS, from lengths that the L2 has, instead of waiting for a launch that does: a step of 64 requests 7.7 -> 5.4 us.  A page number is asked
 // for once for entries of the same page; a division and a search per entry took 19.6 us for 1024 requests of up to 8192 slots.
 template <bool SELF> __global__ __launch_bounds__(kFillThreads) void page_fill(PageTableArgs a) {
   __shared__ uint32_t sh[kFillThreads / kWave + 1];

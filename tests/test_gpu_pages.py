@@ -130,6 +130,25 @@ def test_new_tokens_and_caches_into_pages(dtype, d, heads, rows, page):
             assert torch.equal(pool, expected(x.transpose(1, 2).reshape(-1, heads, d), slots.view(-1)))
 
 
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_the_rest_of_a_free_list_and_a_part_of_a_map(off):
+    """Lists and maps that begin at any of their words."""
+    held, want, page = [0, 20, 33], [40, 21, 33], 16
+    free, table = ints(np.arange(50, 70)), ints(np.full((3, 4), -5))
+    starts, slots = [ints(np.zeros(4)) for _ in range(2)], ints(np.zeros(41))
+    roco.roco_page_tables(ints(held), ints(want), page, free[off:], table, *starts, slots)
+    rest = np.arange(50, 70)[off:]
+    for got, w in zip((table, *starts, slots), trees.page_tables(held, want, page, rest, np.full((3, 4), -5), 41, False)):
+        assert np.array_equal(got.cpu().numpy(), w)
+    K = torch.randn((41 - off, 2, 64), device="cuda")
+    pools = [torch.full((70, 2, page, 64), 9.0, device="cuda") for _ in range(2)]
+    roco.roco_page_store(K, K, slots[off:], *pools)
+    at = slots[off:].long()
+    real = at >= 0  # (request 1 goes on in a page of its own that is none: what lies there is not stored)
+    assert torch.equal(pools[0][at[real] // page, :, at[real] % page], K[real]) and torch.equal(*pools)
+    assert int((pools[0] != 9).any(-1).sum()) == 2 * int(real.sum()) == 2 * (40 - off)
+
+
 def test_store_beyond_32_bits():
     """Rows at the end of pools of 5 GiB, from rows that lie as far apart."""
     n_pages, heads, page, d = 40960, 8, 64, 128
