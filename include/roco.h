@@ -305,6 +305,9 @@ int roco_decode_step_gqa(const roco_params* params, int32_t group,
  * row length of stats and pos, which stay [units, 3, B] and [units, B]).  The scope of a request of fewer slots than params->scope is
  * all of them.  Entries behind the pages that the slots in use need are not read.  What lies in a page outside [0, n_pages) is
  * neither read nor written: such slots are not seen.
+ *
+ * The rows (q, k_new, v_new, out, caches, pools), the workspace and the slot map that roco_page_tables writes are aligned to 16 bytes, the other
+ * arrays of these calls to 4: the rest of a list of free pages, a part of a packed map, or statistics and positions in one buffer.
  */
 typedef struct roco_pages {
   const int32_t* table;   /* device [requests, max_pages]                                            */
@@ -378,8 +381,7 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
  * Where the list is too short (page_start[requests] > n_free), the pages that it lacks are -1, in the table and in the map.
  * held may be NULL (new requests); held is held inside [0, max_pages * page], want inside [held, max_pages * page].  The sums have
  * 32 bits.  No workspace.
- * page: a power of two, 16 .. 1024; n_free >= 0 (free_pages may be NULL with 0); 1 <= requests <= 65535; rows >= 1.  free_pages may be the
- * rest of a list: it is aligned to 4 bytes.
+ * page: a power of two, 16 .. 1024; n_free >= 0 (free_pages may be NULL with 0); 1 <= requests <= 65535; rows >= 1.
  */
 int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const int32_t* held, const int32_t* want,
                      const int32_t* free_pages, int32_t n_free, int32_t* table, int32_t* page_start, int32_t* row_start,
@@ -390,7 +392,7 @@ int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const in
  * [units, B, d] into pages.  Entry (g, i) of the map [groups, rows] names the pool slot of row (g, i) of every head h, which lies
  * group_stride g + row_stride i + head_stride h elements behind K_rows (V_rows); -1 (anything negative, or a page that the pool does
  * not have): the row is not stored.  Two rows of the same slot: either.
- * Pools [n_pages, heads, page, d], disjoint from the rows.  The map may be a part of a packed one: it is aligned to 4 bytes.  Strides are multiples of 16 bytes and not negative; n_pages * heads * page < 2^31.
+ * Pools [n_pages, heads, page, d], disjoint from the rows.  Strides are multiples of 16 bytes and not negative; n_pages * heads * page < 2^31.
  */
 int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t groups, int32_t rows, const void* K_rows,
                     const void* V_rows, int64_t group_stride, int64_t row_stride, int64_t head_stride, const int32_t* slot_map,
@@ -514,6 +516,9 @@ int roco_probe_mfma(int32_t workgroups, int32_t iters, int32_t operands, float* 
  *                              per unit with half of the tokens each, and a kernel that adds their sums / three kernels; above 32
  *                              query rows 8, 4 and 2 are all two workgroups; a step that the shape does not hold takes three kernels
  *                              (default: by units, budget, rows and head_dim)
+ *   ROCO_TREE_SPLITS=1..64     splits of the budget in roco_tree_attend (default: about 512 / units, or of more than 64 query rows of
+ *                              bf16 those whose rounds of 512 workgroups are shortest); roco_tree_workspace_bytes has to see the
+ *                              same value
  *   ROCO_SELECT_THREADS=512|1024  threads of the prompt selection (default: 512 for prompts of up to 512 tokens, and of up to 2048
  *                              with more than 256 units)
  *   ROCO_PREFILL_WAVES_PER_ROW=1|4  waves that share a query row of the vector row pass (default: four for few rows)

@@ -103,7 +103,9 @@ int check_block(const roco_params* p, int32_t block) {
   return ROCO_OK;
 }
 
-// ---- drafted trees: heads, groups, nodes and pages; the paged rows are counted in 31 bits
+// ---- drafted trees: heads, groups, nodes and pages; the paged rows are counted in 31 bits.  Their integers and statistics are read a word at a
+// time, so that any word of a larger buffer may be the first one.
+bool given(const void* words) { return words != nullptr && aligned4(words); }
 bool page_size_ok(int32_t page) { return page >= 16 && page <= 1024 && (page & (page - 1)) == 0; }
 int check_pages(int32_t n_pages, int32_t heads, int32_t page) {
   if (n_pages < 1 || !page_size_ok(page)) return ROCO_EINVAL;
@@ -116,7 +118,7 @@ int check_tree(const roco_params* p, int32_t heads, int32_t group, int32_t nodes
   if (group > kMaxTreeGroup || nodes > kMaxTreeNodes) return ROCO_EUNSUPPORTED;
   out = CachePages{nullptr, nullptr, 0, 0, 0};
   if (pages == nullptr) return static_cast<long long>(p->units) * p->budget < (1ll << 32) ? ROCO_OK : ROCO_EUNSUPPORTED;
-  if (pages->table == nullptr || !aligned16(pages->table) || (pages->budget != nullptr && !aligned16(pages->budget))) return ROCO_EINVAL;
+  if (!given(pages->table) || !aligned4(pages->budget)) return ROCO_EINVAL;
   const int rc2 = check_pages(pages->n_pages, heads, pages->page);
   if (rc2 != ROCO_OK) return rc2;
   if (pages->max_pages < 1 || static_cast<long long>(pages->max_pages) * pages->page < p->budget) return ROCO_EINVAL;
@@ -523,11 +525,10 @@ int roco_tree_attend(const roco_params* params, int32_t heads, int32_t group, in
   TreeArgs a;
   const int rc = check_tree(params, heads, group, nodes, pages, a.pages);
   if (rc != ROCO_OK) return rc;
-  const void* need[] = {q, k_new, v_new, qpos0, K_cache, V_cache, pos, n_used, out, workspace};
+  const void* need[] = {q, k_new, v_new, K_cache, V_cache, out, workspace};
   for (const void* ptr : need)
     if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
-  for (const void* ptr : {static_cast<const void*>(parent), static_cast<const void*>(n_nodes), static_cast<const void*>(lse)})
-    if (ptr != nullptr && !aligned16(ptr)) return ROCO_EINVAL;
+  if (!given(qpos0) || !given(pos) || !given(n_used) || !aligned4(parent) || !aligned4(n_nodes) || !aligned4(lse)) return ROCO_EINVAL;
   const TreeLayout lay = tree_layout(params, group, nodes);
   if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
   a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
@@ -555,11 +556,13 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
   const int rc = check_tree(params, heads, group, nodes, pages, a.pages);
   if (rc != ROCO_OK) return rc;
   if (max_path < 1 || max_path > nodes) return ROCO_EINVAL;
-  const void* need[] = {q, k_new, v_new, lse, path, n_path, qpos0, K_cache, V_cache, stats, pos, n_used, workspace};
+  const void* need[] = {q, k_new, v_new, K_cache, V_cache, workspace};
   for (const void* ptr : need)
     if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
-  for (const void* ptr : {static_cast<const void*>(evicted_slot), static_cast<const void*>(evicted_pos)})
-    if (ptr != nullptr && !aligned16(ptr)) return ROCO_EINVAL;
+  const void* words[] = {lse, path, n_path, qpos0, stats, pos, n_used};
+  for (const void* ptr : words)
+    if (!given(ptr)) return ROCO_EINVAL;
+  if (!aligned4(evicted_slot) || !aligned4(evicted_pos)) return ROCO_EINVAL;
   const TreeLayout lay = tree_layout(params, group, nodes);
   if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
   a.units = params->units; a.heads = heads; a.group = group; a.nodes = nodes; a.B = params->budget;
@@ -591,10 +594,8 @@ int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const in
   if (requests < 1 || max_pages < 1 || n_free < 0 || rows < 1 || !page_size_ok(page)) return ROCO_EINVAL;
   if (requests > 65535 || static_cast<long long>(max_pages) * page >= (1ll << 31)) return ROCO_EUNSUPPORTED;
   if (padded && static_cast<long long>(requests) * rows >= (1ll << 40)) return ROCO_EUNSUPPORTED;
-  const void* need[] = {want, table, page_start, row_start, slot_map};
-  for (const void* ptr : need)
-    if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
-  if ((held != nullptr && !aligned16(held)) || !aligned4(free_pages) || (free_pages == nullptr && n_free > 0)) return ROCO_EINVAL;
+  if (!given(want) || !given(table) || !given(page_start) || !given(row_start) || slot_map == nullptr || !aligned16(slot_map)) return ROCO_EINVAL;
+  if (!aligned4(held) || !aligned4(free_pages) || (free_pages == nullptr && n_free > 0)) return ROCO_EINVAL;
   const PageTableArgs a = {requests, __builtin_ctz(static_cast<unsigned>(page)), max_pages, n_free, rows, padded != 0, held, want,
                            free_pages, table, page_start, row_start, slot_map};
   return launch_page_tables(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
@@ -614,7 +615,7 @@ int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t grou
   const void* need[] = {K_rows, V_rows, K_pool, V_pool};
   for (const void* ptr : need)
     if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
-  if (slot_map == nullptr || !aligned4(slot_map)) return ROCO_EINVAL;
+  if (!given(slot_map)) return ROCO_EINVAL;
   // (a lane per 16 bytes, counted by the grid: at most 2^31 workgroups of 256)
   if (static_cast<double>(groups) * heads * rows * head_dim * element / 16 / 256 >= 2147483647.0) return ROCO_EUNSUPPORTED;
   const PageStoreArgs a = {heads, groups, rows, n_pages, __builtin_ctz(static_cast<unsigned>(page)), static_cast<int>(head_dim * element),

@@ -155,13 +155,13 @@ class Step:
                 lse[u, :t] = self.want(u).lse
         return lse
 
-    def commit(self, lse, **kw):
+    def commit(self, host_lse, **kw):
         path = np.full((self.R, self.max_path), 1 << 20)  # entries behind a path are not read
         for r, p in enumerate(self.paths):
             path[r, :len(p)] = p
         self.ev_slot = torch.full((self.U, self.max_path), -7, dtype=torch.int32, device="cuda")
         self.ev_pos = torch.full((self.U, self.max_path), -7, dtype=torch.int32, device="cuda")
-        a = dict(pages=self.pages, q=self.dq, k_new=self.dk, v_new=self.dv, lse=dev(lse, "f32"), max_path=self.max_path, path=dev(path),
+        a = dict(pages=self.pages, q=self.dq, k_new=self.dk, v_new=self.dv, lse=dev(host_lse, "f32"), max_path=self.max_path, path=dev(path),
                  n_path=dev(np.array([len(p) for p in self.paths])), qpos0=self.dqpos0, K_cache=self.dK, V_cache=self.dV, stats=self.dstats,
                  pos=self.dpos, n_used=self.dn_used, evicted_slot=self.ev_slot, evicted_pos=self.ev_pos, workspace=self.ws)
         a.update(kw)
@@ -462,6 +462,36 @@ def test_equal_statistics_are_told_apart_by_their_slots(n):
     lse = s.exact_lse()
     s.commit(lse)
     s.check_commit(lse)
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+@pytest.mark.parametrize("dtype,d,T", [("bf16", 128, 9), ("bf16", 64, 40), ("f32", 128, 9)])
+def test_words_that_begin_anywhere(dtype, d, T, off):
+    """Statistics, positions, lengths, trees, paths and tables inside larger buffers: the bits of a step whose arrays are on their own."""
+    make = lambda: Step(off, dtype, d, used=[40, 33, 250], B=250, budgets=[40, 40, 250], page=16, T=T, group=2, window=9, max_path=5).upload()  # noqa: E731
+
+    def inside(x):
+        y = torch.empty(x.numel() + 8, dtype=x.dtype, device="cuda").fill_(-3)[off:off + x.numel()].view(x.shape)
+        return y.copy_(x)
+
+    plain, moved = make(), make()
+    for name in ("dparent", "dn_nodes", "dqpos0", "dpos", "dn_used", "dstats", "lse"):
+        setattr(moved, name, inside(getattr(moved, name)))
+    moved.pages = roco.RocoPages(inside(torch.from_numpy(moved.table).to(torch.int32).cuda()), moved.n_pages, moved.page,
+                                 inside(torch.tensor(moved.budgets, dtype=torch.int32, device="cuda")))
+    assert moved.dstats.data_ptr() % 16 == 4 * off
+    (out, lse), (out2, lse2) = plain.attend(), moved.attend()
+    assert np.array_equal(out, out2) and np.array_equal(lse, lse2)
+    plain.commit(lse)
+    path = np.zeros((moved.R, moved.max_path))
+    for r, p in enumerate(moved.paths):
+        path[r, :len(p)] = p
+    evicted = [inside(torch.zeros((moved.U, moved.max_path), dtype=torch.int32, device="cuda")) for _ in range(2)]
+    moved.commit(lse, lse=moved.lse, path=inside(dev(path)), n_path=inside(dev(np.array([len(p) for p in moved.paths]))), evicted_slot=evicted[0],
+                 evicted_pos=evicted[1])
+    for a, b in ((plain.dstats, moved.dstats), (plain.dpos, moved.dpos), (plain.dn_used, moved.dn_used), (plain.ev_slot, evicted[0]), (plain.ev_pos, evicted[1]),
+                 (plain.dK.nan_to_num(7), moved.dK.nan_to_num(7))):
+        assert torch.equal(a, b)
 
 
 def test_pages_outside_the_pool_are_not_written():

@@ -52,7 +52,8 @@ def test_shapes_are_checked(call):
 @pytest.mark.parametrize("call", [_attend, _commit])
 def test_pages_are_checked(call):
     assert call(pages=_pages(), ws=0) == EWORKSPACE
-    assert call(pages=_pages(table=None)) == EINVAL and call(pages=_pages(table=OK + 4)) == EINVAL and call(pages=_pages(budget=OK + 4)) == EINVAL
+    assert call(pages=_pages(table=None)) == EINVAL and call(pages=_pages(table=OK + 2)) == EINVAL and call(pages=_pages(budget=OK + 2)) == EINVAL
+    assert call(pages=_pages(table=OK + 4, budget=OK + 8), ws=0) == EWORKSPACE
     for page in (0, 8, 48, 2048, -16):
         assert call(pages=_pages(page=page, max_pages=1 << 20)) == EINVAL
     assert call(pages=_pages(max_pages=3)) == EINVAL  # 192 slots for a budget of 256
@@ -61,18 +62,23 @@ def test_pages_are_checked(call):
 
 
 def test_pointers_are_checked():
+    # rows and workspaces are aligned to 16 bytes, words to 4
     for i in range(10):
-        for bad in (None, OK + 8):
+        words = i in (3, 6, 7)  # qpos0, pos, n_used
+        assert _attend(ptrs=[OK + 4 if j == i else OK for j in range(10)], ws=0) == (EWORKSPACE if words else EINVAL)
+        for bad in (None, OK + (2 if words else 8)):
             assert _attend(ptrs=[bad if j == i else OK for j in range(10)]) == EINVAL
     for i in range(13):
-        for bad in (None, OK + 8):
+        words = i in (3, 4, 5, 6, 9, 10, 11)  # lse, path, n_path, qpos0, stats, pos, n_used
+        assert _commit(ptrs=[OK + 4 if j == i else OK for j in range(13)], ws=0) == (EWORKSPACE if words else EINVAL)
+        for bad in (None, OK + (2 if words else 8)):
             assert _commit(ptrs=[bad if j == i else OK for j in range(13)]) == EINVAL
     for i in range(3):
         assert _attend(optional=[None if j == i else OK for j in range(3)], ws=0) == EWORKSPACE
-        assert _attend(optional=[OK + 4 if j == i else OK for j in range(3)]) == EINVAL
+        assert _attend(optional=[OK + 2 if j == i else OK for j in range(3)]) == EINVAL
     for i in range(2):
         assert _commit(optional=[None if j == i else OK for j in range(2)], ws=0) == EWORKSPACE
-        assert _commit(optional=[OK + 4 if j == i else OK for j in range(2)]) == EINVAL
+        assert _commit(optional=[OK + 2 if j == i else OK for j in range(2)]) == EINVAL
     assert _commit(max_path=0) == EINVAL and _commit(max_path=9) == EINVAL  # 8 nodes
     assert roco.load_library().roco_tree_attend(None, 1, 1, 1, None, *[OK] * 13, 0, None) == EINVAL
 
@@ -84,7 +90,7 @@ def test_tables_and_stores_are_checked():
         return lib.roco_page_tables(requests, page, max_pages, ptrs[0], ptrs[1], ptrs[2], n_free, ptrs[3], ptrs[4], ptrs[5], ptrs[6], rows, 0, None)
 
     for i in range(7):  # (all but `held` are needed)
-        odd = OK + (2 if i == 2 else 4)  # (the list of free pages may be the rest of one)
+        odd = OK + (8 if i == 6 else 2)  # (the map is written 16 bytes at a time)
         assert tables(ptrs=[odd if j == i else OK for j in range(7)]) == EINVAL
         if i > 0:
             assert tables(ptrs=[None if j == i else OK for j in range(7)]) == EINVAL
@@ -96,7 +102,7 @@ def test_tables_and_stores_are_checked():
         return lib.roco_page_store(dtype, d, heads, groups, rows, ptrs[0], ptrs[1], *strides, *ptrs[2:], n_pages, page, None)
 
     for i in range(5):
-        for bad in (None, OK + (2 if i == 2 else 8)):  # (the map may be a part of one)
+        for bad in (None, OK + (2 if i == 2 else 8)):
             assert store(ptrs=[bad if j == i else OK for j in range(5)]) == EINVAL
     for kw in (dict(heads=0), dict(groups=0), dict(rows=0), dict(n_pages=0), dict(page=17), dict(strides=(0, 256, -128)),
                dict(strides=(0, 252, 128)), dict(strides=(4, 256, 128))):
