@@ -59,39 +59,65 @@ template <int NT> __device__ __forceinline__ void choose_slots(const CommitArgs&
   const float* const cnt = acc2 + B;
   const int32_t* const pos = a.pos + static_cast<size_t>(u) * B;
   uint32_t *const var_key = keys, *const mas_key = keys + B;
-  KSmallest scope = {0u, 0u}, out = {0u, 0u};
+  uint32_t* const found = list_sh + 1;  // the accepted tokens' slots, in any order
+  const auto keep = [&](int j) {
+    const uint32_t at = atomicAdd(&list_sh[0], 1u);
+    if (at < static_cast<uint32_t>(len)) found[at] = static_cast<uint32_t>(j);
+  };
   if (E == 0) {
-    __syncthreads();
+    __syncthreads();  // list_sh[0] is there
   } else {
-#pragma unroll 8
-    for (int i = tid; i < n; i += NT) ranking_keys(acc[i], acc2[i], cnt[i], pos[i], a.pol, mas_key[i], var_key[i]);
+    // (kEach slots of a thread at a time, so that their loads are in flight together: one by one the keys took half of a choice)
+    constexpr int kEach = 4;
+#pragma unroll 1
+    for (int i0 = tid; i0 < n; i0 += kEach * NT) {
+      float first[kEach], second[kEach], count[kEach];
+      int at[kEach];
+      uint32_t mas[kEach], var[kEach];
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int i = min(i0 + e * NT, n - 1);
+        first[e] = acc[i];
+        second[e] = acc2[i];
+        count[e] = cnt[i];
+        at[e] = pos[i];
+      }
+      ranking_keys<kEach>(first, second, count, at, a.pol, mas, var);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int i = min(i0 + e * NT, n - 1);
+        mas_key[i] = mas[e];
+        var_key[i] = var[e];
+      }
+    }
     __syncthreads();
     const uint32_t m = min(static_cast<uint32_t>(n), static_cast<uint32_t>(a.pol.scope_size(min(a.scope, budget), n)) + static_cast<uint32_t>(E) - 1u);
+    KSmallest r = {0u, 0u};
 #pragma unroll 1
     for (int phase = 0; phase < 2; ++phase) {
-      const KSmallest r = select_k_smallest<NT, 1, NT <= 256 ? 4 : 1>(
-          [&](int i) -> uint32_t {
-            const uint32_t vk = var_key[i];
-            return phase == 0 ? vk : scope.has(vk, i) ? mas_key[i] : 0xffffffffu;
-          },
-          n, phase == 0 ? m : static_cast<uint32_t>(E), phase == 0 && a.pol.scope_is_window(), sel_sh, phase == 0 || a.pol.spreads_importance());
-      if (phase == 0) scope = r;
-      else out = r;
+      const uint32_t* const key = phase == 0 ? var_key : mas_key;
+      r = select_k_smallest<NT, 1, NT <= 256 ? 4 : 1>([&](int i) -> uint32_t { return key[i]; }, n, phase == 0 ? m : static_cast<uint32_t>(E),
+                                                      phase == 0 && a.pol.scope_is_window(), sel_sh, phase == 0 || a.pol.spreads_importance());
+#pragma unroll 1
+      for (int i0 = tid; i0 < n; i0 += kEach * NT) {
+        bool in[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int i = i0 + e * NT;
+          in[e] = r.has(key[min(i, n - 1)], i);
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int i = i0 + e * NT;
+          if (i >= n) break;
+          if (phase == 0 && !in[e]) mas_key[i] = 0xffffffffu;
+          if (phase == 1 && in[e]) keep(i);
+        }
+      }
+      __syncthreads();
     }
   }
-  auto is_target = [&](int j) -> bool {
-    if (j >= n) return j < n_new;
-    if (E == 0) return false;
-    return out.has(scope.has(var_key[j], j) ? mas_key[j] : 0xffffffffu, j);
-  };
-  // The targets, `len` of them, in any order, then each by the number of those before it: the i-th takes the i-th token.
-  uint32_t* const found = list_sh + 1;
-#pragma unroll 4
-  for (int j = tid; j < n_new; j += NT)
-    if (is_target(j)) {
-      const uint32_t at = atomicAdd(&list_sh[0], 1u);
-      if (at < static_cast<uint32_t>(len)) found[at] = static_cast<uint32_t>(j);
-    }
+  if (tid < n_new - n) keep(n + tid);
   __syncthreads();
   if (tid >= len) return;
   const int j = static_cast<int>(found[tid]);
