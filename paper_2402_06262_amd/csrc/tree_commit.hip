@@ -11,6 +11,7 @@
 // (One after the other, choice and sums took 14 + 45 us on 512 units x 2048 slots and 9 + 7 on 16 x 500.  The search of a large budget
 // needs more threads and LDS than the sums leave it: above kMostChosenBeside slots it is a launch of its own.)
 #include <algorithm>
+#include <type_traits>
 
 #include "profile.hpp"
 #include "tree.hpp"
@@ -227,11 +228,10 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
   const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
   const int frag = qi * T::kBytes + ((g ^ T::swizzle_k(qi)) << 4);
   // of the lane's four rows of a tile, those whose register holds a token's sum over its heads in the end
-  const int heads_log2 = plan.heads_log2, in_tile = min(heads_log2, 4);
-  const int slices = 1 << (heads_log2 - in_tile);  // tiles of a token
+  const int heads_log2 = plan.heads_log2;
+  const int slices = 1 << max(heads_log2 - 4, 0);  // tiles of a token
+  const bool squares = !a.pol.keeps_last_score() && !a.pol.counts_above_average();
   const bool filled_up = (1 << heads_log2) != a.group;
-  const int stride = 1 << min(in_tile, 2);
-  const bool holds = in_tile < 3 || (g & ((1 << (in_tile - 2)) - 1)) == 0;
   char* const q_s = lds + W * 2 * kTileBytes;
   float* const lse_s = reinterpret_cast<float*>(q_s + static_cast<size_t>(plan.rows(plan.per_pass)) * T::kBytes);  // base 2
 #pragma unroll 1
@@ -281,53 +281,73 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
         own[i] = of_fresh ? j : 0;
         at[i] = !WINDOW ? 0 : of_fresh ? qp0 + j : pos_s[WINDOW ? min(j, kTreeChunk - 1) : 0];
       }
+      // (a copy for each way in which heads share a tile: a dozen branches per tile of rows otherwise)
+      const auto add_rows = [&](auto in_tile_of) {
+        constexpr int in_tile = decltype(in_tile_of)::value, stride = 1 << (in_tile < 2 ? in_tile : 2);
+        const bool holds = in_tile < 3 || (g & ((1 << (in_tile < 3 ? 0 : in_tile - 2)) - 1)) == 0;
 #pragma unroll 1
-      for (int tile0 = 0; tile0 < rows; tile0 += 16 * slices) {
-        const int token0 = first + (tile0 >> heads_log2);
-        f32x4 p[G];
+        for (int tile0 = 0; tile0 < rows; tile0 += 16 * slices) {
+          const int token0 = first + (tile0 >> heads_log2);
+          f32x4 p[G];
 #pragma unroll
-        for (int i = 0; i < G; ++i) p[i] = f32x4{0};
+          for (int i = 0; i < G; ++i) p[i] = f32x4{0};
 #pragma unroll 1
-        for (int row = tile0; row < tile0 + 16 * slices; row += 16) {
-          const f32x4 lse = *reinterpret_cast<const f32x4*>(lse_s + row + 4 * g);
-          const char* const q = q_s + row * T::kBytes;
-          f32x4 s[G];
+          for (int row = tile0; row < tile0 + 16 * slices; row += 16) {
+            const f32x4 lse = *reinterpret_cast<const f32x4*>(lse_s + row + 4 * g);
+            const char* const q = q_s + row * T::kBytes;
+            f32x4 s[G];
 #pragma unroll
-          for (int kk = 0; kk < T::kSteps; ++kk) {
-            const uint4 qf = *reinterpret_cast<const uint4*>(q + (frag ^ (kk << 6)));
+            for (int kk = 0; kk < T::kSteps; ++kk) {
+              const uint4 qf = *reinterpret_cast<const uint4*>(q + (frag ^ (kk << 6)));
 #pragma unroll
-            for (int i = 0; i < G; ++i) s[i] = score_step<DT>(qf, kf[i][kk], kk == 0 ? f32x4{0} : s[i]);
-          }
-#pragma unroll
-          for (int i = 0; i < G; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float x = fmaf(s[i][e], sc, -lse[e]);
-              if (WINDOW) x += static_cast<unsigned>(qp0 + token0 + ((4 * g + e) >> in_tile) - at[i]) < static_cast<unsigned>(w) ? bias : 0.0f;
-              const float v = fast_exp2(x);
-              p[i][e] += filled_up && lse[e] == INFINITY ? 0.0f : v;  // (0 times an infinite key is NaN)
+              for (int i = 0; i < G; ++i) s[i] = score_step<DT>(qf, kf[i][kk], kk == 0 ? f32x4{0} : s[i]);
             }
-        }
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-          if (in_tile >= 1) { p[i][0] += p[i][1]; p[i][2] += p[i][3]; }
-          if (in_tile >= 2) p[i][0] += p[i][2];
-          if (in_tile >= 3) p[i][0] += __shfl_xor(p[i][0], 16, kWave);
-          if (in_tile >= 4) p[i][0] += __shfl_xor(p[i][0], 32, kWave);
-        }
+            for (int i = 0; i < G; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if ((e & (stride - 1)) != 0) continue;
-          const int k = token0 + ((4 * g + e) >> in_tile);  // sees the tokens before it, and itself
+              for (int e = 0; e < 4; ++e) {
+                float x = fmaf(s[i][e], sc, -lse[e]);
+                if (WINDOW) x += static_cast<unsigned>(qp0 + token0 + ((4 * g + e) >> in_tile) - at[i]) < static_cast<unsigned>(w) ? bias : 0.0f;
+                const float v = fast_exp2(x);
+                p[i][e] += filled_up && lse[e] == INFINITY ? 0.0f : v;  // (0 times an infinite key is NaN)
+              }
+          }
 #pragma unroll
           for (int i = 0; i < G; ++i) {
-            const float v = p[i][e] * share;
-            const bool counts = holds && k < len && k >= own[i];
-            const float second = a.pol.keeps_last_score() ? (k == len - 1 ? v : 0.0f) : a.pol.second_statistic(0.0f, v, static_cast<float>(n + k + 1));
-            sum[i] += counts ? v : 0.0f;
-            sum2[i] += counts ? second : 0.0f;
+            if (in_tile >= 1) { p[i][0] += p[i][1]; p[i][2] += p[i][3]; }
+            if (in_tile >= 2) p[i][0] += p[i][2];
+            if (in_tile >= 3) p[i][0] += __shfl_xor(p[i][0], 16, kWave);
+            if (in_tile >= 4) p[i][0] += __shfl_xor(p[i][0], 32, kWave);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; e += stride) {
+            const int k = token0 + ((4 * g + e) >> in_tile);  // sees the tokens before it, and itself
+            float second[G];
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+              p[i][e] *= share;
+              second[i] = p[i][e] * p[i][e];
+            }
+            if (!squares) {
+#pragma unroll
+              for (int i = 0; i < G; ++i)
+                second[i] = a.pol.keeps_last_score() ? (k == len - 1 ? p[i][e] : 0.0f) : a.pol.second_statistic(0.0f, p[i][e], static_cast<float>(n + k + 1));
+            }
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+              const bool counts = holds && k < len && k >= own[i];
+              sum[i] += counts ? p[i][e] : 0.0f;
+              sum2[i] += counts ? second[i] : 0.0f;
+            }
           }
         }
+      };
+      switch (min(heads_log2, 4)) {
+        case 0: add_rows(std::integral_constant<int, 0>()); break;
+        case 1: add_rows(std::integral_constant<int, 1>()); break;
+        case 2: add_rows(std::integral_constant<int, 2>()); break;
+        case 3: add_rows(std::integral_constant<int, 3>()); break;
+        default: add_rows(std::integral_constant<int, 4>()); break;
       }
 #pragma unroll
       for (int i = 0; i < G; ++i) {
