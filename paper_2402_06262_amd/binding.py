@@ -432,24 +432,23 @@ def roco_page_tables(held, want, page: int, free_pages, table, page_start, row_s
 def roco_page_store(K_rows, V_rows, slot_map, K_pool, V_pool, stream=None) -> None:
     """See include/roco.h: rows of K and V to their pool slots.  Rows [rows, heads, d] (of new tokens, with a map [rows]) or
     [groups, heads, rows, d] (caches, with a map [groups, rows]) of any strides but the last dimension's; pools [n_pages, heads, page, d]."""
-    n_pages, heads, page, d = K_pool.shape
-    if K_rows.dim() == 3:
-        rows, groups = K_rows.shape[0], 1
-        row_stride, head_stride, last = K_rows.stride()
-        group_stride = 0
-        shape = (rows, heads, d)
+    pool, shape, strides = K_pool.shape, K_rows.shape, K_rows.stride()
+    n_pages, heads, page, d = pool
+    if len(shape) == 3:
+        rows, of_heads, of_d = shape
+        groups, group_stride = 1, 0
+        row_stride, head_stride, last = strides
     else:
-        groups, _, rows, _ = K_rows.shape
-        group_stride, head_stride, row_stride, last = K_rows.stride()
-        shape = (groups, heads, rows, d)
-    if tuple(K_rows.shape) != shape or V_rows.shape != K_rows.shape or V_pool.shape != K_pool.shape or slot_map.numel() != groups * rows:
+        groups, of_heads, rows, of_d = shape
+        group_stride, head_stride, row_stride, last = strides
+    if of_heads != heads or of_d != d or V_rows.shape != shape or V_pool.shape != pool or slot_map.numel() != groups * rows:
         raise ValueError("roco: rows are [rows, heads, d] or [groups, heads, rows, d], the map has an entry for each, pools are [n_pages, heads, page, d]")
-    if last != 1 or V_rows.stride() != K_rows.stride():
+    if last != 1 or V_rows.stride() != strides:
         raise ValueError("roco: a row's elements lie side by side, and the rows of V as those of K")
-    if not K_rows.dtype == V_rows.dtype == K_pool.dtype == V_pool.dtype:
+    dtype = K_pool.dtype
+    if not K_rows.dtype == V_rows.dtype == dtype == V_pool.dtype:
         raise ValueError("roco: rows and pools are of one type")
-    dtype = _dtype_code(K_pool.dtype)
-    rc = _calls().page_store(dtype, d, heads, groups, rows, K_rows.data_ptr(), V_rows.data_ptr(), group_stride, row_stride, head_stride,
+    rc = _calls().page_store(_dtype_code(dtype), d, heads, groups, rows, K_rows.data_ptr(), V_rows.data_ptr(), group_stride, row_stride, head_stride,
                              slot_map, K_pool, V_pool, n_pages, page, stream)
     if rc != 0:
         raise RocoError(rc, "roco_page_store")
