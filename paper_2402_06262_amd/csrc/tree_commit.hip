@@ -168,6 +168,7 @@ inline RowPlan row_plan(int group, int max_path, int row_bytes) {
 // Q is the A operand here, so that a lane holds four rows of one slot.  The accepted tokens themselves are tiles of the last workgroup, gathered
 // from k_new; token m is not seen by the rows before m.  More rows than the LDS takes: another pass over K (which the L2 mostly has).
 // choosers: the first workgroups, one per unit, that choose its slots (0: they have been chosen).
+// 512 units x 2048 slots of bf16 / 128 with up to six rows 53 us, 5 TB/s of K; 192 x 4096 of bf16 / 64 with up to 32 rows 23, vector issue.
 template <int DT, int HD, bool STREAMING, bool WINDOW>
 __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a, RowPlan plan, int choosers) {
   constexpr int kTileBytes = kStatTile<DT, HD>;
@@ -372,6 +373,7 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
 }
 
 // ------------------------------------------------------------------------------------------------
+// 512 units x 2048 slots 7 us, 5 TB/s of the planes read and written (slot by slot, each with its own trip to memory, 9.7).
 constexpr int kApplyThreads = 256;
 constexpr int kApplySlots = kTreeChunk;  // of a workgroup
 __global__ __launch_bounds__(kApplyThreads) void tree_apply(CommitArgs a, int row_bytes) {
