@@ -130,6 +130,46 @@ def test_new_tokens_and_caches_into_pages(dtype, d, heads, rows, page):
             assert torch.equal(pool, expected(x.transpose(1, 2).reshape(-1, heads, d), slots.view(-1)))
 
 
+def test_tables_and_store_captured_together():
+    """The rows that each replay stores go where its own tables say: other lengths, other rows, with eager calls between."""
+    rng = np.random.default_rng(3)
+    R, page, M, H, d, new = 6, 16, 8, 3, 64, 5
+    held, want = ints(rng.integers(0, 60, R)), ints(np.zeros(R))
+    table, free = ints(rng.permutation(R * M).reshape(R, M)), ints(R * M + rng.permutation(R * M))
+    starts, rows, slots = ints(np.zeros(R + 1)), ints(np.zeros(R + 1)), ints(np.zeros(R * new))
+    K, V = torch.zeros((2, R * new, H, d), device="cuda")
+    pools = [torch.zeros((2 * R * M, H, page, d), device="cuda") for _ in range(2)]
+
+    def call():
+        roco.roco_page_tables(held, want, page, free, table, starts, rows, slots)
+        roco.roco_page_store(K, V, slots, *pools)
+
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        call()
+    for i in range(5):
+        h = rng.integers(0, 60, R)
+        held.copy_(ints(h))
+        want.copy_(ints(h + new))
+        K.normal_()
+        V.normal_()
+        before, kept = table.cpu().numpy(), [x.clone() for x in pools]
+        graph.replay() if i % 2 == 0 else call()
+        torch.cuda.synchronize()
+        for g, x in zip((table, starts, rows, slots), trees.page_tables(h, h + new, page, free.cpu().numpy(), before, R * new, False)):
+            assert np.array_equal(g.cpu().numpy(), x)
+        # (the list begins anew with every call, so that two requests may go on in one page: of two rows of a slot either is right)
+        at = slots.long()
+        _, which, times = at.unique(return_inverse=True, return_counts=True)
+        once = times[which] == 1
+        assert int(once.sum()) > R * new // 2
+        for pool, x, w in zip(pools, (K, V), kept):
+            assert torch.equal(pool[at[once] // page, :, at[once] % page], x[once])
+            w[at // page, :, at % page] = pool[at // page, :, at % page]
+            assert torch.equal(pool, w)  # and nothing else is written
+
+
 @pytest.mark.parametrize("off", [1, 2, 3])
 def test_the_rest_of_a_free_list_and_a_part_of_a_map(off):
     """Lists and maps that begin at any of their words."""

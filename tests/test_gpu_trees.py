@@ -585,6 +585,48 @@ def test_captured_and_replayed_with_eager_work_between():
         assert all(torch.equal(x, y) for x, y in zip(state + [s.out, s.lse, ev], want))
 
 
+def test_two_graphs_that_share_a_workspace():
+    """Replayed in turn: a wide tree over pages in splits, and a commit of another shape; a workspace carries nothing from call to call."""
+    s = Step(17, "bf16", 128, used=[900, 333], heads=2, B=900, page=64, T=20, group=5, max_path=6).upload()
+    t = Step(18, "f32", 64, used=[500, 120], heads=3, B=500, T=7, group=2, max_path=3, chain=True).upload()
+    ws = torch.empty(max(s.ws.numel(), t.ws.numel()), dtype=torch.uint8, device="cuda").fill_(0xEE)
+    wants, graphs, side = [], [], torch.cuda.Stream()
+    starts = []
+    for x in (s, t):
+        path = np.zeros((x.R, x.max_path))
+        for r, p in enumerate(x.paths):
+            path[r, :len(p)] = p
+        x.dpath, x.dlen = dev(path), dev(np.array([len(p) for p in x.paths]))
+        x.state = [x.dK, x.dV, x.dstats, x.dpos, x.dn_used]
+        starts.append([y.clone() for y in x.state])
+
+        def step(x=x):
+            roco.roco_tree_attend(x.p, x.heads, x.group, x.T, x.pages, x.dq, x.dk, x.dv, x.dparent, x.dn_nodes, x.dqpos0, x.dK, x.dV, x.dpos, x.dn_used,
+                                  x.out, x.lse, ws)
+            roco.roco_tree_commit(x.p, x.heads, x.group, x.T, x.pages, x.dq, x.dk, x.dv, x.lse, x.max_path, x.dpath, x.dlen, x.dqpos0, x.dK, x.dV,
+                                  x.dstats, x.dpos, x.dn_used, None, None, ws)
+
+        step()
+        torch.cuda.synchronize()
+        wants.append([y.nan_to_num(7) for y in x.state + [x.out, x.lse]])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+            step()
+        graphs.append(graph)
+    for _ in range(3):
+        for x, start in zip((s, t), starts):
+            for y, z in zip(x.state, start):
+                y.copy_(z)
+            x.out.fill_(77)
+            x.lse.fill_(77)
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for x, want in zip((s, t), wants):
+            assert all(torch.equal(y.nan_to_num(7), z) for y, z in zip(x.state + [x.out, x.lse], want))
+
+
 def test_two_streams_with_workspaces_of_their_own():
     a = Step(15, "bf16", 128, used=[600], heads=4, B=600, T=16, group=4).upload()
     b = Step(16, "f32", 64, used=[500], heads=4, B=500, T=8, group=2).upload()
