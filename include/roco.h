@@ -379,8 +379,9 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
  *                    row_start[r] + i is the i-th new slot of request r; padded (1): map [requests, rows], entry r, i.  Entries without a
  *                    slot are -1.
  * Where the list is too short (page_start[requests] > n_free), the pages that it lacks are -1, in the table and in the map.
- * held may be NULL (new requests); held is held inside [0, max_pages * page], want inside [held, max_pages * page].  The sums have
- * 32 bits.  No workspace.
+ * held may be NULL (new requests); held is held inside [0, max_pages * page], want inside [held, max_pages * page].  A sum above
+ * 2^31 - 1 is given as 2^31 - 1: it lies behind every list and map.  Pages whose slots would be above 2^31 - 1 have no entries in the map.
+ * No workspace.
  * page: a power of two, 16 .. 1024; n_free >= 0 (free_pages may be NULL with 0); 1 <= requests <= 65535; rows >= 1.
  */
 int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const int32_t* held, const int32_t* want,

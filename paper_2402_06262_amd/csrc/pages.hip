@@ -1,5 +1,6 @@
 // Pages of caches of different budgets: block tables and slot maps from the requests' lengths, and rows stored by slot map.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "profile.hpp"
@@ -11,6 +12,41 @@ constexpr int kSumThreads = 1024;
 constexpr int kFillThreads = 256;
 constexpr int kFillEntries = 4;      // of the map, side by side, per thread and step
 constexpr int kSelfSummed = 2048;    // most requests whose sums every workgroup of the fill forms itself
+
+// Pages and slots.  Their sums stay at 2^31 - 1 where they would pass it: a prefix is then behind every entry of a list or map.
+struct Sums { uint32_t pages, rows; };
+__device__ __forceinline__ Sums add_up(const Sums& x, const Sums& y) {
+  return {min(x.pages + y.pages, 0x7fffffffu), min(x.rows + y.rows, 0x7fffffffu)};
+}
+
+// Exclusive prefix of such sums over the workgroup's threads, in their order, and their total.  sh: an entry per wave.
+template <int NT> __device__ __forceinline__ Sums prefix_of(Sums v, Sums* sh, Sums& total) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const auto other = [](uint32_t x, auto ctrl, auto row_mask) {
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, decltype(row_mask)::value, 0xF, false));
+  };
+  const auto step = [&](auto ctrl, auto row_mask) { v = add_up(v, {other(v.pages, ctrl, row_mask), other(v.rows, ctrl, row_mask)}); };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});
+  step(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+  step(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+  step(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
+  Sums before = {__shfl_up(v.pages, 1, kWave), __shfl_up(v.rows, 1, kWave)};
+  if (lane == 0) before = {0u, 0u};
+  __syncthreads();  // nobody reads `sh` of a sum before
+  if (lane == kWave - 1) sh[wave] = v;
+  __syncthreads();
+  Sums off = {0u, 0u};
+  total = off;
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) {
+    if (w == wave) off = total;
+    total = add_up(total, sh[w]);
+  }
+  return add_up(off, before);
+}
 
 struct Need { int first, last, held, want; };  // pages [first, last) are to be taken, slots [held, want) are new
 __device__ __forceinline__ Need need_of(const PageTableArgs& a, int r) {
@@ -26,26 +62,24 @@ __device__ __forceinline__ Need need_of(const PageTableArgs& a, int r) {
 
 // One workgroup: the prefix sums of pages and of new slots over the requests.
 __global__ __launch_bounds__(kSumThreads) void page_sums(PageTableArgs a) {
-  __shared__ uint32_t sh[kSumThreads / kWave + 1];
-  uint32_t pages = 0, rows = 0;
+  __shared__ Sums sh[kSumThreads / kWave];
+  Sums sum = {0u, 0u};
 #pragma unroll 1
   for (int r0 = 0; r0 < a.requests; r0 += kSumThreads) {
     const int r = r0 + threadIdx.x;
     Need x = {0, 0, 0, 0};
     if (r < a.requests) x = need_of(a, r);
-    uint32_t more_pages, more_rows;
-    const uint32_t p = pages + block_exclusive_scan<kSumThreads>(static_cast<uint32_t>(x.last - x.first), sh, more_pages);
-    const uint32_t s = rows + block_exclusive_scan<kSumThreads>(static_cast<uint32_t>(x.want - x.held), sh, more_rows);
+    Sums more;
+    const Sums before = add_up(sum, prefix_of<kSumThreads>({static_cast<uint32_t>(x.last - x.first), static_cast<uint32_t>(x.want - x.held)}, sh, more));
     if (r < a.requests) {
-      a.page_start[r] = static_cast<int32_t>(p);
-      a.row_start[r] = static_cast<int32_t>(s);
+      a.page_start[r] = static_cast<int32_t>(before.pages);
+      a.row_start[r] = static_cast<int32_t>(before.rows);
     }
-    pages += more_pages;
-    rows += more_rows;
+    sum = add_up(sum, more);
   }
   if (threadIdx.x == 0) {
-    a.page_start[a.requests] = static_cast<int32_t>(pages);
-    a.row_start[a.requests] = static_cast<int32_t>(rows);
+    a.page_start[a.requests] = static_cast<int32_t>(sum.pages);
+    a.row_start[a.requests] = static_cast<int32_t>(sum.rows);
   }
 }
 
@@ -53,40 +87,37 @@ __global__ __launch_bounds__(kSumThreads) void page_sums(PageTableArgs a) {
 // LDS, from lengths that the L2 has, instead of waiting for a launch that does: a step of 64 requests 7.7 -> 5.4 us.  A page number is asked
 // for once for entries of the same page; a division and a search per entry took 19.6 us for 1024 requests of up to 8192 slots.
 template <bool SELF> __global__ __launch_bounds__(kFillThreads) void page_fill(PageTableArgs a) {
-  __shared__ uint32_t sh[kFillThreads / kWave + 1];
-  extern __shared__ int32_t sums_s[];  // SELF: pages before a request, new slots before it, slots that it holds
-  int32_t *const page_s = sums_s, *const row_s = page_s + a.requests + 1, *const held_s = row_s + a.requests + 1;
+  __shared__ Sums sh[kFillThreads / kWave];
+  extern __shared__ int32_t sums_s[];  // SELF: pages before a request, new slots before it, slots that it holds and is to have
+  int32_t *const page_s = sums_s, *const row_s = page_s + a.requests + 1, *const held_s = row_s + a.requests + 1, *const want_s = held_s + a.requests;
   const int tid = threadIdx.x;
   if (SELF) {
     constexpr int kEach = kSelfSummed / kFillThreads;
     const int each = (a.requests + kFillThreads - 1) / kFillThreads, r0 = tid * each;
-    uint32_t pages[kEach], rows[kEach], all_pages = 0, all_rows = 0;
+    Sums mine[kEach], all = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      pages[i] = rows[i] = 0;
+      mine[i] = {0u, 0u};
       if (i < each && r0 + i < a.requests) {
         const Need x = need_of(a, r0 + i);
-        pages[i] = static_cast<uint32_t>(x.last - x.first);
-        rows[i] = static_cast<uint32_t>(x.want - x.held);
+        mine[i] = {static_cast<uint32_t>(x.last - x.first), static_cast<uint32_t>(x.want - x.held)};
         held_s[r0 + i] = x.held;
+        want_s[r0 + i] = x.want;
       }
-      all_pages += pages[i];
-      all_rows += rows[i];
+      all = add_up(all, mine[i]);
     }
-    uint32_t page_total, row_total;
-    uint32_t p = block_exclusive_scan<kFillThreads>(all_pages, sh, page_total), s = block_exclusive_scan<kFillThreads>(all_rows, sh, row_total);
+    Sums total, before = prefix_of<kFillThreads>(all, sh, total);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       if (i < each && r0 + i < a.requests) {
-        page_s[r0 + i] = static_cast<int32_t>(p);
-        row_s[r0 + i] = static_cast<int32_t>(s);
+        page_s[r0 + i] = static_cast<int32_t>(before.pages);
+        row_s[r0 + i] = static_cast<int32_t>(before.rows);
       }
-      p += pages[i];
-      s += rows[i];
+      before = add_up(before, mine[i]);
     }
     if (tid == 0) {
-      page_s[a.requests] = static_cast<int32_t>(page_total);
-      row_s[a.requests] = static_cast<int32_t>(row_total);
+      page_s[a.requests] = static_cast<int32_t>(total.pages);
+      row_s[a.requests] = static_cast<int32_t>(total.rows);
     }
     __syncthreads();
     if (blockIdx.x == 0) {
@@ -102,16 +133,16 @@ template <bool SELF> __global__ __launch_bounds__(kFillThreads) void page_fill(P
     if (!SELF) return need_of(a, r);
     Need x;
     x.held = held_s[r];
-    x.want = x.held + row_s[r + 1] - row_s[r];
+    x.want = want_s[r];
     x.first = (x.held + (1 << a.page_log2) - 1) >> a.page_log2;
-    x.last = x.first + page_s[r + 1] - page_s[r];
+    x.last = (x.want + (1 << a.page_log2) - 1) >> a.page_log2;
     return x;
   };
   // Page number i of request r: one of those it takes now, or one that its table holds.
   auto page_of = [&](int r, const Need& x, int i) {
     if (i < x.first) return a.table[static_cast<size_t>(r) * a.max_pages + i];
-    const int at = page_start[r] + i - x.first;
-    return at < a.n_free ? a.free_pages[at] : -1;
+    const uint32_t at = static_cast<uint32_t>(page_start[r]) + static_cast<uint32_t>(i - x.first);
+    return at < static_cast<uint32_t>(a.n_free) ? a.free_pages[at] : -1;
   };
   const int waves = kFillThreads / kWave * gridDim.x;
   for (int r = blockIdx.x * (kFillThreads / kWave) + tid / kWave; r < a.requests; r += waves) {
@@ -120,16 +151,17 @@ template <bool SELF> __global__ __launch_bounds__(kFillThreads) void page_fill(P
   }
   const long long total = a.padded ? static_cast<long long>(a.requests) * a.rows : a.rows;
   const long long step = static_cast<long long>(gridDim.x) * kFillThreads * kFillEntries;
-  const int low = (1 << a.page_log2) - 1;
+  const uint32_t low = (1u << a.page_log2) - 1, most_page = 0x7fffffffu >> a.page_log2, rows = static_cast<uint32_t>(a.rows);
   for (long long i0 = (static_cast<long long>(blockIdx.x) * kFillThreads + tid) * kFillEntries; i0 < total; i0 += step) {
-    int r, k;  // request and new slot of the entry
+    int r;       // request and new slot of the entry.  (New slots are compared with how many there are, not slots with lengths: a map
+    uint32_t k;  // may go on far behind a request's last slot, and held + k pass 2^31)
     if (a.padded) {
       if (total <= 0x7fffffff) {
-        r = static_cast<int>(static_cast<uint32_t>(i0) / static_cast<uint32_t>(a.rows));
-        k = static_cast<int>(static_cast<uint32_t>(i0) - static_cast<uint32_t>(r) * static_cast<uint32_t>(a.rows));
+        r = static_cast<int>(static_cast<uint32_t>(i0) / rows);
+        k = static_cast<uint32_t>(i0) - static_cast<uint32_t>(r) * rows;
       } else {
         r = static_cast<int>(i0 / a.rows);
-        k = static_cast<int>(i0 % a.rows);
+        k = static_cast<uint32_t>(i0 % a.rows);
       }
     } else {
       int lo = 0, hi = a.requests;  // the last request that starts at i0 or before it
@@ -139,36 +171,39 @@ template <bool SELF> __global__ __launch_bounds__(kFillThreads) void page_fill(P
         else hi = mid;
       }
       r = lo;
-      k = static_cast<int>(i0 - row_start[r]);
+      k = static_cast<uint32_t>(i0) - static_cast<uint32_t>(row_start[r]);
     }
     Need x = lengths_of(r);
+    uint32_t fresh = static_cast<uint32_t>(x.want - x.held);
     int at = -1, page = -1;  // page `at` of the request
     int4 entries;
     int* const e = &entries.x;
-    const int last = x.held + k + kFillEntries - 1;  // slot of the last entry, if they are all of this request
-    if (a.padded && k + kFillEntries <= a.rows && x.held + k >= x.want) {
+    const uint32_t last = static_cast<uint32_t>(x.held) + k + kFillEntries - 1;  // slot of the last entry, if they are all of this request
+    if (a.padded && k + kFillEntries <= rows && k >= fresh) {
       entries = make_int4(-1, -1, -1, -1);
-    } else if (k + kFillEntries <= (a.padded ? a.rows : x.want - x.held) && last < x.want && (last & low) >= kFillEntries - 1) {  // of one page
-      page = page_of(r, x, last >> a.page_log2);
-      const int entry = (page << a.page_log2) + (last & low) - (kFillEntries - 1);
-      entries = page < 0 ? make_int4(-1, -1, -1, -1) : make_int4(entry, entry + 1, entry + 2, entry + 3);
+    } else if (k + kFillEntries <= fresh && (!a.padded || k + kFillEntries <= rows) && (last & low) >= kFillEntries - 1) {  // of one page
+      page = page_of(r, x, static_cast<int>(last >> a.page_log2));
+      const int entry = static_cast<int>((static_cast<uint32_t>(page) << a.page_log2) + (last & low) - (kFillEntries - 1));
+      entries = static_cast<uint32_t>(page) > most_page ? make_int4(-1, -1, -1, -1) : make_int4(entry, entry + 1, entry + 2, entry + 3);
     } else {
 #pragma unroll
       for (int j = 0; j < kFillEntries; ++j) {
         // the next request: behind the end of its row of a padded map, or of its new slots in a packed one
-        while (r + 1 < a.requests && k >= (a.padded ? a.rows : x.want - x.held)) {
-          k = a.padded ? 0 : k - (x.want - x.held);
+        while (r + 1 < a.requests && k >= (a.padded ? rows : fresh)) {
+          k = a.padded ? 0 : k - fresh;
           x = lengths_of(++r);
+          fresh = static_cast<uint32_t>(x.want - x.held);
           at = -1;
         }
-        const int slot = x.held + k;
         e[j] = -1;
-        if (slot < x.want && k >= 0) {
+        if (k < fresh) {
+          const int slot = x.held + static_cast<int>(k);
           if (slot >> a.page_log2 != at) {
             at = slot >> a.page_log2;
             page = page_of(r, x, at);
           }
-          if (page >= 0) e[j] = (page << a.page_log2) + (slot & low);
+          // (a page so far on that its slots are no 31-bit numbers is none)
+          if (static_cast<uint32_t>(page) <= most_page) e[j] = (page << a.page_log2) + (slot & static_cast<int>(low));
         }
         ++k;
       }
@@ -221,7 +256,7 @@ hipError_t launch_page_tables(const PageTableArgs& a, hipStream_t s) {
   const long long want = std::max<long long>((total + kFillThreads * kFillEntries - 1) / (kFillThreads * kFillEntries), (a.requests + 3) / 4);
   const dim3 grid(static_cast<unsigned>(std::min<long long>(want, 1536)));
   if (a.requests <= kSelfSummed) {
-    hipLaunchKernelGGL((page_fill<true>), grid, dim3(kFillThreads), (3 * a.requests + 2) * sizeof(int32_t), s, a);
+    hipLaunchKernelGGL((page_fill<true>), grid, dim3(kFillThreads), (4 * a.requests + 2) * sizeof(int32_t), s, a);
   } else {
     hipLaunchKernelGGL(page_sums, dim3(1), dim3(kSumThreads), 0, s, a);
     hipLaunchKernelGGL((page_fill<false>), grid, dim3(kFillThreads), 0, s, a);

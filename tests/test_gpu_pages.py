@@ -290,3 +290,80 @@ def test_a_speculative_loop_on_paged_caches_of_prompts_of_different_lengths(dtyp
             assert np.array_equal(rows_of(cache.K, u, m), st.K[:m]) and np.array_equal(rows_of(cache.V, u, m), st.V[:m])
             assert np.array_equal(cache.pos[u].cpu().numpy(), st.pos)
         at = [n + len(x) for n, x in zip(at, paths)]
+
+
+def _call_tables(held, want, page, free, table, rows, padded):
+    """On tables and maps too long for the oracle: device tensors."""
+    R = len(want)
+    starts = [torch.full((R + 1,), -9, dtype=torch.int32, device="cuda") for _ in range(2)]
+    slots = torch.full((R, rows) if padded else (rows,), -9, dtype=torch.int32, device="cuda")
+    roco.roco_page_tables(None if held is None else ints(held), ints(want), page, ints(free), table, *starts, slots)
+    torch.cuda.synchronize()
+    return (*[x.tolist() for x in starts], slots)
+
+
+@pytest.mark.parametrize("padded", [False, True])
+def test_slots_up_to_31_bits_and_maps_that_go_on_behind_them(padded):
+    page, M = 64, (1 << 25) - 1
+    most = page * M  # the longest request that a call takes: 2^31 - 64 slots
+    table = torch.full((1, M), -1, dtype=torch.int32, device="cuda")
+    table[0, -1] = 7
+    # nothing new behind the last slot
+    pages, rows, slots = _call_tables([most], [most], page, [], table, 100, padded)
+    assert pages == [0, 0] and rows == [0, 0] and (slots == -1).all()
+    # the last 30 slots, then nothing
+    pages, rows, slots = _call_tables([most - 30], [most + 63], page, [], table, 101, padded)
+    assert pages == [0, 0] and rows == [0, 30]
+    assert slots.view(-1).tolist() == [7 * page + 34 + i for i in range(30)] + [-1] * 71
+    assert int(table[0, -1]) == 7 and (table[0, :-1] == -1).all()
+
+
+@pytest.mark.parametrize("padded", [False, True])
+def test_a_map_of_nearly_31_bits(padded):
+    rows = (1 << 31) - 9
+    table = torch.full((1, 4), 5, dtype=torch.int32, device="cuda")
+    pages, starts, slots = _call_tables([20], [40], 16, [9, 11], table, rows, padded)
+    assert pages == [0, 1] and starts == [0, 20] and table.tolist() == [[5, 5, 9, 5]]
+    slots = slots.view(-1)
+    assert slots[:21].tolist() == [5 * 16 + i for i in range(4, 16)] + [9 * 16 + i for i in range(8)] + [-1]
+    for i in range(20, rows, 1 << 28):
+        assert (slots[i:i + (1 << 28)] == -1).all()
+
+
+@pytest.mark.parametrize("R", [3, 2050])
+@pytest.mark.parametrize("padded", [False, True])
+def test_sums_of_lengths_above_31_bits(R, padded):
+    """The requests' own entries stay right; a sum stays at 2^31 - 1."""
+    top = (1 << 31) - 1
+    if R == 3:
+        page, M = 64, (1 << 25) - 1
+    else:
+        page, M = 1024, 2048  # 2^21 slots each
+    most = page * M
+    table = torch.full((R, M), -5, dtype=torch.int32, device="cuda")
+    free = torch.arange(3 * M // 2, dtype=torch.int32, device="cuda").flip(0)
+    starts = [torch.full((R + 1,), -9, dtype=torch.int32, device="cuda") for _ in range(2)]
+    rows = 70
+    slots = torch.full((R, rows) if padded else (rows,), -9, dtype=torch.int32, device="cuda")
+    roco.roco_page_tables(None, ints([most] * R), page, free, table, *starts, slots)
+    torch.cuda.synchronize()
+    assert starts[0].tolist() == [min(r * M, top) for r in range(R + 1)]
+    assert starts[1].tolist() == [min(r * most, top) for r in range(R + 1)]
+    assert torch.equal(table.view(-1)[:len(free)], free) and (table.view(-1)[len(free):] == -1).all()
+    i = torch.arange(rows, device="cuda", dtype=torch.int32)
+    first = (table[:, :2].long()[:, (i // page).long()] * page + i % page)
+    first = torch.where((table[:, :1] >= 0) & (first < 1 << 31), first, -1).int()
+    assert torch.equal(slots, first if padded else first[0])
+
+
+@pytest.mark.parametrize("held", [[0], [3], [16]])
+def test_pages_whose_slots_are_above_31_bits_are_none(held):
+    """A table's entry, or one of the list, so far on that 32 bits would name the slots of another page."""
+    table = ints([[1 << 28, 4, 1 << 27]])
+    pages, rows, slots = _call_tables(held, [47], 16, [1 << 28, (1 << 27) - 1, 1 << 27], table, 47, False)
+    free = iter([1 << 28, (1 << 27) - 1, 1 << 27])
+    want = [[1 << 28, 4, 1 << 27][i] if i < -(-held[0] // 16) else next(free) for i in range(3)]
+    assert table.tolist() == [want]
+    entry = lambda j: want[j // 16] * 16 + j % 16  # noqa: E731
+    expected = [entry(j) if entry(j) < 1 << 31 else -1 for j in range(held[0], 47)]
+    assert slots.tolist() == expected + [-1] * held[0]
