@@ -74,7 +74,7 @@ class RocoPages(ctypes.Structure):
     def __init__(self, table, n_pages, page, budget=None, max_pages=None):
         if max_pages is None:
             max_pages = table.shape[-1]
-        super().__init__(_ptr(table), _ptr(budget), int(max_pages), int(page), int(n_pages))
+        super().__init__(_words(table, "int32"), _words(budget, "int32"), int(max_pages), int(page), int(n_pages))
         self._held = (table, budget)
 
 
@@ -163,17 +163,29 @@ class _PlainCalls:
                 "decode_step_static": (), "encode_block": (0,), "encode_block_gqa": (0, 1), "decode_step_gqa": (0,),
                 "tree_attend": (0, 1, 2), "tree_commit": (0, 1, 2, 8)}
     PAGES = {"tree_attend": 3, "tree_commit": 3}  # ... or a RocoPages
+    # ... or, of tensors, those whose type is checked
+    INT32 = {"tree_attend": (7, 8, 9, 12, 13), "tree_commit": (9, 10, 11, 15, 16, 17, 18), "page_tables": (3, 4, 5, 7, 8, 9, 10), "page_store": (10,)}
+    FLOAT32 = {"tree_attend": (15,), "tree_commit": (7, 14)}
     # the functions without parameters
     PLAIN = {"page_tables": (0, 1, 2, 6, 11, 12), "page_store": (0, 1, 2, 3, 4, 7, 8, 9, 13, 14)}
 
     def __init__(self, lib):
         for name, integers in self.INTEGERS.items():
-            setattr(self, name, self._function(getattr(lib, "roco_" + name), integers, name != "decode_step_static", self.PAGES.get(name)))
+            setattr(self, name, self._function(getattr(lib, "roco_" + name), self._conversions(name, integers), name != "decode_step_static",
+                                               self.PAGES.get(name)))
         for name, integers in self.PLAIN.items():
-            setattr(self, name, self._plain(getattr(lib, "roco_" + name), integers))
+            setattr(self, name, self._plain(getattr(lib, "roco_" + name), self._conversions(name, integers)))
+
+    def _conversions(self, name, integers):
+        how = dict.fromkeys(integers, int)
+        how.update(dict.fromkeys(self.INT32.get(name, ()), lambda t: _words(t, "int32")))
+        how.update(dict.fromkeys(self.FLOAT32.get(name, ()), lambda t: _words(t, "float32")))
+        if name in self.PAGES:
+            how[self.PAGES[name]] = _pages
+        return how
 
     @staticmethod
-    def _function(fn, integers, has_workspace, pages):
+    def _function(fn, how, has_workspace, pages):
         def call(params, *args):
             *args, stream = args
             size = ()
@@ -182,15 +194,14 @@ class _PlainCalls:
                 size = (int(args[-1].nbytes if workspace_bytes is None else workspace_bytes),)
             if pages is not None and args[pages] is not None and not isinstance(args[pages], RocoPages):
                 raise TypeError("roco: pages must be a RocoPages or None")
-            return fn(ctypes.byref(params), *[int(a) if i in integers else _pages(a) if i == pages else _ptr(a) for i, a in enumerate(args)],
-                      *size, _stream(stream))
+            return fn(ctypes.byref(params), *[how.get(i, _ptr)(a) for i, a in enumerate(args)], *size, _stream(stream))
         return call
 
     @staticmethod
-    def _plain(fn, integers):
+    def _plain(fn, how):
         def call(*args):
             *args, stream = args
-            return fn(*[int(a) if i in integers else _ptr(a) for i, a in enumerate(args)], _stream(stream))
+            return fn(*[how.get(i, _ptr)(a) for i, a in enumerate(args)], _stream(stream))
         return call
 
 
@@ -212,7 +223,7 @@ def _bind_native(lib) -> None:
         "roco_prefill_compress", "roco_prefill_compress_gqa", "roco_prefill_compress_lse", "roco_decode_step",
         "roco_decode_step_static", "roco_encode_block", "roco_encode_block_gqa", "roco_decode_step_gqa", "roco_tree_attend",
         "roco_tree_commit", "roco_page_tables", "roco_page_store")),
-        torch.Tensor, torch.nn.Parameter, RocoParams, RocoPages, _ptr, _stream)
+        torch.Tensor, torch.nn.Parameter, RocoParams, RocoPages, _ptr, _words, _stream)
     if _native is None and hasattr(os, "register_at_fork"):
         os.register_at_fork(after_in_child=native.forget_gpu)  # a forked child is refused by torch, as before
     _native, _marshal, _native_lib = native, native, lib
@@ -277,6 +288,13 @@ def _ptr(t) -> Optional[int]:
     if not t.is_contiguous():
         raise ValueError("roco: tensors must be contiguous")
     return t.data_ptr()
+
+
+def _words(t, kind: str) -> Optional[int]:
+    """As _ptr; a tensor has to be of that type, "int32" or "float32"."""
+    if getattr(t, "dtype", None) is not None and str(t.dtype) != "torch." + kind:
+        raise ValueError(f"roco: a tensor of {kind} is wanted, not of {t.dtype}")
+    return _ptr(t)
 
 
 def _ptrs(*ts):

@@ -9,6 +9,7 @@
 
 #include <cstdint>
 #include <cstring>
+#include <type_traits>
 
 #include "../../include/roco.h"
 
@@ -19,6 +20,7 @@ PyObject* g_tensor_types[2];  // torch.Tensor, torch.nn.Parameter: exactly these
 PyObject* g_params_type;      // binding.RocoParams
 PyObject* g_pages_type;       // binding.RocoPages
 PyObject* g_pointer;          // binding._ptr: everything else
+PyObject* g_words;            // binding._words: ... that has to be of a type
 PyObject* g_current_stream;   // binding._stream: anything but an address, and the current stream before it is known how to ask
 PyObject* g_raw_stream;       // torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice: set once the GPU is in use
 PyObject* g_device;
@@ -48,17 +50,7 @@ const at::Tensor* tensor_of(PyObject* o) {
 
 void* address_of_int(PyObject* o) { return reinterpret_cast<void*>(PyLong_AsUnsignedLongLongMask(o)); }
 
-void* pointer(PyObject* o) {
-  if (o == Py_None) return nullptr;
-  if (const at::Tensor* t = tensor_of(o)) {
-    if (!t->is_contiguous()) {
-      PyErr_SetString(PyExc_ValueError, "roco: tensors must be contiguous");
-      throw Failed{};
-    }
-    return t->data_ptr();
-  }
-  if (PyLong_Check(o)) return address_of_int(o);
-  PyObject* const r = PyObject_CallOneArg(g_pointer, o);
+void* address_from(PyObject* r) {  // what binding.py's conversion returned
   if (r == nullptr) throw Failed{};
   void* p = nullptr;
   if (r != Py_None) {
@@ -70,6 +62,37 @@ void* pointer(PyObject* o) {
   }
   Py_DECREF(r);
   return p;
+}
+
+void* address_of(const at::Tensor& t) {
+  if (!t.is_contiguous()) {
+    PyErr_SetString(PyExc_ValueError, "roco: tensors must be contiguous");
+    throw Failed{};
+  }
+  return t.data_ptr();
+}
+
+void* pointer(PyObject* o) {
+  if (o == Py_None) return nullptr;
+  if (const at::Tensor* t = tensor_of(o)) return address_of(*t);
+  if (PyLong_Check(o)) return address_of_int(o);
+  return address_from(PyObject_CallOneArg(g_pointer, o));
+}
+
+// ... of 32-bit integers, or floats: a tensor of another type would be read as what it is not.
+template <class T> T* words(PyObject* o) {
+  constexpr bool kInts = std::is_same<T, int32_t>::value;
+  if (o == Py_None) return nullptr;
+  if (const at::Tensor* t = tensor_of(o)) {
+    if (t->scalar_type() == (kInts ? at::kInt : at::kFloat)) return static_cast<T*>(address_of(*t));
+  } else if (PyLong_Check(o)) {
+    return static_cast<T*>(address_of_int(o));
+  }
+  PyObject* const kind = PyUnicode_FromString(kInts ? "int32" : "float32");
+  if (kind == nullptr) throw Failed{};
+  PyObject* const r = PyObject_CallFunctionObjArgs(g_words, o, kind, nullptr);
+  Py_DECREF(kind);
+  return static_cast<T*>(address_from(r));
 }
 
 // The low 64 bits, as ctypes takes them: sizes from 2^63 on are sizes.
@@ -272,41 +295,50 @@ PyObject* tree_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const roco_params p = params_of(a[0]);
     const int32_t heads = int32_of(a[1]), group = int32_of(a[2]), nodes = int32_of(a[3]);
     const Pages pages(a[4]);
-    void* t[13];
-    for (int i = 0; i < 13; ++i) t[i] = pointer(a[5 + i]);
+    void* q[3];
+    for (int i = 0; i < 3; ++i) q[i] = pointer(a[5 + i]);
+    const int32_t *const parent = words<int32_t>(a[8]), *const n_nodes = words<int32_t>(a[9]), *const qpos0 = words<int32_t>(a[10]);
+    void *const k = pointer(a[11]), *const v = pointer(a[12]);
+    const int32_t *const pos = words<int32_t>(a[13]), *const n_used = words<int32_t>(a[14]);
+    void* const out = pointer(a[15]);
+    float* const lse = words<float>(a[16]);
+    void* const workspace = pointer(a[17]);
     const size_t ws = bytes(a[18], a[17]);
     void* const s = stream_of(a[19]);
     NoGil g;
-    return g_fn.tree_attend(&p, heads, group, nodes, pages.p, t[0], t[1], t[2], static_cast<int32_t*>(t[3]), static_cast<int32_t*>(t[4]),
-                            static_cast<int32_t*>(t[5]), t[6], t[7], static_cast<int32_t*>(t[8]), static_cast<int32_t*>(t[9]), t[10],
-                            static_cast<float*>(t[11]), t[12], ws, s);
+    return g_fn.tree_attend(&p, heads, group, nodes, pages.p, q[0], q[1], q[2], parent, n_nodes, qpos0, k, v, pos, n_used, out, lse, workspace, ws, s);
   });
 }
+// (params, heads, group, nodes, pages, 4 pointers, max_path, 11 pointers, workspace_bytes, stream)
 PyObject* tree_commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 23, [&] {
     const roco_params p = params_of(a[0]);
     const int32_t heads = int32_of(a[1]), group = int32_of(a[2]), nodes = int32_of(a[3]);
     const Pages pages(a[4]);
-    void *in[4], *t[11];
-    for (int i = 0; i < 4; ++i) in[i] = pointer(a[5 + i]);
+    void* q[3];
+    for (int i = 0; i < 3; ++i) q[i] = pointer(a[5 + i]);
+    const float* const lse = words<float>(a[8]);
     const int32_t max_path = int32_of(a[9]);
-    for (int i = 0; i < 11; ++i) t[i] = pointer(a[10 + i]);
+    const int32_t *const path = words<int32_t>(a[10]), *const n_path = words<int32_t>(a[11]), *const qpos0 = words<int32_t>(a[12]);
+    void *const k = pointer(a[13]), *const v = pointer(a[14]);
+    float* const stats = words<float>(a[15]);
+    int32_t* state[4];  // pos, n_used, evicted_slot, evicted_pos
+    for (int i = 0; i < 4; ++i) state[i] = words<int32_t>(a[16 + i]);
+    void* const workspace = pointer(a[20]);
     const size_t ws = bytes(a[21], a[20]);
     void* const s = stream_of(a[22]);
     NoGil g;
-    return g_fn.tree_commit(&p, heads, group, nodes, pages.p, in[0], in[1], in[2], static_cast<float*>(in[3]), max_path,
-                            static_cast<int32_t*>(t[0]), static_cast<int32_t*>(t[1]), static_cast<int32_t*>(t[2]), t[3], t[4],
-                            static_cast<float*>(t[5]), static_cast<int32_t*>(t[6]), static_cast<int32_t*>(t[7]),
-                            static_cast<int32_t*>(t[8]), static_cast<int32_t*>(t[9]), t[10], ws, s);
+    return g_fn.tree_commit(&p, heads, group, nodes, pages.p, q[0], q[1], q[2], lse, max_path, path, n_path, qpos0, k, v, stats, state[0], state[1],
+                            state[2], state[3], workspace, ws, s);
   });
 }
 PyObject* page_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 14, [&] {
     const int32_t requests = int32_of(a[0]), page = int32_of(a[1]), max_pages = int32_of(a[2]);
     int32_t* t[7];
-    for (int i = 0; i < 3; ++i) t[i] = static_cast<int32_t*>(pointer(a[3 + i]));
+    for (int i = 0; i < 3; ++i) t[i] = words<int32_t>(a[3 + i]);
     const int32_t n_free = int32_of(a[6]);
-    for (int i = 3; i < 7; ++i) t[i] = static_cast<int32_t*>(pointer(a[4 + i]));
+    for (int i = 3; i < 7; ++i) t[i] = words<int32_t>(a[4 + i]);
     const int32_t rows = int32_of(a[11]), padded = int32_of(a[12]);
     void* const s = stream_of(a[13]);
     NoGil g;
@@ -321,22 +353,22 @@ PyObject* page_store(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *k = pointer(a[5]), *v = pointer(a[6]);
     int64_t stride[3];
     for (int i = 0; i < 3; ++i) stride[i] = static_cast<int64_t>(integer(a[7 + i]));
-    void* const map = pointer(a[10]);
+    const int32_t* const map = words<int32_t>(a[10]);
     void *k_pool = pointer(a[11]), *v_pool = pointer(a[12]);
     const int32_t n_pages = int32_of(a[13]), page = int32_of(a[14]);
     void* const s = stream_of(a[15]);
     NoGil g;
-    return g_fn.page_store(size[0], size[1], size[2], size[3], size[4], k, v, stride[0], stride[1], stride[2], static_cast<int32_t*>(map),
-                           k_pool, v_pool, n_pages, page, s);
+    return g_fn.page_store(size[0], size[1], size[2], size[3], size[4], k, v, stride[0], stride[1], stride[2], map, k_pool, v_pool, n_pages, page, s);
   });
 }
 
-// bind(addresses, tensor, parameter, RocoParams, RocoPages, _ptr, _stream); use_gpu(getCurrentRawStream, getDevice)
+// bind(addresses, tensor, parameter, RocoParams, RocoPages, _ptr, _words, _stream); use_gpu(getCurrentRawStream, getDevice)
 PyObject* bind(PyObject*, PyObject* args) {
   unsigned long long f[12];
-  PyObject *tensor, *parameter, *params, *pages, *ptr, *stream;
-  if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKK)OOO!O!OO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9], &f[10],
-                        &f[11], &tensor, &parameter, &PyType_Type, &params, &PyType_Type, &pages, &ptr, &stream))
+  PyObject *tensor, *parameter, *params, *pages, *ptr, *typed, *stream;
+  if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKK)OOO!O!OOO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9], &f[10],
+                        &f[11], &tensor, &parameter, &PyType_Type, &params, &PyType_Type, &pages, &ptr, &typed,
+                        &stream))
     return nullptr;
   g_fn.prefill = reinterpret_cast<decltype(g_fn.prefill)>(f[0]);
   g_fn.prefill_gqa = reinterpret_cast<decltype(g_fn.prefill_gqa)>(f[1]);
@@ -350,12 +382,13 @@ PyObject* bind(PyObject*, PyObject* args) {
   g_fn.tree_commit = reinterpret_cast<decltype(g_fn.tree_commit)>(f[9]);
   g_fn.page_tables = reinterpret_cast<decltype(g_fn.page_tables)>(f[10]);
   g_fn.page_store = reinterpret_cast<decltype(g_fn.page_store)>(f[11]);
-  Py_INCREF(tensor); Py_INCREF(parameter); Py_INCREF(params); Py_INCREF(pages); Py_INCREF(ptr); Py_INCREF(stream);
+  Py_INCREF(tensor); Py_INCREF(parameter); Py_INCREF(params); Py_INCREF(pages); Py_INCREF(ptr); Py_INCREF(typed); Py_INCREF(stream);
   Py_XSETREF(g_tensor_types[0], tensor);
   Py_XSETREF(g_tensor_types[1], parameter);
   Py_XSETREF(g_params_type, params);
   Py_XSETREF(g_pages_type, pages);
   Py_XSETREF(g_pointer, ptr);
+  Py_XSETREF(g_words, typed);
   Py_XSETREF(g_current_stream, stream);
   Py_RETURN_NONE;
 }

@@ -176,3 +176,58 @@ def test_the_structure_matches_the_header():
     table = torch.zeros((6, 5), dtype=torch.int32)
     pages = roco.RocoPages(table, 9, 64)
     assert (pages.table, pages.budget, pages.max_pages, pages.page, pages.n_pages) == (table.data_ptr(), None, 5, 64, 9)
+
+
+def _types_of_words():
+    """Integers are int32, statistics and normalisers float32: a tensor of another type is refused before anything is read as what it is not."""
+    t = lambda dtype: torch.zeros((8, 8), dtype=dtype)  # noqa: E731
+
+    def refused(call, args, at, good, bads, **kw):
+        args = list(args)
+        for bad in bads:
+            args[at] = t(bad)
+            with pytest.raises(ValueError, match=str(good).split(".")[1]):
+                call(*args, **kw)
+            args[at] = torch.nn.Parameter(t(bad), requires_grad=False)
+            with pytest.raises(ValueError, match=str(good).split(".")[1]):
+                call(*args, **kw)
+        args[at] = t(good)
+        with pytest.raises(roco.RocoError):  # (the sizes are wrong)
+            call(*args, **kw)
+
+    ints, floats = (torch.int64, torch.int16, torch.float32), (torch.float64, torch.bfloat16, torch.int32)
+    attend = [P, 4, 2, 8, _pages(), *[OK] * 13]
+    for at in (8, 9, 10, 13, 14):  # parent, n_nodes, qpos0, pos, n_used
+        refused(roco.roco_tree_attend, attend, at, torch.int32, ints, workspace_bytes=0, stream=0)
+    refused(roco.roco_tree_attend, attend, 16, torch.float32, floats, workspace_bytes=0, stream=0)
+    commit = [P, 4, 2, 8, _pages(), *[OK] * 4, 4, *[OK] * 11]
+    for at in (10, 11, 12, 16, 17, 18, 19):  # path, n_path, qpos0, pos, n_used, evicted_slot, evicted_pos
+        refused(roco.roco_tree_commit, commit, at, torch.int32, ints, workspace_bytes=0, stream=0)
+    for at in (8, 15):
+        refused(roco.roco_tree_commit, commit, at, torch.float32, floats, workspace_bytes=0, stream=0)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    tables = [i32(3), i32(3), 24, i32(4), i32(3, 2), i32(4), i32(4), i32(9)]  # (24 is no page size)
+    for at in (0, 1, 3, 4, 5, 6, 7):
+        for bad in ints:
+            with pytest.raises(ValueError, match="int32"):
+                roco.roco_page_tables(*[x.to(bad) if i == at else x for i, x in enumerate(tables)], stream=0)
+    rows, pool = torch.zeros((5, 2, 128)), torch.zeros((3, 2, 24, 128))
+    for bad in ints:
+        with pytest.raises(ValueError, match="int32"):
+            roco.roco_page_store(rows, rows, i32(5).to(bad), pool, pool, stream=0)
+        with pytest.raises(ValueError, match="int32"):
+            roco.RocoPages(i32(6, 5).to(bad), 9, 64)
+        with pytest.raises(ValueError, match="int32"):
+            roco.RocoPages(i32(6, 5), 9, 64, i32(6).to(bad))
+
+
+def test_types_of_words_through_the_extension():
+    _types_of_words()
+
+
+def test_types_of_words_through_ctypes_alone(monkeypatch):
+    monkeypatch.setattr(binding, "_NATIVE_NAME", "_not_built")
+    monkeypatch.setattr(binding, "_native_lib", None)
+    monkeypatch.setattr(binding, "_marshal", None, raising=False)
+    _types_of_words()
+    assert isinstance(binding._marshal, binding._PlainCalls)
