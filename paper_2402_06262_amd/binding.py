@@ -450,8 +450,10 @@ def roco_page_tables(held, want, page: int, free_pages, table, page_start, row_s
 def roco_page_store(K_rows, V_rows, slot_map, K_pool, V_pool, stream=None) -> None:
     """See include/roco.h: rows of K and V to their pool slots.  Rows [rows, heads, d] (of new tokens, with a map [rows]) or
     [groups, heads, rows, d] (caches, with a map [groups, rows]) of any strides but the last dimension's; pools [n_pages, heads, page, d]."""
-    pool, shape, strides = K_pool.shape, K_rows.shape, K_rows.stride()
+    pool, shape, strides, of_v = K_pool.shape, K_rows.shape, K_rows.stride(), V_rows.stride()
     n_pages, heads, page, d = pool
+    if 1 in shape:  # the stride of a dimension of one element means nothing
+        strides, of_v = [tuple(0 if n == 1 else step for n, step in zip(shape, x)) for x in (strides, of_v)]
     if len(shape) == 3:
         rows, of_heads, of_d = shape
         groups, group_stride = 1, 0
@@ -461,7 +463,7 @@ def roco_page_store(K_rows, V_rows, slot_map, K_pool, V_pool, stream=None) -> No
         group_stride, head_stride, row_stride, last = strides
     if of_heads != heads or of_d != d or V_rows.shape != shape or V_pool.shape != pool or slot_map.numel() != groups * rows:
         raise ValueError("roco: rows are [rows, heads, d] or [groups, heads, rows, d], the map has an entry for each, pools are [n_pages, heads, page, d]")
-    if last != 1 or V_rows.stride() != strides:
+    if last != 1 or of_v != strides:
         raise ValueError("roco: a row's elements lie side by side, and the rows of V as those of K")
     dtype = K_pool.dtype
     if not K_rows.dtype == V_rows.dtype == dtype == V_pool.dtype:

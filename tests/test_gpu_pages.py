@@ -367,3 +367,27 @@ def test_pages_whose_slots_are_above_31_bits_are_none(held):
     entry = lambda j: want[j // 16] * 16 + j % 16  # noqa: E731
     expected = [entry(j) if entry(j) < 1 << 31 else -1 for j in range(held[0], 47)]
     assert slots.tolist() == expected + [-1] * held[0]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,heads", [(1, 3), (5, 1), (1, 1)])
+def test_strides_of_dimensions_of_one_element(dtype, rows, heads):
+    """They mean nothing: rows of K and V from tensors laid out differently, at strides that are no multiples of 16 bytes."""
+    d, page = 64, 16
+    shape = (rows, heads, d)
+    step = lambda n, real, other: real if n > 1 else other  # noqa: E731
+    at = lambda *other: torch.randn(20 * heads * d * rows, device="cuda").to(dtype).as_strided(  # noqa: E731
+        shape, (step(rows, 8 * heads * d, other[0]), step(heads, 2 * d, other[1]), 1))
+    slots = ints([3, 70, 18, 33, 50][:rows])
+    for k, v in ((at(7, 3), at(64, 12)), (at(1, 1), at(1, 1))):
+        for groups in (None, 1):
+            pools = [torch.full((5, heads, page, d), 9.0, dtype=dtype, device="cuda") for _ in range(2)]
+            if groups:  # caches of one request
+                cache = [x.as_strided((1, heads, rows, d), (5, x.stride(1), x.stride(0), 1)) for x in (k, v)]
+                roco.roco_page_store(*cache, slots.view(1, rows), *pools)
+            else:
+                roco.roco_page_store(k, v, slots, *pools)
+            for pool, x in zip(pools, (k, v)):
+                want = torch.full_like(pool, 9.0)
+                want[slots.long() // page, :, slots.long() % page] = x
+                assert torch.equal(pool, want)
