@@ -382,7 +382,8 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
  * held may be NULL (new requests); held is held inside [0, max_pages * page], want inside [held, max_pages * page].  A sum above
  * 2^31 - 1 is given as 2^31 - 1: it lies behind every list and map.  Pages whose slots would be above 2^31 - 1 have no entries in the map.
  * No workspace.
- * page: a power of two, 16 .. 1024; n_free >= 0 (free_pages may be NULL with 0); 1 <= requests <= 65535; rows >= 1.
+ * page: a power of two, 16 .. 1024; n_free >= 0 (free_pages may be NULL with 0); 1 <= requests <= 65535; rows >= 1, or 0 and slot_map
+ * NULL: no map.
  */
 int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const int32_t* held, const int32_t* want,
                      const int32_t* free_pages, int32_t n_free, int32_t* table, int32_t* page_start, int32_t* row_start,

@@ -433,23 +433,30 @@ def roco_tree_commit(params: RocoParams, heads: int, group: int, nodes: int, pag
 
 def roco_page_tables(held, want, page: int, free_pages, table, page_start, row_start, slot_map, stream=None) -> None:
     """See include/roco.h: block tables and slot maps from the requests' lengths.  `table` [requests, max_pages]; a `slot_map` of two
-    dimensions, [requests, rows], is a padded one; `held` may be None."""
+    dimensions, [requests, rows], is a padded one; `held` may be None, and so may `free_pages` (no page is free) and `slot_map` (or it has no
+    entries: a step without new slots)."""
     requests, max_pages = table.shape
     for t, n in ((held, requests), (want, requests), (page_start, requests + 1), (row_start, requests + 1)):
         if t is not None and t.numel() != n:
             raise ValueError("roco: held and want are [requests], page_start and row_start [requests + 1]")
-    padded = slot_map.dim() == 2
-    if padded and slot_map.shape[0] != requests:
-        raise ValueError("roco: a padded slot_map is [requests, rows]")
-    rc = _calls().page_tables(requests, page, max_pages, held, want, free_pages, free_pages.numel(), table, page_start, row_start, slot_map,
-                              slot_map.shape[-1], padded, stream)
+    rows, padded = 0, False
+    if slot_map is not None:
+        rows, padded = slot_map.shape[-1], slot_map.dim() == 2
+        if padded and slot_map.shape[0] != requests:
+            raise ValueError("roco: a padded slot_map is [requests, rows]")
+        if rows == 0:
+            slot_map = None
+    n_free = 0 if free_pages is None else free_pages.numel()
+    rc = _calls().page_tables(requests, page, max_pages, held, want, free_pages if n_free else None, n_free, table, page_start, row_start, slot_map,
+                              rows, padded, stream)
     if rc != 0:
         raise RocoError(rc, "roco_page_tables")
 
 
 def roco_page_store(K_rows, V_rows, slot_map, K_pool, V_pool, stream=None) -> None:
     """See include/roco.h: rows of K and V to their pool slots.  Rows [rows, heads, d] (of new tokens, with a map [rows]) or
-    [groups, heads, rows, d] (caches, with a map [groups, rows]) of any strides but the last dimension's; pools [n_pages, heads, page, d]."""
+    [groups, heads, rows, d] (caches, with a map [groups, rows]) of any strides but the last dimension's; pools [n_pages, heads, page, d].
+    No rows: nothing is stored."""
     pool, shape, strides, of_v = K_pool.shape, K_rows.shape, K_rows.stride(), V_rows.stride()
     n_pages, heads, page, d = pool
     if 1 in shape:  # the stride of a dimension of one element means nothing
@@ -468,6 +475,8 @@ def roco_page_store(K_rows, V_rows, slot_map, K_pool, V_pool, stream=None) -> No
     dtype = K_pool.dtype
     if not K_rows.dtype == V_rows.dtype == dtype == V_pool.dtype:
         raise ValueError("roco: rows and pools are of one type")
+    if rows == 0 or groups == 0:
+        return
     rc = _calls().page_store(_dtype_code(dtype), d, heads, groups, rows, K_rows.data_ptr(), V_rows.data_ptr(), group_stride, row_stride, head_stride,
                              slot_map, K_pool, V_pool, n_pages, page, stream)
     if rc != 0:

@@ -591,10 +591,10 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
 int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const int32_t* held, const int32_t* want,
                      const int32_t* free_pages, int32_t n_free, int32_t* table, int32_t* page_start, int32_t* row_start,
                      int32_t* slot_map, int32_t rows, int32_t padded, void* hip_stream) {
-  if (requests < 1 || max_pages < 1 || n_free < 0 || rows < 1 || !page_size_ok(page)) return ROCO_EINVAL;
+  if (requests < 1 || max_pages < 1 || n_free < 0 || rows < 0 || (rows == 0) != (slot_map == nullptr) || !page_size_ok(page)) return ROCO_EINVAL;
   if (requests > 65535 || static_cast<long long>(max_pages) * page >= (1ll << 31)) return ROCO_EUNSUPPORTED;
   if (padded && static_cast<long long>(requests) * rows >= (1ll << 40)) return ROCO_EUNSUPPORTED;
-  if (!given(want) || !given(table) || !given(page_start) || !given(row_start) || slot_map == nullptr || !aligned16(slot_map)) return ROCO_EINVAL;
+  if (!given(want) || !given(table) || !given(page_start) || !given(row_start) || !aligned16(slot_map)) return ROCO_EINVAL;
   if (!aligned4(held) || !aligned4(free_pages) || (free_pages == nullptr && n_free > 0)) return ROCO_EINVAL;
   const PageTableArgs a = {requests, __builtin_ctz(static_cast<unsigned>(page)), max_pages, n_free, rows, padded != 0, held, want,
                            free_pages, table, page_start, row_start, slot_map};

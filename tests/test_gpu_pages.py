@@ -391,3 +391,38 @@ def test_strides_of_dimensions_of_one_element(dtype, rows, heads):
                 want = torch.full_like(pool, 9.0)
                 want[slots.long() // page, :, slots.long() % page] = x
                 assert torch.equal(pool, want)
+
+
+@pytest.mark.parametrize("R", [3, 2500])
+@pytest.mark.parametrize("no_map", [None, "packed", "padded"])
+def test_tables_without_a_map(R, no_map):
+    """A step without new slots, or one whose map nobody wants: the table and the sums are made all the same."""
+    rng = np.random.default_rng(R)
+    for held in (rng.integers(0, 60, R), np.full(R, 33)):
+        for want in (held, held + rng.integers(0, 20, R)):
+            M, page = 5, 16
+            before = rng.integers(0, 999, (R, M))
+            free = rng.permutation(3 * R)
+            expected = trees.page_tables(held, want, page, free, before, 1, False)
+            table, starts = ints(before), [ints(np.full(R + 1, -9)) for _ in range(2)]
+            slots = None if no_map is None else ints(np.zeros((R, 0) if no_map == "padded" else 0))
+            roco.roco_page_tables(ints(held), ints(want), page, ints(free), table, *starts, slots)
+            for got, w in zip((table, *starts), expected):
+                assert np.array_equal(got.cpu().numpy(), w)
+
+
+def test_no_list_of_free_pages():
+    for free in (None, ints([])):
+        table, starts, slots = ints([[4, -5], [-5, -5]]), [ints(np.zeros(3)) for _ in range(2)], ints(np.zeros(5))
+        roco.roco_page_tables(ints([14, 0]), ints([17, 1]), 16, free, table, *starts, slots)
+        assert table.tolist() == [[4, -1], [-1, -5]] and starts[0].tolist() == [0, 1, 2] and starts[1].tolist() == [0, 3, 4]
+        assert slots.tolist() == [4 * 16 + 14, 4 * 16 + 15, -1, -1, -1]
+
+
+def test_no_rows_to_store():
+    pools = [torch.full((3, 2, 16, 64), 9.0, device="cuda") for _ in range(2)]
+    for shape in ((0, 2, 64), (2, 2, 0, 64), (0, 2, 5, 64)):
+        rows = torch.zeros(shape, device="cuda")
+        roco.roco_page_store(rows, rows, ints(np.zeros(shape[0] if len(shape) == 3 else (shape[0], shape[2]))), *pools)
+    for pool in pools:
+        assert (pool == 9).all()

@@ -231,3 +231,25 @@ def test_types_of_words_through_ctypes_alone(monkeypatch):
     monkeypatch.setattr(binding, "_marshal", None, raising=False)
     _types_of_words()
     assert isinstance(binding._marshal, binding._PlainCalls)
+
+
+def test_a_map_of_no_entries():
+    lib = roco.load_library()
+    # (of 65536 requests: refused, but only behind the checks of the arguments)
+    tables = lambda rows, slot_map: lib.roco_page_tables(65536, 64, 4, OK, OK, OK, 9, OK, OK, OK, slot_map, rows, 0, None)  # noqa: E731
+    assert tables(0, None) == EUNSUPPORTED and tables(1, OK) == EUNSUPPORTED
+    assert tables(0, OK) == EINVAL and tables(1, None) == EINVAL and tables(-1, None) == EINVAL
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    for slot_map in (None, i32(0), i32(3, 0)):
+        with pytest.raises(roco.RocoError) as e:
+            roco.roco_page_tables(i32(3), i32(3), 24, None, i32(3, 2), i32(4), i32(4), slot_map, stream=0)
+        assert e.value.code == EINVAL  # 24 is no page size
+    with pytest.raises(ValueError, match="padded"):
+        roco.roco_page_tables(i32(3), i32(3), 16, None, i32(3, 2), i32(4), i32(4), i32(2, 0), stream=0)
+    pool, none = torch.zeros((3, 2, 16, 128)), torch.zeros((0, 2, 128))
+    roco.roco_page_store(none, none, i32(0), pool, pool, stream=0)
+    for bad in (torch.zeros((0, 3, 128)), torch.zeros((0, 2, 64)), none.bfloat16()):
+        with pytest.raises(ValueError):
+            roco.roco_page_store(bad, bad, i32(0), pool, pool, stream=0)
+    with pytest.raises(ValueError):
+        roco.roco_page_store(none, none, i32(1), pool, pool, stream=0)
