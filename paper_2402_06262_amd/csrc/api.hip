@@ -616,8 +616,8 @@ int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t grou
   for (const void* ptr : need)
     if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
   if (!given(slot_map)) return ROCO_EINVAL;
-  // (a lane per 16 bytes, counted by the grid: at most 2^31 workgroups of 256)
-  if (static_cast<double>(groups) * heads * rows * head_dim * element / 16 / 256 >= 2147483647.0) return ROCO_EUNSUPPORTED;
+  // (a lane per 16 bytes)
+  if (static_cast<double>(groups) * heads * rows * head_dim * element / 16 / 256 > kStoreSide * 65535.0) return ROCO_EUNSUPPORTED;
   const PageStoreArgs a = {heads, groups, rows, n_pages, __builtin_ctz(static_cast<unsigned>(page)), static_cast<int>(head_dim * element),
                            K_rows, V_rows, group_stride * element, row_stride * element, head_stride * element, slot_map, K_pool, V_pool};
   return launch_page_store(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;

@@ -243,6 +243,7 @@ struct PageStoreArgs {
   const int32_t* map;
   void *K, *V;
 };
+constexpr int kStoreSide = 1 << 20;  // workgroups of 256 along x, and up to 65535 times as many: a launch counts a dimension's threads in 32 bits
 hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s);
 
 // dtype: 0 = f32, 1 = bf16; head_dim: 64 or 128.  Each returns hipGetLastError() of its launches.

@@ -222,7 +222,7 @@ template <bool SELF> __global__ __launch_bounds__(kFillThreads) void page_fill(P
 // last-level cache takes, with the non-temporal hint both ways (16 caches x 32 heads x 2048 rows of 256 bytes, twice: 151 -> 143 us, 5.6 TB/s).
 template <bool STREAMING> __global__ __launch_bounds__(256) void page_store(PageStoreArgs a, int lanes_log2) {
   const int lanes = 1 << lanes_log2;
-  const long long id = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+  const long long id = (static_cast<long long>(blockIdx.y) * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
   const long long row = id >> lanes_log2;  // (group, head, row), rows side by side
   const int col = static_cast<int>(id & (lanes - 1)) * 16;
   const long long i = row % a.rows, gh = row / a.rows;
@@ -268,7 +268,8 @@ hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s) {
   ProfScope ps(kProfPageStore, s);
   const int lanes_log2 = __builtin_ctz(a.row_bytes) - 4;
   const long long lanes = (static_cast<long long>(a.groups) * a.heads * a.rows) << lanes_log2;
-  const dim3 grid(static_cast<unsigned>((lanes + 255) / 256));
+  const long long groups = (lanes + 255) / 256, side = std::min<long long>(groups, kStoreSide);
+  const dim3 grid(static_cast<unsigned>(side), static_cast<unsigned>((groups + side - 1) / side));
   if (lanes * 32 > (192ll << 20)) hipLaunchKernelGGL((page_store<true>), grid, dim3(256), 0, s, a, lanes_log2);
   else hipLaunchKernelGGL((page_store<false>), grid, dim3(256), 0, s, a, lanes_log2);
   return hipGetLastError();

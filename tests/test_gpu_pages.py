@@ -426,3 +426,20 @@ def test_no_rows_to_store():
         roco.roco_page_store(rows, rows, ints(np.zeros(shape[0] if len(shape) == 3 else (shape[0], shape[2]))), *pools)
     for pool in pools:
         assert (pool == 9).all()
+
+
+def test_more_threads_than_a_launch_counts_in_one_dimension():
+    """2^32 lanes of 16 bytes and some more: rows that lie on top of each other, of which a few are stored."""
+    heads, d, page, rows = 32, 128, 16, (1 << 22) + 77
+    k, v = torch.randn((2, 1, heads, d), device="cuda")
+    slots = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    at = [0, 1, (1 << 21) + 3, (1 << 22) - 1, 1 << 22, rows - 1]
+    slots[torch.tensor(at, device="cuda")] = ints([40, 3, 18, 70, 50, 77])
+    pools = [torch.full((5, heads, page, d), 9.0, device="cuda") for _ in range(2)]
+    roco.roco_page_store(k.expand(rows, heads, d), v.expand(rows, heads, d), slots, *pools)
+    torch.cuda.synchronize()
+    for pool, x in zip(pools, (k, v)):
+        want = torch.full_like(pool, 9.0)
+        for slot in (40, 3, 18, 70, 50, 77):
+            want[slot // page, :, slot % page] = x[0]
+        assert torch.equal(pool, want)

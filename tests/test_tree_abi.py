@@ -253,3 +253,9 @@ def test_a_map_of_no_entries():
             roco.roco_page_store(bad, bad, i32(0), pool, pool, stream=0)
     with pytest.raises(ValueError):
         roco.roco_page_store(none, none, i32(1), pool, pool, stream=0)
+
+
+def test_a_store_of_more_than_a_launch_takes():
+    store = lambda groups, rows, heads=8: roco.load_library().roco_page_store(  # noqa: E731
+        roco.ROCO_F32, 128, heads, groups, rows, OK, OK, 0, 0, 0, OK, OK, OK, 4, 16, None)
+    assert store((1 << 31) - 1, (1 << 31) - 1) == EUNSUPPORTED and store(1 << 20, 1 << 24) == EUNSUPPORTED  # (2^49 lanes, then 2^52)
