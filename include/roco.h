@@ -499,7 +499,8 @@ int roco_probe_mfma(int32_t workgroups, int32_t iters, int32_t operands, float* 
  *   ROCO_DECODE_SPLITS=n       splits of the budget in the split pair (default: until about 128 workgroups exist)
  *   ROCO_DECODE_UNROLL=2|4|8   cache rows in flight per lane group (default 8)
  *   ROCO_DECODE_ROTATE=0|1     staggered start row per workgroup (default 1)
- *   ROCO_STREAMING_LOADS=0|1   non-temporal loads of the cache rows (default: caches above 192 MiB)
+ *   ROCO_STREAMING_LOADS=0|1   non-temporal loads of the cache rows (default: caches above 192 MiB); of roco_page_store, loads and stores
+ *                              (default: rows of K and V above 192 MiB)
  *   ROCO_PREFILL_SIMPLE=1      vector-ALU prefill passes for every dtype and head_dim
  *   ROCO_PREFILL_PAIRED=0|1    bf16 / head_dim 128: one block of rows per workgroup / a long and a short one (default 1)
  *   ROCO_PREFILL_QSPLIT=1..16  bf16 / head_dim 128: workgroups per block of rows in the two prefill passes (default: more with

@@ -173,11 +173,13 @@ void choose_splits(const roco_params* p, int unroll, int& splits, int& rows_per_
 // about 160 MiB is partly found again in the chip's last-level cache by the next step when loaded normally (31 vs 34
 // us at 128 units); from 256 MiB on it only thrashes that cache and displaces the statistics (75 vs 69 us at 320
 // units, 106 vs 92 us at 512).
-bool streaming_loads(const roco_params* p) {
+bool streaming_above(double bytes) {
   const int want = env_int("ROCO_STREAMING_LOADS", -1);
-  if (want >= 0) return want != 0;
+  return want >= 0 ? want != 0 : bytes > kStreamingAboveMiB * 1048576.0;
+}
+bool streaming_loads(const roco_params* p) {
   const size_t row = static_cast<size_t>(p->head_dim) * (p->dtype == ROCO_BF16 ? 2 : 4);
-  return static_cast<size_t>(p->units) * p->budget * row * 2 > (static_cast<size_t>(kStreamingAboveMiB) << 20);
+  return streaming_above(static_cast<double>(static_cast<size_t>(p->units) * p->budget * row * 2));
 }
 
 // One workgroup per unit once the units cover half of the compute units (measured, bf16, d = 128: 31 vs 34 us per
@@ -616,9 +618,10 @@ int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t grou
   for (const void* ptr : need)
     if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
   if (!given(slot_map)) return ROCO_EINVAL;
-  // (a lane per 16 bytes)
-  if (static_cast<double>(groups) * heads * rows * head_dim * element / 16 / 256 > kStoreSide * 65535.0) return ROCO_EUNSUPPORTED;
+  const double bytes = static_cast<double>(groups) * heads * rows * head_dim * element;  // of K; a lane has 16
+  if (bytes / 16 / 256 > kStoreSide * 65535.0) return ROCO_EUNSUPPORTED;
   const PageStoreArgs a = {heads, groups, rows, n_pages, __builtin_ctz(static_cast<unsigned>(page)), static_cast<int>(head_dim * element),
+                           streaming_above(2 * bytes) ? 1 : 0,
                            K_rows, V_rows, group_stride * element, row_stride * element, head_stride * element, slot_map, K_pool, V_pool};
   return launch_page_store(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
 }

@@ -238,6 +238,7 @@ hipError_t launch_page_tables(const PageTableArgs& a, hipStream_t s);
 
 struct PageStoreArgs {
   int heads, groups, rows, n_pages, page_log2, row_bytes;
+  int streaming;                              // as DecodeArgs::streaming
   const void *K_rows, *V_rows;
   int64_t group_stride, row_stride, head_stride;  // bytes
   const int32_t* map;

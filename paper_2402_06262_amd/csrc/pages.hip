@@ -270,7 +270,7 @@ hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s) {
   const long long lanes = (static_cast<long long>(a.groups) * a.heads * a.rows) << lanes_log2;
   const long long groups = (lanes + 255) / 256, side = std::min<long long>(groups, kStoreSide);
   const dim3 grid(static_cast<unsigned>(side), static_cast<unsigned>((groups + side - 1) / side));
-  if (lanes * 32 > (192ll << 20)) hipLaunchKernelGGL((page_store<true>), grid, dim3(256), 0, s, a, lanes_log2);
+  if (a.streaming) hipLaunchKernelGGL((page_store<true>), grid, dim3(256), 0, s, a, lanes_log2);
   else hipLaunchKernelGGL((page_store<false>), grid, dim3(256), 0, s, a, lanes_log2);
   return hipGetLastError();
 }

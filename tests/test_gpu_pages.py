@@ -443,3 +443,33 @@ def test_more_threads_than_a_launch_counts_in_one_dimension():
         for slot in (40, 3, 18, 70, 50, 77):
             want[slot // page, :, slot % page] = x[0]
         assert torch.equal(pool, want)
+
+
+@pytest.mark.parametrize("streaming", ["0", "1"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,rows,page", [(3, 7, 16), (5, 301, 64)])
+def test_rows_into_pages_with_and_without_streaming(monkeypatch, dtype, d, heads, rows, page, streaming):
+    monkeypatch.setenv("ROCO_STREAMING_LOADS", streaming)
+    test_new_tokens_and_caches_into_pages(dtype, d, heads, rows, page)
+
+
+def test_rows_above_the_size_from_which_they_are_streamed():
+    """205 MiB of odd rows, some of them not stored."""
+    groups, heads, rows, d, page = 5, 7, 12007, 128, 64
+    g = torch.Generator(device="cuda").manual_seed(5)
+    need = -(-rows // page)
+    order = torch.randperm(groups * need + 2, generator=g, device="cuda")[:groups * need].view(groups, need)
+    i = torch.arange(rows, device="cuda")
+    slots = (order[:, i // page] * page + i % page).int()
+    slots[:, ::13] = -1
+    K, V = torch.randn((2, groups, heads, rows, d), generator=g, device="cuda").bfloat16()
+    assert 2 * K.nbytes > 192 << 20
+    pools = [torch.full((groups * need + 2, heads, page, d), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    roco.roco_page_store(K, V, slots, *pools)
+    real = (slots >= 0).view(-1)
+    at = slots.view(-1)[real].long()
+    for pool, x in zip(pools, (K, V)):
+        want = torch.full_like(pool, 9.0)
+        want[at // page, :, at % page] = x.transpose(1, 2).reshape(-1, heads, d)[real]
+        assert torch.equal(pool, want)
