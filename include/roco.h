@@ -393,7 +393,8 @@ int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const in
  * Rows of K and V to their pool slots: the keys and values of new tokens straight from a projection, or compressed caches
  * [units, B, d] into pages.  Entry (g, i) of the map [groups, rows] names the pool slot of row (g, i) of every head h, which lies
  * group_stride g + row_stride i + head_stride h elements behind K_rows (V_rows); -1 (anything negative, or a page that the pool does
- * not have): the row is not stored.  Two rows of the same slot: either.
+ * not have): the row is not stored.  Of a slot that several rows name each 16 bytes of K and of V are one of these rows', not all the same
+ * one's.
  * Pools [n_pages, heads, page, d], disjoint from the rows.  Strides are multiples of 16 bytes and not negative; n_pages * heads * page < 2^31.
  */
 int roco_page_store(int32_t dtype, int32_t head_dim, int32_t heads, int32_t groups, int32_t rows, const void* K_rows,
