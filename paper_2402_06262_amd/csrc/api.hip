@@ -111,11 +111,19 @@ int check_pages(int32_t n_pages, int32_t heads, int32_t page) {
   if (n_pages < 1 || !page_size_ok(page)) return ROCO_EINVAL;
   return static_cast<long long>(n_pages) * heads * page < (1ll << 31) ? ROCO_OK : ROCO_EUNSUPPORTED;
 }
-int check_tree(const roco_params* p, int32_t heads, int32_t group, int32_t nodes, const roco_pages* pages, CachePages& out) {
+// What the size of a workspace depends on, of dense caches and paged ones alike.
+int check_tree_shape(const roco_params* p, int32_t group, int32_t nodes) {
   const int rc = check_params(p);
   if (rc != ROCO_OK) return rc;
-  if (heads < 1 || group < 1 || nodes < 1 || p->units % heads != 0) return ROCO_EINVAL;
+  if (group < 1 || nodes < 1) return ROCO_EINVAL;
   if (group > kMaxTreeGroup || nodes > kMaxTreeNodes) return ROCO_EUNSUPPORTED;
+  // (tree_apply: a workgroup per unit and kTreeChunk slots)
+  return static_cast<long long>(p->units) * ((p->budget + kTreeChunk - 1) / kTreeChunk) < kMostWorkgroups ? ROCO_OK : ROCO_EUNSUPPORTED;
+}
+int check_tree(const roco_params* p, int32_t heads, int32_t group, int32_t nodes, const roco_pages* pages, CachePages& out) {
+  const int rc = check_tree_shape(p, group, nodes);
+  if (rc != ROCO_OK) return rc;
+  if (heads < 1 || p->units % heads != 0) return ROCO_EINVAL;
   out = CachePages{nullptr, nullptr, 0, 0, 0};
   if (pages == nullptr) return static_cast<long long>(p->units) * p->budget < (1ll << 32) ? ROCO_OK : ROCO_EUNSUPPORTED;
   if (!given(pages->table) || !aligned4(pages->budget)) return ROCO_EINVAL;
@@ -515,8 +523,7 @@ int roco_decode_step_gqa(const roco_params* params, int32_t group, const void* q
 }
 
 size_t roco_tree_workspace_bytes(const roco_params* params, int32_t group, int32_t nodes) {
-  CachePages pages;
-  if (check_tree(params, 1, group, nodes, nullptr, pages) != ROCO_OK) return 0;
+  if (check_tree_shape(params, group, nodes) != ROCO_OK) return 0;
   return tree_layout(params, group, nodes).total;
 }
 

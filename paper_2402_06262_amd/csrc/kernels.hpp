@@ -171,6 +171,7 @@ constexpr int kMaxTreeNodes = 64;     // nodes of a tree: a bit each in a 64-bit
 constexpr int kMaxTreeGroup = 64;     // query heads per unit
 constexpr int kMaxTreeSplits = 64;    // workgroups that share a unit's slots: a lane each in the kernel that joins them
 constexpr int kTreeChunk = 1024;      // most slots of a workgroup of tree_statistics
+constexpr int kMostWorkgroups = 1 << 24;  // of 256 threads, in one dimension: a launch counts fewer than 2^32 threads there
 
 // Where K and V rows lie: [units][B] without a table, else pages of 1 << page_log2 slots, [n_pages][heads][page].
 struct CachePages {

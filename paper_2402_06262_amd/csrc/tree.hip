@@ -175,8 +175,8 @@ int tree_attend_row_tiles(int dtype, int rows, bool window) {
 TreeSplits tree_attend_splits(int dtype, int units, int rows, int B, bool window) {
   const char* const asked = getenv("ROCO_TREE_SPLITS");
   int want = asked != nullptr ? atoi(asked) : 0;
+  const long long groups = static_cast<long long>(units) * tree_attend_row_tiles(dtype, rows, window);
   if (want <= 0) {
-    const long long groups = static_cast<long long>(units) * tree_attend_row_tiles(dtype, rows, window);
     want = static_cast<int>((512 + groups - 1) / groups);
     if (dtype == kBF16 && rows > 64) {
       long long least = -1;
@@ -189,6 +189,9 @@ TreeSplits tree_attend_splits(int dtype, int units, int rows, int B, bool window
       }
     }
   }
+  // (what a launch of the attention takes, and of the joining with a workgroup per row)
+  want = std::min<long long>(want, (kMostWorkgroups - 1) / (groups + 7ll * tree_attend_row_tiles(dtype, rows, window)));
+  if (static_cast<long long>(units) * rows >= kMostWorkgroups) want = std::min(want, kFewSplits);
   want = std::max(1, std::min({want, kMaxTreeSplits, (B + 63) / 64}));
   TreeSplits s;
   s.chunk = ((B + want - 1) / want + 63) / 64 * 64;

@@ -641,3 +641,45 @@ def test_two_streams_with_workspaces_of_their_own():
                                   s.lse, s.ws, stream=stream)
     torch.cuda.synchronize()
     assert np.array_equal(wa[0], a.out.float().cpu().numpy()) and np.array_equal(wb[0], b.out.float().cpu().numpy())
+
+
+def test_more_than_32_bits_of_slots_on_pages():
+    """65532 units of 65552 slots each, of which three are in use, in one page that all requests have: the last units' bits are the first ones',
+    and those of a call of the first ones alone."""
+    heads, B, T, d, n = 4, 65552, 3, 64, 3
+    units = 65532
+    assert units * B > 1 << 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    draw = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    q, k, v, pool = draw(heads, T, 1, d), draw(heads, T, d), draw(heads, T, d), draw(2, 1, heads, 1024, d)
+    stats, pos = draw(heads, 3, n).abs() + 1, torch.arange(n, device="cuda", dtype=torch.int32)
+
+    def step(units):
+        R = units // heads
+        p = roco.RocoParams(units, d, B, 2, roco.ROCO_F32, 0.0, 4, 0.5)
+        all_stats = torch.zeros((units, 3, B), device="cuda")
+        all_stats[:, :, :n] = stats.repeat(R, 1, 1)
+        all_pos = torch.full((units, B), -1, dtype=torch.int32, device="cuda")
+        all_pos[:, :n] = pos
+        used = torch.full((units,), n, dtype=torch.int32, device="cuda")
+        table = torch.zeros((R, -(-B // 1024)), dtype=torch.int32, device="cuda")
+        pages = roco.RocoPages(table, 1, 1024)
+        K, V = pool.clone()
+        x = [y.repeat(R, *[1] * (y.dim() - 1)) for y in (q, k, v)]
+        qpos0 = torch.full((units,), 5, dtype=torch.int32, device="cuda")
+        ws = torch.empty(roco.tree_workspace_bytes(p, 1, T), dtype=torch.uint8, device="cuda")
+        out, lse = torch.empty((units, T, 1, d), device="cuda"), torch.empty((units, T, 1), device="cuda")
+        roco.roco_tree_attend(p, heads, 1, T, pages, *x, None, None, qpos0, K, V, all_pos, used, out, lse, ws)
+        path = dev(np.tile([[0, 1]], (R, 1)))
+        ev = [torch.empty((units, 2), dtype=torch.int32, device="cuda") for _ in range(2)]
+        roco.roco_tree_commit(p, heads, 1, T, pages, *x, lse, 2, path, dev(np.full(R, 2)), qpos0, K, V, all_stats, all_pos, used, *ev, ws)
+        torch.cuda.synchronize()
+        assert (all_stats[-heads:, :, n + 2:] == 0).all() and (all_pos[-heads:, n + 2:] == -1).all()
+        return [y.clone() for y in (out, lse, all_stats[:, :, :n + 2], all_pos[:, :n + 2], used, *ev)], [K, V]
+
+    small, small_pool = step(heads)
+    large, large_pool = step(units)
+    torch.cuda.empty_cache()
+    for a, b in zip(small, large):
+        assert torch.equal(a.repeat(units // heads, *[1] * (a.dim() - 1)), b)
+    assert all(torch.equal(a, b) for a, b in zip(small_pool, large_pool)) and not torch.equal(small_pool[0], pool[0])

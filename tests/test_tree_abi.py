@@ -259,3 +259,35 @@ def test_a_store_of_more_than_a_launch_takes():
     store = lambda groups, rows, heads=8: roco.load_library().roco_page_store(  # noqa: E731
         roco.ROCO_F32, 128, heads, groups, rows, OK, OK, 0, 0, 0, OK, OK, OK, 4, 16, None)
     assert store((1 << 31) - 1, (1 << 31) - 1) == EUNSUPPORTED and store(1 << 20, 1 << 24) == EUNSUPPORTED  # (2^49 lanes, then 2^52)
+
+
+@pytest.mark.parametrize("call", [_attend, _commit])
+def test_large_calls_on_pages_have_a_workspace(call):
+    """2^32 slots and more in all: too many for dense caches, not for pages."""
+    large = roco.RocoParams(16384, 128, 1 << 18, 16, roco.ROCO_BF16)
+    need = roco.tree_workspace_bytes(large, 2, 8)
+    assert need > 8 << 32  # a sum of either kind per slot
+    pages = _pages(max_pages=1 << 12)
+    assert call(large, pages=pages, ws=need - 1) == EWORKSPACE
+    assert call(large, ws=need) == EUNSUPPORTED  # without pages
+    # ... as far as a launch goes: the query and the calls agree
+    for units, budget in ((65532, 1 << 18), (65532, 1 << 20), (16384, 1 << 20), (1024, 1 << 24), (1020, 1 << 24)):
+        p = roco.RocoParams(units, 128, budget, 16, roco.ROCO_BF16)
+        fits = units * budget < 1 << 34
+        need = roco.tree_workspace_bytes(p, 2, 8)
+        assert (need > 0) == fits
+        assert call(p, pages=_pages(max_pages=1 << 18), ws=max(need, 1) - 1) == (EWORKSPACE if fits else EUNSUPPORTED)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("units,budget,nodes,group", [(65535, 4096, 64, 64), (65535, 65000, 64, 1), (4100, 1 << 20, 64, 64), (4097, 9000, 64, 63), (64, 4096, 64, 64)])
+def test_asked_splits_are_as_many_as_launches_take(monkeypatch, dtype, units, budget, nodes, group):
+    """The workspace of the shares tells how many there are: 64 asked for."""
+    p = roco.RocoParams(units, 64, budget, 16, dtype)
+    commit = roco.tree_workspace_bytes(p, 1, 1)
+    monkeypatch.setenv("ROCO_TREE_SPLITS", "64")
+    rows = nodes * group
+    splits = max(0, roco.tree_workspace_bytes(p, group, nodes) - commit) // (units * rows * 4 * 66)
+    tile = 64 if dtype == 0 else 192
+    assert -(-units * max(splits, 1) // 8) * 8 * -(-rows // tile) < 1 << 24
+    assert splits <= 8 or units * rows < 1 << 24
