@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(
     read_queries();
   }
 
-  const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 / sc : 0.0f;  // (the products are multiplied by sc where they become exponents)
+  const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 : 0.0f;  // (without a bias, products are multiplied by sc where they become exponents)
   const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
   const auto token_of = [&](int t2, int q) { return min(first_row + 16 * t2 + q, rows - 1) / late(a.group); };
   const auto see = [&]() { return seen_nodes(parent, nodes, LateLane().lane); };
@@ -306,11 +306,11 @@ __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(
         for (int e = 0; e < 4; ++e) {
           if (WINDOW) {
             const int away = qp[t2] - ps[i][e];
-            s[t2][i][e] += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
+            s[t2][i][e] = fmaf(s[t2][i][e], sc, static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f);
           }
           most = fmaxf(most, s[t2][i][e]);
         }
-      most *= sc;
+      if (!WINDOW) most *= sc;
       if (__any(most > m[t2] + kSlack)) {
         most = fmaxf(most, __shfl_xor(most, 16, kWave));
         most = fmaxf(most, __shfl_xor(most, 32, kWave));
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(
       for (int i = 0; i < G; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s[t2][i][e] = fast_exp2(fmaf(s[t2][i][e], sc, -ref));
+          s[t2][i][e] = fast_exp2(WINDOW ? s[t2][i][e] - ref : fmaf(s[t2][i][e], sc, -ref));
           sum += s[t2][i][e];
         }
       l[t2] += sum;
@@ -530,7 +530,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
     reads_done();
     __syncthreads();
   }
-  const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 / sc : 0.0f;
+  const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 : 0.0f;
   const int w = a.recency_window, qp0 = WINDOW ? a.qpos0[u] : 0;
   const auto token_of = [&](int t2, int q) { return min(first_row + 16 * t2 + q, rows - 1) / late(a.group); };
   uint64_t seen = 0, special = 0;
@@ -637,7 +637,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
 #pragma unroll
           for (int t2 = 0; t2 < NQ; ++t2)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t2][i][e] += static_cast<unsigned>(qp[t2] - ps[e]) < static_cast<unsigned>(w) ? bias : 0.0f;
+            for (int e = 0; e < 4; ++e) s[t2][i][e] = fmaf(s[t2][i][e], sc, static_cast<unsigned>(qp[t2] - ps[e]) < static_cast<unsigned>(w) ? bias : 0.0f);
         }
       }
       if (of_nodes || here != kWhole) {
@@ -682,7 +682,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
         for (int i = 0; i < G; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) most = fmaxf(most, s[t2][i][e]);
-        most *= sc;
+        if (!WINDOW) most *= sc;
         if (__any(most > m[t2] + kSlack)) {
           most = fmaxf(most, __shfl_xor(most, 16, kWave));
           most = fmaxf(most, __shfl_xor(most, 32, kWave));
@@ -699,7 +699,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
         for (int i = 0; i < G; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[t2][i][e] = fast_exp2(fmaf(s[t2][i][e], sc, -ref));
+            s[t2][i][e] = fast_exp2(WINDOW ? s[t2][i][e] - ref : fmaf(s[t2][i][e], sc, -ref));
             sum += s[t2][i][e];
           }
         l[t2] += sum;

@@ -683,3 +683,15 @@ def test_more_than_32_bits_of_slots_on_pages():
     for a, b in zip(small, large):
         assert torch.equal(a.repeat(units // heads, *[1] * (a.dim() - 1)), b)
     assert all(torch.equal(a, b) for a, b in zip(small_pool, large_pool)) and not torch.equal(small_pool[0], pool[0])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("T,group", [(5, 2), (20, 3), (40, 3)])
+@pytest.mark.parametrize("window", [4, 1 << 20])
+@pytest.mark.parametrize("bias", [-1e38, -300.0, 1e38])
+def test_recency_biases_of_any_size(dtype, d, T, group, window, bias):
+    """As masks are made of the type's lowest value: tokens inside the window without weight, or alone with it; where all are inside, all the same."""
+    s = Step(T, dtype, d, used=[0, 90, 310], B=320, T=T, group=group, window=window)
+    s.bias = float(np.float32(bias))
+    s.upload()
+    s.check_attend(*s.attend())
