@@ -170,8 +170,9 @@ int tree_attend_row_tiles(int dtype, int rows, bool window) {
 
 // Two workgroups on every compute unit, while each has 64 slots.  With more than 64 rows of bf16, where a workgroup's products bound it and not the
 // memory: the splits, of 192 slots at least, whose rounds of 512 workgroups are shortest, a workgroup being as long as its tiles of 32 and 8
-// more for its start and its share of the outputs (128 units x 4096 slots x 512 rows: four splits 231 us, two 227, three 243; with requests of
-// different lengths, which fewer splits leave waiting for the longest, 155, 161 and 164; 192 units x 2048 x 160 rows: two splits 53 us, three 62).
+// more for its start and its share of the outputs (128 units x 4096 slots x 512 rows: four splits 273 us, two 271, three 288; with requests of
+// different lengths, which fewer splits leave waiting for the longest, 194, 205 and 206; 192 units x 2048 x 160 rows: two splits 98 us, three 115,
+// one 117; 512 x 4096 x 384 rows: one 673, two 729; 32 x 8192 x 128 rows: the rule's sixteen 57, six 71).
 TreeSplits tree_attend_splits(int dtype, int units, int rows, int B, bool window) {
   const char* const asked = getenv("ROCO_TREE_SPLITS");
   int want = asked != nullptr ? atoi(asked) : 0;

@@ -468,11 +468,11 @@ __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(
 // More than 64 query rows of bf16: four waves with 16 NQ rows each share the tiles, which come two at a time, K or V of one by each
 // wave, while the two before them are used; one barrier for two tiles.  Two workgroups on a compute unit, so that one wave's exponentials run beside another's products: with 64
 // rows to a workgroup and the rest in others, every row tile fetched K and V again, and a wave had its matrix cores to itself.
-// Here the matrix cores are what the step waits for, so that probabilities are rounded to one bf16 number each (2^-9 of each; the
-// outputs, sums over many, are 2.3e-3 of their norm off instead of 1.7e-3, their own rounding): the second number would be a third more
-// products and as much vector work again.
-// 512 units x 4096 slots with 384 rows 510 us, 820 TFLOP/s; 128 units of 919 to 4096 slots with 256 to 496 rows 135 us, whose products would take 49:
-// exponentials, products and fragments' reads follow each other in a wave, and two waves on a SIMD cover a part of it.
+// Probabilities are sums of two bf16 numbers as with fewer rows, so that a tree's outputs do not lose bits to the rows beside it in a call: one number,
+// half a step of 2^-8 off, takes a quarter less time (152 us for 194 on the trees below, whose outputs are then 2.3e-3 of their norm off instead of 1.7e-3,
+// their own rounding).
+// 512 units x 4096 slots with 384 rows 673 us, 610 TFLOP/s, 920 with the second numbers' products; 128 units of 919 to 4096 slots with 256 to 496 rows
+// 177 us, whose products would take 49: exponentials, products and fragments' reads follow each other in a wave, and two waves on a SIMD cover a part of it.
 constexpr int kWideWaves = 4;
 constexpr int kWideThreads = kWideWaves * kWave;
 
@@ -706,13 +706,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
       }
 #pragma unroll
       for (int i = 0; i < G; i += 2) {
-        uint4 p[NQ];
+        uint4 p[NQ][2];
 #pragma unroll
         for (int t2 = 0; t2 < NQ; ++t2) {
-          mfma::bf16x8 r;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) r[e] = static_cast<__bf16>(s[t2][i + (e >> 2)][e & 3]);
-          p[t2] = __builtin_bit_cast(uint4, r);
+          const f32x4 pair[2] = {s[t2][i], s[t2][i + 1]};
+          fused::split_positive(pair, p[t2]);
         }
         uint4 vf[2];
         const auto read_v = [&](int db) {
@@ -725,7 +723,9 @@ __global__ __launch_bounds__(kWideThreads, 2) void tree_attend_wide(TreeArgs a) 
         for (int db = 0; db < T::kBlocks; ++db) {
           if (db + 1 < T::kBlocks) read_v(db + 1);
 #pragma unroll
-          for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(vf[db & 1], p[t2], o[t2][db]);
+          for (int k = 1; k >= 0; --k)
+#pragma unroll
+            for (int t2 = 0; t2 < NQ; ++t2) o[t2][db] = fused::mfma16(vf[db & 1], p[t2][k], o[t2][db]);
           __builtin_amdgcn_sched_barrier(0);
         }
       }

@@ -695,3 +695,33 @@ def test_recency_biases_of_any_size(dtype, d, T, group, window, bias):
     s.bias = float(np.float32(bias))
     s.upload()
     s.check_attend(*s.attend())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,group,window,page", [(33, 2, 0, 0), (64, 3, 0, 64), (24, 8, 0, 0), (64, 8, 0, 16), (40, 3, 50, 0), (64, 5, 50, 32)])
+def test_many_rows_are_as_precise_as_few(d, T, group, window, page):
+    """Probabilities of bf16 are sums of two bf16 numbers however many rows a call has: 2^-16 of sum p |v|, and half a step of the output.  The same
+    trees a request at a time, in calls of up to 64 rows, are within a step of the type of them."""
+    s = Step(T + d, "bf16", d, used=[0, 70, 900], B=900, T=T, group=group, window=window, page=page, n_nodes=[T, T - 1, max(1, 64 // group)]).upload()
+    out, lse = s.attend()
+    s.check_attend(out, lse)
+    for u in range(s.U):
+        t, n = s.n_nodes[u // 2], s.used[u // 2]
+        w = s.want(u)
+        rel = 2 * (d + 8) * U * w.logit + (8 + 2 * math.sqrt(n + t)) * U + 2.0 ** -16
+        err = np.abs(out[u, :t] - w.out)
+        tol = rel * w.mass + 2.0 ** -8 * np.abs(w.out) + 1e-30
+        assert (err <= tol).all(), f"unit {u}: worst {(err / tol).max():.3g} of the tolerance"
+    # the last request's tree again, padded to no more than 64 rows
+    few = s.n_nodes[2]
+    one = slice(2 * s.heads, 3 * s.heads)
+    p = roco.RocoParams(s.heads, d, s.B, 1, roco.ROCO_BF16, 0.0, window, s.bias)
+    pages = roco.RocoPages(dev(s.table[2:3]), s.n_pages, page, dev(np.array(s.budgets[2:3]))) if page else None
+    K, V = (s.dK, s.dV) if page else (s.dK[one].contiguous(), s.dV[one].contiguous())
+    o = torch.zeros((s.heads, few, group, d), dtype=torch.bfloat16, device="cuda")
+    roco.roco_tree_attend(p, s.heads, group, few, pages, s.dq[one, :few].contiguous(), s.dk[one, :few].contiguous(), s.dv[one, :few].contiguous(),
+                          dev(s.parent[2:3, :few]), None, s.dqpos0[one].contiguous(), K, V, s.dpos[one].contiguous(), s.dn_used[one].contiguous(), o, None,
+                          torch.empty(roco.tree_workspace_bytes(p, group, few), dtype=torch.uint8, device="cuda"))
+    a, b = out[one, :few], o.double().cpu().numpy()
+    mass = np.stack([s.want(u).mass[:few] for u in range(*one.indices(s.U))])
+    assert (np.abs(a - b) <= 2.0 ** -7 * np.maximum(np.abs(a), np.abs(b)) + 2.0 ** -13 * mass).all()
