@@ -725,3 +725,94 @@ def test_many_rows_are_as_precise_as_few(d, T, group, window, page):
     a, b = out[one, :few], o.double().cpu().numpy()
     mass = np.stack([s.want(u).mass[:few] for u in range(*one.indices(s.U))])
     assert (np.abs(a - b) <= 2.0 ** -7 * np.maximum(np.abs(a), np.abs(b)) + 2.0 ** -13 * mass).all()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("T", [5, 40])
+@pytest.mark.parametrize("window,splits", [(0, 5), (2, 1), (2, 5), (400, 5)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_values_that_are_not_finite_in_splits_and_under_a_window(monkeypatch, dtype, d, T, window, splits, bad):
+    """As test_what_a_node_does_not_see_does_not_reach_it, where the nodes' values are added to shares of several splits, or a bias moves their weight.
+    The last node's key is near its query, so that its own value is a good part of its output."""
+    monkeypatch.setenv("ROCO_TREE_SPLITS", str(splits))
+    s = Step(T + window, dtype, d, used=[310, 40], heads=1, T=T, group=2, window=window, B=310)
+    s.parent = np.array([[-1] + [0 if i in (1, T - 1) else i - 1 if i - 1 not in (1,) else 0 for i in range(1, T)]] * 2)
+    s.k_new[:, T - 1] = 0.5 * s.q[:, T - 1, 0]
+    if dtype == "bf16":
+        s.k_new = round_to_bf16(s.k_new)
+    s.upload()
+    clean, clean_lse = s.attend()
+    s.check_attend(clean, clean_lse)
+    s.dv[:, 1] = bad
+    s.dv[:, T - 1, 3:9] = bad
+    s.dk[:, 1] = bad
+    s.dq[:, 1] = bad
+    sees = trees.seen_nodes(s.parent[0], T)
+    touched = sees[:, [1, T - 1]].any(1)
+    assert touched.sum() == 2
+    out, lse = s.attend()
+    assert np.array_equal(out[:, ~touched], clean[:, ~touched]) and np.array_equal(lse[:, ~touched], clean_lse[:, ~touched])
+    assert np.array_equal(lse[:, T - 1], clean_lse[:, T - 1]) and not np.isfinite(out[:, 1]).any()
+    if np.isnan(bad):
+        assert np.isnan(out[:, T - 1, :, 3:9]).all()
+    else:
+        assert (out[:, T - 1, :, 3:9] == bad).all()
+    # the other dimensions of the last node's rows: one rounding more, in bf16 of a final row
+    half = 2.0 ** -8 if dtype == "bf16" else U
+    for u in range(s.U):
+        w = s.want(u)
+        n = s.used[u] + T
+        rel = 2 * (d + 8) * U * w.logit + (8 + 2 * math.sqrt(n)) * U + (0 if dtype == "f32" else 2.0 ** -16)
+        rest = [c for c in range(d) if not 3 <= c < 9]
+        # (the row that is rounded first lacks the node's own share: it is no larger than sum p |v|)
+        err = np.abs(out[u, T - 1] - w.out[T - 1])[:, rest]
+        assert (err <= (rel * w.mass[T - 1] + half * (np.abs(w.out[T - 1]) + w.mass[T - 1]))[:, rest]).all(), u
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("T,group,splits", [(3, 2, 64), (3, 2, 33), (12, 8, 64), (1, 1, 0)])
+def test_more_than_32_splits(monkeypatch, dtype, d, T, group, splits):
+    """So many that a row's waves go over them twice; units that use all of them, 33, 32 or fewer; 0: as many as the call takes by itself."""
+    if splits:
+        monkeypatch.setenv("ROCO_TREE_SPLITS", str(splits))
+    B = 64 * (splits or 64) - 3
+    s = Step(T + splits, dtype, d, used=[B, min(B, 64 * 33 - 5), 64 * 32, 65], heads=1, B=B, T=T, group=group, window=0 if T == 3 else 90).upload()
+    s.check_attend(*s.attend())
+
+
+@pytest.mark.parametrize("streaming", ["0", "1"])
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("T,group,page,window", [(1, 1, 0, 0), (9, 1, 16, 0), (7, 3, 0, 9), (13, 4, 32, 20), (64, 1, 64, 0), (40, 3, 16, 9)])
+def test_with_and_without_streaming(monkeypatch, dtype, d, T, group, page, window, streaming):
+    """Loads with the non-temporal hint, which the size of a cache chooses: attention and the accepted path."""
+    monkeypatch.setenv("ROCO_STREAMING_LOADS", streaming)
+    s = Step(T + page, dtype, d, used=[0, 33, 250, 100, 701], B=701, budgets=[40, 33, 300, 111, 701], page=page or 16, T=T, group=group, window=window,
+             n_nodes=[T, (T + 1) // 2, T, T, 1], max_path=min(T, 7))
+    if not page:  # (dense caches have one budget)
+        s.page, s.budgets = 0, [s.B] * s.R
+    s.upload()
+    s.check_attend(*s.attend())
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("group", [1, 3, 4, 8, 16, 33])
+@pytest.mark.parametrize("page", [0, 32])
+def test_commit_under_a_recency_window_for_every_way_of_sharing_tiles(dtype, d, group, page):
+    """Heads of a token in registers, lane groups and tiles; of 4 to 16 heads, by type, and more the rows are too many to be formed at a time."""
+    s = Step(group, dtype, d, used=[0, 90, 310], B=310, T=30, group=group, window=7, page=page, chain=True, max_path=24).upload()
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+
+
+@pytest.mark.parametrize("group", [1, 3, 4, 8, 16, 33])
+@pytest.mark.parametrize("policy", [orc.Policy("aas", "all"), orc.Policy("mas", "window"), orc.Policy("ltas", "all"), orc.Policy("aqas", "window")])
+def test_policies_for_every_way_of_sharing_tiles(policy, group):
+    for dtype, d in (("bf16", 128), ("f32", 64)):
+        s = Step(group, dtype, d, used=[90, 88, 50], B=90, T=20, group=group, policy=policy, scope=30, chain=True, max_path=16).upload()
+        lse = s.exact_lse()
+        s.commit(lse)
+        s.check_commit(lse, str(policy))
