@@ -304,7 +304,7 @@ int roco_decode_step_gqa(const roco_params* params, int32_t group,
  * request r is row j % page of page table[r][j / page], and budget[r] slots are the request's (params->budget is the largest: the
  * row length of stats and pos, which stay [units, 3, B] and [units, B]).  The scope of a request of fewer slots than params->scope is
  * all of them.  Entries behind the pages that the slots in use need are not read.  What lies in a page outside [0, n_pages) is
- * neither read nor written: such slots are not seen.
+ * neither read nor written: such slots are not seen, and their statistics stay (as victims they are chosen like others).
  *
  * The rows (q, k_new, v_new, out, caches, pools), the workspace and the slot map that roco_page_tables writes are aligned to 16 bytes, the other
  * arrays of these calls to 4: the rest of a list of free pages, a part of a packed map, or statistics and positions in one buffer.

@@ -222,9 +222,9 @@ struct CommitArgs {
   CachePages pages;
   int32_t *evicted_slot, *evicted_pos;        // [units][max_path], may be null
   // workspace
-  int32_t* taken;                             // [units][kTakenWords]: slots held before, tokens taken over, slots held then, -, the tokens' slots in order
+  int32_t* taken;                             // [units][kTakenWords]: -, tokens taken over, slots held then, -, the tokens' slots in order
   uint32_t* keys;                             // [units][2][B] when B is too large for LDS
-  float* sums;                                // [units][2][B]: what the accepted rows add to Acc and Acc2 of the slots held before
+  float* sums;                                // [units][2][B]: what the accepted rows add to Acc and Acc2 of the slots held before (below zero: not seen)
   float* fresh;                               // [units][2][kMaxTreeNodes]: ... and of the accepted tokens themselves
 };
 constexpr int kTakenWords = 4 + kMaxTreeNodes;

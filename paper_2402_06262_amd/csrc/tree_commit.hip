@@ -49,7 +49,6 @@ template <int NT> __device__ __forceinline__ void choose_slots(const CommitArgs&
     if (a.evicted_pos != nullptr) a.evicted_pos[static_cast<size_t>(u) * a.max_path + tid] = -1;
   }
   if (tid == 0) {
-    taken[0] = n;
     taken[1] = len;
     taken[2] = n_new;
     list_sh[0] = 0u;
@@ -360,7 +359,7 @@ __global__ __launch_bounds__(kStatThreads, 4) void tree_statistics(CommitArgs a,
         // store of a count that the waits rely on: the first 16 lanes' Acc, the next 16 lanes' Acc2, the others' out of range.
         const int j = j0 + 16 * i + qi, step = of_fresh ? kMaxTreeNodes : a.B;
         float* const to = of_fresh ? fresh_sums : sums;
-        float v = qi < static_cast<int>((there0 >> (8 * i)) & 0xffu) ? g == 0 ? sum[i] : sum2[i] : 0.0f;  // (slots of no page receive nothing)
+        float v = qi < static_cast<int>((there0 >> (8 * i)) & 0xffu) ? g == 0 ? sum[i] : sum2[i] : -1.0f;  // (below zero: a slot of no page, not seen)
         const bool there = g < 2 && j < (of_fresh ? len : row1 - row0);
         if (first > 0 && there) v += to[g * step + j];
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), __builtin_amdgcn_make_buffer_rsrc(to, 0, (step + (of_fresh ? len : row1 - row0)) * 4, 0x00020000),
@@ -436,6 +435,7 @@ __global__ __launch_bounds__(kApplyThreads) void tree_apply(CommitArgs a, int ro
     if (row0 + j >= row1) break;
     const int k = reinterpret_cast<const uint8_t*>(token_s)[j];
     const bool taken_over = k < kMaxTreeNodes;
+    if (!taken_over && more[e] < 0.0f) continue;  // not seen: as it was
     acc[row0 + j] = taken_over ? fresh[k] : first[e] + more[e];
     acc2[row0 + j] = taken_over ? fresh[kMaxTreeNodes + k] : (a.pol.keeps_last_score() ? 0.0f : second[e]) + more2[e];
     cnt[row0 + j] = taken_over ? static_cast<float>(len - k) : count[e] + static_cast<float>(len);

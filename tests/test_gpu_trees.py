@@ -816,3 +816,22 @@ def test_policies_for_every_way_of_sharing_tiles(policy, group):
         lse = s.exact_lse()
         s.commit(lse)
         s.check_commit(lse, str(policy))
+
+
+@pytest.mark.parametrize("group,max_path", [(1, 2), (2, 3), (16, 14)])
+@pytest.mark.parametrize("policy", [None, orc.Policy("ltas", "all"), orc.Policy("aqas", "all")])
+def test_statistics_of_slots_that_are_not_seen_stay(group, max_path, policy):
+    """Slots of a page outside the pool: no accepted row attended them, so that neither sums nor counts move; the others' are as without them."""
+    s = Step(max_path, "bf16", 64, used=[70, 41], heads=2, B=70 + max_path, page=16, T=16, group=group, chain=True, max_path=max_path, policy=policy)
+    s.table[0, 2], s.table[1, 0] = s.n_pages + 1, -1
+    s.upload()
+    lse = np.full((s.U, s.T, group), 4.0, np.float32)
+    s.commit(lse)
+    assert (s.ev_slot == -1).all()
+    got = s.dstats.cpu().numpy()
+    for u in range(s.U):
+        r, n = u // 2, s.used[u // 2]
+        hidden = np.arange(32, 48) if r == 0 else np.arange(16)
+        assert np.array_equal(got[u, :, hidden], s.stats[u, :, hidden])
+        seen = np.setdiff1d(np.arange(n), hidden)
+        assert (got[u, 2, seen] == s.stats[u, 2, seen] + len(s.paths[r])).all() and (got[u, 0, seen] > s.stats[u, 0, seen]).all()
