@@ -84,6 +84,9 @@ template <int DT, int HD, int WAVES> __global__ __launch_bounds__(kJoinThreads) 
 
 // Few splits of many rows: HD / 4 lanes and their 16 bytes have kJoinRows rows each, so that the loads of all of them are in flight (a wave per row
 // took 21 us for 65536 rows of two splits, 63 MB, and these 9.8; 1260 rows 4.8 and 6.2).  The sums over the splits are in their order.
+// The borders, whole attentions in us: 16384 rows of two and four splits 29.1 and 27.5, by a wave per row 32.5 and 29.9, but 4096 rows 32.5 and 26.8 by
+// these, 32.7 and 26.6 by a wave per row.  Eight splits of 65536 and 8192 rows 175 and 45, by four waves per row 214 and 50; 16 splits of 65536 rows
+// 320 by these, 305 by four waves per row.
 constexpr int kJoinRows = 4, kFewSplits = 8, kManyRows = 16384;
 template <int DT, int HD> __global__ __launch_bounds__(kJoinThreads) void tree_join_few(TreeArgs a, int groups) {
   constexpr int LANES = HD / 4, STEP = kJoinThreads / LANES;
