@@ -321,7 +321,8 @@ typedef struct roco_pages {
 size_t roco_tree_workspace_bytes(const roco_params* params, int32_t group, int32_t nodes);
 
 /*
- * Attention of drafted trees (a matrix product over the cache for all nodes and heads at once: K and V are read once):
+ * Attention of drafted trees (a matrix product over the cache for all nodes and heads at once: K and V are read once for 64 query rows, of
+ * bf16 with more than 64 once for 192, or 128 under a recency window):
  *   p_ih = softmax over the unit's n_used slots and the nodes that node i sees of scale q_ih . k + bias
  *   out_ih = sum p_ih v,   lse_ih = ln of the sum of exponentials (roco_tree_commit wants it)
  * Values of nodes that a row does not see do not reach it, infinite and NaN ones neither.

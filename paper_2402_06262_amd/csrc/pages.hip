@@ -252,7 +252,7 @@ hipError_t launch_page_tables(const PageTableArgs& a, hipStream_t s) {
   ProfScope ps(kProfPageTables, s);
   const long long total = a.padded ? static_cast<long long>(a.requests) * a.rows : a.rows;
   // a step of every thread, as far as that gives no more than six workgroups per compute unit (1024 prompts of up to 8192 slots: 512 of them
-  // 16.6 us, 1024 12.9, 1536 12.6, 2048 13.5)
+  // 15.9 us, 1024 13.0, 1536 13.2, 2048 14.1)
   const long long want = std::max<long long>((total + kFillThreads * kFillEntries - 1) / (kFillThreads * kFillEntries), (a.requests + 3) / 4);
   const dim3 grid(static_cast<unsigned>(std::min<long long>(want, 1536)));
   if (a.requests <= kSelfSummed) {

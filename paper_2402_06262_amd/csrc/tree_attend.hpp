@@ -7,7 +7,8 @@
 // O^T = V^T . P^T take these registers as they are.  A tree's nodes are tiles of the last split like any others, but for their mask.
 // The running maximum follows a tile's only when that is more than 2^8 above it: no rescaling, and no exchange between lanes, for most
 // tiles, and the sums stay far from the ends of fp32.
-// Up to 64 rows the memory bounds it: 512 units x 2048 slots of bf16 / 128 with 16 rows 84 us, 6.5 TB/s of K and V; 16 x 65536 with 64 rows 96 us, 5.6.
+// Up to 64 rows the memory bounds it: 512 units x 2048 slots of bf16 / 128 with 16 rows 84 us, 6.5 TB/s of K and V; 16 x 65536 with 64 rows 102 us with the
+// joining of their splits, 5.3.
 // fp32's matrix instructions share that place from 17 rows on: 60 x 1501 slots of 128 with 21 rows (32 are formed) 30 us for 92 MB.
 #pragma once
 #include <type_traits>
@@ -472,7 +473,8 @@ __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(
 // half a step of 2^-8 off, takes a quarter less time (152 us for 194 on the trees below, whose outputs are then 2.3e-3 of their norm off instead of 1.7e-3,
 // their own rounding).
 // 512 units x 4096 slots with 384 rows 673 us, 610 TFLOP/s, 920 with the second numbers' products; 128 units of 919 to 4096 slots with 256 to 496 rows
-// 177 us, whose products would take 49: exponentials, products and fragments' reads follow each other in a wave, and two waves on a SIMD cover a part of it.
+// 194 us, 16 of them to join splits, whose products would take 49: exponentials, products and fragments' reads follow each other in a wave, and two
+// waves on a SIMD cover a part of it.
 constexpr int kWideWaves = 4;
 constexpr int kWideThreads = kWideWaves * kWave;
 
