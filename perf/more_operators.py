@@ -381,6 +381,7 @@ def _plain_verify(s):
             left = torch.where(no, left - pr, left)
             target[r, x] = torch.where(no, 0.0, pr)
         else:
+            no = no & (gone < 1)  # (the earlier ones may hold all of the draft's distribution, by its roundings: then it has no other)
             times = torch.where(no, times + left / (1 - gone), times)
             gone = torch.where(no & distinct, gone + qr, gone)
             left = torch.where(no, (target - times[:, None] * draft).clamp(min=0).sum(1), left)
@@ -395,6 +396,7 @@ def _plain_verify(s):
     weights = torch.where(weights.sum(1, keepdim=True) > 0, weights, p[r, at].double())
     sums = weights.cumsum(1)
     chosen = (sums > s["choose"].double()[:, None] * sums[:, -1:]).int().argmax(1)
+    chosen = torch.where(length > 0, chosen, -1)
     return torch.where(torch.arange(T, device="cuda") < length[:, None], path, -1).int(), length.int(), chosen.int()
 
 
