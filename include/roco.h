@@ -371,6 +371,84 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
                      void* hip_stream);
 
 /*
+ * Verification of drafted trees, between roco_tree_attend and roco_tree_commit: which path the target model takes, and the token behind it,
+ * distributed as the target's probabilities say whatever was drafted.  Row i of p [requests, nodes, vocab] is the target's distribution behind node i,
+ * row i of q the one that the continuations of node i were drawn from; all random numbers are given.
+ *
+ * Node 0 is the request's newest token, which the cache has not: it is accepted.  The continuations x of the last accepted node (rows p, q) are tried
+ * in the order of their numbers, with c = 0, N = 1, Q = 0 to begin with:
+ *   accepted if accept[node] q(x) N < max(p(x) - c q(x), 0) (1 - Q); the walk goes on from there;
+ *   else c += N / (1 - Q), N = sum over the vocabulary of max(p - c q, 0), and with `distinct` Q += q(x).
+ * (The target's distribution after k rejections is max(p - c q, 0) / N.)  distinct 0: every continuation was drawn from q on its own; 1: from what the
+ * earlier ones have left of q, so that they differ (with 1 - Q not above 0 there is none: not accepted, c and N stay).  q NULL: drafts without
+ * probabilities; accepted if accept[node] N < p(x), else N -= p(x) and x is taken out of p.  The walk ends where no continuation is accepted or max_path
+ * nodes are; the next token is then the lowest x whose sum of weights w(0) + .. + w(x) is above choose[r] times the sum of all, w = max(p - c q, 0) (p
+ * without the rejected tokens); where that sum is not above 0, w = p, and if its sum is not either, the token is -1.  All of this in 64 bits.
+ *
+ * dtype         of p and q, ROCO_F32 or ROCO_BF16; 1 <= vocab <= 2^22, 1 <= nodes <= 64 (more: ROCO_EUNSUPPORTED)
+ * p, q          rows of vocab elements, row_stride (>= vocab) elements apart, requests request_stride (>= 0) apart; aligned to their type.  A value that is
+ *               NaN or below zero counts as zero.
+ * tokens        in  [requests, nodes] int32; a token outside the vocabulary is not accepted
+ * parent        in  [requests, nodes] int32, or NULL: a chain.  As in roco_tree_attend, but only what descends from node 0 can be accepted.
+ * n_nodes       in  [requests] int32, 0 .. nodes, or NULL: nodes.  A request without nodes has no path, and -1 for a token.
+ * accept        in  [requests, nodes] fp32, choose in [requests] fp32: uniform in [0, 1)
+ * path          out [requests, max_path] int32, 1 <= max_path <= nodes: the accepted nodes, node 0 first, then -1; n_path out [requests]
+ * next_token    out [requests] int32
+ * path and n_path are what roco_tree_commit takes (n_path may have to be held inside the requests' budgets by max_path).
+ */
+size_t roco_verify_workspace_bytes(int32_t requests, int32_t nodes, int32_t vocab);
+int roco_tree_verify(int32_t dtype, int32_t requests, int32_t nodes, int32_t vocab, const void* p, int64_t p_request_stride, int64_t p_row_stride,
+                     const void* q, int64_t q_request_stride, int64_t q_row_stride, const int32_t* tokens, const int32_t* parent,
+                     const int32_t* n_nodes, const float* accept, const float* choose, int32_t distinct, int32_t max_path, int32_t* path,
+                     int32_t* n_path, int32_t* next_token, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Chunks of new tokens over budgeted caches, dense or in pages: a prompt's next thousand tokens, or one token of a decoding request, and any
+ * mixture of them in one call.  Rows are packed: request r (of units / heads) has the tokens token_start[r] .. token_start[r + 1] - 1, any number of
+ * them from 0 on, token i of them at position qpos0[r] + i.  (token_start is the row_start of roco_page_tables.)
+ *   x_ih = scale q_ih . k + bias over the unit's n_used slots and the request's tokens 0 .. i;   out_ih = sum softmax(x_ih) v,   lse_ih = ln sum exp x_ih
+ * As in roco_tree_attend the cache is not changed, and is seen whole, also where it is full; values of tokens that a row does not see do not reach
+ * it.  Up to 64 tokens are a chain there, with the same results.
+ *
+ * tokens       rows of the packed arrays; rows that are no request's are neither read nor written
+ * q            in  [tokens, heads, group, d] dtype, tokens q_stride elements apart (q_stride >= heads group d)
+ * k_new, v_new in  [tokens, heads, d]        dtype, tokens kv_stride elements apart: q, k_new and v_new may be parts of a fused projection
+ * token_start  in  [requests + 1] int32, ascending, 0 .. tokens;  qpos0 in [requests] int32 (per request, not per unit)
+ * K_cache, V_cache, pos, n_used, pages   in, as in roco_tree_attend
+ * out          out [tokens, heads, group, d] dtype, dense;   lse out [tokens, heads, group] fp32, or NULL
+ * Probabilities of bf16 are rounded to bf16 before they multiply v.
+ * Refused: strides that are not a multiple of 16 bytes (ROCO_EINVAL) or of more than 2^24 bytes, group above 64, tokens heads group of 2^31 or more
+ * (ROCO_EUNSUPPORTED), and what roco_tree_attend refuses of params, heads and pages.
+ */
+size_t roco_chunk_workspace_bytes(const roco_params* params, int32_t heads, int32_t group, int32_t tokens);
+int roco_chunk_attend(const roco_params* params, int32_t heads, int32_t group, int32_t tokens, const roco_pages* pages, const void* q,
+                      int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const int32_t* token_start,
+                      const int32_t* qpos0, const void* K_cache, const void* V_cache, const int32_t* pos, const int32_t* n_used, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Takes the chunks over into the caches: roco_tree_commit for chunks.  Per unit with n = n_used slots, the request's budget B_r and c tokens (of more than
+ * B_r the first B_r; 0: nothing of the request's units changes):
+ *   E = max(0, n + c - B_r) tokens are evicted by the statistics as they stand, as in roco_encode_block (the chunk has still seen them); the chunk's
+ *   tokens go, in order, to the ascending list of freed and still-empty slots, at positions qpos0 + i.
+ *   pbar_i = mean over the group's heads of exp(x_ih - lse_ih) over the remaining older slots and the tokens 0 .. i: Acc += sum_i pbar_i, Acc2 += sum_i
+ *   pbar_i^2, Count += 1 for every row that attended the slot; the chunk's tokens start from 0.  (The other importance scores keep their second plane as
+ *   they do elsewhere.)
+ * next_slot is not kept: before a roco_decode_step, roco_select_victims has to refresh it.
+ *
+ * q, k_new, v_new, strides, token_start, qpos0, heads, group, tokens, pages   as in roco_chunk_attend
+ * lse          in  [tokens, heads, group] fp32 of roco_chunk_attend
+ * K_cache, V_cache, stats, pos, n_used   in/out; disjoint from k_new and v_new
+ * evicted_slot, evicted_pos  out [tokens, heads] int32: the slot that the token took over from an evicted token and that token's position, or -1 (either
+ *              may be NULL)
+ */
+int roco_chunk_commit(const roco_params* params, int32_t heads, int32_t group, int32_t tokens, const roco_pages* pages, const void* q,
+                      int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const float* lse,
+                      const int32_t* token_start, const int32_t* qpos0, void* K_cache, void* V_cache, float* stats, int32_t* pos,
+                      int32_t* n_used, int32_t* evicted_slot, int32_t* evicted_pos, void* workspace, size_t workspace_bytes,
+                      void* hip_stream);
+
+/*
  * Block tables and slot maps from the requests' lengths, on the device: request r, which holds held[r] slots, is to have want[r].
  * It takes the pages that it lacks, ceil(want / page) - ceil(held / page), from the list of free ones, the requests in order:
  *   page_start[r]  = pages taken by the requests before r; page_start[requests] = all
@@ -453,7 +531,8 @@ enum {
   ROCO_PROF_PREFILL_GATHER = 6, ROCO_PROF_READ_PROBE = 7, ROCO_PROF_BLOCK_PREPARE = 8,
   ROCO_PROF_BLOCK_ATTEND = 9, ROCO_PROF_BLOCK_FINISH = 10, ROCO_PROF_MFMA_PROBE = 11, ROCO_PROF_TREE_ATTEND = 12,
   ROCO_PROF_TREE_JOIN = 13, ROCO_PROF_TREE_CHOOSE = 14, ROCO_PROF_TREE_STATISTICS = 15, ROCO_PROF_TREE_APPLY = 16,
-  ROCO_PROF_PAGE_TABLES = 17, ROCO_PROF_PAGE_STORE = 18, ROCO_PROF_KERNELS = 19
+  ROCO_PROF_PAGE_TABLES = 17, ROCO_PROF_PAGE_STORE = 18, ROCO_PROF_CHUNK_ATTEND = 19, ROCO_PROF_CHUNK_JOIN = 20, ROCO_PROF_CHUNK_CHOOSE = 21,
+  ROCO_PROF_CHUNK_COLUMNS = 22, ROCO_PROF_CHUNK_APPLY = 23, ROCO_PROF_VERIFY_PASS = 24, ROCO_PROF_VERIFY_CHOOSE = 25, ROCO_PROF_KERNELS = 26
 };
 int roco_profile_kernel(int which);
 int roco_profile_read(double* total_ms, int64_t* launches);
@@ -524,6 +603,10 @@ int roco_probe_mfma(int32_t workgroups, int32_t iters, int32_t operands, float* 
  *   ROCO_TREE_SPLITS=1..64     splits of the budget in roco_tree_attend (default: about 512 / units, or of more than 64 query rows of
  *                              bf16 those whose rounds of 512 workgroups are shortest); roco_tree_workspace_bytes has to see the
  *                              same value
+ *   ROCO_CHUNK_SPLITS=1..64    workgroups along the keys of a row tile of roco_chunk_attend (default: until three workgroups per compute unit
+ *                              exist); roco_chunk_workspace_bytes has to see the same value
+ *   ROCO_VERIFY_ROUNDS=1..4    passes over the vocabulary that roco_tree_verify makes with the whole chip before a workgroup per request goes on alone
+ *                              (default: 1 for chains, more for trees)
  *   ROCO_SELECT_THREADS=512|1024  threads of the prompt selection (default: 512 for prompts of up to 512 tokens, and of up to 2048
  *                              with more than 256 units)
  *   ROCO_PREFILL_WAVES_PER_ROW=1|4  waves that share a query row of the vector row pass (default: four for few rows)

@@ -131,6 +131,16 @@ def load_library() -> ctypes.CDLL:
     lib.roco_tree_attend.argtypes = [pp, i32, i32, i32, pg, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.roco_tree_commit.restype = ctypes.c_int
     lib.roco_tree_commit.argtypes = [pp, i32, i32, i32, pg, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.roco_chunk_workspace_bytes.restype = sz
+    lib.roco_chunk_workspace_bytes.argtypes = [pp, i32, i32, i32]
+    lib.roco_chunk_attend.restype = ctypes.c_int
+    lib.roco_chunk_attend.argtypes = [pp, i32, i32, i32, pg, vp, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.roco_chunk_commit.restype = ctypes.c_int
+    lib.roco_chunk_commit.argtypes = [pp, i32, i32, i32, pg, vp, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.roco_verify_workspace_bytes.restype = sz
+    lib.roco_verify_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.roco_tree_verify.restype = ctypes.c_int
+    lib.roco_tree_verify.argtypes = [i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.roco_page_tables.restype = ctypes.c_int
     lib.roco_page_tables.argtypes = [i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp]
     lib.roco_page_store.restype = ctypes.c_int
@@ -161,20 +171,22 @@ class _PlainCalls:
     # which of a function's arguments behind the parameters are integers; the others are tensors or addresses
     INTEGERS = {"prefill_compress": (4,), "prefill_compress_gqa": (0, 5), "prefill_compress_lse": (0, 5), "decode_step": (),
                 "decode_step_static": (), "encode_block": (0,), "encode_block_gqa": (0, 1), "decode_step_gqa": (0,),
-                "tree_attend": (0, 1, 2), "tree_commit": (0, 1, 2, 8)}
-    PAGES = {"tree_attend": 3, "tree_commit": 3}  # ... or a RocoPages
+                "tree_attend": (0, 1, 2), "tree_commit": (0, 1, 2, 8), "chunk_attend": (0, 1, 2, 5, 8), "chunk_commit": (0, 1, 2, 5, 8)}
+    PAGES = dict.fromkeys(("tree_attend", "tree_commit", "chunk_attend", "chunk_commit"), 3)  # ... or a RocoPages
     # ... or, of tensors, those whose type is checked
-    INT32 = {"tree_attend": (7, 8, 9, 12, 13), "tree_commit": (9, 10, 11, 15, 16, 17, 18), "page_tables": (3, 4, 5, 7, 8, 9, 10), "page_store": (10,)}
-    FLOAT32 = {"tree_attend": (15,), "tree_commit": (7, 14)}
+    INT32 = {"tree_attend": (7, 8, 9, 12, 13), "tree_commit": (9, 10, 11, 15, 16, 17, 18), "page_tables": (3, 4, 5, 7, 8, 9, 10), "page_store": (10,),
+             "chunk_attend": (9, 10, 13, 14), "chunk_commit": (10, 11, 15, 16, 17, 18), "tree_verify": (10, 11, 12, 17, 18, 19)}
+    FLOAT32 = {"tree_attend": (15,), "tree_commit": (7, 14), "chunk_attend": (16,), "chunk_commit": (9, 14), "tree_verify": (13, 14)}
     # the functions without parameters
-    PLAIN = {"page_tables": (0, 1, 2, 6, 11, 12), "page_store": (0, 1, 2, 3, 4, 7, 8, 9, 13, 14)}
+    PLAIN = {"page_tables": (0, 1, 2, 6, 11, 12), "page_store": (0, 1, 2, 3, 4, 7, 8, 9, 13, 14), "tree_verify": (0, 1, 2, 3, 5, 6, 8, 9, 15, 16)}
+    PLAIN_WORKSPACE = ("tree_verify",)  # ... with a workspace
 
     def __init__(self, lib):
         for name, integers in self.INTEGERS.items():
             setattr(self, name, self._function(getattr(lib, "roco_" + name), self._conversions(name, integers), name != "decode_step_static",
                                                self.PAGES.get(name)))
         for name, integers in self.PLAIN.items():
-            setattr(self, name, self._plain(getattr(lib, "roco_" + name), self._conversions(name, integers)))
+            setattr(self, name, self._plain(getattr(lib, "roco_" + name), self._conversions(name, integers), name in self.PLAIN_WORKSPACE))
 
     def _conversions(self, name, integers):
         how = dict.fromkeys(integers, int)
@@ -198,10 +210,14 @@ class _PlainCalls:
         return call
 
     @staticmethod
-    def _plain(fn, how):
+    def _plain(fn, how, has_workspace):
         def call(*args):
             *args, stream = args
-            return fn(*[how.get(i, _ptr)(a) for i, a in enumerate(args)], _stream(stream))
+            size = ()
+            if has_workspace:
+                *args, workspace_bytes = args
+                size = (int(args[-1].nbytes if workspace_bytes is None else workspace_bytes),)
+            return fn(*[how.get(i, _ptr)(a) for i, a in enumerate(args)], *size, _stream(stream))
         return call
 
 
@@ -222,7 +238,7 @@ def _bind_native(lib) -> None:
     native.bind(tuple(address(getattr(lib, name)) for name in (
         "roco_prefill_compress", "roco_prefill_compress_gqa", "roco_prefill_compress_lse", "roco_decode_step",
         "roco_decode_step_static", "roco_encode_block", "roco_encode_block_gqa", "roco_decode_step_gqa", "roco_tree_attend",
-        "roco_tree_commit", "roco_page_tables", "roco_page_store")),
+        "roco_tree_commit", "roco_page_tables", "roco_page_store", "roco_chunk_attend", "roco_chunk_commit", "roco_tree_verify")),
         torch.Tensor, torch.nn.Parameter, RocoParams, RocoPages, _ptr, _words, _stream)
     if _native is None and hasattr(os, "register_at_fork"):
         os.register_at_fork(after_in_child=native.forget_gpu)  # a forked child is refused by torch, as before
@@ -255,7 +271,8 @@ def decode_workspace_bytes(params: RocoParams) -> int:
 PROF_KERNELS = {"decode_select": 0, "decode_attend": 1, "decode_finish": 2, "prefill_rows": 3,
                 "prefill_columns": 4, "prefill_select": 5, "prefill_gather": 6, "read_probe": 7,
                 "block_prepare": 8, "block_attend": 9, "block_finish": 10, "mfma_probe": 11, "tree_attend": 12, "tree_join": 13,
-                "tree_choose": 14, "tree_statistics": 15, "tree_apply": 16, "page_tables": 17, "page_store": 18}
+                "tree_choose": 14, "tree_statistics": 15, "tree_apply": 16, "page_tables": 17, "page_store": 18,
+                "chunk_attend": 19, "chunk_join": 20, "chunk_choose": 21, "chunk_columns": 22, "chunk_apply": 23, "verify_pass": 24, "verify_choose": 25}
 
 
 def roco_profile_kernel(which: int) -> None:
@@ -429,6 +446,102 @@ def roco_tree_commit(params: RocoParams, heads: int, group: int, nodes: int, pag
                               stats, pos, n_used, evicted_slot, evicted_pos, workspace, workspace_bytes, stream)
     if rc != 0:
         raise RocoError(rc, "roco_tree_commit")
+
+
+def verify_workspace_bytes(requests: int, nodes: int, vocab: int) -> int:
+    return int(load_library().roco_verify_workspace_bytes(int(requests), int(nodes), int(vocab)))
+
+
+def roco_tree_verify(p, q, tokens, parent, n_nodes, accept, choose, path, n_path, next_token, workspace, distinct: bool = False,
+                     workspace_bytes: Optional[int] = None, stream=None) -> None:
+    """See include/roco.h: the path of drafted trees that the target's probabilities take, and the token behind it.  `p`, and `q` or None,
+    [requests, nodes, vocab] of any strides but the last dimension's; `path` [requests, max_path]; `parent` and `n_nodes` may be None."""
+    shape = p.shape
+    requests, nodes, vocab = shape
+    *p_strides, last = p.stride()
+    q_strides, q_rows = (0, vocab), None
+    if q is not None:
+        if q.shape != shape or q.dtype != p.dtype:
+            raise ValueError("roco: p and q are [requests, nodes, vocab] of one type")
+        *q_strides, q_last = q.stride()
+        q_rows, last = q.data_ptr(), last if last != 1 else q_last
+        if nodes == 1:
+            q_strides[1] = vocab
+    if last != 1 and vocab > 1:
+        raise ValueError("roco: a row's probabilities lie side by side")
+    if nodes == 1:  # the stride of a dimension of one element means nothing
+        p_strides[1] = vocab
+    each, all_nodes = (requests,), (requests, nodes)
+    for t, of in ((tokens, all_nodes), (accept, all_nodes), (choose, each), (n_path, each), (next_token, each), (parent, all_nodes), (n_nodes, each)):
+        if t is not None and t.shape != of:
+            raise ValueError("roco: tokens, parent and accept are [requests, nodes], n_nodes, choose, n_path and next_token [requests]")
+    if path.dim() != 2 or path.shape[0] != requests:
+        raise ValueError("roco: path is [requests, max_path]")
+    rc = _calls().tree_verify(_dtype_code(p.dtype), requests, nodes, vocab, p.data_ptr(), *p_strides, q_rows, *q_strides, tokens, parent, n_nodes, accept,
+                              choose, bool(distinct), path.shape[1], path, n_path, next_token, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise RocoError(rc, "roco_tree_verify")
+
+
+def chunk_workspace_bytes(params: RocoParams, heads: int, group: int, tokens: int) -> int:
+    return int(load_library().roco_chunk_workspace_bytes(ctypes.byref(params), int(heads), int(group), int(tokens)))
+
+
+def _chunk_rows(params, heads, group, q, k_new, v_new, token_start, qpos0):
+    """(tokens, distance of the tokens in q, in k_new and v_new) of packed rows, or a ValueError."""
+    tokens, d, dtype = q.shape[0], params.head_dim, q.dtype
+    strides = []
+    for t, rows in ((q, heads * group), (k_new, heads), (v_new, heads)):
+        shape, steps = t.shape, t.stride()
+        dense = 1
+        for n, step in zip(shape[:0:-1], steps[:0:-1]):
+            if step != dense and n != 1:
+                break
+            dense *= n
+        if shape[0] != tokens or shape[-1] != d or dense != rows * d or t.dtype != dtype:
+            raise ValueError("roco: rows are [tokens, heads x group, d] and [tokens, heads, d] of one type, a token's side by side")
+        strides.append(steps[0] if tokens > 1 else rows * d)
+    if strides[1] != strides[2]:
+        raise ValueError("roco: the rows of V lie as those of K")
+    if _dtype_code(dtype) != params.dtype:
+        raise ValueError("roco: the rows are of the parameters' type")
+    requests = params.units // max(heads, 1)
+    if token_start.numel() != requests + 1 or qpos0.numel() != requests:
+        raise ValueError("roco: token_start is [requests + 1], qpos0 [requests]")
+    return tokens, strides[0], strides[1]
+
+
+def roco_chunk_attend(params: RocoParams, heads: int, group: int, pages: Optional[RocoPages], q, k_new, v_new, token_start, qpos0, K_cache, V_cache,
+                      pos, n_used, out, lse, workspace, workspace_bytes: Optional[int] = None, stream=None) -> None:
+    """See include/roco.h: attention of chunks of new tokens over the budgeted cache, which is not changed.  q [tokens, heads x group, d] (or [tokens,
+    heads, group, d]), k_new and v_new [tokens, heads, d], of any distance between tokens; `pages` and `lse` may be None.  No tokens: nothing is done."""
+    tokens, q_stride, kv_stride = _chunk_rows(params, heads, group, q, k_new, v_new, token_start, qpos0)
+    if out.numel() != tokens * heads * group * params.head_dim or out.dtype != q.dtype or (lse is not None and lse.numel() != tokens * heads * group):
+        raise ValueError("roco: out is [tokens, heads x group, d] of the rows' type, lse [tokens, heads x group]")
+    if tokens == 0:
+        return
+    rc = _calls().chunk_attend(params, heads, group, tokens, pages, q.data_ptr(), q_stride, k_new.data_ptr(), v_new.data_ptr(), kv_stride, token_start, qpos0,
+                               K_cache, V_cache, pos, n_used, out, lse, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise RocoError(rc, "roco_chunk_attend")
+
+
+def roco_chunk_commit(params: RocoParams, heads: int, group: int, pages: Optional[RocoPages], q, k_new, v_new, lse, token_start, qpos0, K_cache, V_cache,
+                      stats, pos, n_used, evicted_slot, evicted_pos, workspace, workspace_bytes: Optional[int] = None, stream=None) -> None:
+    """See include/roco.h: takes chunks over into the budgeted cache.  Rows as in roco_chunk_attend; `pages`, `evicted_slot` and `evicted_pos` may be
+    None.  No tokens: nothing changes."""
+    tokens, q_stride, kv_stride = _chunk_rows(params, heads, group, q, k_new, v_new, token_start, qpos0)
+    if lse.numel() != tokens * heads * group:
+        raise ValueError("roco: lse is [tokens, heads x group]")
+    for t in (evicted_slot, evicted_pos):
+        if t is not None and t.numel() != tokens * heads:
+            raise ValueError("roco: evicted_slot and evicted_pos are [tokens, heads]")
+    if tokens == 0:
+        return
+    rc = _calls().chunk_commit(params, heads, group, tokens, pages, q.data_ptr(), q_stride, k_new.data_ptr(), v_new.data_ptr(), kv_stride, lse, token_start,
+                               qpos0, K_cache, V_cache, stats, pos, n_used, evicted_slot, evicted_pos, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise RocoError(rc, "roco_chunk_commit")
 
 
 def roco_page_tables(held, want, page: int, free_pages, table, page_start, row_start, slot_map, stream=None) -> None:

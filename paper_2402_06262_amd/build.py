@@ -12,9 +12,10 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libroco.so")
 NATIVE_PATH = os.path.join(HERE, "_native.so")  # extension module of the binding (host code)
 SOURCES = ["api.hip", "decode.hip", "prefill_simple.hip", "prefill_mfma.hip", "prefill_planes.hip",
-           "select_compact.hip", "block.hip", "block_fused.hip", "profile.hip", "tree.hip", "tree_commit.hip", "pages.hip"]
+           "select_compact.hip", "block.hip", "block_fused.hip", "profile.hip", "tree.hip", "tree_commit.hip", "pages.hip",
+           "chunk.hip", "verify.hip"]
 SOURCES += [f"block_fused_{shape}_{d}.hip" for d in (128, 64) for shape in ("eight", "pairs", "rows8", "rows4", "halves")]
-SOURCES += [f"tree_attend_{dtype}_{d}.hip" for dtype in ("bf16", "f32") for d in (128, 64)]
+SOURCES += [f"{kernel}_{dtype}_{d}.hip" for kernel in ("tree_attend", "chunk_attend", "chunk_columns") for dtype in ("bf16", "f32") for d in (128, 64)]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -134,6 +134,83 @@ int check_tree(const roco_params* p, int32_t heads, int32_t group, int32_t nodes
   return ROCO_OK;
 }
 
+// ---- chunks: tree_attend's checks, and the packed rows
+int check_chunk_shape(const roco_params* p, int32_t heads, int32_t group, int32_t tokens) {
+  const int rc = check_tree_shape(p, group, 1);
+  if (rc != ROCO_OK) return rc;
+  if (heads < 1 || p->units % heads != 0 || tokens < 1) return ROCO_EINVAL;
+  if (static_cast<long long>(tokens) * heads * group >= (1ll << 31)) return ROCO_EUNSUPPORTED;
+  // (workgroups: of the attention's row tiles, of the sums' keys, of the slots)
+  const long long requests = p->units / heads, tiles = (static_cast<long long>(tokens) * group / 128 + requests) * heads;
+  const long long slots = static_cast<long long>(p->units) * ((p->budget + 127) / 128) + (tokens / 128 + requests) * heads;
+  return tiles < kMostWorkgroups && slots < kMostWorkgroups ? ROCO_OK : ROCO_EUNSUPPORTED;
+}
+// A token's rows, `count` of them, lie side by side; the tokens `stride` elements apart.
+int check_stride(const roco_params* p, int64_t stride, long long count) {
+  const long long element = p->dtype == ROCO_BF16 ? 2 : 4;
+  if (stride < count * p->head_dim || stride * element % 16 != 0) return ROCO_EINVAL;
+  return stride * element <= (1ll << 24) ? ROCO_OK : ROCO_EUNSUPPORTED;
+}
+
+// ---- workspace of the chunks: chunk_attend's part_m | part_l | part_o, or chunk_commit's info | mark | sums | fresh | keys
+struct ChunkLayout { size_t part_l, part_o, mark, sums, fresh, keys, total; int splits; };
+ChunkLayout chunk_layout(const roco_params* p, int32_t heads, int32_t group, int32_t tokens) {
+  ChunkLayout l;
+  const size_t U = p->units, B = p->budget, rows = static_cast<size_t>(tokens) * heads * group;
+  l.splits = chunk_attend_splits(p->dtype, p->head_dim, p->units / heads, heads, group, tokens, p->budget);
+  const size_t parts = l.splits > 1 ? rows * l.splits : 0;
+  l.part_l = align_up(parts * sizeof(float));
+  l.part_o = 2 * l.part_l;
+  const size_t attend = l.part_o + align_up(parts * p->head_dim * sizeof(float));
+  l.mark = align_up(U * 4 * sizeof(int32_t));
+  l.sums = l.mark + align_up(U * B * sizeof(int32_t));
+  l.fresh = l.sums + align_up(U * 2 * B * sizeof(float));
+  l.keys = l.fresh + align_up(static_cast<size_t>(tokens) * heads * 2 * sizeof(float));
+  const size_t commit = l.keys + (p->budget > kMaxDecodeBudgetLds ? align_up(U * 2 * B * sizeof(uint32_t)) : 0);
+  l.total = std::max(attend, commit);
+  return l;
+}
+// What the two calls of chunks have in common.
+int chunk_args(const roco_params* params, int32_t heads, int32_t group, int32_t tokens, const roco_pages* pages, const void* q, int64_t q_stride,
+               const void* k_new, const void* v_new, int64_t kv_stride, const int32_t* token_start, const int32_t* qpos0, const void* K_cache,
+               const void* V_cache, const int32_t* pos, const int32_t* n_used, const void* workspace, size_t workspace_bytes, ChunkArgs& a, ChunkLayout& lay) {
+  int rc = check_chunk_shape(params, heads, group, tokens);
+  if (rc != ROCO_OK) return rc;
+  a = ChunkArgs{};
+  rc = check_tree(params, heads, group, 1, pages, a.pages);
+  if (rc != ROCO_OK) return rc;
+  rc = check_stride(params, q_stride, static_cast<long long>(heads) * group);
+  if (rc != ROCO_OK) return rc;
+  rc = check_stride(params, kv_stride, heads);
+  if (rc != ROCO_OK) return rc;
+  const void* need[] = {q, k_new, v_new, K_cache, V_cache, workspace};
+  for (const void* ptr : need)
+    if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
+  if (!given(token_start) || !given(qpos0) || !given(pos) || !given(n_used)) return ROCO_EINVAL;
+  lay = chunk_layout(params, heads, group, tokens);
+  if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
+  const int64_t element = params->dtype == ROCO_BF16 ? 2 : 4;
+  a.units = params->units; a.requests = params->units / heads; a.heads = heads; a.group = group; a.tokens = tokens;
+  a.B = params->budget; a.scope = params->scope;
+  a.splits = lay.splits;
+  a.pol = policy_of(params);
+  a.scale_log2 = scale_log2(params);
+  a.recency_window = params->recency_window;
+  a.recency_bias_log2 = params->recency_bias * 1.4426950408889634f;
+  a.q = q; a.k_new = k_new; a.v_new = v_new; a.q_stride = q_stride * element; a.kv_stride = kv_stride * element;
+  a.start = token_start; a.qpos0 = qpos0;
+  a.K = const_cast<void*>(K_cache); a.V = const_cast<void*>(V_cache);
+  a.pos = const_cast<int32_t*>(pos); a.n_used = const_cast<int32_t*>(n_used);
+  return ROCO_OK;
+}
+
+// ---- verification
+int check_verify(int32_t requests, int32_t nodes, int32_t vocab) {
+  if (requests < 1 || nodes < 1 || vocab < 1) return ROCO_EINVAL;
+  return requests <= 65535 && nodes <= kMaxTreeNodes && vocab <= kMaxVocab ? ROCO_OK : ROCO_EUNSUPPORTED;
+}
+int verify_blocks(int32_t vocab) { return (vocab + 7 + kVerifyBlock - 1) / kVerifyBlock; }  // (the first begins up to seven elements before the row)
+
 // ---- workspace of the trees: tree_attend's part_m | part_l | part_o, or tree_commit's taken | sums | fresh | keys
 struct TreeLayout { size_t part_l, part_o, sums, fresh, keys, total; TreeSplits split; };
 TreeLayout tree_layout(const roco_params* p, int32_t group, int32_t nodes) {
@@ -595,6 +672,82 @@ int roco_tree_commit(const roco_params* params, int32_t heads, int32_t group, in
   a.fresh = reinterpret_cast<float*>(ws + lay.fresh);
   a.keys = reinterpret_cast<uint32_t*>(ws + lay.keys);
   return launch_tree_commit(params->dtype, params->head_dim, a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
+}
+
+size_t roco_chunk_workspace_bytes(const roco_params* params, int32_t heads, int32_t group, int32_t tokens) {
+  if (check_chunk_shape(params, heads, group, tokens) != ROCO_OK) return 0;
+  return chunk_layout(params, heads, group, tokens).total;
+}
+
+int roco_chunk_attend(const roco_params* params, int32_t heads, int32_t group, int32_t tokens, const roco_pages* pages, const void* q,
+                      int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const int32_t* token_start,
+                      const int32_t* qpos0, const void* K_cache, const void* V_cache, const int32_t* pos, const int32_t* n_used, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  ChunkArgs a;
+  ChunkLayout lay;
+  const int rc = chunk_args(params, heads, group, tokens, pages, q, q_stride, k_new, v_new, kv_stride, token_start, qpos0, K_cache, V_cache, pos, n_used,
+                            workspace, workspace_bytes, a, lay);
+  if (rc != ROCO_OK) return rc;
+  if (out == nullptr || !aligned16(out) || !aligned4(lse)) return ROCO_EINVAL;
+  a.out = out; a.lse = lse;
+  char* ws = static_cast<char*>(workspace);
+  a.part_m = reinterpret_cast<float*>(ws);
+  a.part_l = reinterpret_cast<float*>(ws + lay.part_l);
+  a.part_o = reinterpret_cast<float*>(ws + lay.part_o);
+  return launch_chunk_attend(params->dtype, params->head_dim, a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
+}
+
+int roco_chunk_commit(const roco_params* params, int32_t heads, int32_t group, int32_t tokens, const roco_pages* pages, const void* q,
+                      int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const float* lse,
+                      const int32_t* token_start, const int32_t* qpos0, void* K_cache, void* V_cache, float* stats, int32_t* pos,
+                      int32_t* n_used, int32_t* evicted_slot, int32_t* evicted_pos, void* workspace, size_t workspace_bytes,
+                      void* hip_stream) {
+  ChunkArgs a;
+  ChunkLayout lay;
+  const int rc = chunk_args(params, heads, group, tokens, pages, q, q_stride, k_new, v_new, kv_stride, token_start, qpos0, K_cache, V_cache, pos, n_used,
+                            workspace, workspace_bytes, a, lay);
+  if (rc != ROCO_OK) return rc;
+  if (!given(lse) || !given(stats) || !aligned4(evicted_slot) || !aligned4(evicted_pos)) return ROCO_EINVAL;
+  a.lse = const_cast<float*>(lse); a.stats = stats; a.evicted_slot = evicted_slot; a.evicted_pos = evicted_pos;
+  char* ws = static_cast<char*>(workspace);
+  a.info = reinterpret_cast<int32_t*>(ws);
+  a.mark = reinterpret_cast<int32_t*>(ws + lay.mark);
+  a.sums = reinterpret_cast<float*>(ws + lay.sums);
+  a.fresh = reinterpret_cast<float*>(ws + lay.fresh);
+  a.keys = reinterpret_cast<uint32_t*>(ws + lay.keys);
+  return launch_chunk_commit(params->dtype, params->head_dim, a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
+}
+
+size_t roco_verify_workspace_bytes(int32_t requests, int32_t nodes, int32_t vocab) {
+  if (check_verify(requests, nodes, vocab) != ROCO_OK) return 0;
+  return align_up(static_cast<size_t>(kMaxVerifyRounds) * requests * verify_blocks(vocab) * sizeof(double));
+}
+
+int roco_tree_verify(int32_t dtype, int32_t requests, int32_t nodes, int32_t vocab, const void* p, int64_t p_request_stride, int64_t p_row_stride,
+                     const void* q, int64_t q_request_stride, int64_t q_row_stride, const int32_t* tokens, const int32_t* parent,
+                     const int32_t* n_nodes, const float* accept, const float* choose, int32_t distinct, int32_t max_path, int32_t* path,
+                     int32_t* n_path, int32_t* next_token, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (dtype != ROCO_F32 && dtype != ROCO_BF16) return ROCO_EUNSUPPORTED;
+  const int rc = check_verify(requests, nodes, vocab);
+  if (rc != ROCO_OK) return rc;
+  if (max_path < 1 || max_path > nodes) return ROCO_EINVAL;
+  const uintptr_t element = dtype == ROCO_BF16 ? 2 : 4;
+  const auto rows_ok = [&](const void* rows, int64_t request_stride, int64_t row_stride) {
+    return reinterpret_cast<uintptr_t>(rows) % element == 0 && row_stride >= vocab && request_stride >= 0 && row_stride <= (1ll << 40) && request_stride <= (1ll << 44);
+  };
+  if (p == nullptr || !rows_ok(p, p_request_stride, p_row_stride)) return ROCO_EINVAL;
+  if (q != nullptr && !rows_ok(q, q_request_stride, q_row_stride)) return ROCO_EINVAL;
+  const void* words[] = {tokens, accept, choose, path, n_path, next_token};
+  for (const void* ptr : words)
+    if (!given(ptr)) return ROCO_EINVAL;
+  if (!aligned4(parent) || !aligned4(n_nodes) || workspace == nullptr || !aligned16(workspace)) return ROCO_EINVAL;
+  if (workspace_bytes < roco_verify_workspace_bytes(requests, nodes, vocab)) return ROCO_EWORKSPACE;
+  // A chain has one pass: behind its first rejection, or its end.  A tree has one more for every rejection that another continuation follows.
+  int rounds = env_int("ROCO_VERIFY_ROUNDS", 0);
+  if (rounds < 1 || rounds > kMaxVerifyRounds) rounds = parent == nullptr || nodes <= 2 ? 1 : 3;
+  const VerifyArgs a = {requests, nodes, vocab, distinct != 0, max_path, dtype == ROCO_BF16, p, q, p_request_stride, p_row_stride, q_request_stride, q_row_stride,
+                        tokens, parent, n_nodes, accept, choose, path, n_path, next_token, static_cast<double*>(workspace), verify_blocks(vocab), rounds};
+  return launch_tree_verify(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
 }
 
 int roco_page_tables(int32_t requests, int32_t page, int32_t max_pages, const int32_t* held, const int32_t* want,

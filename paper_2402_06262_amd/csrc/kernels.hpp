@@ -230,6 +230,58 @@ struct CommitArgs {
 constexpr int kTakenWords = 4 + kMaxTreeNodes;
 hipError_t launch_tree_commit(int dtype, int head_dim, const CommitArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------- chunks of new tokens
+// Packed rows: request r has the tokens start[r] .. start[r + 1] - 1 of `tokens`; a unit's query rows are (token, head) pairs, the heads of a
+// token side by side.
+struct ChunkArgs {
+  int units, requests, heads, group, tokens, B, scope;
+  int splits;             // chunk_attend: workgroups along a row tile's keys
+  int streaming;          // as DecodeArgs::streaming
+  Policy pol;
+  float scale_log2;
+  int recency_window;
+  float recency_bias_log2;
+  const void *q, *k_new, *v_new;              // q [tokens][heads][group][d], k_new / v_new [tokens][heads][d], tokens q_stride / kv_stride bytes apart
+  int64_t q_stride, kv_stride;
+  const int32_t *start, *qpos0;               // [requests + 1], [requests]
+  void *K, *V;
+  int32_t *pos, *n_used;                      // [units][B], [units]
+  CachePages pages;
+  // chunk_attend
+  void* out;                                  // [tokens][heads][group][d]
+  float* lse;                                 // [tokens][heads][group]: written, may be null; chunk_commit: read
+  float *part_m, *part_l, *part_o;            // workspace, with more than one split: [splits][tokens * heads * group] (part_o: [d])
+  // chunk_commit
+  float* stats;
+  int32_t *evicted_slot, *evicted_pos;        // [tokens][heads], may be null
+  int32_t* mark;                              // workspace [units][B]: the token that takes the slot, or -1
+  int32_t* info;                              // workspace [units][4]: tokens taken over, slots held before, slots held then, -
+  float* sums;                                // workspace [units][2][B]: what the chunk's rows add to Acc and Acc2 of the slots held before (below zero: not seen)
+  float* fresh;                               // workspace [2][tokens][heads]: ... and of the tokens themselves
+  uint32_t* keys;                             // workspace [units][2][B] when B is too large for LDS
+};
+int chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
+hipError_t launch_chunk_attend(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);
+hipError_t launch_chunk_commit(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);
+constexpr int kMostChunkSplits = 64;
+
+// ---------------------------------------------------------------- verification of drafted tokens
+struct VerifyArgs {
+  int requests, nodes, vocab, distinct, max_path;
+  int bf16;               // type of p and q
+  const void *p, *q;      // q may be null: drafts without probabilities
+  int64_t p_request, p_row, q_request, q_row;  // strides in elements
+  const int32_t *tokens, *parent, *n_nodes;
+  const float *accept, *choose;
+  int32_t *path, *n_path, *next;
+  double* sums;           // workspace [rounds][requests][blocks]
+  int blocks, rounds;
+};
+constexpr int kVerifyBlock = 2048;    // of the vocabulary: what a partial sum covers
+constexpr int kMaxVerifyRounds = 4;
+constexpr int kMaxVocab = 1 << 22;
+hipError_t launch_tree_verify(const VerifyArgs& a, hipStream_t s);
+
 struct PageTableArgs {
   int requests, page_log2, max_pages, n_free, rows, padded;
   const int32_t *held, *want, *free_pages;    // held may be null

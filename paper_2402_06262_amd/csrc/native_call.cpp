@@ -38,6 +38,9 @@ struct Functions {
   decltype(&roco_tree_commit) tree_commit;
   decltype(&roco_page_tables) page_tables;
   decltype(&roco_page_store) page_store;
+  decltype(&roco_chunk_attend) chunk_attend;
+  decltype(&roco_chunk_commit) chunk_commit;
+  decltype(&roco_tree_verify) tree_verify;
 } g_fn;
 
 // ------------------------------------------------------------------ arguments
@@ -362,12 +365,83 @@ PyObject* page_store(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (params, heads, group, tokens, pages, q, q_stride, k_new, v_new, kv_stride, 9 pointers, workspace_bytes, stream)
+PyObject* chunk_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 21, [&] {
+    const roco_params p = params_of(a[0]);
+    const int32_t heads = int32_of(a[1]), group = int32_of(a[2]), tokens = int32_of(a[3]);
+    const Pages pages(a[4]);
+    void* const q = pointer(a[5]);
+    const int64_t q_stride = static_cast<int64_t>(integer(a[6]));
+    void *const k_new = pointer(a[7]), *const v_new = pointer(a[8]);
+    const int64_t kv_stride = static_cast<int64_t>(integer(a[9]));
+    const int32_t *const start = words<int32_t>(a[10]), *const qpos0 = words<int32_t>(a[11]);
+    void *const k = pointer(a[12]), *const v = pointer(a[13]);
+    const int32_t *const pos = words<int32_t>(a[14]), *const n_used = words<int32_t>(a[15]);
+    void* const out = pointer(a[16]);
+    float* const lse = words<float>(a[17]);
+    void* const workspace = pointer(a[18]);
+    const size_t ws = bytes(a[19], a[18]);
+    void* const s = stream_of(a[20]);
+    NoGil g;
+    return g_fn.chunk_attend(&p, heads, group, tokens, pages.p, q, q_stride, k_new, v_new, kv_stride, start, qpos0, k, v, pos, n_used, out, lse, workspace, ws, s);
+  });
+}
+// (params, heads, group, tokens, pages, q, q_stride, k_new, v_new, kv_stride, lse, 9 pointers, workspace, workspace_bytes, stream)
+PyObject* chunk_commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 23, [&] {
+    const roco_params p = params_of(a[0]);
+    const int32_t heads = int32_of(a[1]), group = int32_of(a[2]), tokens = int32_of(a[3]);
+    const Pages pages(a[4]);
+    void* const q = pointer(a[5]);
+    const int64_t q_stride = static_cast<int64_t>(integer(a[6]));
+    void *const k_new = pointer(a[7]), *const v_new = pointer(a[8]);
+    const int64_t kv_stride = static_cast<int64_t>(integer(a[9]));
+    const float* const lse = words<float>(a[10]);
+    const int32_t *const start = words<int32_t>(a[11]), *const qpos0 = words<int32_t>(a[12]);
+    void *const k = pointer(a[13]), *const v = pointer(a[14]);
+    float* const stats = words<float>(a[15]);
+    int32_t* state[4];  // pos, n_used, evicted_slot, evicted_pos
+    for (int i = 0; i < 4; ++i) state[i] = words<int32_t>(a[16 + i]);
+    void* const workspace = pointer(a[20]);
+    const size_t ws = bytes(a[21], a[20]);
+    void* const s = stream_of(a[22]);
+    NoGil g;
+    return g_fn.chunk_commit(&p, heads, group, tokens, pages.p, q, q_stride, k_new, v_new, kv_stride, lse, start, qpos0, k, v, stats, state[0], state[1],
+                             state[2], state[3], workspace, ws, s);
+  });
+}
+// (dtype, requests, nodes, vocab, p, two strides, q, two strides, tokens, parent, n_nodes, accept, choose, distinct, max_path, path, n_path, next,
+// workspace, workspace_bytes, stream)
+PyObject* tree_verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 23, [&] {
+    int32_t size[4];
+    for (int i = 0; i < 4; ++i) size[i] = int32_of(a[i]);
+    void* const p = pointer(a[4]);
+    const int64_t p_request = static_cast<int64_t>(integer(a[5])), p_row = static_cast<int64_t>(integer(a[6]));
+    void* const q = pointer(a[7]);
+    const int64_t q_request = static_cast<int64_t>(integer(a[8])), q_row = static_cast<int64_t>(integer(a[9]));
+    int32_t* in[3];
+    for (int i = 0; i < 3; ++i) in[i] = words<int32_t>(a[10 + i]);
+    const float *const accept = words<float>(a[13]), *const choose = words<float>(a[14]);
+    const int32_t distinct = int32_of(a[15]), max_path = int32_of(a[16]);
+    int32_t* out[3];
+    for (int i = 0; i < 3; ++i) out[i] = words<int32_t>(a[17 + i]);
+    void* const workspace = pointer(a[20]);
+    const size_t ws = bytes(a[21], a[20]);
+    void* const s = stream_of(a[22]);
+    NoGil g;
+    return g_fn.tree_verify(size[0], size[1], size[2], size[3], p, p_request, p_row, q, q_request, q_row, in[0], in[1], in[2], accept, choose, distinct, max_path,
+                            out[0], out[1], out[2], workspace, ws, s);
+  });
+}
+
 // bind(addresses, tensor, parameter, RocoParams, RocoPages, _ptr, _words, _stream); use_gpu(getCurrentRawStream, getDevice)
 PyObject* bind(PyObject*, PyObject* args) {
-  unsigned long long f[12];
+  unsigned long long f[15];
   PyObject *tensor, *parameter, *params, *pages, *ptr, *typed, *stream;
-  if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKK)OOO!O!OOO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9], &f[10],
-                        &f[11], &tensor, &parameter, &PyType_Type, &params, &PyType_Type, &pages, &ptr, &typed,
+  if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKKKKK)OOO!O!OOO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9], &f[10],
+                        &f[11], &f[12], &f[13], &f[14], &tensor, &parameter, &PyType_Type, &params, &PyType_Type, &pages, &ptr, &typed,
                         &stream))
     return nullptr;
   g_fn.prefill = reinterpret_cast<decltype(g_fn.prefill)>(f[0]);
@@ -382,6 +456,9 @@ PyObject* bind(PyObject*, PyObject* args) {
   g_fn.tree_commit = reinterpret_cast<decltype(g_fn.tree_commit)>(f[9]);
   g_fn.page_tables = reinterpret_cast<decltype(g_fn.page_tables)>(f[10]);
   g_fn.page_store = reinterpret_cast<decltype(g_fn.page_store)>(f[11]);
+  g_fn.chunk_attend = reinterpret_cast<decltype(g_fn.chunk_attend)>(f[12]);
+  g_fn.chunk_commit = reinterpret_cast<decltype(g_fn.chunk_commit)>(f[13]);
+  g_fn.tree_verify = reinterpret_cast<decltype(g_fn.tree_verify)>(f[14]);
   Py_INCREF(tensor); Py_INCREF(parameter); Py_INCREF(params); Py_INCREF(pages); Py_INCREF(ptr); Py_INCREF(typed); Py_INCREF(stream);
   Py_XSETREF(g_tensor_types[0], tensor);
   Py_XSETREF(g_tensor_types[1], parameter);
@@ -411,7 +488,7 @@ PyObject* forget_gpu(PyObject*, PyObject*) {  // in a forked child
 PyMethodDef methods[] = {
     FAST(decode_step), FAST(decode_step_static), FAST(decode_step_gqa), FAST(encode_block), FAST(encode_block_gqa),
     FAST(prefill_compress), FAST(prefill_compress_gqa), FAST(prefill_compress_lse), FAST(tree_attend), FAST(tree_commit),
-    FAST(page_tables), FAST(page_store),
+    FAST(page_tables), FAST(page_store), FAST(chunk_attend), FAST(chunk_commit), FAST(tree_verify),
     {"bind", bind, METH_VARARGS, nullptr}, {"use_gpu", use_gpu, METH_VARARGS, nullptr},
     {"forget_gpu", forget_gpu, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef FAST

@@ -10,7 +10,8 @@ enum ProfKernel : int {
   kProfBlockPrepare = 8, kProfBlockAttend = 9, kProfBlockFinish = 10,
   kProfMfmaProbe = 11,
   kProfTreeAttend = 12, kProfTreeJoin = 13, kProfTreeChoose = 14, kProfTreeStatistics = 15, kProfTreeApply = 16, kProfPageTables = 17, kProfPageStore = 18,
-  kProfKernels = 19
+  kProfChunkAttend = 19, kProfChunkJoin = 20, kProfChunkChoose = 21, kProfChunkColumns = 22, kProfChunkApply = 23, kProfVerifyPass = 24, kProfVerifyChoose = 25,
+  kProfKernels = 26
 };
 
 extern int g_prof_which;  // -1 = off
