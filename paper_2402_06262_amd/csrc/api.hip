@@ -140,8 +140,8 @@ int check_chunk_shape(const roco_params* p, int32_t heads, int32_t group, int32_
   if (rc != ROCO_OK) return rc;
   if (heads < 1 || p->units % heads != 0 || tokens < 1) return ROCO_EINVAL;
   if (static_cast<long long>(tokens) * heads * group >= (1ll << 31)) return ROCO_EUNSUPPORTED;
-  // (workgroups: of the attention's row tiles, of the sums' keys, of the slots)
-  const long long requests = p->units / heads, tiles = (static_cast<long long>(tokens) * group / 128 + requests) * heads;
+  // (workgroups: of the attention's row tiles and, 32 rows each, their joining, of the sums' keys, of the slots)
+  const long long requests = p->units / heads, tiles = (static_cast<long long>(tokens) * group / 32 + 8 * requests) * heads;
   const long long slots = static_cast<long long>(p->units) * ((p->budget + 127) / 128) + (tokens / 128 + requests) * heads;
   return tiles < kMostWorkgroups && slots < kMostWorkgroups ? ROCO_OK : ROCO_EUNSUPPORTED;
 }
@@ -153,12 +153,12 @@ int check_stride(const roco_params* p, int64_t stride, long long count) {
 }
 
 // ---- workspace of the chunks: chunk_attend's part_m | part_l | part_o, or chunk_commit's info | mark | sums | fresh | keys
-struct ChunkLayout { size_t part_l, part_o, mark, sums, fresh, keys, total; int splits; };
+struct ChunkLayout { size_t part_l, part_o, mark, sums, fresh, keys, total; ChunkSplits split; };
 ChunkLayout chunk_layout(const roco_params* p, int32_t heads, int32_t group, int32_t tokens) {
   ChunkLayout l;
   const size_t U = p->units, B = p->budget, rows = static_cast<size_t>(tokens) * heads * group;
-  l.splits = chunk_attend_splits(p->dtype, p->head_dim, p->units / heads, heads, group, tokens, p->budget);
-  const size_t parts = l.splits > 1 ? rows * l.splits : 0;
+  l.split = chunk_attend_splits(p->dtype, p->head_dim, p->units / heads, heads, group, tokens, p->budget);
+  const size_t parts = l.split.splits > 1 ? rows * l.split.splits : 0;
   l.part_l = align_up(parts * sizeof(float));
   l.part_o = 2 * l.part_l;
   const size_t attend = l.part_o + align_up(parts * p->head_dim * sizeof(float));
@@ -192,7 +192,7 @@ int chunk_args(const roco_params* params, int32_t heads, int32_t group, int32_t 
   const int64_t element = params->dtype == ROCO_BF16 ? 2 : 4;
   a.units = params->units; a.requests = params->units / heads; a.heads = heads; a.group = group; a.tokens = tokens;
   a.B = params->budget; a.scope = params->scope;
-  a.splits = lay.splits;
+  a.row_tile = lay.split.row_tile; a.row_tiles = lay.split.row_tiles; a.splits = lay.split.splits;
   a.pol = policy_of(params);
   a.scale_log2 = scale_log2(params);
   a.recency_window = params->recency_window;

@@ -82,15 +82,25 @@ template <int DT, int HD> struct Rows {
 
 // Scores of 32 rows `a` against 32 rows `b`, the chunk that the lane holds of either (lane l: row l % 32, half l / 32 of a step's two chunks);
 // register e of the result belongs to row 8 (e / 4) + 4 (l / 32) + e % 4 of `a` and row l % 32 of `b`.
-template <int DT> __device__ __forceinline__ f32x16 score_step(const uint4& a, const uint4& b, f32x16 c) {
+typedef uint4_vec Frag;  // (a vector of the language: of a structure of four words the compiler makes four values, and copies to put them together again)
+template <int DT> __device__ __forceinline__ f32x16 score_step(const Frag& a, const Frag& b, f32x16 c) {
   if constexpr (DT == kBF16) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   } else {
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+    return c;
   }
+}
+__device__ __forceinline__ Frag read_frag(uint32_t lds_addr) {
+  typedef const __attribute__((address_space(3))) Frag* LdsFrag;
+  return *(LdsFrag)(static_cast<uintptr_t>(lds_addr));
+}
+// Two transposed reads of 16-bit elements.
+__device__ __forceinline__ Frag read_frag_transposed(uint32_t lo_addr, uint32_t hi_addr) {
+  const mfma::v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mfma::lds_v4i16*)(static_cast<uintptr_t>(lo_addr)));
+  const mfma::v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mfma::lds_v4i16*)(static_cast<uintptr_t>(hi_addr)));
+  return __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // A unit's slots in groups of 16: a page holds whole groups.

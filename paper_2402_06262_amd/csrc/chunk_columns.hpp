@@ -68,7 +68,7 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
 
   // the keys
   const Groups groups(a.pages, a.B, a.heads, at.request, head);
-  uint4 own[NG][R::kSteps];
+  Frag own[NG][R::kSteps];
   int kj[NG], kpos[NG];
   bool there[NG];
 #pragma unroll
@@ -88,7 +88,7 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
       kpos[g] = a.recency_window > 0 ? a.pos[static_cast<size_t>(u) * a.B + j] - a.qpos0[at.request] : 0;  // against the chunk's first token
     }
 #pragma unroll
-    for (int kk = 0; kk < R::kSteps; ++kk) own[g][kk] = load16(base + (2 * kk + half) * 16);
+    for (int kk = 0; kk < R::kSteps; ++kk) own[g][kk] = *reinterpret_cast<const Frag*>(base + (2 * kk + half) * 16);
   }
 
   // the walk over the rows: of the chunk's own keys, only from the block's first token on
@@ -153,7 +153,7 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
       for (int g = 0; g < NG; ++g) s[g] = f32x16{0};
 #pragma unroll
       for (int kk = 0; kk < R::kSteps; ++kk) {
-        const uint4 qf = tree::lds_read16((st ^ (kk << 5)) + sub * 32 * R::kBytes);
+        const Frag qf = read_frag((st ^ (kk << 5)) + sub * 32 * R::kBytes);
 #pragma unroll
         for (int g = 0; g < NG; ++g) s[g] = score_step<DT>(qf, own[g][kk], s[g]);
       }

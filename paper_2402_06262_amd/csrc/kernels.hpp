@@ -235,8 +235,8 @@ hipError_t launch_tree_commit(int dtype, int head_dim, const CommitArgs& a, hipS
 // token side by side.
 struct ChunkArgs {
   int units, requests, heads, group, tokens, B, scope;
-  int splits;             // chunk_attend: workgroups along a row tile's keys
-  int streaming;          // as DecodeArgs::streaming
+  // chunk_attend: rows of a tile, tiles, workgroups along a tile's keys
+  int row_tile, row_tiles, splits;
   Policy pol;
   float scale_log2;
   int recency_window;
@@ -260,7 +260,9 @@ struct ChunkArgs {
   float* fresh;                               // workspace [2][tokens][heads]: ... and of the tokens themselves
   uint32_t* keys;                             // workspace [units][2][B] when B is too large for LDS
 };
-int chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
+constexpr int kLeastKeys = 128;       // of a workgroup of chunk_attend, if its tile sees more than that
+struct ChunkSplits { int row_tile, row_tiles, splits; };
+ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
 hipError_t launch_chunk_attend(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);
 hipError_t launch_chunk_commit(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);
 constexpr int kMostChunkSplits = 64;
