@@ -153,7 +153,7 @@ int check_stride(const roco_params* p, int64_t stride, long long count) {
 }
 
 // ---- workspace of the chunks: chunk_attend's part_m | part_l | part_o, or chunk_commit's info | mark | sums | fresh | keys
-struct ChunkLayout { size_t part_l, part_o, mark, sums, fresh, keys, total; ChunkSplits split; };
+struct ChunkLayout { size_t part_l, part_o, mark, sums, fresh, keys, total; ChunkSplits split; int row_splits; };
 ChunkLayout chunk_layout(const roco_params* p, int32_t heads, int32_t group, int32_t tokens) {
   ChunkLayout l;
   const size_t U = p->units, B = p->budget, rows = static_cast<size_t>(tokens) * heads * group;
@@ -163,9 +163,10 @@ ChunkLayout chunk_layout(const roco_params* p, int32_t heads, int32_t group, int
   l.part_o = 2 * l.part_l;
   const size_t attend = l.part_o + align_up(parts * p->head_dim * sizeof(float));
   l.mark = align_up(U * 4 * sizeof(int32_t));
+  l.row_splits = chunk_row_splits(p->dtype, p->units / heads, heads, group, tokens, p->budget);
   l.sums = l.mark + align_up(U * B * sizeof(int32_t));
-  l.fresh = l.sums + align_up(U * 2 * B * sizeof(float));
-  l.keys = l.fresh + align_up(static_cast<size_t>(tokens) * heads * 2 * sizeof(float));
+  l.fresh = l.sums + align_up(l.row_splits * U * 2 * B * sizeof(float));
+  l.keys = l.fresh + align_up(l.row_splits * static_cast<size_t>(tokens) * heads * 2 * sizeof(float));
   const size_t commit = l.keys + (p->budget > kMaxDecodeBudgetLds ? align_up(U * 2 * B * sizeof(uint32_t)) : 0);
   l.total = std::max(attend, commit);
   return l;
@@ -192,7 +193,7 @@ int chunk_args(const roco_params* params, int32_t heads, int32_t group, int32_t 
   const int64_t element = params->dtype == ROCO_BF16 ? 2 : 4;
   a.units = params->units; a.requests = params->units / heads; a.heads = heads; a.group = group; a.tokens = tokens;
   a.B = params->budget; a.scope = params->scope;
-  a.row_tile = lay.split.row_tile; a.row_tiles = lay.split.row_tiles; a.splits = lay.split.splits;
+  a.row_tile = lay.split.row_tile; a.row_tiles = lay.split.row_tiles; a.splits = lay.split.splits; a.row_splits = lay.row_splits;
   a.pol = policy_of(params);
   a.scale_log2 = scale_log2(params);
   a.recency_window = params->recency_window;

@@ -1,14 +1,15 @@
-// Chunks of new tokens: which form of the attention a call takes, and the taking over into the budgeted cache, in three launches.
+// Chunks of new tokens: which form of the attention a call takes, and the taking over into the budgeted cache, in two launches or three.
 //
-//   chunk_choose  : one workgroup per unit.  E = max(0, n + c - budget) victims by the statistics as they stand (two exact searches, as in
-//                   block_prepare), and the slots that the chunk's tokens take, in ascending order: ChunkArgs::mark.
-//   chunk_columns : the sums of the chunk's probabilities (chunk_columns.hpp), for slots that are evicted too.
+//   chunk_columns : the sums of the chunk's probabilities (chunk_columns.hpp), for slots that are evicted too.  Beside them, or before them in
+//   chunk_choose    a launch of its own for large budgets, one workgroup per unit chooses E = max(0, n + c - budget) victims by the statistics
+//                   as they stand (two exact searches, as in block_prepare), and the slots that the chunk's tokens take, in ascending
+//                   order: ChunkArgs::mark (chunk_choose.hpp).
 //   chunk_apply   : the sums added to the statistics; the tokens' rows, positions and statistics to their slots.
 #include <stdlib.h>
 
 #include <algorithm>
 
-#include "chunk.hpp"
+#include "chunk_choose.hpp"
 #include "profile.hpp"
 
 namespace roco {
@@ -31,93 +32,13 @@ constexpr int kChooseThreads = 1024;
 // LDS: the ranking keys are in LDS (B <= kMaxDecodeBudgetLds).
 template <bool LDS> __global__ __launch_bounds__(kChooseThreads, 8) void chunk_choose(ChunkArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint32_t lds_keys[];  // [2][B]
-  __shared__ __attribute__((aligned(16))) uint32_t sel_sh[SelectLds<1>::kWords];
-  __shared__ uint32_t scan_sh[kChooseThreads / kWave + 1];
-  const int u = blockIdx.x, tid = threadIdx.x, B = a.B;
-  const int request = u / a.heads, head = u - request * a.heads;
-  const int first = min(max(a.start[request], 0), a.tokens), count = max(min(max(a.start[request + 1], 0), a.tokens) - first, 0);
-  const int budget = budget_of(a.pages, B, request);
-  const int n = min(max(a.n_used[u], 0), budget), c = min(count, budget);
-  const int n_new = min(budget, n + c), E = n + c - n_new;
-  int32_t* const info = a.info + static_cast<size_t>(u) * 4;
-  if (tid == 0) {
-    info[0] = c;
-    info[1] = n;
-    info[2] = n_new;
-  }
-  // tokens that took the place of none
-  const auto record = [&](int k, int slot, int position) {
-    const size_t at = static_cast<size_t>(first + k) * a.heads + head;
-    if (a.evicted_slot != nullptr) a.evicted_slot[at] = slot;
-    if (a.evicted_pos != nullptr) a.evicted_pos[at] = position;
-  };
-  for (int k = E + tid; k < count; k += kChooseThreads) record(k, -1, -1);  // (the freed slots come before the empty ones)
-  if (c == 0) return;
-  int32_t* const mark = a.mark + static_cast<size_t>(u) * B;
-  for (int j = n + tid; j < n_new; j += kChooseThreads) mark[j] = E + j - n;
-  if (E == 0) {
-    for (int j = tid; j < n; j += kChooseThreads) mark[j] = -1;
-    return;
-  }
-  const float* const acc = a.stats + static_cast<size_t>(u) * 3 * B;
-  const float* const acc2 = acc + B;
-  const float* const cnt = acc2 + B;
-  const int32_t* const pos = a.pos + static_cast<size_t>(u) * B;
-  uint32_t *const var_key = LDS ? lds_keys : a.keys + static_cast<size_t>(u) * 2 * B, *const mas_key = var_key + B;
-  constexpr int kEach = 4;  // slots of a thread at a time: their loads are in flight together
-#pragma unroll 1
-  for (int i0 = tid; i0 < n; i0 += kEach * kChooseThreads) {
-    float f[kEach], f2[kEach], fc[kEach];
-    int fp[kEach];
-    uint32_t mas[kEach], var[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = min(i0 + e * kChooseThreads, n - 1);
-      f[e] = acc[i];
-      f2[e] = acc2[i];
-      fc[e] = cnt[i];
-      fp[e] = pos[i];
-    }
-    ranking_keys<kEach>(f, f2, fc, fp, a.pol, mas, var);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = min(i0 + e * kChooseThreads, n - 1);
-      mas_key[i] = mas[e];
-      var_key[i] = var[e];
-    }
-  }
-  __syncthreads();
-  const uint32_t m = min(static_cast<uint32_t>(n), static_cast<uint32_t>(a.pol.scope_size(min(a.scope, budget), n)) + static_cast<uint32_t>(E) - 1u);
-  KSmallest r = {0u, 0u};
-#pragma unroll 1
-  for (int phase = 0; phase < 2; ++phase) {
-    const uint32_t* const key = phase == 0 ? var_key : mas_key;
-    r = select_k_smallest<kChooseThreads, 1, 1>([&](int i) -> uint32_t { return key[i]; }, n, phase == 0 ? m : static_cast<uint32_t>(E),
-                                                phase == 0 && a.pol.scope_is_window(), sel_sh, phase == 0 || a.pol.spreads_importance());
-    if (phase == 0) {
-      for (int i = tid; i < n; i += kChooseThreads)
-        if (!r.has(var_key[i], i)) mas_key[i] = 0xffffffffu;  // outside the scope
-      __syncthreads();
-    }
-  }
-  // the i-th victim's slot gets token i: thread t has the contiguous slots from t * per on
-  const int per = (n + kChooseThreads - 1) / kChooseThreads, lo = min(n, tid * per), hi = min(n, lo + per);
-  uint32_t mine = 0, all;
-#pragma unroll 1
-  for (int j = lo; j < hi; ++j) mine += r.has(mas_key[j], j) ? 1u : 0u;
-  uint32_t rank = block_exclusive_scan<kChooseThreads>(mine, scan_sh, all);
-#pragma unroll 1
-  for (int j = lo; j < hi; ++j) {
-    const bool out = r.has(mas_key[j], j);
-    const int k = out ? static_cast<int>(rank++) : -1;
-    mark[j] = k;
-    if (out) record(k, j, pos[j]);
-  }
+  __shared__ __attribute__((aligned(16))) uint32_t words[kChoiceWords<kChooseThreads>];
+  choose_slots<kChooseThreads>(a, blockIdx.x, words, LDS ? lds_keys : a.keys + static_cast<size_t>(blockIdx.x) * 2 * a.B);
 }
 
 // A workgroup's slots of one unit.
 constexpr int kApplySlots = 256;
-__global__ __launch_bounds__(kThreads) void chunk_apply(ChunkArgs a, int row_bytes, int blocks) {
+__global__ __launch_bounds__(kThreads) void chunk_apply(ChunkArgs a, int row_bytes, int blocks, int tile_tokens, int keys) {
   __shared__ int32_t list_s[kApplySlots], listed_s;  // slots that tokens take
   const int u = blockIdx.x / blocks, row0 = blockIdx.x % blocks * kApplySlots, tid = threadIdx.x;
   const int request = u / a.heads, head = u - request * a.heads;
@@ -137,13 +58,28 @@ __global__ __launch_bounds__(kThreads) void chunk_apply(ChunkArgs a, int row_byt
     float* const acc = a.stats + 3 * at + j;
     if (k >= 0) {
       const size_t i = static_cast<size_t>(first + k) * a.heads + head;
-      acc[0] = a.fresh[i];
-      acc[a.B] = a.fresh[static_cast<size_t>(a.tokens) * a.heads + i];
+      const RowShares shares((c + tile_tokens - 1) / tile_tokens - k / keys * keys / tile_tokens, a.row_splits);
+      float own = 0.0f, own2 = 0.0f;
+#pragma unroll 4
+      for (int s = 0; s < shares.used; ++s) {
+        const float* const from = a.fresh + s * 2 * a.fresh_plane() + i;
+        own += from[0];
+        own2 += from[a.fresh_plane()];
+      }
+      acc[0] = own;
+      acc[a.B] = own2;
       acc[2 * static_cast<size_t>(a.B)] = static_cast<float>(c - k);
       a.pos[at + j] = a.qpos0[request] + k;
       list_s[atomicAdd(&listed_s, 1)] = tid;
     } else {
-      const float more = a.sums[2 * at + j], more2 = a.sums[2 * at + a.B + j];
+      const RowShares shares((c + tile_tokens - 1) / tile_tokens, a.row_splits);
+      float more = 0.0f, more2 = 0.0f;
+#pragma unroll 4
+      for (int s = 0; s < shares.used; ++s) {
+        const float* const from = a.sums + 2 * (static_cast<size_t>(s) * a.units * a.B + at) + j;
+        more += from[0];
+        more2 += from[a.B];
+      }
       if (!(more < 0.0f)) {  // (below zero: not seen)
         acc[0] += more;
         acc[a.B] = (a.pol.keeps_last_score() ? 0.0f : acc[a.B]) + more2;
@@ -201,6 +137,17 @@ ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads
   return c;
 }
 
+// Until there are 2048 workgroups, four rounds of them, while a chunk has four tiles of rows for each.
+int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B) {
+  const char* const asked = getenv("ROCO_CHUNK_ROW_SPLITS");
+  const int splits = asked != nullptr ? std::min(atoi(asked), kMostRowSplits) : 0;
+  if (splits >= 1) return splits;
+  const int keys = column_keys(dtype);
+  const long long blocks = (static_cast<long long>(requests) * ((B + keys - 1) / keys) + tiles_of(requests, tokens, 1, keys)) * heads;
+  const long long most = tokens / column_tokens(group) / RowShares::kLeastTiles;
+  return static_cast<int>(std::max(1ll, std::min({2048 / blocks, most, static_cast<long long>(kMostRowSplits)})));
+}
+
 hipError_t launch_chunk_attend(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s) {
   if (dtype == kBF16) return head_dim == 128 ? launch_chunk_attend_bf16_128(a, s) : launch_chunk_attend_bf16_64(a, s);
   return head_dim == 128 ? launch_chunk_attend_f32_128(a, s) : launch_chunk_attend_f32_64(a, s);
@@ -208,21 +155,22 @@ hipError_t launch_chunk_attend(int dtype, int head_dim, const ChunkArgs& a, hipS
 
 hipError_t launch_chunk_commit(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s) {
   hipError_t e;
-  {
+  if (!chosen_beside(a.B)) {
     ProfScope ps(kProfChunkChoose, s);
     const size_t key_lds = key_lds_bytes(a.B);
     if (!allow_key_lds(reinterpret_cast<const void*>(chunk_choose<true>), key_lds)) return hipErrorInvalidValue;
     if (key_lds == 0) hipLaunchKernelGGL((chunk_choose<false>), dim3(a.units), dim3(kChooseThreads), 0, s, a);
     else hipLaunchKernelGGL((chunk_choose<true>), dim3(a.units), dim3(kChooseThreads), key_lds, s, a);
     e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  if (e != hipSuccess) return e;
   if (dtype == kBF16) e = head_dim == 128 ? launch_chunk_columns_bf16_128(a, s) : launch_chunk_columns_bf16_64(a, s);
   else e = head_dim == 128 ? launch_chunk_columns_f32_128(a, s) : launch_chunk_columns_f32_64(a, s);
   if (e != hipSuccess) return e;
   ProfScope ps(kProfChunkApply, s);
   const int blocks = (a.B + kApplySlots - 1) / kApplySlots;
-  hipLaunchKernelGGL(chunk_apply, dim3(static_cast<unsigned>(a.units) * blocks), dim3(kThreads), 0, s, a, head_dim * (dtype == kBF16 ? 2 : 4), blocks);
+  hipLaunchKernelGGL(chunk_apply, dim3(static_cast<unsigned>(a.units) * blocks), dim3(kThreads), 0, s, a, head_dim * (dtype == kBF16 ? 2 : 4), blocks,
+                     column_tokens(a.group), column_keys(dtype));
   return hipGetLastError();
 }
 

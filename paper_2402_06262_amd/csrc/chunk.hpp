@@ -1,5 +1,7 @@
 // What the kernels of chunks share: which request a tile of packed rows belongs to, and the matrix products of 32 x 32 tiles.
 #pragma once
+#include <algorithm>
+
 #include "tree.hpp"
 
 namespace roco {
@@ -121,6 +123,24 @@ struct Groups {
     row = (static_cast<uint32_t>(page * heads + head) << page_log2) + static_cast<uint32_t>(slot & ((1 << page_log2) - 1));
     return true;
   }
+};
+
+// The sums of a chunk's probabilities: tiles of 64 rows of queries, of as many tokens as there are powers of two of heads in them; keys of a workgroup.
+constexpr int kQueryTile = 64;
+constexpr int column_keys(int dtype) { return dtype == kBF16 ? 256 : 128; }
+inline int column_tokens(int group) {
+  int tokens = kQueryTile;
+  while (kQueryTile / tokens < group) tokens /= 2;
+  return tokens;
+}
+// Up to this budget a unit's slots are chosen by a workgroup of 256 threads beside those of the sums, not by one of 1024 before them (8 heads of 4 queries, 128
+// dimensions, chunks of 16: 64 units of 1024 slots 26 -> 19 us, of 4096 43 -> 35; 8 units of 2048 25 -> 21, of 4096 25 -> 26).
+inline bool chosen_beside(int B) { return B <= 4096; }
+// Tiles of rows, shared by the workgroups of a block of keys.
+struct RowShares {
+  int tiles, per, used;
+  __device__ __forceinline__ RowShares(int tiles_, int splits) : tiles(tiles_), per(max((tiles + splits - 1) / splits, kLeastTiles)), used((tiles + per - 1) / per) {}
+  static constexpr int kLeastTiles = 4;
 };
 
 #pragma clang diagnostic pop

@@ -6,8 +6,14 @@
 // of 64 through a ring in LDS; the result tile has its key in the lane and 16 rows in the lane's registers, so that the sums run down the
 // registers: no exchange between lanes, no atomics, a fixed order.  Which (token, head) a tile's row holds is the choice of the lane that
 // fetches it: the heads of a token, filled up to a power of two, lie in consecutive registers of one lane, and their mean is a sum of registers.
+// The scores of the next 32 rows are formed between the exponentials of these.  A chunk's rows are shared by up to 16 workgroups of a block of keys,
+// whose sums chunk_apply adds in their order.
+// Measured, with all of roco_chunk_commit: 4 requests of 512 tokens, 8 heads of 4 queries, 4096 slots, bf16, 128 dimensions, 108 us (the products would
+// take 33 at 2.1 PFLOP/s, the vector instructions 50), with one workgroup along the rows 125; 12 of up to 200, groups of 8, 2048 slots, 64 dimensions,
+// 61 us and 67.  With one path for all rows, of selects and of branches within, 154 and 102 us of the kernel alone, and the requests side by
+// side on a die, so that one had the longest.
 #pragma once
-#include "chunk.hpp"
+#include "chunk_choose.hpp"
 #include "profile.hpp"
 
 namespace roco {
@@ -16,20 +22,17 @@ namespace chunk {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 
-constexpr int kQueryTile = 64;  // rows of a stage
-
 template <int DT, int HD> struct ColumnForm {
   using R = Rows<DT, HD>;
-  static constexpr int kGroups = DT == kBF16 ? 2 : 1;              // of 32 keys of a wave
-  static constexpr int kKeys = kWaves * 32 * kGroups;              // of a workgroup
+  static constexpr int kGroups = column_keys(DT) / kWaves / 32;    // of 32 keys of a wave
+  static constexpr int kKeys = column_keys(DT);                    // of a workgroup
   static constexpr int kTileBytes = kQueryTile * R::kBytes;
-  static constexpr int kStages = kTileBytes <= 16384 ? 4 : 2;
-  static constexpr int kAhead = kStages - 1;
+  static constexpr int kStages = kTileBytes > 16384 ? 3 : 4;       // the tile in use, the next one, and others on their way
   static constexpr int kLoads = kTileBytes / kWaves / 1024;        // of a wave and tile
 };
 
 // P: heads of a token, filled up to a power of two (32: 17 to 32 heads, 64: 33 to 64).
-template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void chunk_columns(ChunkArgs a, int cache_blocks, int fresh_blocks) {
+template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void chunk_columns(ChunkArgs a, int choosers, int cache_blocks, int fresh_blocks) {
   using R = Rows<DT, HD>;
   using F = ColumnForm<DT, HD>;
   constexpr int NG = F::kGroups;
@@ -37,23 +40,33 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
   constexpr int kTileLoads = F::kLoads + 1;
   extern __shared__ __attribute__((aligned(1024))) char ring[];
   __shared__ __attribute__((aligned(256))) float lse_s[F::kStages][kWaves][kQueryTile];  // (a copy for each wave, which waits for its own loads)
-  // workgroups of the slots, and behind them of the chunk's tokens; a unit's side by side on a die
-  const int total = cache_blocks * a.units + fresh_blocks * a.heads, share = (total + 7) / 8;
-  const int id = static_cast<int>(blockIdx.x % 8) * share + static_cast<int>(blockIdx.x / 8);
-  if (static_cast<int>(blockIdx.x / 8) >= share || id >= total) return;
-  const bool of_fresh = id >= cache_blocks * a.units;
+  // a workgroup for each unit that chooses its slots, if it has not been done; whole eights of them
+  if (static_cast<int>(blockIdx.x) < choosers) {
+    uint32_t* const words = reinterpret_cast<uint32_t*>(ring);
+    if (static_cast<int>(blockIdx.x) < a.units) choose_slots<kThreads>(a, blockIdx.x, words, words + kChoiceWords<kThreads>);
+    return;
+  }
+  // workgroups of the chunk's tokens, then of the slots; either in contiguous shares of the eight dies, with a unit's, which read the same queries, side by side
+  // (and a head's units: a share of requests would have longer chunks than another)
+  const int cache_each = cache_blocks * a.row_splits, fresh_each = fresh_blocks * a.row_splits;  // of a unit, and of a head
+  const int cache_total = cache_each * a.units, fresh_total = fresh_each * a.heads, cache_share = (cache_total + 7) / 8, fresh_share = (fresh_total + 7) / 8;
+  const int die = static_cast<int>(blockIdx.x % 8), i_die = (static_cast<int>(blockIdx.x) - choosers) / 8;
+  const bool of_fresh = i_die < fresh_share;
+  const int id = of_fresh ? die * fresh_share + i_die : die * cache_share + i_die - fresh_share;
+  if (id >= (of_fresh ? fresh_total : cache_total)) return;
   Located at;
-  int head, block;
+  int head, block, split;
   if (of_fresh) {
-    const int i = id - cache_blocks * a.units;
-    head = i / fresh_blocks;
-    if (!locate_tile<F::kKeys>(a, 1, i % fresh_blocks, at)) return;
+    head = id / fresh_each;
+    split = id % fresh_each / fresh_blocks;
+    if (!locate_tile<F::kKeys>(a, 1, id % fresh_blocks, at)) return;
     block = at.tile;
   } else {
-    const int u = id / cache_blocks;
+    const int pair = id / cache_each;
+    split = id % cache_each / cache_blocks;
     block = id % cache_blocks;
-    at.request = u / a.heads;
-    head = u % a.heads;
+    head = pair / a.requests;
+    at.request = __builtin_amdgcn_readfirstlane(pair % a.requests);
     at.first = __builtin_amdgcn_readfirstlane(min(max(a.start[at.request], 0), a.tokens));
     at.count = __builtin_amdgcn_readfirstlane(min(max(a.start[at.request + 1], 0), a.tokens)) - at.first;
   }
@@ -65,6 +78,11 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
   const int c = __builtin_amdgcn_readfirstlane(min(at.count, budget));  // tokens taken over
   const int keys = of_fresh ? c : n, j0 = block * F::kKeys;
   if (c <= 0 || j0 >= keys) return;
+  // the walk over the rows: of the chunk's own keys, only from the block's first token on
+  const int first_tile = of_fresh ? j0 / kTokens : 0;
+  const RowShares shares((c + kTokens - 1) / kTokens - first_tile, a.row_splits);
+  const int t0 = first_tile + split * shares.per, t1 = min(first_tile + shares.tiles, t0 + shares.per);
+  if (t0 >= t1) return;
 
   // the keys
   const Groups groups(a.pages, a.B, a.heads, at.request, head);
@@ -91,8 +109,6 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
     for (int kk = 0; kk < R::kSteps; ++kk) own[g][kk] = *reinterpret_cast<const Frag*>(base + (2 * kk + half) * 16);
   }
 
-  // the walk over the rows: of the chunk's own keys, only from the block's first token on
-  const int t0 = of_fresh ? j0 / kTokens : 0, t1 = (c + kTokens - 1) / kTokens;
   const uint32_t ring_addr = lds_address(ring), lse_addr = lds_address(&lse_s[0][wave][0]);
   // row x of a half tile of 32 is register 4 (x / 8) + x % 4 of half x / 4 % 2
   const auto virtual_row = [](int x) { return (x & 32) + ((x >> 2) & 1) * 16 + ((x >> 3) & 3) * 4 + (x & 3); };
@@ -115,89 +131,120 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
     mfma::load4_to_lds(lbuf, lse_addr + stage * (kWaves * kQueryTile * 4), loff, 0);
   };
 #pragma unroll
-  for (int i = 0; i < F::kAhead; ++i)
+  for (int i = 0; i < F::kStages - 1; ++i)
     if (t0 + i < t1) request(t0 + i, i);
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the keys are in before the loop
+  __syncthreads();                     // the other waves' shares of the first tiles, too
 
-  const float sc = a.scale_log2, bias = a.recency_bias_log2, inv = 1.0f / static_cast<float>(a.group);
+  const float sc = a.scale_log2, bias = a.recency_bias_log2, log2_group = __log2f(static_cast<float>(a.group));
   const int w = a.recency_window;
   const bool squares = !a.pol.keeps_last_score() && !a.pol.counts_above_average(), filled_up = P != a.group;
   const uint32_t frag = (lane & 31) * R::kBytes + ((half ^ R::swizzle_k(lane & 31)) << 4);
   const int last_key = j0 + (wave * NG + NG) * 32 - 1;  // of the wave's
-  const bool idle = j0 + wave * NG * 32 >= keys;
-  float sum[NG], sum2[NG], heads_sum[NG];
+  float sum[NG], sum2[NG], mean[NG];
 #pragma unroll
-  for (int g = 0; g < NG; ++g) sum[g] = sum2[g] = heads_sum[g] = 0.0f;
+  for (int g = 0; g < NG; ++g) sum[g] = sum2[g] = mean[g] = 0.0f;
+  int from[NG];  // the first token that sees the key
+#pragma unroll
+  for (int g = 0; g < NG; ++g) from[g] = of_fresh ? kj[g] : 0;
   int stage = 0;
-#pragma unroll 1
-  for (int t = t0; t < t1; ++t) {
-    if (t + F::kAhead - 1 < t1) wait_loads<(F::kAhead - 1) * kTileLoads>();
+  const auto next_tile = [&](int t) {  // the one behind t is wanted
+    if (t + F::kStages - 2 < t1) wait_loads<(F::kStages - 3) * kTileLoads>();
     else wait_loads<0>();
     __syncthreads();
-    if (t + F::kAhead < t1) request(t + F::kAhead, stage == 0 ? F::kStages - 1 : stage - 1);
-    const uint32_t st = ring_addr + stage * F::kTileBytes + frag;
-    const float* const lse_t = &lse_s[stage][wave][16 * half];
-    stage = stage == F::kStages - 1 ? 0 : stage + 1;
+    if (t + F::kStages - 1 < t1) request(t + F::kStages - 1, stage == 0 ? F::kStages - 1 : stage - 1);
+  };
+  // Rows 32 h .. of tile t, in stage `at_stage`, from scores s; the scores of the 32 rows behind them, which begin at `next` in LDS, into s_next.
+  // A matrix instruction, then vector work on the scores before: a wave keeps both busy, and two of them fill the gaps.
+  constexpr int kEach = 16 / R::kSteps, kEarly = R::kSteps >= 4 ? 2 : 1;
+  // The kinds of tiles: every key sees every row, and the heads of a token are a power of two; they are filled up; some keys do not see some rows; of
+  // the rest, with recency windows or other statistics than the squares' sum.
+  constexpr int kInside = 0, kFilled = 1, kPartly = 2, kAny = 3;
+  const bool last_only = a.pol.keeps_last_score();
+  const auto half_tile = [&](auto h_, auto kind_, int t, int at_stage, uint32_t next, f32x16 (&s)[NG], f32x16 (&s_next)[NG]) {
+    constexpr int h = decltype(h_)::value, kKind = decltype(kind_)::value;
     const int first = t * kTokens;
-    if (idle || (of_fresh && first + kTokens - 1 < last_key - 32 * NG + 1)) continue;
-    // everything is seen by every key, and outside the recency windows
-    bool interior = squares && first + kTokens <= c && !(of_fresh && first < last_key);
-    if (w > 0) {
+    const float* const lse_t = &lse_s[at_stage][wave][16 * half + 32 * h];
+    Frag qf[R::kSteps];
 #pragma unroll
-      for (int g = 0; g < NG; ++g) interior = interior && !__any(first - kpos[g] < w && first + kTokens - 1 - kpos[g] >= 0);
+    for (int i = 0; i < kEarly; ++i) qf[i] = read_frag(next ^ (i << 5));
+    float less[16];
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const tree::f32x4 v = *reinterpret_cast<const tree::f32x4*>(lse_t + 4 * e4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) less[4 * e4 + e] = fmaf(v[e], -kLog2e, -log2_group);
     }
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      f32x16 s[NG];
+    for (int g = 0; g < NG; ++g) s_next[g] = f32x16{0};
 #pragma unroll
-      for (int g = 0; g < NG; ++g) s[g] = f32x16{0};
+    for (int kk = 0; kk < R::kSteps; ++kk) {
+      if (kk + kEarly < R::kSteps) qf[kk + kEarly] = read_frag(next ^ ((kk + kEarly) << 5));
 #pragma unroll
-      for (int kk = 0; kk < R::kSteps; ++kk) {
-        const Frag qf = read_frag((st ^ (kk << 5)) + sub * 32 * R::kBytes);
+      for (int g = 0; g < NG; ++g) {
+        s_next[g] = score_step<DT>(qf[kk], own[g][kk], s_next[g]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) s[g] = score_step<DT>(qf, own[g][kk], s[g]);
-      }
-      float lse[16];
-#pragma unroll
-      for (int e4 = 0; e4 < 4; ++e4) {
-        const tree::f32x4 v = *reinterpret_cast<const tree::f32x4*>(lse_t + 32 * sub + 4 * e4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lse[4 * e4 + e] = v[e] * kLog2e;
-      }
-      const auto add = [&](auto inside) {
-        constexpr bool kInside = decltype(inside)::value;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float x = fmaf(s[g][e], sc, -lse[e]);
-            const int local = (32 * sub + 16 * half + e) / P;  // the row's token
-            if (!kInside && w > 0) x += static_cast<unsigned>(first + local - kpos[g]) < static_cast<unsigned>(w) ? bias : 0.0f;
-            float p = fast_exp2(x);
-            if (filled_up && e % P >= a.group && P <= 16) p = 0.0f;
-            if (P > 16 && filled_up) p = (32 * sub + 16 * half + e) % P >= a.group ? 0.0f : p;
-            heads_sum[g] = (P <= 16 ? e % P == 0 : e == 0 && (P == 32 || sub == 0)) ? p : heads_sum[g] + p;
-            if ((P <= 16 && (e + 1) % P == 0) || (e == 15 && (P == 32 || (P == 64 && sub == 1)))) {
-              float mean = heads_sum[g];
-              if (P > 16) mean += __shfl_xor(mean, 32, kWave);
-              mean *= inv;
-              const int token = first + local;
-              if (kInside) {
-                sum[g] += mean;
-                sum2[g] = fmaf(mean, mean, sum2[g]);
-              } else {
-                const bool counts = token < c && !(of_fresh && token < kj[g]);
-                const float second = squares ? mean * mean : a.pol.keeps_last_score() ? (token == c - 1 ? mean : 0.0f)
-                                                           : a.pol.second_statistic(0.0f, mean, static_cast<float>(n + token + 1));
-                sum[g] += counts ? mean : 0.0f;
-                sum2[g] += counts ? second : 0.0f;
-              }
+        for (int e = kEach * kk; e < kEach * kk + kEach; ++e) {
+          float x = fmaf(s[g][e], sc, less[e]);
+          const int local = (32 * h + 16 * half + e) / P;  // the row's token
+          if (kKind == kAny) x += static_cast<unsigned>(first + local - kpos[g]) < static_cast<unsigned>(w) ? bias : 0.0f;
+          float p = fast_exp2(x);
+          if (kKind != kInside) p = (P <= 16 ? e : 32 * h + 16 * half + e) % P >= a.group ? 0.0f : p;
+          mean[g] = (P <= 16 ? e % P == 0 : e == 0 && (P == 32 || h == 0)) ? p : mean[g] + p;
+          if ((P <= 16 && (e + 1) % P == 0) || (e == 15 && (P == 32 || (P == 64 && h == 1)))) {
+            if (P > 16) mean[g] += __shfl_xor(mean[g], 32, kWave);
+            const int token = first + local;
+            if (kKind >= kPartly) mean[g] = token >= from[g] && token < c ? mean[g] : 0.0f;
+            sum[g] += mean[g];
+            if (kKind != kAny) {
+              sum2[g] = fmaf(mean[g], mean[g], sum2[g]);
+            } else {
+              const float last = token == c - 1 ? mean[g] : 0.0f, above = mean[g] * static_cast<float>(n + token + 1) > 1.0f ? 1.0f : 0.0f;
+              sum2[g] += squares ? mean[g] * mean[g] : last_only ? last : above;
             }
           }
         }
+        asm volatile("" : "+v"(mean[g]), "+v"(sum[g]), "+v"(sum2[g]));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  if (j0 + wave * NG * 32 >= keys) {  // no keys of this wave, but the other waves want its loads
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+      next_tile(t);
+      stage = stage + 1 == F::kStages ? 0 : stage + 1;
+    }
+  } else {
+    f32x16 s0[NG], s1[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) s0[g] = f32x16{0};
+#pragma unroll
+    for (int kk = 0; kk < R::kSteps; ++kk) {
+      const Frag qf = read_frag((ring_addr + frag) ^ (kk << 5));
+#pragma unroll
+      for (int g = 0; g < NG; ++g) s0[g] = score_step<DT>(qf, own[g][kk], s0[g]);
+    }
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+      next_tile(t);
+      const int first = t * kTokens, now = stage;
+      stage = stage + 1 == F::kStages ? 0 : stage + 1;
+      bool window = false;  // some row and key in reach of one another
+      if (w > 0) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) window = window || __any(first - kpos[g] < w && first + kTokens - 1 - kpos[g] >= 0);
+      }
+      const uint32_t second = ring_addr + now * F::kTileBytes + 32 * R::kBytes + frag, next = ring_addr + stage * F::kTileBytes + frag;
+      const auto tile = [&](auto kind) {
+        half_tile(std::integral_constant<int, 0>(), kind, t, now, second, s0, s1);
+        half_tile(std::integral_constant<int, 1>(), kind, t, now, next, s1, s0);
       };
-      if (interior) add(std::true_type());
-      else add(std::false_type());
+      if (window || !squares) tile(std::integral_constant<int, kAny>());
+      else if (first + kTokens > c || (of_fresh && first < last_key)) tile(std::integral_constant<int, kPartly>());
+      else if (filled_up) tile(std::integral_constant<int, kFilled>());
+      else tile(std::integral_constant<int, kInside>());
     }
   }
 #pragma unroll
@@ -209,10 +256,11 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
     if (half != 0 || kj[g] >= keys) continue;
     if (of_fresh) {
       const size_t i = static_cast<size_t>(at.first + kj[g]) * a.heads + head;
-      a.fresh[i] = sum[g];
-      a.fresh[static_cast<size_t>(a.tokens) * a.heads + i] = sum2[g];
+      float* const to = a.fresh + split * 2 * a.fresh_plane() + i;
+      to[0] = sum[g];
+      to[a.fresh_plane()] = sum2[g];
     } else {
-      float* const to = a.sums + static_cast<size_t>(u) * 2 * a.B + kj[g];
+      float* const to = a.sums + (static_cast<size_t>(split) * a.units + u) * 2 * a.B + kj[g];
       to[0] = there[g] ? sum[g] : -1.0f;  // (not seen)
       to[a.B] = sum2[g];
     }
@@ -223,22 +271,26 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
 
 template <int DT, int HD, int P> hipError_t launch_columns_form(const ChunkArgs& a, hipStream_t s) {
   using F = ColumnForm<DT, HD>;
-  constexpr int kLds = F::kStages * F::kTileBytes;
+  const int choosers = chosen_beside(a.B) ? (a.units + 7) / 8 * 8 : 0;
+  const int lds = std::max(F::kStages * F::kTileBytes, choosers > 0 ? (kChoiceWords<kThreads> + 2 * a.B) * 4 : 0);
   const void* const fn = reinterpret_cast<const void*>(chunk_columns<DT, HD, P>);
-  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) return hipErrorInvalidValue;
+  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return hipErrorInvalidValue;
   const int cache_blocks = (a.B + F::kKeys - 1) / F::kKeys, fresh_blocks = tiles_of(a.requests, a.tokens, 1, F::kKeys);
-  const int total = cache_blocks * a.units + fresh_blocks * a.heads;
-  hipLaunchKernelGGL((chunk_columns<DT, HD, P>), dim3(static_cast<unsigned>((total + 7) / 8 * 8)), dim3(kThreads), kLds, s, a, cache_blocks, fresh_blocks);
+  const int total = (cache_blocks * a.row_splits * a.units + 7) / 8 + (fresh_blocks * a.row_splits * a.heads + 7) / 8;
+  hipLaunchKernelGGL((chunk_columns<DT, HD, P>), dim3(static_cast<unsigned>(total) * 8 + choosers), dim3(kThreads), lds, s, a, choosers, cache_blocks, fresh_blocks);
   return hipGetLastError();
 }
 template <int DT, int HD> hipError_t launch_columns(const ChunkArgs& a, hipStream_t s) {
   ProfScope ps(kProfChunkColumns, s);
-  if (a.group <= 1) return launch_columns_form<DT, HD, 1>(a, s);
-  if (a.group <= 2) return launch_columns_form<DT, HD, 2>(a, s);
-  if (a.group <= 4) return launch_columns_form<DT, HD, 4>(a, s);
-  if (a.group <= 8) return launch_columns_form<DT, HD, 8>(a, s);
-  if (a.group <= 16) return launch_columns_form<DT, HD, 16>(a, s);
-  return a.group <= 32 ? launch_columns_form<DT, HD, 32>(a, s) : launch_columns_form<DT, HD, 64>(a, s);
+  switch (kQueryTile / column_tokens(a.group)) {
+    case 1: return launch_columns_form<DT, HD, 1>(a, s);
+    case 2: return launch_columns_form<DT, HD, 2>(a, s);
+    case 4: return launch_columns_form<DT, HD, 4>(a, s);
+    case 8: return launch_columns_form<DT, HD, 8>(a, s);
+    case 16: return launch_columns_form<DT, HD, 16>(a, s);
+    case 32: return launch_columns_form<DT, HD, 32>(a, s);
+    default: return launch_columns_form<DT, HD, 64>(a, s);
+  }
 }
 
 }  // namespace chunk

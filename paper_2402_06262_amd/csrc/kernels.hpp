@@ -256,16 +256,19 @@ struct ChunkArgs {
   int32_t *evicted_slot, *evicted_pos;        // [tokens][heads], may be null
   int32_t* mark;                              // workspace [units][B]: the token that takes the slot, or -1
   int32_t* info;                              // workspace [units][4]: tokens taken over, slots held before, slots held then, -
-  float* sums;                                // workspace [units][2][B]: what the chunk's rows add to Acc and Acc2 of the slots held before (below zero: not seen)
-  float* fresh;                               // workspace [2][tokens][heads]: ... and of the tokens themselves
+  float* sums;                                // workspace [row_splits][units][2][B]: what the chunk's rows add to Acc and Acc2 of the slots held before (below zero: not seen)
+  float* fresh;                               // workspace [row_splits][2][tokens][heads]: ... and of the tokens themselves
+  int row_splits;                             // chunk_commit: workgroups along a chunk's rows
+  __host__ __device__ size_t fresh_plane() const { return static_cast<size_t>(tokens) * heads; }
   uint32_t* keys;                             // workspace [units][2][B] when B is too large for LDS
 };
 constexpr int kLeastKeys = 128;       // of a workgroup of chunk_attend, if its tile sees more than that
 struct ChunkSplits { int row_tile, row_tiles, splits; };
 ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
+int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B);
 hipError_t launch_chunk_attend(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);
 hipError_t launch_chunk_commit(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);
-constexpr int kMostChunkSplits = 64;
+constexpr int kMostChunkSplits = 64, kMostRowSplits = 16;
 
 // ---------------------------------------------------------------- verification of drafted tokens
 struct VerifyArgs {
