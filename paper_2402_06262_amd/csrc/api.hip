@@ -211,6 +211,16 @@ int check_verify(int32_t requests, int32_t nodes, int32_t vocab) {
   return requests <= 65535 && nodes <= kMaxTreeNodes && vocab <= kMaxVocab ? ROCO_OK : ROCO_EUNSUPPORTED;
 }
 int verify_blocks(int32_t vocab) { return (vocab + 7 + kVerifyBlock - 1) / kVerifyBlock; }  // (the first begins up to seven elements before the row)
+// workspace: sums | walks | nodes
+struct VerifyLayout { size_t walks, found, total; };
+VerifyLayout verify_layout(int32_t requests, int32_t nodes, int32_t vocab) {
+  const size_t rows = static_cast<size_t>(kMaxVerifyRounds) * requests;
+  VerifyLayout l;
+  l.walks = align_up(rows * verify_blocks(vocab) * sizeof(double));
+  l.found = l.walks + align_up(rows * sizeof(VerifyWalk));
+  l.total = l.found + align_up(static_cast<size_t>(requests) * nodes * sizeof(VerifyNode));
+  return l;
+}
 
 // ---- workspace of the trees: tree_attend's part_m | part_l | part_o, or tree_commit's taken | sums | fresh | keys
 struct TreeLayout { size_t part_l, part_o, sums, fresh, keys, total; TreeSplits split; };
@@ -721,7 +731,7 @@ int roco_chunk_commit(const roco_params* params, int32_t heads, int32_t group, i
 
 size_t roco_verify_workspace_bytes(int32_t requests, int32_t nodes, int32_t vocab) {
   if (check_verify(requests, nodes, vocab) != ROCO_OK) return 0;
-  return align_up(static_cast<size_t>(kMaxVerifyRounds) * requests * verify_blocks(vocab) * sizeof(double));
+  return verify_layout(requests, nodes, vocab).total;
 }
 
 int roco_tree_verify(int32_t dtype, int32_t requests, int32_t nodes, int32_t vocab, const void* p, int64_t p_request_stride, int64_t p_row_stride,
@@ -742,12 +752,17 @@ int roco_tree_verify(int32_t dtype, int32_t requests, int32_t nodes, int32_t voc
   for (const void* ptr : words)
     if (!given(ptr)) return ROCO_EINVAL;
   if (!aligned4(parent) || !aligned4(n_nodes) || workspace == nullptr || !aligned16(workspace)) return ROCO_EINVAL;
-  if (workspace_bytes < roco_verify_workspace_bytes(requests, nodes, vocab)) return ROCO_EWORKSPACE;
-  // A chain has one pass: behind its first rejection, or its end.  A tree has one more for every rejection that another continuation follows.
+  const VerifyLayout lay = verify_layout(requests, nodes, vocab);
+  if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
+  char* const ws = static_cast<char*>(workspace);
+  // A chain has one pass: behind its first rejection, or its end.  So has a tree without the drafts' probabilities; with them it has one more for every rejection
+  // that another continuation follows.  A round that nobody needs costs 2.7 us, one too few, over 65536 tokens, 10 (32 requests of 32 nodes, 7 rounds 54 us, 5 49,
+  // 3 70; 16 of 8 nodes, 4 rounds 37 us, 3 44, 6 43; 16 of 16, 5 rounds 65 us, 6 54, 3 85).
   int rounds = env_int("ROCO_VERIFY_ROUNDS", 0);
-  if (rounds < 1 || rounds > kMaxVerifyRounds) rounds = parent == nullptr || nodes <= 2 ? 1 : 3;
+  if (rounds < 1 || rounds > kMaxVerifyRounds) rounds = parent == nullptr || q == nullptr || nodes <= 2 ? 1 : std::min(kMaxVerifyRounds, 3 + nodes / 8);
   const VerifyArgs a = {requests, nodes, vocab, distinct != 0, max_path, dtype == ROCO_BF16, p, q, p_request_stride, p_row_stride, q_request_stride, q_row_stride,
-                        tokens, parent, n_nodes, accept, choose, path, n_path, next_token, static_cast<double*>(workspace), verify_blocks(vocab), rounds};
+                        tokens, parent, n_nodes, accept, choose, path, n_path, next_token, reinterpret_cast<double*>(ws),
+                        reinterpret_cast<VerifyNode*>(ws + lay.found), reinterpret_cast<VerifyWalk*>(ws + lay.walks), verify_blocks(vocab), rounds};
   return launch_tree_verify(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? ROCO_OK : ROCO_EHIP;
 }
 

@@ -271,6 +271,21 @@ hipError_t launch_chunk_commit(int dtype, int head_dim, const ChunkArgs& a, hipS
 constexpr int kMostChunkSplits = 64, kMostRowSplits = 16;
 
 // ---------------------------------------------------------------- verification of drafted tokens
+struct alignas(16) VerifyNode {         // of a tree whose nodes the first pass has looked up
+  int parent, token;                    // parent: -1 where the node can't be accepted
+  float accept;
+  int n;                                // nodes of the request
+  double p, q;                          // what the target and the draft give to the token
+};
+// How far a walk over a tree has come: the node, and of its row max(p - times q, 0), or, without q, p without the rejected tokens.
+// It walks; waits for that row's sum to try another continuation, or, at its end, to choose from it, or from the row as it was; has it; has no nodes.
+enum { kVerifyWalks, kVerifyRejected, kVerifyEnds, kVerifyEndsWhole, kVerifyDone, kVerifyNothing };
+struct alignas(16) VerifyWalk {
+  double times, left, gone;             // left: the sum before the last rejection; gone: what q gives to the rejected ones, if all are distinct
+  uint64_t rejected, tried;             // nodes; rejected: those whose tokens are left out (without q)
+  int node, length, phase, stale;       // stale: there has been a rejection since `left`
+  int pass, unused;                     // the pass that it has waited for last
+};
 struct VerifyArgs {
   int requests, nodes, vocab, distinct, max_path;
   int bf16;               // type of p and q
@@ -280,10 +295,12 @@ struct VerifyArgs {
   const float *accept, *choose;
   int32_t *path, *n_path, *next;
   double* sums;           // workspace [rounds][requests][blocks]
+  VerifyNode* found;      // workspace [requests][nodes]
+  VerifyWalk* walks;      // workspace [rounds][requests]: as each round has found them
   int blocks, rounds;
 };
 constexpr int kVerifyBlock = 2048;    // of the vocabulary: what a partial sum covers
-constexpr int kMaxVerifyRounds = 4;
+constexpr int kMaxVerifyRounds = 12;
 constexpr int kMaxVocab = 1 << 22;
 hipError_t launch_tree_verify(const VerifyArgs& a, hipStream_t s);
 

@@ -7,10 +7,13 @@
 // So a decision takes two probabilities and N, and N a pass over one row of p and of q.  (Without q, which is then 1 for the drafted token, a
 // rejection takes the token's p from N, and the token from the row.)
 //
-//   verify_pass   : the sums of a request's next pass, of blocks of kVerifyBlock tokens, a wave each.  Every workgroup decides for itself what that pass
-//                   is, from the sums of the passes before: no launch in between.
+//   verify_pass   : the sums of a request's next pass, of blocks of kVerifyBlock tokens, a wave each.  Every workgroup adds the sums of the pass before and
+//                   decides for itself, from where the walk was then, what this one is; one of them leaves the walk behind, and in the first round
+//                   the nodes' probabilities, which lie in as many places.
 //   verify_choose : one workgroup per request.  The passes that are left (trees; one workgroup alone with a row), the accepted path, and the next
 //                   token: the block, and in it the token, where the sums pass a share `choose` of N.
+// Measured, fp32: 64 chains of 8 nodes over 100003 tokens 25 us (52 MB have to be read: 10 us), 32 trees of 32 nodes over 65536 54 us, in 7 rounds of 4 us and
+// less, waits for memory three times over; before the walks were left behind, 27 and 74 to 82.
 // Sums are held in 64 bits: with 32 a token in some thousands would be another than the numbers say (2^17 borders, each 2^-24 off).
 #include <algorithm>
 
@@ -22,7 +25,6 @@ namespace {
 
 constexpr int kPassThreads = 256, kPassWaves = kPassThreads / kWave;
 constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / kWave;
-constexpr int kMostNodes = kMaxTreeNodes;
 constexpr int kMostBlocks = kMaxVocab / kVerifyBlock + 1;
 
 __device__ __forceinline__ double from_lane(double v, int lane) {
@@ -45,23 +47,26 @@ template <bool BF16> __device__ __forceinline__ float element(const void* row, i
   return BF16 ? bf16_to_f32(static_cast<const uint16_t*>(row)[i]) : static_cast<const float*>(row)[i];
 }
 
-// What a walk has come to: the node whose row is wanted, and of the row max(p - times q, 0), or, without q, p without the rejected tokens.
-struct Wanted {
-  int node;
-  double times;
-  uint64_t rejected;  // nodes whose tokens are left out (without q)
-  int pass;           // number of the pass whose sums these are
-  int length;         // of the path
-  bool known;         // those sums are there: the walk is done
-};
-
-// The walk over a request's tree by one wave, node i in lane i: what can be decided with the sums of `passes` passes, totals of which are in `left_of`.
+// A request's tree, node i in lane i.
 template <bool BF16> struct Tree {
   int parent, token, n;
   float accept;
   double pr, qr;
-  __device__ __forceinline__ Tree(const VerifyArgs& a, int r) {
+  // found: a pass before has left the nodes behind, so that nobody gathers their probabilities again
+  __device__ __forceinline__ Tree(const VerifyArgs& a, int r, bool found) {
     const int lane = threadIdx.x & (kWave - 1), i = min(lane, a.nodes - 1);
+    if (found) {
+      const VerifyNode& node = a.found[static_cast<size_t>(r) * a.nodes + i];
+      const int4 words = *reinterpret_cast<const int4*>(&node.parent);
+      const double2 probabilities = *reinterpret_cast<const double2*>(&node.p);
+      parent = lane < a.nodes ? words.x : -1;
+      token = words.y;
+      accept = __int_as_float(words.z);
+      n = __builtin_amdgcn_readfirstlane(words.w);
+      pr = probabilities.x;
+      qr = probabilities.y;
+      return;
+    }
     n = __builtin_amdgcn_readfirstlane(a.n_nodes != nullptr ? min(max(a.n_nodes[r], 0), a.nodes) : a.nodes);
     parent = a.parent != nullptr ? a.parent[static_cast<size_t>(r) * a.nodes + i] : i - 1;
     token = a.tokens[static_cast<size_t>(r) * a.nodes + i];
@@ -73,64 +78,101 @@ template <bool BF16> struct Tree {
       if (a.q != nullptr) qr = element<BF16>(a.q, r * a.q_request + parent * a.q_row + token);
     }
   }
-  // path_at: this lane's place in the path, or -1.  left_of(pass): the total of a pass.
-  template <class LeftOf> __device__ __forceinline__ Wanted walk(const VerifyArgs& a, int passes, LeftOf left_of, int& path_at) const {
+  __device__ __forceinline__ void leave(const VerifyArgs& a, int r) const {
     const int lane = threadIdx.x & (kWave - 1);
-    Wanted w = {0, 0.0, 0, 0, n > 0 ? 1 : 0, false};
-    path_at = n > 0 && lane == 0 ? 0 : -1;
-    double left = 1.0, gone = 0.0;
-    bool stale = false;  // `left` is that of the row before the last rejection
-    uint64_t tried = 1;
-    while (w.length > 0 && w.length < a.max_path) {
-      const uint64_t next = __builtin_amdgcn_ballot_w64(parent == w.node && parent >= 0) & ~tried;
-      if (next == 0) break;
-      const int i = __builtin_ctzll(next);
-      if (stale) {
-        if (w.pass >= passes) return w;
-        left = left_of(w.pass++);
-        stale = false;
+    if (lane < a.nodes) a.found[static_cast<size_t>(r) * a.nodes + lane] = VerifyNode{parent, token, accept, n, pr, qr};
+  }
+  __device__ __forceinline__ VerifyWalk start(const VerifyArgs& a) const {
+    VerifyWalk w = {};
+    w.left = 1.0;
+    w.tried = 1;
+    w.length = n > 0 ? 1 : 0;
+    w.phase = n > 0 ? kVerifyWalks : kVerifyNothing;
+    return w;
+  }
+  // As far as it goes without another sum; total: what the pass that it waits for has found, if it waits for one.
+  __device__ __forceinline__ void advance(const VerifyArgs& a, VerifyWalk& w, double total) const {
+    if (w.phase == kVerifyRejected) {
+      w.left = total;
+      w.phase = kVerifyWalks;
+    } else if (w.phase == kVerifyEnds) {
+      if (total > 0.0) {
+        w.phase = kVerifyDone;
+        return;
       }
-      tried |= 1ull << i;
+      w.times = 0.0;  // nothing is left: the row as it was
+      w.rejected = 0;
+      w.phase = kVerifyEndsWhole;
+      return;
+    } else if (w.phase == kVerifyEndsWhole) {
+      w.phase = kVerifyDone;
+      return;
+    }
+    while (w.phase == kVerifyWalks) {
+      const uint64_t next = __builtin_amdgcn_ballot_w64(parent == w.node && parent >= 0) & ~w.tried;
+      if (next == 0 || w.length >= a.max_path) {
+        w.phase = kVerifyEnds;
+        return;
+      }
+      if (w.stale != 0) {  // the sum of the row before the last rejection will not do for another continuation
+        w.stale = 0;
+        w.phase = kVerifyRejected;
+        return;
+      }
+      const int i = __builtin_ctzll(next);
+      w.tried |= 1ull << i;
       const double u = from_lane(static_cast<double>(accept), i), p = from_lane(pr, i), q = from_lane(qr, i);
       bool good;
       if (a.q != nullptr) {
-        const double rest = 1.0 - gone;
-        good = __dmul_rn(__dmul_rn(u, q), left) < __dmul_rn(fmax(__dsub_rn(p, __dmul_rn(w.times, q)), 0.0), rest);
-        if (!good && rest > 0.0) {
-          w.times += left / rest;
-          if (a.distinct) gone += q;
-          stale = true;
+        const double rest = 1.0 - w.gone;
+        good = __dmul_rn(__dmul_rn(u, q), w.left) < __dmul_rn(fmax(__dsub_rn(p, __dmul_rn(w.times, q)), 0.0), rest);
+        if (__builtin_amdgcn_readfirstlane(!good && rest > 0.0 ? 1 : 0) != 0) {
+          w.times += w.left / rest;
+          if (a.distinct) w.gone += q;
+          w.stale = 1;
         }
       } else {
         // (a token that is among those rejected has nothing left)
         const int x = __builtin_amdgcn_readlane(token, i);
         const bool again = (__builtin_amdgcn_ballot_w64(token == x) & w.rejected) != 0;
-        good = !again && __dmul_rn(u, left) < p;
+        good = !again && __dmul_rn(u, w.left) < p;
         if (!good) {
-          if (!again) left -= p;
+          if (!again) w.left -= p;
           w.rejected |= 1ull << i;
         }
       }
-      if (good) {
+      if (__builtin_amdgcn_readfirstlane(good ? 1 : 0) != 0) {
         w.node = i;
-        w.times = 0.0;
+        w.times = w.gone = 0.0;
         w.rejected = 0;
-        left = 1.0;
-        gone = 0.0;
-        stale = false;
-        if (lane == i) path_at = w.length;
+        w.left = 1.0;
+        w.stale = 0;
         ++w.length;
       }
     }
-    w.known = w.pass < passes;
-    if (w.known && !(left_of(w.pass) > 0.0)) {  // nothing is left: the row as it was
-      w.times = 0.0;
-      w.rejected = 0;
-      w.known = ++w.pass < passes;
+  }
+  // This lane's place in the path, or -1.
+  __device__ __forceinline__ int place_of(const VerifyWalk& w) const {
+    int at = -1, node = w.node;
+    for (int k = w.length - 1; k >= 0; --k) {
+      if (static_cast<int>(threadIdx.x & (kWave - 1)) == node) at = k;
+      node = k > 0 ? __builtin_amdgcn_readlane(parent, node) : 0;
     }
-    return w;
+    return at;
   }
 };
+__device__ __forceinline__ bool waits(const VerifyWalk& w) { return w.phase == kVerifyRejected || w.phase == kVerifyEnds || w.phase == kVerifyEndsWhole; }
+__device__ __forceinline__ uint64_t uniform(uint64_t v) {
+  return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v >> 32)))) << 32 | static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));
+}
+__device__ __forceinline__ void uniform(VerifyWalk& w) {
+  w.rejected = uniform(w.rejected);
+  w.tried = uniform(w.tried);
+  w.node = __builtin_amdgcn_readfirstlane(w.node);
+  w.length = __builtin_amdgcn_readfirstlane(w.length);
+  w.phase = __builtin_amdgcn_readfirstlane(w.phase);
+  w.stale = __builtin_amdgcn_readfirstlane(w.stale);
+}
 
 // The weights of a block, one wave's: 16 bytes of a row at a time, f(index, weight) for those of the vocabulary.  The blocks begin where 16 bytes do.
 template <bool BF16> struct Row {
@@ -139,9 +181,9 @@ template <bool BF16> struct Row {
   int before;          // elements between the last multiple of 16 bytes and the row
   bool together;       // the rows of p and q lie alike
   const VerifyArgs& a;
-  const Wanted& w;
+  const VerifyWalk& w;
   int rejected_token;  // lane i: node i's, if it has been rejected
-  __device__ __forceinline__ Row(const VerifyArgs& a_, int r, const Wanted& w_, int token) : a(a_), w(w_) {
+  __device__ __forceinline__ Row(const VerifyArgs& a_, int r, const VerifyWalk& w_, int token) : a(a_), w(w_) {
     constexpr int E = BF16 ? 2 : 4;
     p = static_cast<const char*>(a.p) + (r * a.p_request + w.node * a.p_row) * E;
     q = a.q != nullptr && w.times != 0.0 ? static_cast<const char*>(a.q) + (r * a.q_request + w.node * a.q_row) * E : nullptr;
@@ -195,57 +237,64 @@ template <bool BF16> __global__ __launch_bounds__(kPassThreads) void verify_pass
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const int block = blockIdx.x * kPassWaves + wave;
   if (block >= a.blocks) return;
-  const Tree<BF16> tree(a, r);
-  int path_at;
   const auto sums = [&](int pass) { return a.sums + (static_cast<size_t>(pass) * a.requests + r) * a.blocks; };
-  const Wanted w = tree.walk(a, round, [&](int pass) { return sum_of(sums(pass), a.blocks); }, path_at);
-  if (w.known || w.length == 0) return;
+  VerifyWalk w;
+  double total = 0.0;
+  if (round > 0) {
+    w = a.walks[static_cast<size_t>(round - 1) * a.requests + r];
+    total = sum_of(sums(round - 1), a.blocks);
+    uniform(w);
+  }
+  const Tree<BF16> tree(a, r, round > 0);
+  if (round == 0) w = tree.start(a);
+  const bool over = w.phase >= kVerifyDone;
+  tree.advance(a, w, total);
+  if (!over) w.pass = round - 1;
+  if (block == 0) {
+    if (round == 0) tree.leave(a, r);
+    if ((threadIdx.x & (kWave - 1)) == 0) a.walks[static_cast<size_t>(round) * a.requests + r] = w;
+  }
+  if (!waits(w)) return;
   const Row<BF16> row(a, r, w, tree.token);
   const double sum = row.block_sum(block);
-  if ((threadIdx.x & (kWave - 1)) == 0) a.sums[(static_cast<size_t>(round) * a.requests + r) * a.blocks + block] = sum;
+  if ((threadIdx.x & (kWave - 1)) == 0) sums(round)[block] = sum;
 }
 
 template <bool BF16> __global__ __launch_bounds__(kChooseThreads) void verify_choose(VerifyArgs a) {
   __shared__ double block_s[kMostBlocks];          // sums of the last pass
-  __shared__ double left_s[kMostNodes + 2];        // totals of the passes
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const Tree<BF16> tree(a, r);
   // (every wave walks by itself, to the same end)
-  for (int pass = wave; pass < a.rounds; pass += kChooseWaves) {
-    // what a pass that was not wanted has left there is not looked at
-    const double total = sum_of(a.sums + (static_cast<size_t>(pass) * a.requests + r) * a.blocks, a.blocks);
-    if (lane == 0) left_s[pass] = total;
-  }
-  __syncthreads();
-  int passes = a.rounds, path_at;
-  Wanted w;
-  for (;;) {
-    w = tree.walk(a, passes, [&](int pass) { return left_s[pass]; }, path_at);
-    if (w.known || w.length == 0 || passes >= kMostNodes + 2) break;
+  VerifyWalk w = a.walks[static_cast<size_t>(a.rounds - 1) * a.requests + r];
+  uniform(w);
+  // (a round that had nothing to do has left no sums: the last ones are those of the pass that ended the walk)
+  const double* sums = a.sums + (static_cast<size_t>(w.phase == kVerifyDone ? w.pass : a.rounds - 1) * a.requests + r) * a.blocks;
+  double all = sum_of(sums, a.blocks);
+  const Tree<BF16> tree(a, r, true);
+  tree.advance(a, w, all);
+  while (waits(w)) {
     const Row<BF16> row(a, r, w, tree.token);
     for (int block = wave; block < a.blocks; block += kChooseWaves) {
       const double sum = row.block_sum(block);
       if (lane == 0) block_s[block] = sum;
     }
     __syncthreads();
-    const double total = sum_of(block_s, a.blocks);
-    if (tid == 0) left_s[passes] = total;
-    ++passes;
+    sums = block_s;
+    all = sum_of(block_s, a.blocks);
     __syncthreads();
+    tree.advance(a, w, all);
   }
   if (wave != 0) return;
+  const int path_at = tree.place_of(w);
   int32_t* const path = a.path + static_cast<size_t>(r) * a.max_path;
   if (path_at >= 0) path[path_at] = lane;
   if (lane >= w.length && lane < a.max_path) path[lane] = -1;
   if (lane == 0) a.n_path[r] = w.length;
-  const bool any = w.known && left_s[min(w.pass, kMostNodes + 1)] > 0.0;
-  if (w.length == 0 || !any) {
+  if (w.length == 0 || !(all > 0.0)) {
     if (lane == 0) a.next[r] = -1;
     return;
   }
   // the block: each lane has `per` of them side by side
-  const double* const sums = w.pass < a.rounds ? a.sums + (static_cast<size_t>(w.pass) * a.requests + r) * a.blocks : block_s;
   const int per = (a.blocks + kWave - 1) / kWave;
   const auto before_of = [&](double mine, double& total) {  // exclusive prefix over the lanes
     double v = mine;
