@@ -140,8 +140,8 @@ int check_chunk_shape(const roco_params* p, int32_t heads, int32_t group, int32_
   if (rc != ROCO_OK) return rc;
   if (heads < 1 || p->units % heads != 0 || tokens < 1) return ROCO_EINVAL;
   if (static_cast<long long>(tokens) * heads * group >= (1ll << 31)) return ROCO_EUNSUPPORTED;
-  // (workgroups: of the attention's row tiles and, 32 rows each, their joining, of the sums' keys, of the slots)
-  const long long requests = p->units / heads, tiles = (static_cast<long long>(tokens) * group / 32 + 8 * requests) * heads;
+  // (workgroups: of the attention's row tiles, of the sums' keys, of the slots)
+  const long long requests = p->units / heads, tiles = (static_cast<long long>(tokens) * group / 128 + requests) * heads;
   const long long slots = static_cast<long long>(p->units) * ((p->budget + 127) / 128) + (tokens / 128 + requests) * heads;
   return tiles < kMostWorkgroups && slots < kMostWorkgroups ? ROCO_OK : ROCO_EUNSUPPORTED;
 }

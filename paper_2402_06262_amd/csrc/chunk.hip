@@ -123,7 +123,7 @@ ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads
   c.row_tile = pair ? 256 : 128;
   c.row_tiles = tiles_of(requests, tokens, group, c.row_tile);
   const long long tiles = static_cast<long long>(c.row_tiles) * heads, full = pair ? rows / 256 * heads : tiles;
-  const int most = static_cast<int>(std::max(1ll, std::min({static_cast<long long>(kMostChunkSplits), keys * 32 / kLeastKeys, kMostTiles / tiles})));
+  const int most = static_cast<int>(std::max(1ll, std::min({static_cast<long long>(kMostChunkSplits), keys * 32 / chunk_least_keys(dtype, c.row_tile), kMostTiles / tiles})));
   c.splits = 1;
   long long least = -1;
   for (int i = 1; i <= most; ++i) {
@@ -133,7 +133,7 @@ ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads
       c.splits = i;
     }
   }
-  if (splits >= 1) c.splits = static_cast<int>(std::max(1ll, std::min<long long>(splits, (kMostWorkgroups - 8) / tiles)));
+  if (splits >= 1 && tiles * 32 < kMostWorkgroups) c.splits = static_cast<int>(std::max(1ll, std::min<long long>(splits, (kMostWorkgroups - 8) / tiles)));
   return c;
 }
 

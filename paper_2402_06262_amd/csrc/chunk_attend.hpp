@@ -43,13 +43,13 @@ template <int ROWS> __device__ __forceinline__ bool row_tile_of(const ChunkArgs&
   return t.rows > 0;
 }
 // What it sees, in stages of KEYS keys: the cache's and the chunk's, and the shares of them that its workgroups take.
-template <int KEYS> struct Plan {
+template <int DT, int ROWS, int KEYS> struct Plan {
   int n, cache_stages, stages, per, used;
   __device__ __forceinline__ Plan(const ChunkArgs& a, const RowTile& t) {
     n = __builtin_amdgcn_readfirstlane(min(max(a.n_used[t.at.request * a.heads + t.head], 0), budget_of(a.pages, a.B, t.at.request)));
     cache_stages = (n + KEYS - 1) / KEYS;
     stages = __builtin_amdgcn_readfirstlane(cache_stages + (t.first_row + t.rows - 1) / a.group / KEYS + 1);
-    per = __builtin_amdgcn_readfirstlane(max((stages + a.splits - 1) / a.splits, kLeastKeys / KEYS));
+    per = __builtin_amdgcn_readfirstlane(max((stages + a.splits - 1) / a.splits, chunk_least_keys(DT, ROWS) / KEYS));
     used = __builtin_amdgcn_readfirstlane((stages + per - 1) / per);
   }
 };
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(kThreads, 1) void chunk_attend_pair(ChunkArgs a) {
   const int u = at.request * a.heads + head;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int half = lane >> 5;
-  const Plan<64> plan(a, mine);
+  const Plan<DT, 4 * 32 * NG, 64> plan(a, mine);
   const int n = plan.n, cache_stages = plan.cache_stages;
   const int t0 = mine.split * plan.per, t1 = min(plan.stages, t0 + plan.per);
   if (t0 >= t1) return;
@@ -525,8 +525,9 @@ __global__ __launch_bounds__(kThreads, 1) void chunk_attend_pair(ChunkArgs a) {
 }
 
 // 32 rows of a wave, 32 keys of a stage, one after the other, and as many waves as there is room for.
-// Measured: 24 requests, of which 18 decode a token and the others take 384 or fewer, 8 heads of 4 queries, over 4096 keys or fewer, 174 us; 6 requests of up to
-// 333 tokens over 2048, 12 heads, 64 dimensions, with a recency window, 50 us; fp32, 5 requests of up to 101 tokens over 1501, 5 heads of 3 queries, 77 us.
+// Measured: 24 requests, of which 18 decode a token and the others take 384 or fewer, 8 heads of 4 queries, over 4096 keys or fewer, 166 us; 32 that decode a token
+// over 4096 keys each 112 us (4.8 TB/s); 6 of up to 333 tokens over 2048, 12 heads, 64 dimensions, with a recency window, 45 us; fp32, 5 of up to 101 over 1501,
+// 5 heads of 3 queries, 70 us, and 4 that decode a token over 500, 4 heads, 64 dimensions, 14 us.
 template <int DT, int HD> struct TileForm {
   using R = Rows<DT, HD>;
   static constexpr int kTileBytes = kSub * R::kBytes;             // of K, then as many of V
@@ -553,7 +554,7 @@ __global__ __launch_bounds__(kThreads, (TileForm<DT, HD>::kWavesPerSimd)) void c
   const int u = at.request * a.heads + head;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int half = lane >> 5;
-  const Plan<kSub> plan(a, mine);
+  const Plan<DT, 128, kSub> plan(a, mine);
   const int n = plan.n, cache_tiles = plan.cache_stages;
   const int t0 = mine.split * plan.per, t1 = min(plan.stages, t0 + plan.per);
   if (t0 >= t1) return;
@@ -751,35 +752,47 @@ __global__ __launch_bounds__(kThreads, (TileForm<DT, HD>::kWavesPerSimd)) void c
   if (!idle) Finish<DT, HD, 1, WINDOW>::run(a, mine, plan.used, row, token, own, m, l, o, zeroed, min((t1 - cache_tiles) * kSub - 1, wave_last));
 }
 
-// The splits' shares of 32 rows of a tile, HD / 4 lanes with 16 bytes of a row each; in the order of the splits.
+// The splits' shares of a few rows of a tile, HD / 4 lanes with 16 bytes of a row each; four splits at a time, in their order.
 template <int DT, int HD, int ROWS, int KEYS> __global__ __launch_bounds__(kThreads) void chunk_join(ChunkArgs a) {
-  constexpr int LANES = HD / 4, PER = kThreads / LANES, kParts = ROWS / 32;
-  const int part = blockIdx.x % kParts;
+  constexpr int LANES = HD / 4, PER = kThreads / LANES, kParts = ROWS / PER, kAtOnce = 4;
   RowTile t;
   if (!row_tile_of<ROWS>(a, blockIdx.x / kParts, t)) return;
-  const Plan<KEYS> plan(a, t);
-  if (plan.used == 1) return;  // (it has written its rows)
-  const int sub = threadIdx.x % LANES;
+  const Plan<DT, ROWS, KEYS> plan(a, t);
+  const int i = blockIdx.x % kParts * PER + threadIdx.x / LANES, sub = threadIdx.x % LANES;
+  if (plan.used == 1 || i >= t.rows) return;  // (one split has written its rows)
   const size_t plane = static_cast<size_t>(a.tokens) * a.heads * a.group;
+  const int row = t.first_row + i;
+  const size_t at = packed_row(a, t, row, row / a.group);
+  float M = -INFINITY, sum = 0.0f;
+  tree::f32x4 o = tree::f32x4{0};
 #pragma unroll 1
-  for (int i = 32 * part + threadIdx.x / LANES; i < min(t.rows, 32 * part + 32); i += PER) {
-    const int row = t.first_row + i;
-    const size_t at = packed_row(a, t, row, row / a.group);
-    float M = -INFINITY;
-#pragma unroll 4
-    for (int k = 0; k < plan.used; ++k) M = fmaxf(M, a.part_m[k * plane + at]);
-    tree::f32x4 o = tree::f32x4{0};
-    float sum = 0.0f;
-#pragma unroll 4
-    for (int k = 0; k < plan.used; ++k) {
-      const float mk = a.part_m[k * plane + at], lk = a.part_l[k * plane + at];
-      const float w = mk > -INFINITY ? fast_exp2(mk - M) : 1.0f;  // (no maximum: a sum of zero, or NaN)
-      o += *reinterpret_cast<const tree::f32x4*>(a.part_o + (k * plane + at) * HD + 4 * sub) * w;
-      sum += lk * w;
+  for (int k0 = 0; k0 < plan.used; k0 += kAtOnce) {
+    float m[kAtOnce], l[kAtOnce];
+    tree::f32x4 part[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const size_t from = min(k0 + k, plan.used - 1) * plane + at;
+      m[k] = a.part_m[from];
+      l[k] = a.part_l[from];
+      part[k] = *reinterpret_cast<const tree::f32x4*>(a.part_o + from * HD + 4 * sub);
     }
-    tree::store4<DT>(a.out, at * HD + 4 * sub, o * (1.0f / sum));
-    if (a.lse != nullptr && sub == 0) a.lse[at] = kLn2 * (M + __log2f(sum));
+    float most = M;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) most = fmaxf(most, m[k]);
+    const float before = M > -INFINITY ? fast_exp2(M - most) : 1.0f;
+    o *= before;
+    sum *= before;
+    M = most;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (k0 + k >= plan.used) break;
+      const float w = m[k] > -INFINITY ? fast_exp2(m[k] - M) : 1.0f;  // (no maximum: a sum of zero, or NaN)
+      o += part[k] * w;
+      sum += l[k] * w;
+    }
   }
+  tree::store4<DT>(a.out, at * HD + 4 * sub, o * (1.0f / sum));
+  if (a.lse != nullptr && sub == 0) a.lse[at] = kLn2 * (M + __log2f(sum));
 }
 
 #pragma clang diagnostic pop
@@ -794,7 +807,7 @@ template <int DT, int HD, int ROWS, int KEYS, class Kernel> hipError_t launch_ti
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   ProfScope ps(kProfChunkJoin, s);
-  hipLaunchKernelGGL((chunk_join<DT, HD, ROWS, KEYS>), dim3(static_cast<unsigned>(a.row_tiles * a.heads * (ROWS / 32))), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((chunk_join<DT, HD, ROWS, KEYS>), dim3(static_cast<unsigned>(a.row_tiles) * a.heads * (ROWS / (kThreads / (HD / 4)))), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 template <int DT, int HD, bool WINDOW> hipError_t launch_attend_form(const ChunkArgs& a, hipStream_t s) {

@@ -262,7 +262,9 @@ struct ChunkArgs {
   __host__ __device__ size_t fresh_plane() const { return static_cast<size_t>(tokens) * heads; }
   uint32_t* keys;                             // workspace [units][2][B] when B is too large for LDS
 };
-constexpr int kLeastKeys = 128;       // of a workgroup of chunk_attend, if its tile sees more than that
+// Keys of a workgroup of chunk_attend, if its tile sees more than that.  (With 128 of them everywhere 4 requests that decode a token over 500 keys, 4 heads, fp32,
+// took 20 us, not 14; 1 over 1024, 8 heads, bf16, 15 us either way.)
+__host__ __device__ constexpr int chunk_least_keys(int dtype, int row_tile) { return dtype != 1 ? 32 : row_tile == 256 ? 128 : 64; }
 struct ChunkSplits { int row_tile, row_tiles, splits; };
 ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
 int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B);
