@@ -12,10 +12,11 @@ def tree_verify(p, q, tokens: Sequence[int], parent: Optional[Sequence[int]], n_
     """p, q [nodes, vocab] (q may be None); the accepted nodes and the next token (-1: none)."""
     if n_nodes == 0:
         return [], -1
-    p = np.asarray(p, dtype=np.float64)
+    clean = lambda v: np.where(np.asarray(v, dtype=np.float64) > 0, v, 0.0).astype(np.float64)  # noqa: E731
+    p = clean(p)
+    q = None if q is None else clean(q)
     vocab = p.shape[1]
     path, at, tried = [0], 0, 0
-    clean = lambda v: np.where(np.asarray(v, dtype=np.float64) > 0, v, 0.0).astype(np.float64)  # noqa: E731
     target = p[at].copy()          # (as it is given: not normalised before the first rejection)
     draft = None if q is None else np.asarray(q[at], dtype=np.float64).copy()
     spent, left = 0.0, 1.0         # what distinct continuations have taken of q; what rejections have left of p, without q

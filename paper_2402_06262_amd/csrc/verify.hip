@@ -46,6 +46,7 @@ __device__ __forceinline__ double sum_of(const double* sums, int blocks) {  // i
 template <bool BF16> __device__ __forceinline__ float element(const void* row, int64_t i) {
   return BF16 ? bf16_to_f32(static_cast<const uint16_t*>(row)[i]) : static_cast<const float*>(row)[i];
 }
+__device__ __forceinline__ float probability(float v) { return fmaxf(v, 0.0f); }  // (NaN: zero)
 
 // A request's tree, node i in lane i.
 template <bool BF16> struct Tree {
@@ -74,8 +75,8 @@ template <bool BF16> struct Tree {
     if (lane >= n || lane == 0 || parent < 0 || parent >= lane || token < 0 || token >= a.vocab) parent = -1;  // such a node is never accepted
     pr = qr = 0.0;
     if (parent >= 0) {
-      pr = element<BF16>(a.p, r * a.p_request + parent * a.p_row + token);
-      if (a.q != nullptr) qr = element<BF16>(a.q, r * a.q_request + parent * a.q_row + token);
+      pr = probability(element<BF16>(a.p, r * a.p_request + parent * a.p_row + token));
+      if (a.q != nullptr) qr = probability(element<BF16>(a.q, r * a.q_request + parent * a.q_row + token));
     }
   }
   __device__ __forceinline__ void leave(const VerifyArgs& a, int r) const {
@@ -202,7 +203,7 @@ template <bool BF16> struct Row {
     }
   }
   __device__ __forceinline__ double weight(float x, float y) const {
-    const double v = q != nullptr ? __dsub_rn(static_cast<double>(x), __dmul_rn(w.times, static_cast<double>(y))) : static_cast<double>(x);
+    const double v = q != nullptr ? __dsub_rn(static_cast<double>(x), __dmul_rn(w.times, static_cast<double>(probability(y)))) : static_cast<double>(x);
     return v > 0.0 ? v : 0.0;  // (NaN: none)
   }
   __device__ __forceinline__ bool left_out(int i) const {

@@ -95,3 +95,102 @@ def test_short_paths_and_sizes_of_trees(max_path):
 def test_large_vocabulary():
     b = Batch(5, 3, 6, 131072, 2, "distinct", spread=4.0)
     b.check(*b.run())
+
+
+@pytest.mark.parametrize("drafts", ["sampled", "distinct", "given"])
+@pytest.mark.parametrize("bad", [np.nan, -0.25, -np.inf])
+def test_what_is_no_probability_counts_as_zero(drafts, bad):
+    b = Batch(11, 8, 9, 300, 3, drafts, apart=1.5)
+    for t in (b.p, b.q):
+        t[:, :, 5::7] = bad
+    b.tokens[:, 3::4] = 12  # (one of those)
+    b.hp, b.hq = b.p.double().cpu().numpy(), b.q.double().cpu().numpy()
+    b.check(*b.run())
+    b.p[2:4] = bad  # nothing is left at all
+    b.hp = b.p.double().cpu().numpy()
+    path, n_path, nxt = b.run()
+    b.check(path, n_path, nxt)
+    assert (nxt[2:4] == -1).all()
+
+
+def test_tokens_outside_the_vocabulary_and_parents_that_are_none():
+    b = Batch(12, 4, 8, 200, 2, "sampled", apart=0.1)
+    b.tokens[0, 1], b.tokens[1, 1], b.tokens[2, 2] = -1, 200, 2 ** 31 - 1
+    b.parent[0, 2], b.parent[1, 3], b.parent[3, 4] = 5, -3, 4
+    b.check(*b.run())
+
+
+@pytest.mark.parametrize("value", [0.0, 1.0 - 2.0 ** -24])
+def test_random_numbers_at_the_ends(value):
+    for drafts in ("sampled", "distinct", "given"):
+        b = Batch(13, 5, 7, 5000, 2, drafts)
+        b.accept[:], b.choose[:] = value, value
+        b.check(*b.run())
+
+
+def test_accepted_whole_where_draft_and_target_agree():
+    b = Batch(14, 6, 8, 1000, 1, apart=0.0)
+    b.q = b.p.clone()
+    b.hq = b.hp
+    for r in range(6):
+        b.tokens[r, 1:] = [np.argmax(b.hp[r, i]) for i in range(7)]
+    path, n_path, nxt = b.run()
+    b.check(path, n_path, nxt)
+    assert (n_path == 8).all()
+
+
+def test_requests_that_share_rows_of_the_draft():
+    b = Batch(15, 6, 5, 800, 2)
+    shared = b.q[:1].expand(6, -1, -1)
+    b.hq = shared.double().cpu().numpy()
+    b.check(*b.run(q=shared))
+
+
+def test_many_requests():
+    b = Batch(16, 700, 3, 64, 2, "distinct")
+    b.check(*b.run())
+
+
+def test_captured_and_replayed_with_other_inputs():
+    """Graphs of two shapes that share a workspace; a pass leaves nothing for the next."""
+    batches = [Batch(17, 5, 12, 9000, 3, "distinct"), Batch(18, 9, 5, 3000, 1)]
+    f = lambda x: torch.from_numpy(np.ascontiguousarray(x)).float().cuda()  # noqa: E731
+    ws = torch.full((max(roco.verify_workspace_bytes(b.R, b.T, b.V) for b in batches),), 0xEE, dtype=torch.uint8, device="cuda")
+    side, graphs = torch.cuda.Stream(), []
+    for b in batches:
+        b.max_path = b.T
+        i = lambda x: torch.from_numpy(np.ascontiguousarray(x)).int().cuda()  # noqa: E731
+        b.out = [torch.full((b.R, b.T), -9, dtype=torch.int32, device="cuda")] + [torch.full((b.R,), -9, dtype=torch.int32, device="cuda") for _ in range(2)]
+        b.numbers = f(b.accept), f(b.choose)
+        args = (b.p, b.q, i(b.tokens), None if b.chain else i(b.parent), i(b.n_nodes), *b.numbers, *b.out, ws)
+        b.call = lambda b=b, args=args: roco.roco_tree_verify(*args, distinct=b.drafts == "distinct")
+        b.call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+            b.call()
+        graphs.append(graph)
+    rng = np.random.default_rng(0)
+    for turn in range(4):
+        for b, graph in zip(batches, graphs):
+            b.accept, b.choose = rng.random((b.R, b.T), dtype=np.float32), rng.random(b.R, dtype=np.float32)
+            for t, x in zip(b.numbers, (b.accept, b.choose)):
+                t.copy_(f(x))
+            torch.cuda.synchronize()
+            if turn == 2:
+                b.call()
+            else:
+                graph.replay()
+            torch.cuda.synchronize()
+            b.check(*(t.cpu().numpy() for t in b.out))
+
+
+def test_rows_beyond_32_bits_of_elements():
+    """The last request's rows begin behind 2^32 bytes."""
+    R, T = 3, 2
+    b = Batch(19, R, T, 500, 1)
+    far = torch.zeros((R, (1 << 29) + 64), device="cuda")
+    p = far.as_strided((R, T, 500), (far.stride(0), 600, 1))
+    p.copy_(b.p)
+    assert p.stride(0) * (R - 1) * 4 > 1 << 32
+    b.check(*b.run(p=p))
