@@ -142,7 +142,7 @@ int check_chunk_shape(const roco_params* p, int32_t heads, int32_t group, int32_
   if (static_cast<long long>(tokens) * heads * group >= (1ll << 31)) return ROCO_EUNSUPPORTED;
   // (workgroups: of the attention's row tiles, of the sums' keys, of the slots)
   const long long requests = p->units / heads, tiles = (static_cast<long long>(tokens) * group / 128 + requests) * heads;
-  const long long slots = static_cast<long long>(p->units) * ((p->budget + 127) / 128) + (tokens / 128 + requests) * heads;
+  const long long slots = static_cast<long long>(p->units) * ((p->budget + 127) / 128 + 1) + (tokens / 128 + requests) * heads + 16;
   return tiles < kMostWorkgroups && slots < kMostWorkgroups ? ROCO_OK : ROCO_EUNSUPPORTED;
 }
 // A token's rows, `count` of them, lie side by side; the tokens `stride` elements apart.
@@ -174,7 +174,7 @@ ChunkLayout chunk_layout(const roco_params* p, int32_t heads, int32_t group, int
 // What the two calls of chunks have in common.
 int chunk_args(const roco_params* params, int32_t heads, int32_t group, int32_t tokens, const roco_pages* pages, const void* q, int64_t q_stride,
                const void* k_new, const void* v_new, int64_t kv_stride, const int32_t* token_start, const int32_t* qpos0, const void* K_cache,
-               const void* V_cache, const int32_t* pos, const int32_t* n_used, const void* workspace, size_t workspace_bytes, ChunkArgs& a, ChunkLayout& lay) {
+               const void* V_cache, const int32_t* pos, const int32_t* n_used, const void* workspace, ChunkArgs& a, ChunkLayout& lay) {
   int rc = check_chunk_shape(params, heads, group, tokens);
   if (rc != ROCO_OK) return rc;
   a = ChunkArgs{};
@@ -189,7 +189,6 @@ int chunk_args(const roco_params* params, int32_t heads, int32_t group, int32_t 
     if (ptr == nullptr || !aligned16(ptr)) return ROCO_EINVAL;
   if (!given(token_start) || !given(qpos0) || !given(pos) || !given(n_used)) return ROCO_EINVAL;
   lay = chunk_layout(params, heads, group, tokens);
-  if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
   const int64_t element = params->dtype == ROCO_BF16 ? 2 : 4;
   a.units = params->units; a.requests = params->units / heads; a.heads = heads; a.group = group; a.tokens = tokens;
   a.B = params->budget; a.scope = params->scope;
@@ -697,9 +696,10 @@ int roco_chunk_attend(const roco_params* params, int32_t heads, int32_t group, i
   ChunkArgs a;
   ChunkLayout lay;
   const int rc = chunk_args(params, heads, group, tokens, pages, q, q_stride, k_new, v_new, kv_stride, token_start, qpos0, K_cache, V_cache, pos, n_used,
-                            workspace, workspace_bytes, a, lay);
+                            workspace, a, lay);
   if (rc != ROCO_OK) return rc;
   if (out == nullptr || !aligned16(out) || !aligned4(lse)) return ROCO_EINVAL;
+  if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
   a.out = out; a.lse = lse;
   char* ws = static_cast<char*>(workspace);
   a.part_m = reinterpret_cast<float*>(ws);
@@ -716,9 +716,10 @@ int roco_chunk_commit(const roco_params* params, int32_t heads, int32_t group, i
   ChunkArgs a;
   ChunkLayout lay;
   const int rc = chunk_args(params, heads, group, tokens, pages, q, q_stride, k_new, v_new, kv_stride, token_start, qpos0, K_cache, V_cache, pos, n_used,
-                            workspace, workspace_bytes, a, lay);
+                            workspace, a, lay);
   if (rc != ROCO_OK) return rc;
   if (!given(lse) || !given(stats) || !aligned4(evicted_slot) || !aligned4(evicted_pos)) return ROCO_EINVAL;
+  if (workspace_bytes < lay.total) return ROCO_EWORKSPACE;
   a.lse = const_cast<float*>(lse); a.stats = stats; a.evicted_slot = evicted_slot; a.evicted_pos = evicted_pos;
   char* ws = static_cast<char*>(workspace);
   a.info = reinterpret_cast<int32_t*>(ws);

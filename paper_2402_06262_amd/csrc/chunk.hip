@@ -141,9 +141,9 @@ ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads
 int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B) {
   const char* const asked = getenv("ROCO_CHUNK_ROW_SPLITS");
   const int splits = asked != nullptr ? std::min(atoi(asked), kMostRowSplits) : 0;
-  if (splits >= 1) return splits;
   const int keys = column_keys(dtype);
   const long long blocks = (static_cast<long long>(requests) * ((B + keys - 1) / keys) + tiles_of(requests, tokens, 1, keys)) * heads;
+  if (splits >= 1) return static_cast<int>(std::max(1ll, std::min<long long>(splits, (kMostWorkgroups - 16ll - static_cast<long long>(requests) * heads) / blocks)));
   const long long most = tokens / column_tokens(group) / RowShares::kLeastTiles;
   return static_cast<int>(std::max(1ll, std::min({2048 / blocks, most, static_cast<long long>(kMostRowSplits)})));
 }

@@ -347,7 +347,7 @@ __global__ __launch_bounds__(kThreads, 1) void chunk_attend_pair(ChunkArgs a) {
     const bool of_new = t >= cache_stages;
     const int j0 = (c - 2 * cache_stages) * kSub;  // the first token
     const int32_t* const pos_c = &pos_s[WINDOW ? wave : 0][WINDOW ? t & (kSide - 1) : 0][kSub * h];
-    bool interior = of_new ? j0 + kSub - 1 + w <= wave_first : full;
+    bool interior = of_new ? w <= wave_first - (j0 + kSub - 1) : full;  // (in this order: w may be the largest number)
     if (WINDOW && !of_new) {  // outside the window of every row
       const int at_slot = pos_c[lane & 31];
       interior = interior && !__any(at_slot <= qp0 + wave_last && at_slot > qp0 + wave_first - w);

@@ -299,3 +299,376 @@ def test_policies(policy, group):
     lse = s.exact_lse()
     s.commit(lse)
     s.check_commit(lse)
+
+
+# ---------------------------------------------------------------------------------------------------- many rows of bf16 / 128: 64 rows of a wave
+@pytest.mark.parametrize("used,tokens,group,page", [([300, 70, 0], [400, 500, 300], 4, 0), ([129], [1100], 1, 0), ([65, 31], [600, 0], 8, 16), ([500, 16, 64], [70, 3, 1], 64, 64),
+                                                    ([1], [257], 5, 32), ([640], [128], 16, 0)])
+@pytest.mark.parametrize("splits", [0, 1, 3])
+def test_many_rows(used, tokens, group, page, splits, monkeypatch):
+    if splits:
+        monkeypatch.setenv("ROCO_CHUNK_SPLITS", str(splits))
+    assert sum(tokens) * group >= 1024 * len(used)
+    s = Step(sum(tokens) + page, "bf16", 128, used, tokens, heads=2, group=group, page=page, B=max(used) + 5, spare=(1, 4)).upload()
+    s.check_attend(*s.attend())
+
+
+@pytest.mark.parametrize("window", [1, 33, 200, 2 ** 31 - 1])
+@pytest.mark.parametrize("page,splits", [(0, 0), (32, 2)])
+def test_many_rows_under_a_window(window, page, splits, monkeypatch):
+    if splits:
+        monkeypatch.setenv("ROCO_CHUNK_SPLITS", str(splits))
+    s = Step(page, "bf16", 128, [200, 333], [300, 250], heads=1, group=4, window=window, page=page).upload()
+    s.check_attend(*s.attend())
+
+
+FORMS = [(dtype, d, [90, 33], [70, 40], 2) for dtype, d in TYPES] + [("bf16", 128, [90, 33], [300, 250], 4)]
+
+
+@pytest.mark.parametrize("dtype,d,used,tokens,group", FORMS)
+@pytest.mark.parametrize("window", [0, 25])
+@pytest.mark.parametrize("splits", [1, 2])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_what_a_row_does_not_see_does_not_reach_it(dtype, d, used, tokens, group, window, splits, bad, monkeypatch):
+    """Values and keys of one token, some values of another: rows before them keep their bits, rows that see the second alone take it in its dimensions."""
+    monkeypatch.setenv("ROCO_CHUNK_SPLITS", str(splits))
+    s = Step(1, dtype, d, used, tokens, heads=1, group=group, window=window).upload()
+    clean, clean_lse = s.attend()
+    s.check_attend(clean, clean_lse)
+    second, first = s.start[1] - 30, s.start[1] - 9  # tokens of the first request
+    s.dv[second, :, 3:9] = bad
+    s.dv[first], s.dk[first] = bad, bad
+    out, lse = s.attend()
+    before = np.r_[0:second, s.start[1]:s.total]
+    assert np.array_equal(out[before], clean[before]) and np.array_equal(lse[before], clean_lse[before])
+    between = slice(second, first)
+    assert np.array_equal(lse[between], clean_lse[between])
+    touched = out[between][..., 3:9]
+    assert np.isnan(touched).all() if math.isnan(bad) else (touched == bad).all()
+    assert not np.isfinite(out[first]).any()
+    # the other dimensions: the token's own share is added in another place, one rounding more
+    w = s.want(0)
+    i, rest = slice(second, first), [c for c in range(d) if not 3 <= c < 9]
+    rel = 2 * (d + 8) * U * w.logit + (8 + 2 * math.sqrt(sum(used) + sum(tokens))) * U + (0 if dtype == "f32" else 2.0 ** -8)
+    half = 2.0 ** -8 if dtype == "bf16" else U
+    err = np.abs(out[i] - w.out[i])[..., rest]
+    assert (err <= (rel * w.mass[i] + half * np.abs(w.out[i]) + 1e-30)[..., rest]).all()
+
+
+@pytest.mark.parametrize("dtype,d,used,tokens,group", FORMS)
+@pytest.mark.parametrize("window", [4, 1 << 20])
+@pytest.mark.parametrize("bias", [-1e38, -300.0, 1e38])
+def test_recency_biases_of_any_size(dtype, d, used, tokens, group, window, bias):
+    s = Step(2, dtype, d, used, tokens, heads=1, group=group, window=window)
+    s.bias = float(np.float32(bias))
+    s.upload()
+    s.check_attend(*s.attend())
+
+
+@pytest.mark.parametrize("dtype,d,used,tokens,group", FORMS)
+def test_logits_far_apart(dtype, d, used, tokens, group):
+    """Scores that rise by hundreds from tile to tile: the sums' reference has to follow, and what is far below it has no weight."""
+    s = Step(3, dtype, d, used, tokens, heads=1, group=group)
+    rnd = round_to_bf16 if dtype == "bf16" else (lambda x: x)
+    s.K = rnd((s.K * np.linspace(0.1, 30, s.B)[None, :, None]).astype(np.float32))
+    s.k_new = rnd((s.k_new * np.linspace(60, 0.1, s.total)[:, None, None]).astype(np.float32))
+    s.upload()
+    s.check_attend(*s.attend())
+
+
+@pytest.mark.parametrize("dtype,d,used,tokens,group", FORMS)
+def test_pages_outside_the_pool_are_not_seen(dtype, d, used, tokens, group):
+    """... and neither read nor written: the slots' statistics stay, the others' are as if those were not there."""
+    s = Step(4, dtype, d, used, tokens, heads=1, group=group, page=16, B=90 + 16, budgets=[106, 40]).upload()
+    bad = s.table.copy()
+    bad[0, 1], bad[0, 3], bad[1, 0] = -5, s.n_pages, 2 ** 31 - 1
+    s.pages = roco.RocoPages(dev(bad), s.n_pages, 16, dev(np.array(s.budgets)))
+    out, lse = s.attend()
+    gone = [np.r_[16:32, 48:64], np.r_[0:16]]
+    for u in range(2):
+        keep = np.setdiff1d(np.arange(used[u]), gone[u])
+        q, k, v = s.rows(u)
+        w = trees.tree_attend(s.K[u, keep], s.V[u, keep], s.pos[u, keep], q, k, v, list(range(-1, tokens[u] - 1)), int(s.qpos0[u]), s.sc)
+        a, b = s.start[u], s.start[u + 1]
+        x = (d + 8) * U * w.logit
+        rel = 2 * x + (8 + 2 * math.sqrt(used[u] + tokens[u])) * U + (0 if dtype == "f32" else 2.0 ** -8)
+        assert (np.abs(out[a:b] - w.out) <= rel * w.mass + (2.0 ** -8 if dtype == "bf16" else U) * np.abs(w.out) + 1e-30).all()
+        assert (np.abs(lse[a:b] - w.lse) <= x + (8 + math.sqrt(used[u] + tokens[u])) * U + 2.0 ** -22 * np.abs(w.lse)).all()
+    K, stats = s.dK.clone(), s.dstats.clone()
+    s.commit(lse.astype(np.float32))
+    ev = s.ev_slot.cpu().numpy()
+    after, pos = s.dstats.cpu().numpy(), s.dpos.cpu().numpy()
+    for u in range(2):
+        taken = set(ev[s.start[u]:s.start[u + 1], 0].tolist())
+        stay = [j for j in gone[u] if j not in taken]
+        assert (after[u][:, stay] == stats[u].cpu().numpy()[:, stay]).all() and (pos[u, stay] == s.pos[u, stay]).all()
+        seen = [j for j in range(used[u]) if j not in taken and j not in gone[u]]
+        assert (after[u][2, seen] == s.stats[u][2, seen] + min(tokens[u], s.budgets[u])).all()
+    named = np.unique(bad[(bad >= 0) & (bad < s.n_pages)])
+    others = np.setdiff1d(np.arange(s.n_pages), named)
+    assert len(others) and torch.equal(s.dK[others].nan_to_num(7), K[others].nan_to_num(7))
+
+
+# ---------------------------------------------------------------------------------------------------- taking over: sizes and shares
+@pytest.mark.parametrize("row_splits", [1, 2, 5, 16])
+@pytest.mark.parametrize("dtype,d,group", [("bf16", 128, 4), ("bf16", 64, 1), ("f32", 128, 3), ("f32", 64, 40)])
+def test_rows_shared_by_workgroups(row_splits, dtype, d, group, monkeypatch):
+    monkeypatch.setenv("ROCO_CHUNK_ROW_SPLITS", str(row_splits))
+    s = Step(row_splits, dtype, d, [300, 10, 150], [290, 40, 1], group=group, B=300, budgets=None, spare=(0, 1)).upload()
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+
+
+@pytest.mark.parametrize("B", [4095, 4096, 4097, 19000, 30000])
+def test_large_budgets(B):
+    s = Step(B, "bf16", 64, [B, B - 3], [40, 9], heads=1, group=2, B=B, scope=300).upload()
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+
+
+@pytest.mark.parametrize("n", [5, 64, 500])
+def test_equal_statistics_are_told_apart_by_their_slots(n):
+    s = Step(n, "f32", 64, [n], [n - 2], B=n, scope=n)
+    s.stats[:] = np.array([3.0, 5.0, 2.0], np.float32)[None, :, None]
+    s.upload()
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+    assert s.ev_slot[:, 0].tolist() == list(range(n - 2))
+
+
+def test_no_records_of_the_evicted_and_chunks_larger_than_the_budget():
+    s = Step(5, "bf16", 128, [64, 30], [100, 64], group=2, B=64, budgets=None).upload()
+    lse = s.exact_lse()
+    s.commit(lse, evicted_slot=None, evicted_pos=None)
+    first = [x.clone() for x in (s.dK, s.dV, s.dstats, s.dpos, s.dn_used)]
+    s.upload()
+    s.commit(lse)
+    s.check_commit(lse)
+    assert all(torch.equal(x, y) for x, y in zip(first, (s.dK, s.dV, s.dstats, s.dpos, s.dn_used)))
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_words_that_begin_anywhere(off):
+    """Statistics, positions, lengths and normalisers are parts of larger buffers."""
+    s = Step(off, "bf16", 64, [120, 40], [70, 33], group=3, B=130, window=20).upload()
+
+    def moved(t):
+        buffer = torch.empty(t.numel() + 8, dtype=t.dtype, device="cuda")
+        part = buffer[off:off + t.numel()].view(t.shape)
+        part.copy_(t)
+        return part
+
+    s.dstart, s.dqpos0, s.dpos, s.dn_used, s.dstats, s.lse = (moved(t) for t in (s.dstart, s.dqpos0, s.dpos, s.dn_used, s.dstats, s.lse))
+    s.check_attend(*s.attend())
+    lse = s.exact_lse()
+    s.commit(lse, lse=moved(dev(lse, "f32")))
+    s.check_commit(lse)
+
+
+# ---------------------------------------------------------------------------------------------------- large caches
+def test_offsets_beyond_32_bits():
+    """Dense caches of 4.3 GB: the last unit's rows lie behind 2^32 bytes, its keys fill 2^21 slots."""
+    heads, B, d, n = 8, (1 << 21) + 40, 128, (1 << 21) + 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    K, V = (torch.randn((heads, B, d), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    assert heads * B * d * 2 > 1 << 32
+    T = 3
+    q, k, v = (torch.randn((T, heads, d), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    p = roco.RocoParams(heads, d, B, 16, roco.ROCO_BF16)
+    pos = torch.arange(B, dtype=torch.int32, device="cuda").repeat(heads, 1)
+    used, start, first = i32(*[n] * heads), i32(0, T), i32(B + 7)
+    stats = torch.rand((heads, 3, B), generator=g, device="cuda")
+    stats[:, 2] = 10.0
+    before = stats.clone()
+    out, lse = torch.zeros((T, heads, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((T, heads), device="cuda")
+    ws = torch.empty(roco.chunk_workspace_bytes(p, heads, 1, T), dtype=torch.uint8, device="cuda")
+    roco.roco_chunk_attend(p, heads, 1, None, q, k, v, start, first, K, V, pos, used, out, lse, ws)
+    last = K[-1, :n].clone()
+    roco.roco_chunk_commit(p, heads, 1, None, q, k, v, lse, start, first, K, V, stats, pos, used, None, None, ws)
+    torch.cuda.synchronize()
+    u = heads - 1
+    keys, values = torch.cat([last.float(), k[:, u].float()]), torch.cat([V[u, :n].float(), v[:, u].float()])
+    x = (q[:, u].float() @ keys.t()).double() / math.sqrt(d)
+    x[:, n:].masked_fill_(torch.ones((T, T), dtype=torch.bool, device="cuda").triu(1), -math.inf)
+    want_lse = torch.logsumexp(x, 1)
+    prob = torch.exp(x - want_lse[:, None])
+    mass, want = (prob.float() @ values.abs()).double(), (prob.float() @ values).double()
+    logit = float((q[:, u].float().abs() @ keys.abs().t()).max()) / math.sqrt(d)
+    # (the products above are of 32 bits too: twice what the kernel may be off)
+    rel = 2 * (2 * (d + 8) * U * logit + (8 + 2 * math.sqrt(n)) * U) + 2.0 ** -8
+    assert ((out[:, u].double() - want).abs() <= rel * mass + 2.0 ** -8 * want.abs()).all()
+    assert ((lse[:, u].double() - want_lse).abs() <= 2 * ((d + 8) * U * logit + (8 + math.sqrt(n)) * U) + 2.0 ** -22 * want_lse.abs()).all()
+    assert torch.equal(K[u, n:n + T], k[:, u]) and torch.equal(V[u, n:n + T], v[:, u]) and torch.equal(K[u, :n], last)
+    assert used.tolist() == [n + T] * heads and pos[u, n:n + T].tolist() == [B + 7, B + 8, B + 9]
+    more = torch.exp(x - lse[:, u].double()[:, None]).sum(0)[:n]
+    err = (stats[u, 0, :n].double() - (before[u, 0, :n].double() + more)).abs()
+    assert (err <= 2 * (2 * (d + 8) * U * logit + 10 * U) * more + 2 * U * stats[u, 0, :n].double()).all()
+    assert (stats[u, 2, :n] == 10.0 + T).all() and stats[u, 2, n:n + T].tolist() == [3.0, 2.0, 1.0]
+
+
+# ---------------------------------------------------------------------------------------------------- streams, graphs, repetition
+def _step_of(s, ws=None):
+    ws = s.ws if ws is None else ws
+    roco.roco_chunk_attend(s.p, s.heads, s.group, s.pages, s.dq, s.dk, s.dv, s.dstart, s.dqpos0, s.dK, s.dV, s.dpos, s.dn_used, s.out, s.lse, ws)
+    roco.roco_chunk_commit(s.p, s.heads, s.group, s.pages, s.dq, s.dk, s.dv, s.lse, s.dstart, s.dqpos0, s.dK, s.dV, s.dstats, s.dpos, s.dn_used, None, None, ws)
+
+
+def _shapes():
+    return [Step(7, "bf16", 128, [400, 100], [300, 280], group=4, B=420).upload(),
+            Step(8, "f32", 64, [290, 0, 300], [40, 1, 90], heads=3, group=2, B=300, page=16).upload(),
+            Step(9, "bf16", 64, [300], [33], group=5, B=300, window=9).upload()]
+
+
+def test_repeated_calls_give_the_same_bits_and_leave_the_cache():
+    for s in _shapes():
+        K, V = s.dK.clone(), s.dV.clone()
+        first = s.attend()
+        for _ in range(3):
+            s.ws.fill_(0xFF)
+            assert all(np.array_equal(a, b) for a, b in zip(first, s.attend()))
+        assert torch.equal(K.nan_to_num(7), s.dK.nan_to_num(7)) and torch.equal(V.nan_to_num(7), s.dV.nan_to_num(7))
+
+
+def test_graphs_that_share_a_workspace():
+    """Attention and taking over of three shapes, captured, replayed in turn with eager work between."""
+    steps = _shapes()
+    ws = torch.empty(max(s.ws.numel() for s in steps), dtype=torch.uint8, device="cuda").fill_(0xEE)
+    side, graphs, wants, starts = torch.cuda.Stream(), [], [], []
+    for s in steps:
+        s.state = [s.dK, s.dV, s.dstats, s.dpos, s.dn_used]
+        starts.append([x.clone() for x in s.state])
+        _step_of(s, ws)
+        torch.cuda.synchronize()
+        wants.append([x.nan_to_num(7) for x in s.state + [s.out, s.lse]])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+            _step_of(s, ws)
+        graphs.append(graph)
+    for turn in range(4):
+        for s, start in zip(steps, starts):
+            for x, y in zip(s.state, start):
+                x.copy_(y)
+            s.out.fill_(77)
+            s.lse.fill_(77)
+        torch.cuda.synchronize()
+        for s, graph in zip(steps, graphs):
+            if turn == 2:
+                _step_of(s, ws)
+            else:
+                graph.replay()
+        torch.cuda.synchronize()
+        for s, want in zip(steps, wants):
+            assert all(torch.equal(x.nan_to_num(7), y) for x, y in zip(s.state + [s.out, s.lse], want))
+
+
+def test_streams_with_workspaces_of_their_own():
+    steps, streams = _shapes(), [torch.cuda.Stream() for _ in range(3)]
+    wants = [[x.copy() for x in s.attend()] for s in steps]
+    for s in steps:
+        s.out.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, stream in zip(steps, streams):
+            roco.roco_chunk_attend(s.p, s.heads, s.group, s.pages, s.dq, s.dk, s.dv, s.dstart, s.dqpos0, s.dK, s.dV, s.dpos, s.dn_used, s.out, s.lse, s.ws, stream=stream)
+    torch.cuda.synchronize()
+    for s, want in zip(steps, wants):
+        assert np.array_equal(want[0], s.out.float().cpu().numpy()) and np.array_equal(want[1], s.lse.cpu().numpy())
+
+
+# ---------------------------------------------------------------------------------------------------- together, and beside what there was
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("T,group,page,window", [(1, 1, 0, 0), (17, 4, 16, 0), (64, 2, 64, 30)])
+def test_a_chunk_is_a_drafted_chain(dtype, d, T, group, page, window):
+    """roco_tree_attend and roco_tree_commit of a chain: outputs within what either may be off, the same slots and counts."""
+    s = Step(T + d, dtype, d, [200, 100, 33], [T] * 3, group=group, page=page, window=window, B=210, scope=20, fused=False).upload()
+    out, lse = s.attend()
+    s.check_attend(out, lse)
+    state = [s.dK, s.dV, s.dstats, s.dpos, s.dn_used]
+    start = [x.clone() for x in state]
+    s.commit(lse.astype(np.float32))
+    mine = [x.clone() for x in state]
+    for x, y in zip(state, start):
+        x.copy_(y)
+    per_unit = lambda t, n: t.view(3, T, 2, n, -1).transpose(1, 2).reshape(6, T, n, -1).contiguous()  # noqa: E731
+    q, k, v = per_unit(s.dq, group), per_unit(s.dk, 1).squeeze(2), per_unit(s.dv, 1).squeeze(2)
+    qpos0 = s.dqpos0.repeat_interleave(2)
+    t_out, t_lse = torch.empty_like(q), torch.empty((6, T, group), device="cuda")
+    ws = torch.empty(roco.tree_workspace_bytes(s.p, group, T), dtype=torch.uint8, device="cuda")
+    roco.roco_tree_attend(s.p, 2, group, T, s.pages, q, k, v, None, None, qpos0, s.dK, s.dV, s.dpos, s.dn_used, t_out, t_lse, ws)
+    path = torch.arange(T, dtype=torch.int32, device="cuda").repeat(3, 1)
+    roco.roco_tree_commit(s.p, 2, group, T, s.pages, q, k, v, per_unit(dev(lse, "f32"), group).squeeze(-1).contiguous(), T, path, dev(np.array([T] * 3)), qpos0, s.dK,
+                          s.dV, s.dstats, s.dpos, s.dn_used, None, None, ws)
+    torch.cuda.synchronize()
+    s.check_attend(t_out.view(3, 2, T, group, d).transpose(1, 2).reshape(3 * T, 2 * group, d).float().cpu().numpy().astype(np.float64),
+                   t_lse.view(3, 2, T, group).transpose(1, 2).reshape(3 * T, 2 * group).cpu().numpy().astype(np.float64), "tree")
+    for i in (0, 1, 3, 4):
+        assert torch.equal(mine[i].nan_to_num(7), state[i].nan_to_num(7))
+    assert torch.equal(mine[2][:, 2], s.dstats[:, 2])
+
+
+def test_prompts_in_chunks_then_drafts():
+    """A server's steps on pages that the requests take as they grow: two prompts in chunks beside a request that decodes, then drafted trees that are scored,
+    verified and taken over, path and length straight from the one call to the next.  Every step against the oracles, from the state that the last one left."""
+    from oracle.verify import tree_verify
+    heads, group, d, page, B = 2, 2, 128, 16, 120
+    budgets, chunks = [120, 70, 100], [[60, 33, 1], [50, 60, 1], [45, 7, 1]]
+    table = np.full((3, 8), -1)
+    free = np.random.default_rng(3).permutation(30)
+    given = 0
+    s = None
+    first = [0, 0, 0]
+    for n_step, tokens in enumerate(chunks):
+        used = [0, 0, 0] if s is None else [int(s.dn_used[2 * r]) for r in range(3)]
+        t = Step(40 + n_step, "bf16", d, used, tokens, heads=heads, group=group, page=page, B=B, budgets=budgets, scope=24, n_extra=8)
+        # the pages that the requests want now, from the list
+        want = [min(b, u + c) for b, u, c in zip(budgets, used, tokens)]
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        dtable, starts, rows, slots = i32(table.tolist()), i32([0] * 4), i32([0] * 4), i32([0] * 400)
+        roco.roco_page_tables(i32(used), i32(want), page, i32(free[given:].tolist()), dtable, starts, rows, slots)
+        given += int(starts[-1])
+        table = dtable.cpu().numpy()
+        t.table, t.n_pages, t.M = table.copy(), 30, 8
+        t.qpos0 = np.array(first)
+        if s is not None:
+            t.stats, t.pos = s.dstats.cpu().numpy(), s.dpos.cpu().numpy()
+            pools = [x.float().cpu().numpy() for x in (s.dK, s.dV)]
+            for u in range(t.U):
+                for rows_of, pool in ((t.K, pools[0]), (t.V, pools[1])):
+                    rows_of[u, :used[u // heads]] = s.unpool(pool, u, used[u // heads])
+        else:
+            t.stats[:], t.pos[:] = 0.0, -1
+        t.upload()
+        out, lse = t.attend()
+        t.check_attend(out, lse, f"step {n_step}")
+        t.commit(lse.astype(np.float32))
+        t.check_commit(lse.astype(np.float32), f"step {n_step}")
+        first = [a + c for a, c in zip(first, tokens)]
+        s = t
+    # drafted trees over the caches that the chunks have left
+    T, vocab, g = 6, 50, torch.Generator(device="cuda").manual_seed(5)
+    parent = i32([[-1, 0, 0, 1, 2, 3]] * 3)
+    q, k, v = (torch.randn(shape, generator=g, device="cuda", dtype=torch.bfloat16) for shape in ((6, T, group, d), (6, T, d), (6, T, d)))
+    qpos0 = i32(first).repeat_interleave(heads)
+    t_out, t_lse = torch.empty_like(q), torch.empty((6, T, group), device="cuda")
+    ws = torch.empty(max(roco.tree_workspace_bytes(s.p, group, T), roco.verify_workspace_bytes(3, T, vocab)), dtype=torch.uint8, device="cuda")
+    logits = torch.randn((3, T, vocab), generator=g, device="cuda")
+    p, draft = torch.softmax(logits, -1), torch.softmax(logits + 0.3 * torch.randn(logits.shape, generator=g, device="cuda"), -1)
+    drafted = torch.randint(0, vocab, (3, T), generator=g, device="cuda", dtype=torch.int32)
+    accept, choose = torch.rand((3, T), generator=g, device="cuda"), torch.rand(3, generator=g, device="cuda")
+    path, n_path, nxt = i32([[-9] * T] * 3), i32([-9] * 3), i32([-9] * 3)
+    before = [int(x) for x in s.dn_used]
+    roco.roco_tree_attend(s.p, heads, group, T, s.pages, q, k, v, parent, None, qpos0, s.dK, s.dV, s.dpos, s.dn_used, t_out, t_lse, ws)
+    roco.roco_tree_verify(p, draft, drafted, parent, None, accept, choose, path, n_path, nxt, ws)
+    roco.roco_tree_commit(s.p, heads, group, T, s.pages, q, k, v, t_lse, T, path, n_path, qpos0, s.dK, s.dV, s.dstats, s.dpos, s.dn_used, None, None, ws)
+    torch.cuda.synchronize()
+    for r in range(3):
+        want, token = tree_verify(p[r].cpu().numpy(), draft[r].cpu().numpy(), drafted[r].tolist(), parent[r].tolist(), T, accept[r].cpu().numpy(), float(choose[r]))
+        assert path[r].tolist() == want + [-1] * (T - len(want)) and int(n_path[r]) == len(want) and int(nxt[r]) == token
+        for u in (2 * r, 2 * r + 1):
+            n = int(s.dn_used[u])
+            assert n == min(budgets[r], before[u] + len(want))
+            assert {first[r] + i for i in range(len(want))} <= set(s.dpos[u, :n].tolist())
