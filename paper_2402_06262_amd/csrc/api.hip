@@ -192,7 +192,7 @@ int chunk_args(const roco_params* params, int32_t heads, int32_t group, int32_t 
   const int64_t element = params->dtype == ROCO_BF16 ? 2 : 4;
   a.units = params->units; a.requests = params->units / heads; a.heads = heads; a.group = group; a.tokens = tokens;
   a.B = params->budget; a.scope = params->scope;
-  a.row_tile = lay.split.row_tile; a.row_tiles = lay.split.row_tiles; a.splits = lay.split.splits; a.row_splits = lay.row_splits;
+  a.row_tile = lay.split.row_tile; a.row_tiles = lay.split.row_tiles; a.splits = lay.split.splits; a.equal_shares = lay.split.equal_shares; a.row_splits = lay.row_splits;
   a.pol = policy_of(params);
   a.scale_log2 = scale_log2(params);
   a.recency_window = params->recency_window;

@@ -32,24 +32,41 @@ struct RowTile {
   Located at;
   int head, split, first_row, rows;
 };
-// (the later row tiles, which see more, first)
-template <int ROWS> __device__ __forceinline__ bool row_tile_of(const ChunkArgs& a, int id, RowTile& t) {
+// (The later row tiles, which see more, first; a split's heads, or, where the splits differ, a head's splits side by side.)
+template <int ROWS> __device__ __forceinline__ bool row_tile_of(const ChunkArgs& a, int id, RowTile& t, int splits) {
   if (!locate_tile<ROWS>(a, a.group, a.row_tiles - 1 - id % a.row_tiles, t.at)) return false;
   const int pair = id / a.row_tiles;
-  t.head = __builtin_amdgcn_readfirstlane(pair % a.heads);
-  t.split = __builtin_amdgcn_readfirstlane(pair / a.heads);
+  const int by = a.equal_shares ? splits : a.heads, first = pair / by, second = pair - first * by;
+  t.head = __builtin_amdgcn_readfirstlane(a.equal_shares ? first : second);
+  t.split = __builtin_amdgcn_readfirstlane(a.equal_shares ? second : first);
   t.first_row = t.at.tile * ROWS;
   t.rows = min(t.at.count * a.group - t.first_row, ROWS);
   return t.rows > 0;
 }
-// What it sees, in stages of KEYS keys: the cache's and the chunk's, and the shares of them that its workgroups take.
+// What it sees, in stages of KEYS keys: the cache's and the chunk's, and the shares of them that its workgroups take.  With equal_shares a share of a tile of more
+// than a wave's rows is as long as one of the request that sees the most: shorter ones have fewer, and no more of their outputs to be joined.
 template <int DT, int ROWS, int KEYS> struct Plan {
+  static constexpr int kFewRows = 32;
   int n, cache_stages, stages, per, used;
   __device__ __forceinline__ Plan(const ChunkArgs& a, const RowTile& t) {
     n = __builtin_amdgcn_readfirstlane(min(max(a.n_used[t.at.request * a.heads + t.head], 0), budget_of(a.pages, a.B, t.at.request)));
     cache_stages = (n + KEYS - 1) / KEYS;
     stages = __builtin_amdgcn_readfirstlane(cache_stages + (t.first_row + t.rows - 1) / a.group / KEYS + 1);
-    per = __builtin_amdgcn_readfirstlane(max((stages + a.splits - 1) / a.splits, chunk_least_keys(DT, ROWS) / KEYS));
+    per = max((stages + a.splits - 1) / a.splits, chunk_least_keys(DT, ROWS) / KEYS);
+    if (a.equal_shares && t.rows > kFewRows) {
+      const int lane = threadIdx.x & (kWave - 1);
+      int longest = 0;
+#pragma unroll 1
+      for (int r = lane; r < a.requests; r += kWave) {
+        const int count = min(max(a.start[r + 1], 0), a.tokens) - min(max(a.start[r], 0), a.tokens);
+        const int held = min(max(a.n_used[r * a.heads + t.head], 0), budget_of(a.pages, a.B, r));
+        if (count > 0) longest = max(longest, held + count);
+      }
+#pragma unroll
+      for (int s = 1; s < kWave; s *= 2) longest = max(longest, __shfl_xor(longest, s, kWave));
+      per = max(per, (longest + KEYS * a.splits - 1) / (KEYS * a.splits));
+    }
+    per = __builtin_amdgcn_readfirstlane(per);
     used = __builtin_amdgcn_readfirstlane((stages + per - 1) / per);
   }
 };
@@ -62,7 +79,7 @@ __device__ __forceinline__ size_t packed_row(const ChunkArgs& a, const RowTile& 
 template <int ROWS> __device__ __forceinline__ bool my_tile(const ChunkArgs& a, RowTile& mine) {
   const int total = a.row_tiles * a.heads * a.splits, share = (total + 7) / 8;
   const int id = static_cast<int>(blockIdx.x % 8) * share + static_cast<int>(blockIdx.x / 8);
-  return id < total && row_tile_of<ROWS>(a, id, mine);
+  return id < total && row_tile_of<ROWS>(a, id, mine, a.splits);
 }
 
 // A wave's results for NG groups of 32 rows: the values that were taken out (see below) added, and the rows written, or a split's share of them.
@@ -525,8 +542,10 @@ __global__ __launch_bounds__(kThreads, 1) void chunk_attend_pair(ChunkArgs a) {
 }
 
 // 32 rows of a wave, 32 keys of a stage, one after the other, and as many waves as there is room for.
-// Measured: 24 requests, of which 18 decode a token and the others take 384 or fewer, 8 heads of 4 queries, over 4096 keys or fewer, 166 us; 32 that decode a token
-// over 4096 keys each 112 us (4.8 TB/s); 6 of up to 333 tokens over 2048, 12 heads, 64 dimensions, with a recency window, 45 us; fp32, 5 of up to 101 over 1501,
+// Measured: 24 requests, of which 18 decode a token and the others take 384 or fewer, 8 heads of 4 queries, over 4096 keys or fewer, 148 us (164 with as many
+// shares for short requests as for long ones); 32 that decode a token
+// over 4096 keys each 112 us (4.8 TB/s); 6 of up to 333 tokens over 2048, 12 heads, 64 dimensions, with a recency window, 40 us (45 with the
+// window looked for in every score); fp32, 5 of up to 101 over 1501,
 // 5 heads of 3 queries, 70 us, and 4 that decode a token over 500, 4 heads, 64 dimensions, 14 us.
 template <int DT, int HD> struct TileForm {
   using R = Rows<DT, HD>;
@@ -679,7 +698,11 @@ __global__ __launch_bounds__(kThreads, (TileForm<DT, HD>::kWavesPerSimd)) void c
     f32x16 s = {0};
 #pragma unroll
     for (int kk = 0; kk < R::kSteps; ++kk) s = score_step<DT>(read_frag((st + kfrag) ^ (kk << 5)), own[0][kk], s);
-    const bool interior = !WINDOW && (of_new ? j0 + kSub - 1 <= wave_first : here == 0x1010u);
+    bool interior = of_new ? (WINDOW ? w : 0) <= wave_first - (j0 + kSub - 1) : here == 0x1010u;
+    if (WINDOW && !of_new) {  // outside the window of every row
+      const int at_slot = pos_t[lane & 31];
+      interior = interior && !__any(at_slot <= qp0 + wave_last && at_slot > qp0 + wave_first - w);
+    }
     float sum = 0.0f;
     bool done = false;
     float p[16];  // the probabilities, of bf16 rounded to bf16
@@ -756,7 +779,7 @@ __global__ __launch_bounds__(kThreads, (TileForm<DT, HD>::kWavesPerSimd)) void c
 template <int DT, int HD, int ROWS, int KEYS> __global__ __launch_bounds__(kThreads) void chunk_join(ChunkArgs a) {
   constexpr int LANES = HD / 4, PER = kThreads / LANES, kParts = ROWS / PER, kAtOnce = 4;
   RowTile t;
-  if (!row_tile_of<ROWS>(a, blockIdx.x / kParts, t)) return;
+  if (!row_tile_of<ROWS>(a, blockIdx.x / kParts, t, 1)) return;
   const Plan<DT, ROWS, KEYS> plan(a, t);
   const int i = blockIdx.x % kParts * PER + threadIdx.x / LANES, sub = threadIdx.x % LANES;
   if (plan.used == 1 || i >= t.rows) return;  // (one split has written its rows)

@@ -235,8 +235,8 @@ hipError_t launch_tree_commit(int dtype, int head_dim, const CommitArgs& a, hipS
 // token side by side.
 struct ChunkArgs {
   int units, requests, heads, group, tokens, B, scope;
-  // chunk_attend: rows of a tile, tiles, workgroups along a tile's keys
-  int row_tile, row_tiles, splits;
+  // chunk_attend: rows of a tile, tiles, workgroups along a tile's keys, and whether these have as many keys whatever their request sees
+  int row_tile, row_tiles, splits, equal_shares;
   Policy pol;
   float scale_log2;
   int recency_window;
@@ -265,7 +265,7 @@ struct ChunkArgs {
 // Keys of a workgroup of chunk_attend, if its tile sees more than that.  (With 128 of them everywhere 4 requests that decode a token over 500 keys, 4 heads, fp32,
 // took 20 us, not 14; 1 over 1024, 8 heads, bf16, 15 us either way.)
 __host__ __device__ constexpr int chunk_least_keys(int dtype, int row_tile) { return dtype != 1 ? 32 : row_tile == 256 ? 128 : 64; }
-struct ChunkSplits { int row_tile, row_tiles, splits; };
+struct ChunkSplits { int row_tile, row_tiles, splits, equal_shares; };
 ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
 int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B);
 hipError_t launch_chunk_attend(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);

@@ -46,7 +46,7 @@ __device__ __forceinline__ double sum_of(const double* sums, int blocks) {  // i
 template <bool BF16> __device__ __forceinline__ float element(const void* row, int64_t i) {
   return BF16 ? bf16_to_f32(static_cast<const uint16_t*>(row)[i]) : static_cast<const float*>(row)[i];
 }
-__device__ __forceinline__ float probability(float v) { return fmaxf(v, 0.0f); }  // (NaN: zero)
+__device__ __forceinline__ float probability(float v) { return __builtin_amdgcn_fmed3f(v, 0.0f, INFINITY); }  // (NaN: zero; one instruction)
 
 // A request's tree, node i in lane i.
 template <bool BF16> struct Tree {

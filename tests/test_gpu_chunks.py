@@ -257,6 +257,14 @@ def test_splits(dtype, d, splits, monkeypatch):
     s.check_attend(*s.attend())
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("tokens", [[40, 3, 20], [200, 190, 1]])
+def test_shares_of_equal_length(dtype, d, tokens):
+    """Work enough, and heads for every die: shares as long as the longest request's, beside one with few rows."""
+    s = Step(d, dtype, d, [16000, 5000, 200], tokens, heads=8, group=8, B=16384).upload()
+    s.check_attend(*s.attend(), units=[0, 5, 8, 13, 16, 23])
+
+
 @pytest.mark.parametrize("dtype,d", TYPES)
 def test_rows_of_their_own(dtype, d):
     s = Step(d, dtype, d, [50, 10], [20, 3], group=2, fused=False).upload()
