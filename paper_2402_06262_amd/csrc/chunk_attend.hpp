@@ -542,9 +542,9 @@ __global__ __launch_bounds__(kThreads, 1) void chunk_attend_pair(ChunkArgs a) {
 }
 
 // 32 rows of a wave, 32 keys of a stage, one after the other, and as many waves as there is room for.
-// Measured: 24 requests, of which 18 decode a token and the others take 384 or fewer, 8 heads of 4 queries, over 4096 keys or fewer, 148 us (164 with as many
+// Measured: 24 requests, of which 18 decode a token and the others take 384 or fewer, 8 heads of 4 queries, over 4096 keys or fewer, 140 us (156 with as many
 // shares for short requests as for long ones); 32 that decode a token
-// over 4096 keys each 112 us (4.8 TB/s); 6 of up to 333 tokens over 2048, 12 heads, 64 dimensions, with a recency window, 40 us (45 with the
+// over 4096 keys each 107 us (5.0 TB/s); 6 of up to 333 tokens over 2048, 12 heads, 64 dimensions, with a recency window, 40 us (45 with the
 // window looked for in every score); fp32, 5 of up to 101 over 1501,
 // 5 heads of 3 queries, 70 us, and 4 that decode a token over 500, 4 heads, 64 dimensions, 14 us.
 template <int DT, int HD> struct TileForm {
@@ -775,47 +775,51 @@ __global__ __launch_bounds__(kThreads, (TileForm<DT, HD>::kWavesPerSimd)) void c
   if (!idle) Finish<DT, HD, 1, WINDOW>::run(a, mine, plan.used, row, token, own, m, l, o, zeroed, min((t1 - cache_tiles) * kSub - 1, wave_last));
 }
 
-// The splits' shares of a few rows of a tile, HD / 4 lanes with 16 bytes of a row each; four splits at a time, in their order.
-template <int DT, int HD, int ROWS, int KEYS> __global__ __launch_bounds__(kThreads) void chunk_join(ChunkArgs a) {
-  constexpr int LANES = HD / 4, PER = kThreads / LANES, kParts = ROWS / PER, kAtOnce = 4;
+// The splits' shares of a tile's rows, HD / 4 lanes with 16 bytes of a row each; four splits at a time, in their order.  `parts` workgroups a tile: with one for
+// every few rows most of the time goes into finding out which (24 requests with 6 chunks of 384 tokens, 148 -> 140 us; 32 that decode a token, 112 -> 107).
+template <int DT, int HD, int ROWS, int KEYS> __global__ __launch_bounds__(kThreads) void chunk_join(ChunkArgs a, int parts) {
+  constexpr int LANES = HD / 4, PER = kThreads / LANES, kAtOnce = 4;
   RowTile t;
-  if (!row_tile_of<ROWS>(a, blockIdx.x / kParts, t, 1)) return;
+  if (!row_tile_of<ROWS>(a, blockIdx.x / parts, t, 1)) return;
   const Plan<DT, ROWS, KEYS> plan(a, t);
-  const int i = blockIdx.x % kParts * PER + threadIdx.x / LANES, sub = threadIdx.x % LANES;
-  if (plan.used == 1 || i >= t.rows) return;  // (one split has written its rows)
+  if (plan.used == 1) return;  // (one split has written its rows)
+  const int sub = threadIdx.x % LANES;
   const size_t plane = static_cast<size_t>(a.tokens) * a.heads * a.group;
-  const int row = t.first_row + i;
-  const size_t at = packed_row(a, t, row, row / a.group);
-  float M = -INFINITY, sum = 0.0f;
-  tree::f32x4 o = tree::f32x4{0};
 #pragma unroll 1
-  for (int k0 = 0; k0 < plan.used; k0 += kAtOnce) {
-    float m[kAtOnce], l[kAtOnce];
-    tree::f32x4 part[kAtOnce];
+  for (int i = blockIdx.x % parts * PER + threadIdx.x / LANES; i < t.rows; i += parts * PER) {
+    const int row = t.first_row + i;
+    const size_t at = packed_row(a, t, row, row / a.group);
+    float M = -INFINITY, sum = 0.0f;
+    tree::f32x4 o = tree::f32x4{0};
+#pragma unroll 1
+    for (int k0 = 0; k0 < plan.used; k0 += kAtOnce) {
+      float m[kAtOnce], l[kAtOnce];
+      tree::f32x4 part[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const size_t from = min(k0 + k, plan.used - 1) * plane + at;
-      m[k] = a.part_m[from];
-      l[k] = a.part_l[from];
-      part[k] = *reinterpret_cast<const tree::f32x4*>(a.part_o + from * HD + 4 * sub);
+      for (int k = 0; k < kAtOnce; ++k) {
+        const size_t from = min(k0 + k, plan.used - 1) * plane + at;
+        m[k] = a.part_m[from];
+        l[k] = a.part_l[from];
+        part[k] = *reinterpret_cast<const tree::f32x4*>(a.part_o + from * HD + 4 * sub);
+      }
+      float most = M;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) most = fmaxf(most, m[k]);
+      const float before = M > -INFINITY ? fast_exp2(M - most) : 1.0f;
+      o *= before;
+      sum *= before;
+      M = most;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (k0 + k >= plan.used) break;
+        const float w = m[k] > -INFINITY ? fast_exp2(m[k] - M) : 1.0f;  // (no maximum: a sum of zero, or NaN)
+        o += part[k] * w;
+        sum += l[k] * w;
+      }
     }
-    float most = M;
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) most = fmaxf(most, m[k]);
-    const float before = M > -INFINITY ? fast_exp2(M - most) : 1.0f;
-    o *= before;
-    sum *= before;
-    M = most;
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      if (k0 + k >= plan.used) break;
-      const float w = m[k] > -INFINITY ? fast_exp2(m[k] - M) : 1.0f;  // (no maximum: a sum of zero, or NaN)
-      o += part[k] * w;
-      sum += l[k] * w;
-    }
+    tree::store4<DT>(a.out, at * HD + 4 * sub, o * (1.0f / sum));
+    if (a.lse != nullptr && sub == 0) a.lse[at] = kLn2 * (M + __log2f(sum));
   }
-  tree::store4<DT>(a.out, at * HD + 4 * sub, o * (1.0f / sum));
-  if (a.lse != nullptr && sub == 0) a.lse[at] = kLn2 * (M + __log2f(sum));
 }
 
 #pragma clang diagnostic pop
@@ -830,7 +834,11 @@ template <int DT, int HD, int ROWS, int KEYS, class Kernel> hipError_t launch_ti
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   ProfScope ps(kProfChunkJoin, s);
-  hipLaunchKernelGGL((chunk_join<DT, HD, ROWS, KEYS>), dim3(static_cast<unsigned>(a.row_tiles) * a.heads * (ROWS / (kThreads / (HD / 4)))), dim3(kThreads), 0, s, a);
+  // (at most 4096 of them, and no more than four times an average tile's rows are for)
+  const int per = kThreads / (HD / 4), tiles = a.row_tiles * a.heads;
+  const long long rows = 4ll * a.tokens * a.group / a.requests;
+  const int parts = static_cast<int>(std::max(1ll, std::min({static_cast<long long>(ROWS / per), 4096ll / tiles, (rows + per - 1) / per})));
+  hipLaunchKernelGGL((chunk_join<DT, HD, ROWS, KEYS>), dim3(static_cast<unsigned>(tiles) * parts), dim3(kThreads), 0, s, a, parts);
   return hipGetLastError();
 }
 template <int DT, int HD, bool WINDOW> hipError_t launch_attend_form(const ChunkArgs& a, hipStream_t s) {
