@@ -408,7 +408,7 @@ int roco_tree_verify(int32_t dtype, int32_t requests, int32_t nodes, int32_t voc
  * them from 0 on, token i of them at position qpos0[r] + i.  (token_start is the row_start of roco_page_tables.)
  *   x_ih = scale q_ih . k + bias over the unit's n_used slots and the request's tokens 0 .. i;   out_ih = sum softmax(x_ih) v,   lse_ih = ln sum exp x_ih
  * As in roco_tree_attend the cache is not changed, and is seen whole, also where it is full; values of tokens that a row does not see do not reach
- * it.  Up to 64 tokens are a chain there (the same sums in another order).
+ * it.  Up to 64 tokens are a chain there: the same sums in another order, with 16 bits of bf16 probabilities where here they have 8.
  *
  * tokens       rows of the packed arrays; rows that are no request's are neither read nor written
  * q            in  [tokens, heads, group, d] dtype, tokens q_stride elements apart (q_stride >= heads group d)
