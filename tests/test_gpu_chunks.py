@@ -573,6 +573,50 @@ def test_graphs_that_share_a_workspace():
             assert all(torch.equal(x.nan_to_num(7), y) for x, y in zip(s.state + [s.out, s.lse], want))
 
 
+@pytest.mark.parametrize("dtype,d,group", [("bf16", 128, 1), ("bf16", 128, 20), ("f32", 64, 2)])
+def test_a_graph_of_one_size_for_steps_of_many(dtype, d, group):
+    """Captured once with room for 120 tokens; every replay finds other requests' lengths, caches and tokens in the same arrays."""
+    kw = dict(heads=2, group=group, B=160, page=16, budgets=[160, 90, 120], scope=20, n_extra=0)
+    steps = [Step(70 + i, dtype, d, used, tokens, spare=(0, 120 - sum(tokens)), **kw).upload()
+             for i, (used, tokens) in enumerate([([160, 90, 7], [50, 40, 30]), ([0, 33, 120], [1, 1, 1]), ([100, 90, 0], [0, 0, 119]), ([160, 0, 120], [1, 80, 1])])]
+    s = steps[0]
+    names = ["dstart", "dqpos0", "dK", "dV", "dstats", "dpos", "dn_used", "out", "lse"]
+    ev = [torch.full((120, 2), -7, dtype=torch.int32, device="cuda") for _ in range(2)]
+    dtable, dbudget = dev(s.table), dev(np.array(s.budgets))
+    s.pages = roco.RocoPages(dtable, s.n_pages, 16, dbudget)
+    first = [getattr(s, n).clone() for n in names] + [s.dq.clone(), s.dk.clone(), s.dv.clone()]
+
+    def step():
+        roco.roco_chunk_attend(s.p, 2, group, s.pages, s.dq, s.dk, s.dv, s.dstart, s.dqpos0, s.dK, s.dV, s.dpos, s.dn_used, s.out, s.lse, s.ws)
+        roco.roco_chunk_commit(s.p, 2, group, s.pages, s.dq, s.dk, s.dv, s.lse, s.dstart, s.dqpos0, s.dK, s.dV, s.dstats, s.dpos, s.dn_used, *ev, s.ws)
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        step()
+    for t in [*steps, steps[1], steps[0]]:
+        given = first if t is s else [getattr(t, n) for n in names] + [t.dq, t.dk, t.dv]
+        for n, x in zip(names + ["dq", "dk", "dv"], given):
+            getattr(s, n).copy_(x)
+        s.out.fill_(77)
+        s.lse.fill_(77)
+        dtable.copy_(dev(t.table))
+        for x in ev:
+            x.fill_(-7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        lse = s.lse.cpu().numpy()
+        t.check_attend(s.out.float().cpu().numpy().astype(np.float64), lse.astype(np.float64))
+        mine = {n: getattr(t, n) for n in names}
+        for n in names:
+            setattr(t, n, getattr(s, n))
+        t.ev_slot, t.ev_pos = ev
+        t.check_commit(lse)
+        for n in names:
+            setattr(t, n, mine[n])
+
+
 def test_streams_with_workspaces_of_their_own():
     steps, streams = _shapes(), [torch.cuda.Stream() for _ in range(3)]
     wants = [[x.copy() for x in s.attend()] for s in steps]
