@@ -111,23 +111,33 @@ constexpr long long kMostTiles = 4096;
 
 // The form of the attention that a call takes.  Row tiles of 256, where requests of bf16 rows of 128 dimensions have 1024 of them or more on average: 4096 cached keys,
 // group 4, 8 heads, 8 requests of 256 tokens: 160 us against 216 with 128; 1 request of as many: 61 against 59; 8 requests of 100: 148 against 127; with 64
-// dimensions, 8 requests of 512: 244 against 237.
+// dimensions, 8 requests of 512: 244 against 237.  Of 32, where they have few: one token of 32 requests, 8 heads, over 2048 keys, fp32 / 128 104 us against 286, fp32 / 64 62 and 165,
+// bf16 / 64 35 and 36; of 4 heads over 4096, bf16 / 128, 103 and 106.  12 tokens of 8 requests, 4 heads each, over 2048: bf16 / 128 25 and 32, bf16 / 64 26 and 25, fp32 / 128 77 and
+// 152; 64 tokens bf16 / 128 61 and 45, fp32 / 128 207 and 221; 512, groups of 2, fp32 / 128 386 and 359.  And where there is little work in all, which they share out more finely: 100
+// tokens of 4 requests, 16 heads, over 300 keys 13 and 26; 64 of 16, 8 heads, over 1000 36 and 32.
 // Splits: those with the shortest time, of a compute unit's workgroups one after the other, or of one that has four waves alone half as long again for each
-// further one; a workgroup being as long as its tiles of 32 keys and, for its start, its share of the outputs and the joining, eight more (at 128 dimensions).
+// further one; a workgroup being as long as its waves' tiles of 32 keys and, for its start, its share of the outputs and the joining, eight more (at 128 dimensions).
 ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B) {
   const char* const asked = getenv("ROCO_CHUNK_SPLITS");
   const int splits = asked != nullptr ? std::min(atoi(asked), kMostChunkSplits) : 0;
   ChunkSplits c;
   const long long rows = static_cast<long long>(tokens) * group, keys = (static_cast<long long>(B) + tokens + 31) / 32;
-  const bool pair = dtype == kBF16 && head_dim == 128 && rows >= 1024ll * requests;
-  c.row_tile = pair ? 256 : 128;
+  const char* const rows_asked = getenv("ROCO_CHUNK_ROWS");
+  const int asked_tile = rows_asked != nullptr ? atoi(rows_asked) : 0;
+  const bool can_pair = dtype == kBF16 && head_dim == 128;
+  c.row_tile = rows <= (dtype == kF32 ? 256ll : head_dim == 128 ? 32ll : 8ll) * requests || rows * heads * keys <= 160000 ? 32 : can_pair && rows >= 1024ll * requests ? 256 : 128;
+  if (asked_tile == 32 || asked_tile == 128 || (asked_tile == 256 && can_pair)) c.row_tile = asked_tile;
+  const bool pair = c.row_tile == 256, few = c.row_tile == 32;
   c.row_tiles = tiles_of(requests, tokens, group, c.row_tile);
   const long long tiles = static_cast<long long>(c.row_tiles) * heads, full = pair ? rows / 256 * heads : tiles;
-  const int most = static_cast<int>(std::max(1ll, std::min({static_cast<long long>(kMostChunkSplits), keys * 32 / chunk_least_keys(dtype, c.row_tile), kMostTiles / tiles})));
+  const int least_keys = chunk_least_keys(dtype, c.row_tile);
+  const int most = static_cast<int>(std::max(1ll, std::min({static_cast<long long>(kMostChunkSplits), (keys * 32 + (few ? least_keys - 1 : 0)) / least_keys, kMostTiles / tiles})));
+  const bool alone = pair || (few ? dtype == kF32 && head_dim == 128 : dtype == kF32);  // on its compute unit
   c.splits = 1;
   long long least = -1;
   for (int i = 1; i <= most; ++i) {
-    const long long each = (full * i + 255) / 256, cost = (pair || dtype == kF32 ? 2 * each : 1 + each) * ((keys + i - 1) / i + head_dim / 16);
+    const long long each = (full * i + 255) / 256, waves = few ? 4 * i : i;
+    const long long cost = 4 * (alone ? 2 * each : 1 + each) * ((keys + waves - 1) / waves + head_dim / 16) + (few ? i : 0);
     if (least < 0 || cost < least) {
       least = cost;
       c.splits = i;

@@ -45,16 +45,15 @@ template <int ROWS> __device__ __forceinline__ bool row_tile_of(const ChunkArgs&
   return t.rows > 0;
 }
 // What it sees, in stages of KEYS keys: the cache's and the chunk's, and the shares of them that its workgroups take.  With equal_shares a share of a tile of more
-// than a wave's rows is as long as one of the request that sees the most: shorter ones have fewer, and no more of their outputs to be joined.
+// than a quarter of its rows is as long as one of the request that sees the most: shorter ones have fewer, and no more of their outputs to be joined.
 template <int DT, int ROWS, int KEYS> struct Plan {
-  static constexpr int kFewRows = 32;
   int n, cache_stages, stages, per, used;
   __device__ __forceinline__ Plan(const ChunkArgs& a, const RowTile& t) {
     n = __builtin_amdgcn_readfirstlane(min(max(a.n_used[t.at.request * a.heads + t.head], 0), budget_of(a.pages, a.B, t.at.request)));
     cache_stages = (n + KEYS - 1) / KEYS;
     stages = __builtin_amdgcn_readfirstlane(cache_stages + (t.first_row + t.rows - 1) / a.group / KEYS + 1);
     per = max((stages + a.splits - 1) / a.splits, chunk_least_keys(DT, ROWS) / KEYS);
-    if (a.equal_shares && t.rows > kFewRows) {
+    if (a.equal_shares && t.rows > ROWS / 4) {
       const int lane = threadIdx.x & (kWave - 1);
       int longest = 0;
 #pragma unroll 1
@@ -86,10 +85,9 @@ template <int ROWS> __device__ __forceinline__ bool my_tile(const ChunkArgs& a, 
 // A wave's results for NG groups of 32 rows: the values that were taken out (see below) added, and the rows written, or a split's share of them.
 template <int DT, int HD, int NG, bool WINDOW> struct Finish {
   using R = Rows<DT, HD>;
-  static __device__ __forceinline__ void run(const ChunkArgs& a, const RowTile& mine, int used, const int (&row)[NG], const int (&token)[NG], const Frag (&own)[NG][R::kSteps],
-                                             float (&m)[NG], float (&l)[NG], f32x16 (&o)[NG][R::kBlocks], int zeroed, int last_token) {
+  static __device__ __forceinline__ void add_back(const ChunkArgs& a, const RowTile& mine, const int (&token)[NG], const Frag (&own)[NG][R::kSteps], const float (&m)[NG],
+                                                  f32x16 (&o)[NG][R::kBlocks], int zeroed, int last_token) {
     const int lane = late_thread_id() & (kWave - 1), half = lane >> 5;
-    const int first_row = mine.first_row, rows = first_row + mine.rows;
     if (zeroed != 0x7fffffff) {
       const size_t at_head = static_cast<size_t>(mine.head) * R::kBytes;
 #pragma unroll 1
@@ -131,6 +129,12 @@ template <int DT, int HD, int NG, bool WINDOW> struct Finish {
         }
       }
     }
+  }
+  static __device__ __forceinline__ void run(const ChunkArgs& a, const RowTile& mine, int used, const int (&row)[NG], const int (&token)[NG], const Frag (&own)[NG][R::kSteps],
+                                             float (&m)[NG], float (&l)[NG], f32x16 (&o)[NG][R::kBlocks], int zeroed, int last_token) {
+    const int lane = late_thread_id() & (kWave - 1), half = lane >> 5;
+    add_back(a, mine, token, own, m, o, zeroed, last_token);
+    const int first_row = mine.first_row, rows = first_row + mine.rows;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       l[g] += __shfl_xor(l[g], 32, kWave);  // each half has summed different keys of the same query
@@ -544,10 +548,8 @@ __global__ __launch_bounds__(kThreads, 1) void chunk_attend_pair(ChunkArgs a) {
 
 // 32 rows of a wave, 32 keys of a stage, one after the other, and as many waves as there is room for.
 // Measured: 24 requests, of which 18 decode a token and the others take 384 or fewer, 8 heads of 4 queries, over 4096 keys or fewer, 140 us (156 with as many
-// shares for short requests as for long ones); 32 that decode a token
-// over 4096 keys each 107 us (5.0 TB/s); 6 of up to 333 tokens over 2048, 12 heads, 64 dimensions, with a recency window, 40 us (45 with the
-// window looked for in every score); fp32, 5 of up to 101 over 1501,
-// 5 heads of 3 queries, 70 us, and 4 that decode a token over 500, 4 heads, 64 dimensions, 14 us.
+// shares for short requests as for long ones); 6 of up to 333 tokens over 2048, 12 heads, 64 dimensions, with a recency window, 40 us (45 with the
+// window looked for in every score).
 template <int DT, int HD> struct TileForm {
   using R = Rows<DT, HD>;
   static constexpr int kTileBytes = kSub * R::kBytes;             // of K, then as many of V
@@ -776,6 +778,258 @@ __global__ __launch_bounds__(kThreads, (TileForm<DT, HD>::kWavesPerSimd)) void c
   if (!idle) Finish<DT, HD, 1, WINDOW>::run(a, mine, plan.used, row, token, own, m, l, o, zeroed, min((t1 - cache_tiles) * kSub - 1, wave_last));
 }
 
+// One to 32 rows of a request: four waves that share them, each with a quarter of the workgroup's keys, tiles of its own and no barrier until their shares are joined
+// in LDS.  A tile's K is asked for as soon as the scores of the one before are formed, its V after that one's products.
+// Measured: a token of 32 requests, 8 heads of 4 queries, over 4096 keys each, bf16 / 128, 103 us (5.2 TB/s); of 8 heads of one over 2048, fp32 / 128, 104 us (5.2 TB/s; with
+// tiles of 128 rows, three waves of four without any, 286); fp32, 5 of up to 101 tokens over 1501, 5 heads of 3 queries, 70 us; 4 that decode a token over 500, 4 heads, 64
+// dimensions, 14 us.
+template <int DT, int HD> struct FewForm {
+  using R = Rows<DT, HD>;
+  static constexpr int kOperand = kSub * R::kBytes, kWaveBytes = 2 * kOperand, kBytes = kWaves * kWaveBytes;
+  static constexpr int kLoads = kOperand / 1024;                  // of a tile's K, or V
+  static constexpr int kWavesPerSimd = kBytes > 65536 ? 1 : kBytes > 32768 ? 2 : 4;
+};
+
+template <int DT, int HD, bool WINDOW>
+__global__ __launch_bounds__(kThreads, (FewForm<DT, HD>::kWavesPerSimd)) void chunk_attend_few(ChunkArgs a) {
+  using R = Rows<DT, HD>;
+  using F = FewForm<DT, HD>;
+  constexpr int kSide = WINDOW ? 1 : 0;
+  extern __shared__ __attribute__((aligned(1024))) char ring[];
+  __shared__ __attribute__((aligned(256))) int32_t pos_s[WINDOW ? kWaves : 1][WINDOW ? 2 : 1][kWave];
+  __shared__ float m_s[kWaves][kWave], l_s[kWaves][kWave];
+  RowTile mine;
+  if (!my_tile<32>(a, mine)) return;
+  const Located& at = mine.at;
+  const int head = mine.head, first_row = mine.first_row, rows = first_row + mine.rows;
+  const int u = at.request * a.heads + head;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int half = lane >> 5;
+  const Plan<DT, 32, kSub> plan(a, mine);
+  const int n = plan.n, cache_tiles = plan.cache_stages;
+  const int first_tile = mine.split * plan.per, last_tile = min(plan.stages, first_tile + plan.per);
+  if (first_tile >= last_tile) return;
+  const int each = (last_tile - first_tile + kWaves - 1) / kWaves;
+  const int t0 = __builtin_amdgcn_readfirstlane(min(last_tile, first_tile + wave * each)), t1 = __builtin_amdgcn_readfirstlane(min(last_tile, t0 + each));
+  const Groups groups(a.pages, a.B, a.heads, at.request, head);
+  char* const my_lds = ring + wave * F::kWaveBytes;
+  const uint32_t lds = lds_address(my_lds), pos_addr = lds_address(&pos_s[WINDOW ? wave : 0][0][0]);
+  int koff[F::kLoads], voff[F::kLoads];
+#pragma unroll
+  for (int i = 0; i < F::kLoads; ++i) {
+    const int r = R::kPerLoad * i + lane / R::kChunks;
+    koff[i] = r * R::kBytes + (((lane % R::kChunks) ^ R::swizzle_k(r)) << 4);
+    voff[i] = r * R::kBytes + (((lane % R::kChunks) ^ R::swizzle_v(r)) << 4);
+  }
+  const v4i32 pbuf = make_buffer(a.pos + static_cast<size_t>(u) * a.B, WINDOW ? static_cast<uint32_t>(n) * 4u : 0u);
+  const int64_t new_byte = static_cast<int64_t>(at.first) * a.kv_stride + static_cast<int64_t>(head) * R::kBytes;
+  const int more_stride = static_cast<int>(a.kv_stride) - R::kBytes;
+  int ahead[2] = {0, 0};  // pages of the two groups of the tile that is asked for next
+  const auto look_ahead = [&](int t) {
+    if (t >= min(t1, cache_tiles)) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ahead[i] = __builtin_amdgcn_readfirstlane(groups.page_of(min(t * kSub + 16 * i, n - 1)));
+  };
+  // A tile's place: rows of the cache, 16 of a page each, or of the chunk, side by side but for the stride.
+  struct Place { uint32_t row[2]; int count[2]; };
+  const auto place_of = [&](int t) {
+    Place p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (t < cache_tiles) {
+        const int slot = t * kSub + 16 * i;
+        p.count[i] = __builtin_amdgcn_readfirstlane(min(max(n - slot, 0), 16));
+        if (!groups.row_of(slot, ahead[i], p.row[i])) p.count[i] = 0;
+        if (p.count[i] == 0) p.row[i] = 0;
+      } else {
+        const int j = (t - cache_tiles) * kSub + 16 * i;
+        p.count[i] = __builtin_amdgcn_readfirstlane(min(max(at.count - j, 0), 16));
+        p.row[i] = static_cast<uint32_t>(p.count[i] > 0 ? j : 0);
+      }
+    }
+    return p;
+  };
+  const auto request = [&](auto of_v, int t, const Place& p) {
+    constexpr bool kOfV = decltype(of_v)::value;
+    const bool of_new = t >= cache_tiles;
+    const char* const base = static_cast<const char*>(kOfV ? (of_new ? a.v_new : a.V) : (of_new ? a.k_new : a.K));
+    const int more = of_new ? more_stride : 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const char* const from = base + (of_new ? new_byte + static_cast<int64_t>(p.row[i]) * a.kv_stride : static_cast<int64_t>(p.row[i]) * R::kBytes);
+      const v4i32 buf = make_buffer(from, p.count[i] > 0 ? static_cast<uint32_t>(p.count[i] - 1) * static_cast<uint32_t>(R::kBytes + more) + R::kBytes : 0u);
+#pragma unroll
+      for (int k = 0; k < F::kLoads / 2; ++k) {
+        const int at_load = i * (F::kLoads / 2) + k;
+        // (a group's offsets begin at its first row: 16 rows are whole loads, and the swizzles repeat)
+        load16_to_lds(buf, lds + (kOfV ? F::kOperand : 0) + at_load * 1024, (kOfV ? voff[at_load] : koff[at_load]) - 16 * i * R::kBytes + (R::kPerLoad * k + lane / R::kChunks) * more, 0);
+      }
+    }
+  };
+  const auto request_k = [&](int t, const Place& p) {
+    if (WINDOW) mfma::load4_to_lds(pbuf, pos_addr + (t & 1) * (kWave * 4), t < cache_tiles ? (t * kSub + lane) * 4 : 0x7ffffffc, 0);
+    request(std::false_type(), t, p);
+  };
+  const auto reads_done = [&]() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };  // what is overwritten next has been read
+  int row[1], token[1];
+  Frag own[1][R::kSteps];
+  look_ahead(t0);
+  take_rows<DT, HD, 1>(a, mine, first_row, row, token, own);
+  const int rows_first = __builtin_amdgcn_readfirstlane(first_row / a.group), rows_last = __builtin_amdgcn_readfirstlane((rows - 1) / a.group);
+  float m[1] = {-INFINITY}, l[1] = {0.0f};
+  f32x16 o[1][R::kBlocks];
+#pragma unroll
+  for (int db = 0; db < R::kBlocks; ++db) o[0][db] = f32x16{0};
+  const float sc = a.scale_log2, bias = WINDOW ? a.recency_bias_log2 : 0.0f;
+  const int w = WINDOW ? a.recency_window : 0, qp0 = WINDOW ? a.qpos0[at.request] : 0;
+  const uint32_t kfrag = lds + (lane & 31) * R::kBytes + ((half ^ R::swizzle_k(lane & 31)) << 4);
+  const int vrow = 4 * half + (DT == kBF16 ? (lane & 15) >> 2 : 0);
+  const uint32_t vt = lds + F::kOperand + vrow * R::kBytes + (R::swizzle_v(vrow) << 4) + (DT == kBF16 ? ((lane >> 4) & 1) * 32 + (lane & 3) * 8 : (lane & 31) * 4);
+  int zeroed = 0x7fffffff;
+  // (the queries have arrived: a wait for them below would also wait for the tiles requested last)
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  Place here = {{0, 0}, {0, 0}};
+  if (t0 < t1) {
+    here = place_of(t0);
+    request_k(t0, here);
+    request(std::true_type(), t0, here);
+    look_ahead(t0 + 1);
+  }
+#pragma unroll 1
+  for (int t = t0; t < t1; ++t) {
+    const bool of_new = t >= cache_tiles, more_tiles = t + 1 < t1;
+    const int j0 = (t - cache_tiles) * kSub;
+    const int there[2] = {here.count[0], here.count[1]};
+    wait_loads<F::kLoads>();  // K is there; V may still be on its way
+    f32x16 s = {0};
+#pragma unroll
+    for (int kk = 0; kk < R::kSteps; ++kk) s = score_step<DT>(read_frag(kfrag ^ (kk << 5)), own[0][kk], s);
+    reads_done();
+    if (more_tiles) {
+      here = place_of(t + 1);
+      request_k(t + 1, here);
+      look_ahead(t + 2);
+    }
+    const int32_t* const pos_t = &pos_s[WINDOW ? wave : 0][WINDOW ? t & 1 : 0][0];
+    bool interior = of_new ? w <= rows_first - (j0 + kSub - 1) : there[0] + there[1] == kSub;
+    if (WINDOW && !of_new) {  // outside the window of every row
+      const int at_slot = pos_t[lane & 31];
+      interior = interior && !__any(at_slot <= qp0 + rows_last && at_slot > qp0 + rows_first - w);
+    }
+    float most = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float x = s[e] * sc;
+      if (!interior) {
+        const int k = 8 * (e >> 2) + 4 * half + (e & 3);
+        if (WINDOW) {
+          const int away = qp0 + token[0] - (of_new ? qp0 + j0 + k : pos_t[k]);
+          x += static_cast<unsigned>(away) < static_cast<unsigned>(w) ? bias : 0.0f;
+        }
+        const bool seen = of_new ? j0 + k <= token[0] : (k & 15) < there[e >> 3];
+        x = seen ? x : -INFINITY;
+      }
+      s[e] = x;
+      most = fmaxf(most, x);
+    }
+    most = fmaxf(most, __shfl_xor(most, 32, kWave));
+    const float m_new = fmaxf(m[0], most);
+    if (__any(m_new > m[0])) {
+      const float alpha = m[0] > -INFINITY ? fast_exp2(m[0] - m_new) : 0.0f;
+      l[0] *= alpha;
+#pragma unroll
+      for (int db = 0; db < R::kBlocks; ++db) o[0][db] *= alpha;
+    }
+    m[0] = m_new;
+    const float ref = m_new > -INFINITY ? m_new : 0.0f;  // nothing seen yet: every term is 2^-inf = 0
+    float p[16];
+    bf16x8 pf[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float v = fast_exp2(s[e] - ref);
+      if (DT == kBF16) pf[e >> 3][e & 7] = static_cast<__bf16>(v);
+      else p[e] = v;
+      l[0] += v;
+    }
+    if (more_tiles) wait_loads<F::kLoads + kSide>();  // V is there; K of the next tile may still be on its way
+    else wait_loads<0>();
+    if (of_new && j0 + kSub - 1 > rows_first) {  // (as take_out of chunk_attend_pair)
+      char* const tileV = my_lds + F::kOperand;
+      bool any = false;
+#pragma unroll 2
+      for (int i = 0; i < F::kLoads; ++i) any |= holds_special<DT>(*reinterpret_cast<const uint4*>(tileV + i * 1024 + lane * 16));
+      if (__any(any)) {
+        zeroed = min(zeroed, j0);
+#pragma unroll 1
+        for (int j = 0; j < kSub; ++j) {
+          uint4* const chunk = reinterpret_cast<uint4*>(tileV + j * R::kBytes) + lane % R::kChunks;
+          if (__any(holds_special<DT>(*chunk))) *chunk = make_uint4(0u, 0u, 0u, 0u);
+        }
+        reads_done();
+      }
+    }
+    if constexpr (DT == kBF16) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int db = 0; db < R::kBlocks; ++db) {
+          const uint32_t v_at = (vt ^ (db << 6)) + ks * 16 * R::kBytes;
+          o[0][db] = score_step<DT>(read_frag_transposed(v_at, v_at + 8 * R::kBytes), __builtin_bit_cast(Frag, pf[ks]), o[0][db]);
+        }
+    } else {
+      typedef const __attribute__((address_space(3))) float* LdsFloats;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int db = 0; db < R::kBlocks; ++db) {
+          const float v = *(LdsFloats)(static_cast<uintptr_t>((vt ^ (db << 7)) + (8 * (e >> 2) + (e & 3)) * R::kBytes));
+          o[0][db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[e], o[0][db], 0, 0, 0);
+        }
+    }
+    reads_done();
+    if (more_tiles) request(std::true_type(), t + 1, here);
+  }
+  Finish<DT, HD, 1, WINDOW>::add_back(a, mine, token, own, m, o, zeroed, min((t1 - cache_tiles) * kSub - 1, rows_last));
+  // ---- the waves' shares: 16 bytes of a row a lane, each wave then has a quarter of the dimensions
+  constexpr int kParts = 4 * R::kBlocks, kMine = kParts / kWaves;
+  l[0] += __shfl_xor(l[0], 32, kWave);
+  m_s[wave][lane] = m[0];
+  l_s[wave][lane] = l[0];
+#pragma unroll
+  for (int k = 0; k < kParts; ++k)
+    *reinterpret_cast<tree::f32x4*>(my_lds + (k * kWave + lane) * 16) = tree::f32x4{o[0][k / 4][4 * (k % 4)], o[0][k / 4][4 * (k % 4) + 1], o[0][k / 4][4 * (k % 4) + 2], o[0][k / 4][4 * (k % 4) + 3]};
+  __syncthreads();
+  if (row[0] >= rows) return;
+  float M = -INFINITY, sum = 0.0f, weight[kWaves];
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) M = fmaxf(M, m_s[v][lane]);
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) {
+    weight[v] = m_s[v][lane] > -INFINITY ? fast_exp2(m_s[v][lane] - M) : 1.0f;  // (no maximum: a sum of zero, or NaN)
+    sum += l_s[v][lane] * weight[v];
+  }
+  const size_t out_row = packed_row(a, mine, row[0], token[0]);
+  const size_t part = mine.split * static_cast<size_t>(a.tokens) * a.heads * a.group + out_row;
+  if (wave == 0 && half == 0) {
+    if (plan.used > 1) {
+      a.part_m[part] = M;
+      a.part_l[part] = sum;
+    } else if (a.lse != nullptr) {
+      a.lse[out_row] = kLn2 * (M + __log2f(sum));
+    }
+  }
+  const float inv = 1.0f / sum;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int k = wave * kMine + i, d0 = 32 * (k / 4) + 8 * (k % 4) + 4 * half;
+    tree::f32x4 all = tree::f32x4{0};
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) all += *reinterpret_cast<const tree::f32x4*>(ring + v * F::kWaveBytes + (k * kWave + lane) * 16) * weight[v];
+    if (plan.used > 1) *reinterpret_cast<tree::f32x4*>(a.part_o + part * HD + d0) = all;
+    else tree::store4<DT>(a.out, out_row * HD + d0, all * inv);
+  }
+}
+
 // The splits' shares of a tile's rows, HD / 4 lanes with 16 bytes of a row each; four splits at a time, in their order.  `parts` workgroups a tile: with one for
 // every few rows most of the time goes into finding out which (24 requests with 6 chunks of 384 tokens, 148 -> 140 us; 32 that decode a token, 112 -> 107).
 template <int DT, int HD, int ROWS, int KEYS> __global__ __launch_bounds__(kThreads) void chunk_join(ChunkArgs a, int parts) {
@@ -845,6 +1099,7 @@ template <int DT, int HD, int ROWS, int KEYS, class Kernel> hipError_t launch_ti
 template <int DT, int HD, bool WINDOW> hipError_t launch_attend_form(const ChunkArgs& a, hipStream_t s) {
   if constexpr (DT == kBF16 && HD == 128)
     if (a.row_tile == 256) return launch_tiles<DT, HD, 256, 64>(chunk_attend_pair<HD, WINDOW>, PairForm<HD>::kBytes, a, s);
+  if (a.row_tile == 32) return launch_tiles<DT, HD, 32, 32>(chunk_attend_few<DT, HD, WINDOW>, FewForm<DT, HD>::kBytes, a, s);
   return launch_tiles<DT, HD, 128, 32>(chunk_attend<DT, HD, WINDOW>, TileForm<DT, HD>::kBytes, a, s);
 }
 template <int DT, int HD> hipError_t launch_attend(const ChunkArgs& a, hipStream_t s) {

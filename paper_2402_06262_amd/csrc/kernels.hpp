@@ -264,7 +264,7 @@ struct ChunkArgs {
 };
 // Keys of a workgroup of chunk_attend, if its tile sees more than that.  (With 128 of them everywhere 4 requests that decode a token over 500 keys, 4 heads, fp32,
 // took 20 us, not 14; 1 over 1024, 8 heads, bf16, 15 us either way.)
-__host__ __device__ constexpr int chunk_least_keys(int dtype, int row_tile) { return dtype != 1 ? 32 : row_tile == 256 ? 128 : 64; }
+__host__ __device__ constexpr int chunk_least_keys(int dtype, int row_tile) { return row_tile == 32 ? 128 : dtype != 1 ? 32 : row_tile == 256 ? 128 : 64; }
 struct ChunkSplits { int row_tile, row_tiles, splits, equal_shares; };
 ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
 int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B);

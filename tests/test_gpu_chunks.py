@@ -29,6 +29,16 @@ _IMPORTANCE = {"mas": 0, "aas": 1, "oldest": 2, "ltas": 3, "aqas": 4}
 _SCOPE = {"std": 0, "window": 1, "all": 2}
 
 
+@pytest.fixture(params=["", "32", "128", "256"], ids=lambda p: "rows" + p)
+def row_tile(request, monkeypatch):
+    """Every form of the attention, whatever a call of this size would take."""
+    if request.param:
+        monkeypatch.setenv("ROCO_CHUNK_ROWS", request.param)
+
+
+every_form = pytest.mark.usefixtures("row_tile")
+
+
 def dev(x, dtype=None):
     x = torch.from_numpy(np.ascontiguousarray(x))
     return (x.to(torch.int32) if dtype is None else x.float().to(_DT[dtype])).cuda()
@@ -225,6 +235,7 @@ def near_average(s, u, q, lse, st):
     return near
 
 
+@every_form
 # ---------------------------------------------------------------------------------------------------- attention
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("used,tokens,group", [
@@ -235,6 +246,7 @@ def test_attention(dtype, d, used, tokens, group):
     s.check_attend(*s.attend())
 
 
+@every_form
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("page", [16, 32, 64, 1024])
 def test_pages(dtype, d, page):
@@ -242,6 +254,7 @@ def test_pages(dtype, d, page):
     s.check_attend(*s.attend())
 
 
+@every_form
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("window,page", [(1, 0), (20, 0), (300, 16), (100000, 64)])
 def test_recency_windows(dtype, d, window, page):
@@ -249,6 +262,7 @@ def test_recency_windows(dtype, d, window, page):
     s.check_attend(*s.attend())
 
 
+@every_form
 @pytest.mark.parametrize("splits", [1, 2, 3, 7, 64])
 @pytest.mark.parametrize("dtype,d", TYPES)
 def test_splits(dtype, d, splits, monkeypatch):
@@ -265,12 +279,14 @@ def test_shares_of_equal_length(dtype, d, tokens):
     s.check_attend(*s.attend(), units=[0, 5, 8, 13, 16, 23])
 
 
+@every_form
 @pytest.mark.parametrize("dtype,d", TYPES)
 def test_rows_of_their_own(dtype, d):
     s = Step(d, dtype, d, [50, 10], [20, 3], group=2, fused=False).upload()
     s.check_attend(*s.attend())
 
 
+@every_form
 @pytest.mark.parametrize("requests", [63, 64, 65, 130])
 def test_many_requests(requests):
     rng = np.random.default_rng(requests)
@@ -309,6 +325,7 @@ def test_policies(policy, group):
     s.check_commit(lse)
 
 
+@every_form
 # ---------------------------------------------------------------------------------------------------- many rows of bf16 / 128: 64 rows of a wave
 @pytest.mark.parametrize("used,tokens,group,page", [([300, 70, 0], [400, 500, 300], 4, 0), ([129], [1100], 1, 0), ([65, 31], [600, 0], 8, 16), ([500, 16, 64], [70, 3, 1], 64, 64),
                                                     ([1], [257], 5, 32), ([640], [128], 16, 0)])
@@ -321,6 +338,7 @@ def test_many_rows(used, tokens, group, page, splits, monkeypatch):
     s.check_attend(*s.attend())
 
 
+@every_form
 @pytest.mark.parametrize("window", [1, 33, 200, 2 ** 31 - 1])
 @pytest.mark.parametrize("page,splits", [(0, 0), (32, 2)])
 def test_many_rows_under_a_window(window, page, splits, monkeypatch):
@@ -333,6 +351,7 @@ def test_many_rows_under_a_window(window, page, splits, monkeypatch):
 FORMS = [(dtype, d, [90, 33], [70, 40], 2) for dtype, d in TYPES] + [("bf16", 128, [90, 33], [300, 250], 4)]
 
 
+@every_form
 @pytest.mark.parametrize("dtype,d,used,tokens,group", FORMS)
 @pytest.mark.parametrize("window", [0, 25])
 @pytest.mark.parametrize("splits", [1, 2])
@@ -363,6 +382,7 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, d, used, tokens, group
     assert (err <= (rel * w.mass[i] + half * np.abs(w.out[i]) + 1e-30)[..., rest]).all()
 
 
+@every_form
 @pytest.mark.parametrize("dtype,d,used,tokens,group", FORMS)
 @pytest.mark.parametrize("window", [4, 1 << 20])
 @pytest.mark.parametrize("bias", [-1e38, -300.0, 1e38])
@@ -373,6 +393,7 @@ def test_recency_biases_of_any_size(dtype, d, used, tokens, group, window, bias)
     s.check_attend(*s.attend())
 
 
+@every_form
 @pytest.mark.parametrize("dtype,d,used,tokens,group", FORMS)
 def test_logits_far_apart(dtype, d, used, tokens, group):
     """Scores that rise by hundreds from tile to tile: the sums' reference has to follow, and what is far below it has no weight."""
@@ -384,6 +405,7 @@ def test_logits_far_apart(dtype, d, used, tokens, group):
     s.check_attend(*s.attend())
 
 
+@every_form
 @pytest.mark.parametrize("dtype,d,used,tokens,group", FORMS)
 def test_pages_outside_the_pool_are_not_seen(dtype, d, used, tokens, group):
     """... and neither read nor written: the slots' statistics stay, the others' are as if those were not there."""
@@ -458,6 +480,7 @@ def test_no_records_of_the_evicted_and_chunks_larger_than_the_budget():
     assert all(torch.equal(x, y) for x, y in zip(first, (s.dK, s.dV, s.dstats, s.dpos, s.dn_used)))
 
 
+@every_form
 @pytest.mark.parametrize("off", [1, 2, 3])
 def test_words_that_begin_anywhere(off):
     """Statistics, positions, lengths and normalisers are parts of larger buffers."""
@@ -531,6 +554,7 @@ def _shapes():
             Step(9, "bf16", 64, [300], [33], group=5, B=300, window=9).upload()]
 
 
+@every_form
 def test_repeated_calls_give_the_same_bits_and_leave_the_cache():
     for s in _shapes():
         K, V = s.dK.clone(), s.dV.clone()
