@@ -11,7 +11,8 @@
 // Measured, with all of roco_chunk_commit: 4 requests of 512 tokens, 8 heads of 4 queries, 4096 slots, bf16, 128 dimensions, 108 us (the products would
 // take 33 at 2.1 PFLOP/s, the vector instructions 50), with one workgroup along the rows 125; 12 of up to 200, groups of 8, 2048 slots, 64 dimensions,
 // 61 us and 67.  With one path for all rows, of selects and of branches within, 154 and 102 us of the kernel alone, and the requests side by
-// side on a die, so that one had the longest.
+// side on a die, so that one had the longest.  A token of 32 requests, 8 heads, 2048 slots, fp32 / 128, 135 us (213 with the rows that a tile has not), of 8 heads of
+// 4 queries over 4096 slots, bf16 / 128, 97 us and 105 (K alone, 268 MB of either, would take 52).
 #pragma once
 #include "chunk_choose.hpp"
 #include "profile.hpp"
@@ -161,13 +162,14 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
   // the rest, with recency windows or other statistics than the squares' sum.
   constexpr int kInside = 0, kFilled = 1, kPartly = 2, kAny = 3;
   const bool last_only = a.pol.keeps_last_score();
-  const auto half_tile = [&](auto h_, auto kind_, int t, int at_stage, uint32_t next, f32x16 (&s)[NG], f32x16 (&s_next)[NG]) {
+  const auto half_tile = [&](auto h_, auto kind_, auto ahead_, int t, int at_stage, uint32_t next, f32x16 (&s)[NG], f32x16 (&s_next)[NG]) {
     constexpr int h = decltype(h_)::value, kKind = decltype(kind_)::value;
+    constexpr bool kAhead = decltype(ahead_)::value;  // there are rows behind them
     const int first = t * kTokens;
     const float* const lse_t = &lse_s[at_stage][wave][16 * half + 32 * h];
     Frag qf[R::kSteps];
 #pragma unroll
-    for (int i = 0; i < kEarly; ++i) qf[i] = read_frag(next ^ (i << 5));
+    for (int i = 0; i < kEarly && kAhead; ++i) qf[i] = read_frag(next ^ (i << 5));
     float less[16];
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
@@ -179,10 +181,10 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
     for (int g = 0; g < NG; ++g) s_next[g] = f32x16{0};
 #pragma unroll
     for (int kk = 0; kk < R::kSteps; ++kk) {
-      if (kk + kEarly < R::kSteps) qf[kk + kEarly] = read_frag(next ^ ((kk + kEarly) << 5));
+      if (kAhead && kk + kEarly < R::kSteps) qf[kk + kEarly] = read_frag(next ^ ((kk + kEarly) << 5));
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        s_next[g] = score_step<DT>(qf[kk], own[g][kk], s_next[g]);
+        if (kAhead) s_next[g] = score_step<DT>(qf[kk], own[g][kk], s_next[g]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int e = kEach * kk; e < kEach * kk + kEach; ++e) {
@@ -210,14 +212,7 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
       }
     }
   };
-  if (j0 + wave * NG * 32 >= keys) {  // no keys of this wave, but the other waves want its loads
-#pragma unroll 1
-    for (int t = t0; t < t1; ++t) {
-      next_tile(t);
-      stage = stage + 1 == F::kStages ? 0 : stage + 1;
-    }
-  } else {
-    f32x16 s0[NG], s1[NG];
+  const auto first_scores = [&](f32x16 (&s0)[NG]) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) s0[g] = f32x16{0};
 #pragma unroll
@@ -226,20 +221,42 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
 #pragma unroll
       for (int g = 0; g < NG; ++g) s0[g] = score_step<DT>(qf, own[g][kk], s0[g]);
     }
+  };
+  const auto in_reach = [&](int first) {  // some row and key of one another
+    bool window = false;
+    if (w > 0) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g) window = window || __any(first - kpos[g] < w && first + kTokens - 1 - kpos[g] >= 0);
+    }
+    return window;
+  };
+  const bool no_keys = j0 + wave * NG * 32 >= keys;
+  if (t1 - t0 == 1 && c - t0 * kTokens <= kTokens / 2) {  // half a tile has all the rows, a decoding token's for one
+    if (!no_keys) {
+      f32x16 s0[NG], s1[NG];
+      first_scores(s0);
+      if (in_reach(t0 * kTokens) || !squares) half_tile(std::integral_constant<int, 0>(), std::integral_constant<int, kAny>(), std::false_type(), t0, 0, 0u, s0, s1);
+      else half_tile(std::integral_constant<int, 0>(), std::integral_constant<int, kPartly>(), std::false_type(), t0, 0, 0u, s0, s1);
+    }
+  } else if (no_keys) {  // no keys of this wave, but the other waves want its loads
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+      next_tile(t);
+      stage = stage + 1 == F::kStages ? 0 : stage + 1;
+    }
+  } else {
+    f32x16 s0[NG], s1[NG];
+    first_scores(s0);
 #pragma unroll 1
     for (int t = t0; t < t1; ++t) {
       next_tile(t);
       const int first = t * kTokens, now = stage;
       stage = stage + 1 == F::kStages ? 0 : stage + 1;
-      bool window = false;  // some row and key in reach of one another
-      if (w > 0) {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) window = window || __any(first - kpos[g] < w && first + kTokens - 1 - kpos[g] >= 0);
-      }
+      const bool window = in_reach(first);
       const uint32_t second = ring_addr + now * F::kTileBytes + 32 * R::kBytes + frag, next = ring_addr + stage * F::kTileBytes + frag;
       const auto tile = [&](auto kind) {
-        half_tile(std::integral_constant<int, 0>(), kind, t, now, second, s0, s1);
-        half_tile(std::integral_constant<int, 1>(), kind, t, now, next, s1, s0);
+        half_tile(std::integral_constant<int, 0>(), kind, std::true_type(), t, now, second, s0, s1);
+        half_tile(std::integral_constant<int, 1>(), kind, std::true_type(), t, now, next, s1, s0);
       };
       if (window || !squares) tile(std::integral_constant<int, kAny>());
       else if (first + kTokens > c || (of_fresh && first < last_key)) tile(std::integral_constant<int, kPartly>());
