@@ -610,7 +610,7 @@ int roco_probe_mfma(int32_t workgroups, int32_t iters, int32_t operands, float* 
  *   ROCO_CHUNK_ROW_SPLITS=1..16  workgroups along the rows of a chunk in the sums of roco_chunk_commit (default: until there are about 2048,
  *                              with four tiles of 64 rows each); part of roco_chunk_workspace_bytes: set it before asking
  *   ROCO_VERIFY_ROUNDS=1..12   passes over the vocabulary that roco_tree_verify makes with the whole chip before a workgroup per request goes on alone
- *                              (default: 1 for chains and without q, 3 + nodes / 8 for trees)
+ *                              (default: 1 for chains and without q, for trees 3 + nodes / 8, but 4 + log2(requests) at most)
  *   ROCO_SELECT_THREADS=512|1024  threads of the prompt selection (default: 512 for prompts of up to 512 tokens, and of up to 2048
  *                              with more than 256 units)
  *   ROCO_PREFILL_WAVES_PER_ROW=1|4  waves that share a query row of the vector row pass (default: four for few rows)

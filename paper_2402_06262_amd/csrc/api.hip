@@ -758,9 +758,10 @@ int roco_tree_verify(int32_t dtype, int32_t requests, int32_t nodes, int32_t voc
   char* const ws = static_cast<char*>(workspace);
   // A chain has one pass: behind its first rejection, or its end.  So has a tree without the drafts' probabilities; with them it has one more for every rejection
   // that another continuation follows.  A round that nobody needs costs 2.7 us, one too few, over 65536 tokens, 10 (32 requests of 32 nodes, 7 rounds 54 us, 5 49,
-  // 3 70; 16 of 8 nodes, 4 rounds 37 us, 3 44, 6 43; 16 of 16, 5 rounds 65 us, 6 54, 3 85).
+  // 3 70; 16 of 8 nodes, 4 rounds 37 us, 3 44, 6 43; 16 of 16, 5 rounds 65 us, 6 54, 3 85).  The slowest request of many counts: of 600 drawn trees of 32 nodes, three
+  // continuations each, one needs 2.5 rounds, the slowest of 32 six.
   int rounds = env_int("ROCO_VERIFY_ROUNDS", 0);
-  if (rounds < 1 || rounds > kMaxVerifyRounds) rounds = parent == nullptr || q == nullptr || nodes <= 2 ? 1 : std::min(kMaxVerifyRounds, 3 + nodes / 8);
+  if (rounds < 1 || rounds > kMaxVerifyRounds) rounds = parent == nullptr || q == nullptr || nodes <= 2 ? 1 : std::min({kMaxVerifyRounds, 3 + nodes / 8, 4 + 31 - __builtin_clz(requests)});
   const VerifyArgs a = {requests, nodes, vocab, distinct != 0, max_path, dtype == ROCO_BF16, p, q, p_request_stride, p_row_stride, q_request_stride, q_row_stride,
                         tokens, parent, n_nodes, accept, choose, path, n_path, next_token, reinterpret_cast<double*>(ws),
                         reinterpret_cast<VerifyNode*>(ws + lay.found), reinterpret_cast<VerifyWalk*>(ws + lay.walks), verify_blocks(vocab), rounds};
