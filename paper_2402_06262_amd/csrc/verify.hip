@@ -13,7 +13,8 @@
 //   verify_choose : one workgroup per request.  The passes that are left (trees; one workgroup alone with a row), the accepted path, and the next
 //                   token: the block, and in it the token, where the sums pass a share `choose` of N.
 // Measured, fp32: 64 chains of 8 nodes over 100003 tokens 25 us (52 MB have to be read: 10 us), 32 trees of 32 nodes over 65536 54 us, in 7 rounds of 4 us and
-// less, waits for memory three times over; before the walks were left behind, 27 and 74 to 82.
+// less, waits for memory three times over; before the walks were left behind, 27 and 74 to 82.  Without q, 57 trees of 18 over 2727, five continuations each, 20 us (50 with every
+// element compared with every rejected token in a loop of its own).
 // Sums are held in 64 bits: with 32 a token in some thousands would be another than the numbers say (2^17 borders, each 2^-24 off).
 #include <algorithm>
 
@@ -206,29 +207,30 @@ template <bool BF16> struct Row {
     const double v = q != nullptr ? __dsub_rn(static_cast<double>(x), __dmul_rn(w.times, static_cast<double>(probability(y)))) : static_cast<double>(x);
     return v > 0.0 ? v : 0.0;  // (NaN: none)
   }
-  __device__ __forceinline__ bool left_out(int i) const {
-    bool out = false;
-    for (uint64_t left = w.rejected; left != 0; left &= left - 1) out |= __builtin_amdgcn_readlane(rejected_token, __builtin_ctzll(left)) == i;
-    return out;
+  // Zeros for the rejected tokens (without q, whose weights are p): token after token, so that an element costs a comparison and nothing else.  index(k): that of f[k].
+  template <int N, class Index> __device__ __forceinline__ void take_out(float (&f)[N], Index index) const {
+#pragma unroll 1
+    for (uint64_t left = w.rejected; left != 0; left &= left - 1) {
+      const int out = __builtin_amdgcn_readlane(rejected_token, __builtin_ctzll(left));
+#pragma unroll
+      for (int k = 0; k < N; ++k) f[k] = index(k) == out ? 0.0f : f[k];
+    }
   }
   __device__ __forceinline__ double block_sum(int block) const {
     const int lane = threadIdx.x & (kWave - 1), first = first_of(block);
-    float x[kSteps][PER], y[kSteps][PER];
+    float x[kSteps * PER], y[kSteps][PER];
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) elements(p, true, first + (s * kWave + lane) * PER, x[s]);
+    for (int s = 0; s < kSteps; ++s) elements(p, true, first + (s * kWave + lane) * PER, x + s * PER);
     if (q != nullptr) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) elements(q, together, first + (s * kWave + lane) * PER, y[s]);
     }
+    take_out(x, [&](int k) { return first + (k / PER * kWave + lane) * PER + k % PER; });
     double sum = 0.0;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        double v = weight(x[s][e], q != nullptr ? y[s][e] : 0.0f);
-        if (w.rejected != 0 && left_out(first + (s * kWave + lane) * PER + e)) v = 0.0;
-        sum += v;
-      }
+      for (int e = 0; e < PER; ++e) sum += weight(x[s * PER + e], q != nullptr ? y[s][e] : 0.0f);
     return wave_sum(sum);
   }
 };
@@ -354,12 +356,12 @@ template <bool BF16> __global__ __launch_bounds__(kChooseThreads) void verify_ch
 #pragma unroll
     for (int s = 0; s < kMine / PER; ++s) row.elements(row.q, row.together, first + s * PER, y + s * PER);
   }
+  row.take_out(x, [&](int k) { return first + k; });
   double weights[kMine];
   mine = 0.0;
 #pragma unroll
   for (int e = 0; e < kMine; ++e) {
     weights[e] = row.weight(x[e], y[e]);
-    if (w.rejected != 0 && row.left_out(first + e)) weights[e] = 0.0;
     mine += weights[e];
   }
   before = found_before + before_of(mine, total);
