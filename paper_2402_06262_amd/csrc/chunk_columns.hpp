@@ -11,7 +11,7 @@
 // Measured, with all of roco_chunk_commit: 4 requests of 512 tokens, 8 heads of 4 queries, 4096 slots, bf16, 128 dimensions, 108 us (the products would
 // take 33 at 2.1 PFLOP/s, the vector instructions 50), with one workgroup along the rows 125; 12 of up to 200, groups of 8, 2048 slots, 64 dimensions,
 // 61 us and 67.  With one path for all rows, of selects and of branches within, 154 and 102 us of the kernel alone, and the requests side by
-// side on a die, so that one had the longest.  A token of 32 requests, 8 heads, 2048 slots, fp32 / 128, 135 us (213 with the rows that a tile has not), of 8 heads of
+// side on a die, so that one had the longest.  A token of 32 requests, 8 heads, 2048 slots, fp32 / 128, 102 us (213 with the rows that a tile has not, 134 with room for three tiles), of 8 heads of
 // 4 queries over 4096 slots, bf16 / 128, 97 us and 105 (K alone, 268 MB of either, would take 52).
 #pragma once
 #include "chunk_choose.hpp"
@@ -33,7 +33,7 @@ template <int DT, int HD> struct ColumnForm {
 };
 
 // P: heads of a token, filled up to a power of two (32: 17 to 32 heads, 64: 33 to 64).
-template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void chunk_columns(ChunkArgs a, int choosers, int cache_blocks, int fresh_blocks) {
+template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void chunk_columns(ChunkArgs a, int choosers, int cache_blocks, int fresh_blocks, int stages) {
   using R = Rows<DT, HD>;
   using F = ColumnForm<DT, HD>;
   constexpr int NG = F::kGroups;
@@ -242,7 +242,7 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
 #pragma unroll 1
     for (int t = t0; t < t1; ++t) {
       next_tile(t);
-      stage = stage + 1 == F::kStages ? 0 : stage + 1;
+      stage = stage + 1 == stages ? 0 : stage + 1;
     }
   } else {
     f32x16 s0[NG], s1[NG];
@@ -251,7 +251,7 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
     for (int t = t0; t < t1; ++t) {
       next_tile(t);
       const int first = t * kTokens, now = stage;
-      stage = stage + 1 == F::kStages ? 0 : stage + 1;
+      stage = stage + 1 == stages ? 0 : stage + 1;
       const bool window = in_reach(first);
       const uint32_t second = ring_addr + now * F::kTileBytes + 32 * R::kBytes + frag, next = ring_addr + stage * F::kTileBytes + frag;
       const auto tile = [&](auto kind) {
@@ -289,12 +289,14 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
 template <int DT, int HD, int P> hipError_t launch_columns_form(const ChunkArgs& a, hipStream_t s) {
   using F = ColumnForm<DT, HD>;
   const int choosers = chosen_beside(a.B) ? (a.units + 7) / 8 * 8 : 0;
-  const int lds = std::max(F::kStages * F::kTileBytes, choosers > 0 ? (kChoiceWords<kThreads> + 2 * a.B) * 4 : 0);
+  // (no more stages than a request can have tiles: fewer of them let more workgroups onto a compute unit)
+  const int tokens = column_tokens(a.group), stages = std::min(F::kStages, (a.tokens + tokens - 1) / tokens);
+  const int lds = std::max(stages * F::kTileBytes, choosers > 0 ? (kChoiceWords<kThreads> + 2 * a.B) * 4 : 0);
   const void* const fn = reinterpret_cast<const void*>(chunk_columns<DT, HD, P>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return hipErrorInvalidValue;
   const int cache_blocks = (a.B + F::kKeys - 1) / F::kKeys, fresh_blocks = tiles_of(a.requests, a.tokens, 1, F::kKeys);
   const int total = (cache_blocks * a.row_splits * a.units + 7) / 8 + (fresh_blocks * a.row_splits * a.heads + 7) / 8;
-  hipLaunchKernelGGL((chunk_columns<DT, HD, P>), dim3(static_cast<unsigned>(total) * 8 + choosers), dim3(kThreads), lds, s, a, choosers, cache_blocks, fresh_blocks);
+  hipLaunchKernelGGL((chunk_columns<DT, HD, P>), dim3(static_cast<unsigned>(total) * 8 + choosers), dim3(kThreads), lds, s, a, choosers, cache_blocks, fresh_blocks, stages);
   return hipGetLastError();
 }
 template <int DT, int HD> hipError_t launch_columns(const ChunkArgs& a, hipStream_t s) {
