@@ -147,9 +147,9 @@ int check_chunk_shape(const roco_params* p, int32_t heads, int32_t group, int32_
 }
 // A token's rows, `count` of them, lie side by side; the tokens `stride` elements apart.
 int check_stride(const roco_params* p, int64_t stride, long long count) {
-  const long long element = p->dtype == ROCO_BF16 ? 2 : 4;
-  if (stride < count * p->head_dim || stride * element % 16 != 0) return ROCO_EINVAL;
-  return stride * element <= (1ll << 24) ? ROCO_OK : ROCO_EUNSUPPORTED;
+  const int64_t element = p->dtype == ROCO_BF16 ? 2 : 4;
+  if (stride < count * p->head_dim || stride % (16 / element) != 0) return ROCO_EINVAL;
+  return stride <= (1ll << 24) / element ? ROCO_OK : ROCO_EUNSUPPORTED;  // (in elements: the bytes of any stride need not fit 64 bits)
 }
 
 // ---- workspace of the chunks: chunk_attend's part_m | part_l | part_o, or chunk_commit's info | mark | sums | fresh | keys

@@ -59,6 +59,19 @@ def test_strides_are_checked(call):
 
 
 @pytest.mark.parametrize("call", [_attend, _commit])
+@pytest.mark.parametrize("dtype", [roco.ROCO_BF16, roco.ROCO_F32])
+def test_strides_whose_bytes_pass_64_bits(call, dtype):
+    """Distances of a token are bounded before they are counted in bytes: 2^62 elements of four bytes are 0 in 64 bits, and 2^62 + 2^20 an ordinary stride."""
+    p = roco.RocoParams(8, 128, 256, 16, dtype)
+    for far in (1 << 60, 1 << 61, 1 << 62, (1 << 62) + (1 << 20), (1 << 63) - (1 << 20), (1 << 63) - 8):
+        for strides in ((far, 512), (1024, far)):
+            assert call(p, strides=strides, ws=0) == EUNSUPPORTED, (far, strides)
+    for far in ((1 << 63) - 1, (1 << 24) + 1):  # neither a multiple of 16 bytes nor near enough
+        for strides in ((far, 512), (1024, far)):
+            assert call(p, strides=strides, ws=0) in (EINVAL, EUNSUPPORTED), (far, strides)
+
+
+@pytest.mark.parametrize("call", [_attend, _commit])
 def test_pages_are_checked(call):
     assert call(pages=_pages(), ws=0) == EWORKSPACE
     assert call(pages=_pages(table=None)) == EINVAL and call(pages=_pages(table=OK + 2)) == EINVAL and call(pages=_pages(budget=OK + 2)) == EINVAL
