@@ -190,7 +190,7 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
         for (int e = kEach * kk; e < kEach * kk + kEach; ++e) {
           float x = fmaf(s[g][e], sc, less[e]);
           const int local = (32 * h + 16 * half + e) / P;  // the row's token
-          if (kKind == kAny) x += static_cast<unsigned>(first + local - kpos[g]) < static_cast<unsigned>(w) ? bias : 0.0f;
+          if (kKind == kAny) x += static_cast<unsigned>(first + local) - static_cast<unsigned>(kpos[g]) < static_cast<unsigned>(w) ? bias : 0.0f;
           float p = fast_exp2(x);
           if (kKind != kInside) p = (P <= 16 ? e : 32 * h + 16 * half + e) % P >= a.group ? 0.0f : p;
           mean[g] = (P <= 16 ? e % P == 0 : e == 0 && (P == 32 || h == 0)) ? p : mean[g] + p;
@@ -222,11 +222,11 @@ template <int DT, int HD, int P> __global__ __launch_bounds__(kThreads, 2) void 
       for (int g = 0; g < NG; ++g) s0[g] = score_step<DT>(qf, own[g][kk], s0[g]);
     }
   };
-  const auto in_reach = [&](int first) {  // some row and key of one another
+  const auto in_reach = [&](int first) {  // some row and key of one another (a row that there is not may be farther from its key than any number)
     bool window = false;
     if (w > 0) {
 #pragma unroll
-      for (int g = 0; g < NG; ++g) window = window || __any(first - kpos[g] < w && first + kTokens - 1 - kpos[g] >= 0);
+      for (int g = 0; g < NG; ++g) window = window || __any(first - kpos[g] < w && first + kTokens - 1 >= kpos[g]);
     }
     return window;
   };

@@ -499,6 +499,23 @@ def test_words_that_begin_anywhere(off):
     s.check_commit(lse)
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("group", [1, 3])
+def test_positions_up_to_the_largest_number(dtype, d, group):
+    """The newest token lies at 2^31 - 1, the cached ones at the beginning, and the window reaches all of them but the first: the distance of a tile's last row,
+    which need not exist, from a key passes 31 bits."""
+    s = Step(d, dtype, d, [200, 33], [40, 7], group=group, window=2 ** 31 - 1, B=300)
+    s.qpos0 = np.array([2 ** 31 - t for t in s.tokens])
+    for u in range(s.U):
+        n = s.used[u // s.heads]
+        s.pos[u, :n] = s.rng.permutation(n)
+    s.upload()
+    s.check_attend(*s.attend())
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+
+
 # ---------------------------------------------------------------------------------------------------- large caches
 def test_offsets_beyond_32_bits():
     """Dense caches of 4.3 GB: the last unit's rows lie behind 2^32 bytes, its keys fill 2^21 slots."""
