@@ -420,6 +420,8 @@ int roco_tree_verify(int32_t dtype, int32_t requests, int32_t nodes, int32_t voc
  * Refused: strides that are not a multiple of 16 bytes (ROCO_EINVAL) or of more than 2^24 bytes, group above 64, tokens heads group of 2^31 or more
  * (ROCO_EUNSUPPORTED), and what roco_tree_attend refuses of params, heads and pages.
  */
+/* Bytes of scratch of the two calls (0 on invalid shapes), and of every call with fewer tokens over the same caches: a server's steps share what the
+ * largest asks for. */
 size_t roco_chunk_workspace_bytes(const roco_params* params, int32_t heads, int32_t group, int32_t tokens);
 int roco_chunk_attend(const roco_params* params, int32_t heads, int32_t group, int32_t tokens, const roco_pages* pages, const void* q,
                       int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const int32_t* token_start,

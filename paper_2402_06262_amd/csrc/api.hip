@@ -152,23 +152,28 @@ int check_stride(const roco_params* p, int64_t stride, long long count) {
   return stride <= (1ll << 24) / element ? ROCO_OK : ROCO_EUNSUPPORTED;  // (in elements: the bytes of any stride need not fit 64 bits)
 }
 
-// ---- workspace of the chunks: chunk_attend's part_m | part_l | part_o, or chunk_commit's info | mark | sums | fresh | keys
+// ---- workspace of the chunks: chunk_attend's part_m | part_l | part_o, or chunk_commit's info | mark | sums | fresh | keys.  The offsets are the call's own,
+// the size that of any call with as many tokens or fewer: a workspace for the largest step holds the others.
 struct ChunkLayout { size_t part_l, part_o, mark, sums, fresh, keys, total; ChunkSplits split; int row_splits; };
 ChunkLayout chunk_layout(const roco_params* p, int32_t heads, int32_t group, int32_t tokens) {
   ChunkLayout l;
+  const int requests = p->units / heads;
   const size_t U = p->units, B = p->budget, rows = static_cast<size_t>(tokens) * heads * group;
-  l.split = chunk_attend_splits(p->dtype, p->head_dim, p->units / heads, heads, group, tokens, p->budget);
-  const size_t parts = l.split.splits > 1 ? rows * l.split.splits : 0;
-  l.part_l = align_up(parts * sizeof(float));
+  l.split = chunk_attend_splits(p->dtype, p->head_dim, requests, heads, group, tokens, p->budget);
+  l.part_l = align_up((l.split.splits > 1 ? rows * l.split.splits : 0) * sizeof(float));
   l.part_o = 2 * l.part_l;
-  const size_t attend = l.part_o + align_up(parts * p->head_dim * sizeof(float));
-  l.mark = align_up(U * 4 * sizeof(int32_t));
-  l.row_splits = chunk_row_splits(p->dtype, p->units / heads, heads, group, tokens, p->budget);
-  l.sums = l.mark + align_up(U * B * sizeof(int32_t));
-  l.fresh = l.sums + align_up(l.row_splits * U * 2 * B * sizeof(float));
-  l.keys = l.fresh + align_up(l.row_splits * static_cast<size_t>(tokens) * heads * 2 * sizeof(float));
-  const size_t commit = l.keys + (p->budget > kMaxDecodeBudgetLds ? align_up(U * 2 * B * sizeof(uint32_t)) : 0);
-  l.total = std::max(attend, commit);
+  const size_t shares = chunk_most_shares(p->dtype, p->head_dim, requests, heads, group, tokens, p->budget);
+  const size_t attend = 2 * align_up(shares * sizeof(float)) + align_up(shares * p->head_dim * sizeof(float));
+  const auto commit = [&](int row_splits) {
+    l.row_splits = row_splits;
+    l.mark = align_up(U * 4 * sizeof(int32_t));
+    l.sums = l.mark + align_up(U * B * sizeof(int32_t));
+    l.fresh = l.sums + align_up(row_splits * U * 2 * B * sizeof(float));
+    l.keys = l.fresh + align_up(row_splits * static_cast<size_t>(tokens) * heads * 2 * sizeof(float));
+    return l.keys + (p->budget > kMaxDecodeBudgetLds ? align_up(U * 2 * B * sizeof(uint32_t)) : 0);
+  };
+  l.total = std::max(attend, commit(chunk_row_splits(p->dtype, requests, heads, group, tokens, p->budget, true)));
+  commit(chunk_row_splits(p->dtype, requests, heads, group, tokens, p->budget, false));
   return l;
 }
 // What the two calls of chunks have in common.

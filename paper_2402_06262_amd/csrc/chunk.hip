@@ -117,21 +117,32 @@ constexpr long long kMostTiles = 4096;
 // tokens of 4 requests, 16 heads, over 300 keys 13 and 26; 64 of 16, 8 heads, over 1000 36 and 32.
 // Splits: those with the shortest time, of a compute unit's workgroups one after the other, or of one that has four waves alone half as long again for each
 // further one; a workgroup being as long as its waves' tiles of 32 keys and, for its start, its share of the outputs and the joining, eight more (at 128 dimensions).
-ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B) {
-  const char* const asked = getenv("ROCO_CHUNK_SPLITS");
-  const int splits = asked != nullptr ? std::min(atoi(asked), kMostChunkSplits) : 0;
-  ChunkSplits c;
-  const long long rows = static_cast<long long>(tokens) * group, keys = (static_cast<long long>(B) + tokens + 31) / 32;
+static int chunk_row_tile(int dtype, int head_dim, int requests, int heads, long long rows, long long keys) {
   const char* const rows_asked = getenv("ROCO_CHUNK_ROWS");
   const int asked_tile = rows_asked != nullptr ? atoi(rows_asked) : 0;
   const bool can_pair = dtype == kBF16 && head_dim == 128;
-  c.row_tile = rows <= (dtype == kF32 ? 256ll : head_dim == 128 ? 32ll : 8ll) * requests || rows * heads * keys <= 160000 ? 32 : can_pair && rows >= 1024ll * requests ? 256 : 128;
-  if (asked_tile == 32 || asked_tile == 128 || (asked_tile == 256 && can_pair)) c.row_tile = asked_tile;
+  if (asked_tile == 32 || asked_tile == 128 || (asked_tile == 256 && can_pair)) return asked_tile;
+  return rows <= (dtype == kF32 ? 256ll : head_dim == 128 ? 32ll : 8ll) * requests || rows * heads * keys <= 160000 ? 32 : can_pair && rows >= 1024ll * requests ? 256 : 128;
+}
+static int chunk_splits_asked() {
+  const char* const asked = getenv("ROCO_CHUNK_SPLITS");
+  return asked != nullptr ? std::min(atoi(asked), kMostChunkSplits) : 0;
+}
+static long long chunk_key_tiles(int tokens, int B) { return (static_cast<long long>(B) + tokens + 31) / 32; }
+// Splits that `keys` tiles of them have work for.
+static long long chunk_most_splits(int dtype, int row_tile, long long keys) {
+  const int least_keys = chunk_least_keys(dtype, row_tile);
+  return std::min<long long>(kMostChunkSplits, (keys * 32 + (row_tile == 32 ? least_keys - 1 : 0)) / least_keys);
+}
+ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B) {
+  const int splits = chunk_splits_asked();
+  ChunkSplits c;
+  const long long rows = static_cast<long long>(tokens) * group, keys = chunk_key_tiles(tokens, B);
+  c.row_tile = chunk_row_tile(dtype, head_dim, requests, heads, rows, keys);
   const bool pair = c.row_tile == 256, few = c.row_tile == 32;
   c.row_tiles = tiles_of(requests, tokens, group, c.row_tile);
   const long long tiles = static_cast<long long>(c.row_tiles) * heads, full = pair ? rows / 256 * heads : tiles;
-  const int least_keys = chunk_least_keys(dtype, c.row_tile);
-  const int most = static_cast<int>(std::max(1ll, std::min({static_cast<long long>(kMostChunkSplits), (keys * 32 + (few ? least_keys - 1 : 0)) / least_keys, kMostTiles / tiles})));
+  const int most = static_cast<int>(std::max(1ll, std::min(chunk_most_splits(dtype, c.row_tile, keys), kMostTiles / tiles)));
   const bool alone = pair || (few ? dtype == kF32 && head_dim == 128 : dtype == kF32);  // on its compute unit
   c.splits = 1;
   long long least = -1;
@@ -151,12 +162,26 @@ ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads
   return c;
 }
 
+// A call with more tokens has more row tiles and so, often, fewer splits, and a smaller share of a workspace.  What it asks for is what every call with fewer may
+// want: no more splits than there are keys for; and where tiles of R rows have more than one split, tiles times splits are kMostTiles at most, R kMostTiles rows.
+long long chunk_most_shares(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B) {
+  const long long rows = static_cast<long long>(tokens) * group, keys = chunk_key_tiles(tokens, B);
+  const int asked = chunk_splits_asked(), largest = chunk_row_tile(dtype, head_dim, requests, heads, rows, keys);
+  if (asked >= 1) return asked > 1 ? rows * heads * asked : 0;
+  long long most = 0;
+  for (int row_tile : {32, 128, 256}) {
+    const long long splits = chunk_most_splits(dtype, row_tile, keys);
+    if (row_tile <= largest && splits > 1) most = std::max(most, std::min(rows * heads * splits, row_tile * kMostTiles));
+  }
+  return most;
+}
+
 // Until there are 2048 workgroups, four rounds of them, while a chunk has four tiles of rows for each.
-int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B) {
+int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B, bool or_fewer) {
   const char* const asked = getenv("ROCO_CHUNK_ROW_SPLITS");
   const int splits = asked != nullptr ? std::min(atoi(asked), kMostRowSplits) : 0;
   const int keys = column_keys(dtype);
-  const long long blocks = (static_cast<long long>(requests) * ((B + keys - 1) / keys) + tiles_of(requests, tokens, 1, keys)) * heads;
+  const long long blocks = (static_cast<long long>(requests) * ((B + keys - 1) / keys) + tiles_of(requests, or_fewer ? 0 : tokens, 1, keys)) * heads;
   if (splits >= 1) return static_cast<int>(std::max(1ll, std::min<long long>(splits, (kMostWorkgroups - 16ll - static_cast<long long>(requests) * heads) / blocks)));
   const long long most = tokens / column_tokens(group) / RowShares::kLeastTiles;
   return static_cast<int>(std::max(1ll, std::min({2048 / blocks, most, static_cast<long long>(kMostRowSplits)})));

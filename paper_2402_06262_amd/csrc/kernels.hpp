@@ -267,7 +267,10 @@ struct ChunkArgs {
 __host__ __device__ constexpr int chunk_least_keys(int dtype, int row_tile) { return row_tile == 32 ? 128 : dtype != 1 ? 32 : row_tile == 256 ? 128 : 64; }
 struct ChunkSplits { int row_tile, row_tiles, splits, equal_shares; };
 ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
-int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B);
+// Rows times splits, where there is more than one, of no call with as many tokens or fewer above this.
+long long chunk_most_shares(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B);
+// or_fewer: the most of all calls with as many tokens or fewer.
+int chunk_row_splits(int dtype, int requests, int heads, int group, int tokens, int B, bool or_fewer);
 hipError_t launch_chunk_attend(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);
 hipError_t launch_chunk_commit(int dtype, int head_dim, const ChunkArgs& a, hipStream_t s);
 constexpr int kMostChunkSplits = 64, kMostRowSplits = 16;

@@ -104,6 +104,20 @@ def test_workspaces_follow_the_choice_of_shares(monkeypatch):
     assert sizes[0] < sizes[1] <= sizes[2]
 
 
+@pytest.mark.parametrize("env", [{}, {"ROCO_CHUNK_SPLITS": "7"}, {"ROCO_CHUNK_SPLITS": "1"}, {"ROCO_CHUNK_ROWS": "32"}, {"ROCO_CHUNK_ROWS": "128"}, {"ROCO_CHUNK_ROWS": "256"},
+                                 {"ROCO_CHUNK_ROW_SPLITS": "5"}], ids=str)
+@pytest.mark.parametrize("requests,heads,group,B,d,dtype", [
+    (4, 8, 4, 4096, 128, roco.ROCO_BF16), (32, 8, 4, 2048, 128, roco.ROCO_BF16), (1, 8, 8, 20000, 64, roco.ROCO_BF16), (5, 5, 3, 1501, 128, roco.ROCO_F32),
+    (2, 4, 2, 256, 128, roco.ROCO_BF16), (1, 1, 1, 7, 64, roco.ROCO_F32), (40, 1, 64, 300, 64, roco.ROCO_F32)])
+def test_a_workspace_for_more_tokens_holds_fewer(env, requests, heads, group, B, d, dtype, monkeypatch):
+    """One allocation, for the largest step, serves every smaller one of the same caches: what a call asks for does not fall as its tokens rise."""
+    for name, value in env.items():
+        monkeypatch.setenv(name, value)
+    p = roco.RocoParams(requests * heads, d, B, 1, dtype)
+    sizes = [roco.chunk_workspace_bytes(p, heads, group, t) for t in [*range(1, 1200), *range(1200, 20000, 171), 1 << 17, 1 << 20]]
+    assert sizes[0] > 0 and all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
 def _verify(dtype=roco.ROCO_F32, requests=3, nodes=8, vocab=1000, p=OK, p_strides=(8000, 1000), q=OK, q_strides=(8000, 1000), ptrs=None, optional=(OK, OK), max_path=8,
             workspace=OK, ws=None):
     t = [OK] * 6 if ptrs is None else ptrs

@@ -658,6 +658,21 @@ def test_a_graph_of_one_size_for_steps_of_many(dtype, d, group):
             setattr(t, n, mine[n])
 
 
+@pytest.mark.parametrize("dtype,d,heads,group", [("bf16", 128, 4, 2), ("f32", 64, 4, 3)])
+def test_the_largest_steps_workspace_serves_the_smaller_ones(dtype, d, heads, group):
+    """Steps of many sizes over caches of one shape, in the workspace that the largest asks for; what lies behind it stays."""
+    shapes = [([256, 100], [512, 0]), ([200, 256], [250, 50]), ([256, 256], [150, 1]), ([3, 250], [90, 10]), ([256, 17], [1, 1])]
+    steps = [Step(i + d, dtype, d, used, tokens, heads=heads, group=group, B=256).upload() for i, (used, tokens) in enumerate(shapes)]
+    size = roco.chunk_workspace_bytes(steps[0].p, heads, group, steps[0].total)
+    ws = torch.full((size + 4096,), 0xEE, dtype=torch.uint8, device="cuda")
+    for s in steps:
+        out, lse = s.attend(workspace=ws, workspace_bytes=size)
+        s.check_attend(out, lse, f"{s.tokens}", units=[0, heads])
+        s.commit(lse.astype(np.float32), workspace=ws, workspace_bytes=size)
+        s.check_commit(lse.astype(np.float32), f"{s.tokens}")
+        assert (ws[size:] == 0xEE).all()
+
+
 def test_streams_with_workspaces_of_their_own():
     steps, streams = _shapes(), [torch.cuda.Stream() for _ in range(3)]
     wants = [[x.copy() for x in s.attend()] for s in steps]
