@@ -135,7 +135,8 @@ inline int column_tokens(int group) {
 }
 // Up to this budget a unit's slots are chosen by a workgroup of 256 threads beside those of the sums, not by one of 1024 before them (8 heads of 4 queries, 128
 // dimensions, chunks of 16: 64 units of 1024 slots 26 -> 19 us, of 4096 43 -> 35; 8 units of 2048 25 -> 21, of 4096 25 -> 26).
-inline bool chosen_beside(int B) { return B <= 4096; }
+constexpr int kMostChosenBeside = 4096;
+inline bool chosen_beside(int B) { return B <= kMostChosenBeside; }
 // Tiles of rows, shared by the workgroups of a block of keys.
 struct RowShares {
   int tiles, per, used;

@@ -293,7 +293,9 @@ template <int DT, int HD, int P> hipError_t launch_columns_form(const ChunkArgs&
   const int tokens = column_tokens(a.group), stages = std::min(F::kStages, (a.tokens + tokens - 1) / tokens);
   const int lds = std::max(stages * F::kTileBytes, choosers > 0 ? (kChoiceWords<kThreads> + 2 * a.B) * 4 : 0);
   const void* const fn = reinterpret_cast<const void*>(chunk_columns<DT, HD, P>);
-  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return hipErrorInvalidValue;
+  // (the most that any call asks for: another thread's smaller call could lower a limit of this one's own before the launch)
+  constexpr int kMostLds = std::max(F::kStages * F::kTileBytes, (kChoiceWords<kThreads> + 2 * kMostChosenBeside) * 4);
+  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds) != hipSuccess) return hipErrorInvalidValue;
   const int cache_blocks = (a.B + F::kKeys - 1) / F::kKeys, fresh_blocks = tiles_of(a.requests, a.tokens, 1, F::kKeys);
   const int total = (cache_blocks * a.row_splits * a.units + 7) / 8 + (fresh_blocks * a.row_splits * a.heads + 7) / 8;
   hipLaunchKernelGGL((chunk_columns<DT, HD, P>), dim3(static_cast<unsigned>(total) * 8 + choosers), dim3(kThreads), lds, s, a, choosers, cache_blocks, fresh_blocks, stages);

@@ -687,6 +687,49 @@ def test_streams_with_workspaces_of_their_own():
         assert np.array_equal(want[0], s.out.float().cpu().numpy()) and np.array_equal(want[1], s.lse.cpu().numpy())
 
 
+def test_two_threads_with_steps_of_their_own():
+    """Host threads that call at the same time, one with a token (few bytes of LDS), one with chunks (the most that its kernel takes), each on a stream of its own:
+    the bits of the same steps one after the other."""
+    import threading
+    steps = [Step(60, "f32", 128, [300, 20], [1, 1], group=2, B=310).upload(), Step(61, "f32", 128, [300, 290], [250, 64], group=2, B=310).upload(),
+             Step(62, "bf16", 64, [40], [1], B=64).upload(), Step(63, "bf16", 64, [200, 100], [130, 200], B=250).upload()]
+    streams = [torch.cuda.Stream() for _ in steps]
+    state = lambda s: [s.dK, s.dV, s.dstats, s.dpos, s.dn_used, s.out, s.lse]  # noqa: E731
+    starts, wants, problems = [[x.clone() for x in state(s)] for s in steps], [], []
+    rounds = 25
+
+    def run(s, start, stream, check):
+        with torch.cuda.stream(stream):
+            for _ in range(rounds if check else 1):
+                for x, y in zip(state(s), start):
+                    x.copy_(y)
+                _step_of(s)
+                if check is not None:
+                    same = [torch.equal(x, y) for x, y in zip(state(s), check)]
+                    if not all(same):
+                        problems.append((s.tokens, same))
+            stream.synchronize()
+
+    torch.cuda.synchronize()
+    for s, start, stream in zip(steps, starts, streams):
+        run(s, start, stream, None)
+        wants.append([x.clone() for x in state(s)])
+    torch.cuda.synchronize()
+
+    def thread(i):
+        try:
+            run(steps[i], starts[i], streams[i], wants[i])
+        except Exception as e:  # noqa: BLE001
+            problems.append((steps[i].tokens, e))
+
+    threads = [threading.Thread(target=thread, args=(i,)) for i in range(len(steps))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not problems
+
+
 # ---------------------------------------------------------------------------------------------------- together, and beside what there was
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("T,group,page,window", [(1, 1, 0, 0), (17, 4, 16, 0), (64, 2, 64, 30)])
