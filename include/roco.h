@@ -607,7 +607,8 @@ int roco_probe_mfma(int32_t workgroups, int32_t iters, int32_t operands, float* 
  *                              same value
  *   ROCO_CHUNK_SPLITS=1..64    workgroups along the keys of a row tile of roco_chunk_attend (default: those with the shortest estimated time);
  *                              part of roco_chunk_workspace_bytes: set it before asking
- *   ROCO_CHUNK_ROWS=32|128|256  rows of a tile of roco_chunk_attend (default: by the number of rows and keys; 256 only of bf16 with 128 dimensions);
+ *   ROCO_CHUNK_ROWS=32|128|256  rows of a tile of roco_chunk_attend (default: by the number of rows and keys; 256 only of bf16 with 128 dimensions, 32 only
+ *                              while a launch has workgroups for them);
  *                              part of roco_chunk_workspace_bytes: set it before asking
  *   ROCO_CHUNK_ROW_SPLITS=1..16  workgroups along the rows of a chunk in the sums of roco_chunk_commit (default: until there are about 2048,
  *                              with four tiles of 64 rows each); part of roco_chunk_workspace_bytes: set it before asking

@@ -143,7 +143,7 @@ int check_chunk_shape(const roco_params* p, int32_t heads, int32_t group, int32_
   // (workgroups: of the attention's row tiles, of the sums' keys, of the slots)
   const long long requests = p->units / heads, tiles = (static_cast<long long>(tokens) * group / 128 + requests) * heads;
   const long long slots = static_cast<long long>(p->units) * ((p->budget + 127) / 128 + 1) + (tokens / 128 + requests) * heads + 16;
-  return tiles < kMostWorkgroups && slots < kMostWorkgroups ? ROCO_OK : ROCO_EUNSUPPORTED;
+  return tiles <= kMostWorkgroups - 8 && slots < kMostWorkgroups ? ROCO_OK : ROCO_EUNSUPPORTED;
 }
 // A token's rows, `count` of them, lie side by side; the tokens `stride` elements apart.
 int check_stride(const roco_params* p, int64_t stride, long long count) {

@@ -117,11 +117,13 @@ constexpr long long kMostTiles = 4096;
 // tokens of 4 requests, 16 heads, over 300 keys 13 and 26; 64 of 16, 8 heads, over 1000 36 and 32.
 // Splits: those with the shortest time, of a compute unit's workgroups one after the other, or of one that has four waves alone half as long again for each
 // further one; a workgroup being as long as its waves' tiles of 32 keys and, for its start, its share of the outputs and the joining, eight more (at 128 dimensions).
-static int chunk_row_tile(int dtype, int head_dim, int requests, int heads, long long rows, long long keys) {
+static int chunk_row_tile(int dtype, int head_dim, int requests, int heads, int group, int tokens, long long keys) {
   const char* const rows_asked = getenv("ROCO_CHUNK_ROWS");
   const int asked_tile = rows_asked != nullptr ? atoi(rows_asked) : 0;
   const bool can_pair = dtype == kBF16 && head_dim == 128;
-  if (asked_tile == 32 || asked_tile == 128 || (asked_tile == 256 && can_pair)) return asked_tile;
+  const bool can_few = static_cast<long long>(tiles_of(requests, tokens, group, 32)) * heads <= kMostWorkgroups - 8;  // (as workgroups of a launch, whole eights)
+  if ((asked_tile == 32 && can_few) || asked_tile == 128 || (asked_tile == 256 && can_pair)) return asked_tile;
+  const long long rows = static_cast<long long>(tokens) * group;
   return rows <= (dtype == kF32 ? 256ll : head_dim == 128 ? 32ll : 8ll) * requests || rows * heads * keys <= 160000 ? 32 : can_pair && rows >= 1024ll * requests ? 256 : 128;
 }
 static int chunk_splits_asked() {
@@ -138,7 +140,7 @@ ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads
   const int splits = chunk_splits_asked();
   ChunkSplits c;
   const long long rows = static_cast<long long>(tokens) * group, keys = chunk_key_tiles(tokens, B);
-  c.row_tile = chunk_row_tile(dtype, head_dim, requests, heads, rows, keys);
+  c.row_tile = chunk_row_tile(dtype, head_dim, requests, heads, group, tokens, keys);
   const bool pair = c.row_tile == 256, few = c.row_tile == 32;
   c.row_tiles = tiles_of(requests, tokens, group, c.row_tile);
   const long long tiles = static_cast<long long>(c.row_tiles) * heads, full = pair ? rows / 256 * heads : tiles;
@@ -166,7 +168,7 @@ ChunkSplits chunk_attend_splits(int dtype, int head_dim, int requests, int heads
 // want: no more splits than there are keys for; and where tiles of R rows have more than one split, tiles times splits are kMostTiles at most, R kMostTiles rows.
 long long chunk_most_shares(int dtype, int head_dim, int requests, int heads, int group, int tokens, int B) {
   const long long rows = static_cast<long long>(tokens) * group, keys = chunk_key_tiles(tokens, B);
-  const int asked = chunk_splits_asked(), largest = chunk_row_tile(dtype, head_dim, requests, heads, rows, keys);
+  const int asked = chunk_splits_asked(), largest = chunk_row_tile(dtype, head_dim, requests, heads, group, tokens, keys);
   if (asked >= 1) return asked > 1 ? rows * heads * asked : 0;
   long long most = 0;
   for (int row_tile : {32, 128, 256}) {

@@ -118,6 +118,17 @@ def test_a_workspace_for_more_tokens_holds_fewer(env, requests, heads, group, B,
     assert sizes[0] > 0 and all(a <= b for a, b in zip(sizes, sizes[1:]))
 
 
+def test_small_tiles_are_not_asked_for_beyond_a_launch(monkeypatch):
+    """ROCO_CHUNK_ROWS=32 where as many tiles would be more workgroups than a launch has: the call takes the tiles that it takes by itself, to be seen by its workspace."""
+    p = roco.RocoParams(1, 128, 256, 1, roco.ROCO_BF16)
+    monkeypatch.setenv("ROCO_CHUNK_ROW_SPLITS", "1")
+    tokens = [1 << 22, (1 << 23) - 1, 1 << 23, 1 << 24]  # times 64 / 32
+    by_itself = [roco.chunk_workspace_bytes(p, 1, 64, t) for t in tokens]
+    monkeypatch.setenv("ROCO_CHUNK_ROWS", "32")
+    asked = [roco.chunk_workspace_bytes(p, 1, 64, t) for t in tokens]
+    assert asked[0] < by_itself[0] and asked[1:] == by_itself[1:]
+
+
 def _verify(dtype=roco.ROCO_F32, requests=3, nodes=8, vocab=1000, p=OK, p_strides=(8000, 1000), q=OK, q_strides=(8000, 1000), ptrs=None, optional=(OK, OK), max_path=8,
             workspace=OK, ws=None):
     t = [OK] * 6 if ptrs is None else ptrs
