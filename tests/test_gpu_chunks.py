@@ -439,6 +439,49 @@ def test_pages_outside_the_pool_are_not_seen(dtype, d, used, tokens, group):
     assert len(others) and torch.equal(s.dK[others].nan_to_num(7), K[others].nan_to_num(7))
 
 
+def check_sums(s, lse, what=""):
+    """What a chunk adds to Acc and Acc2 within the header's bound, with L of the unit's own rows and keys; and how far the same sums of probabilities that were
+    rounded to bf16 would be off, in units of it."""
+    stats, pos, used = s.dstats.cpu().numpy().astype(np.float64), s.dpos.cpu().numpy().astype(np.int64), s.dn_used.cpu().numpy()
+    K, seen_by_bound = s.dK.float().cpu().numpy(), 0.0
+    for u in range(s.U):
+        r, h = divmod(u, s.heads)
+        c, m, a = min(s.tokens[r], s.budgets[r]), used[u], s.start[r]
+        if c == 0:
+            continue
+        keys = (s.unpool(K, u, m) if s.page else K[u, :m]).astype(np.float64)
+        q = s.rows(u)[0][:c].astype(np.float64)
+        token = np.where(pos[u, :m] >= s.qpos0[r], pos[u, :m] - s.qpos0[r], -1)
+        at = s.qpos0[r] + np.arange(c)
+        away = at[:, None] - pos[u, :m]
+        x = np.einsum("cgd,md->cgm", q, keys) * s.sc + (s.bias * ((away >= 0) & (away < s.window)))[:, None]
+        p = np.exp(x - lse[a:a + c, h * s.group:(h + 1) * s.group].astype(np.float64)[..., None])
+        there = (token[None] <= np.arange(c)[:, None])[:, None]
+        L = float(np.einsum("cgd,md->cgm", np.abs(q), np.abs(keys)).max()) * s.sc
+        rel = 2 * (s.d + 8) * U * L + (8 + math.sqrt(c * s.group)) * U
+        exactly, rounded = ((np.where(there, v, 0.0).mean(1)) for v in (p, round_to_bf16(p.astype(np.float32)).astype(np.float64)))
+        base = np.where(token >= 0, 0.0, s.stats[u, :2, :m].astype(np.float64))
+        for plane, power in ((0, 1), (1, 2)):
+            more = (exactly ** power).sum(0)
+            want = base[plane] + more
+            tol = power * rel * more + U * want + 1e-30
+            err = np.abs(stats[u, plane, :m] - want)
+            assert (err <= tol).all(), f"{what} unit {u}: {('Acc', 'Acc2')[plane]}, worst {(err / tol).max():.3g} of the tolerance"
+            seen_by_bound = max(seen_by_bound, float((np.abs((rounded ** power).sum(0) - more) / tol).max()))
+    return seen_by_bound
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("used,tokens,group,B,page,window", [
+    ([300, 20], [1, 1], 1, 310, 0, 0), ([310, 64], [1, 3], 4, 310, 0, 0), ([300, 100, 0], [40, 70, 33], 3, 310, 16, 0), ([200, 310], [300, 200], 2, 310, 0, 40),
+    ([90, 33], [20, 9], 17, 100, 32, 0), ([40], [25], 64, 60, 0, 0)])
+def test_sums_within_what_the_roundings_allow(dtype, d, used, tokens, group, B, page, window):
+    s = Step(sum(used) + d + group, dtype, d, used, tokens, group=group, B=B, page=page, window=window, spare=(1, 2)).upload()
+    lse = s.exact_lse()
+    s.commit(lse)
+    assert check_sums(s, lse) > 1  # probabilities of bf16 would not pass (of 64 heads and 25 rows either, whose 1600 roundings fall to a fortieth of one)
+
+
 # ---------------------------------------------------------------------------------------------------- taking over: sizes and shares
 @pytest.mark.parametrize("row_splits", [1, 2, 5, 16])
 @pytest.mark.parametrize("dtype,d,group", [("bf16", 128, 4), ("bf16", 64, 1), ("f32", 128, 3), ("f32", 64, 40)])
