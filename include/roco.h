@@ -432,7 +432,8 @@ int roco_chunk_attend(const roco_params* params, int32_t heads, int32_t group, i
  * Takes the chunks over into the caches: roco_tree_commit for chunks.  Per unit with n = n_used slots, the request's budget B_r and c tokens (of more than
  * B_r the first B_r; 0: nothing of the request's units changes):
  *   E = max(0, n + c - B_r) tokens are evicted by the statistics as they stand, as in roco_encode_block (the chunk has still seen them); the chunk's
- *   tokens go, in order, to the ascending list of freed and still-empty slots, at positions qpos0 + i.
+ *   tokens go, in order, to the ascending list of freed and still-empty slots, at positions qpos0 + i.  (What a chunk has above B_r, its newest tokens, does not
+ *   come into the cache, and evicted_slot has -1 there as for a token that took an empty slot: feed chunks of B_r tokens or fewer.)
  *   pbar_i = mean over the group's heads of exp(x_ih - lse_ih) over the remaining older slots and the tokens 0 .. i: Acc += sum_i pbar_i, Acc2 += sum_i
  *   pbar_i^2, Count += 1 for every row that attended the slot; the chunk's tokens start from 0.  (The other importance scores keep their second plane as
  *   they do elsewhere.)

@@ -4,7 +4,9 @@
 // One pass over the keys with a running reference and sum.  Query rows, (token, head) pairs of a unit, lie in registers, 32 to a matrix tile; keys and values come
 // through a ring in LDS, filled by loads that go straight there, first the cache's, then the chunk's.  Scores = K . Q^T on the matrix cores, so that a
 // lane holds 16 keys of one query, and the outputs' products O^T = V^T . P^T take these registers as they are.  Probabilities of bf16 are rounded to bf16, their
-// sums are not: outputs 2.3e-3 of their norm off, of which their own rounding is 1.7e-3; a second number each would be half as many products again.
+// sums are not: outputs 2.3e-3 of their norm off, of which their own rounding is 1.7e-3.  A second number each would be half as many products again, which bound the tiles of many
+// rows; of few rows, which the memory should bound, it takes 2 to 12 % more: a token of 32 requests, 8 heads of 4 queries over 4096 keys, 128 dimensions, 100.4 and 102.7 us, of 8
+// heads over 2048, 64 dimensions, 34.8 and 39.5, of 64 requests over 1024, 128 dimensions, 23.3 and 26.2.
 #pragma once
 #include "chunk.hpp"
 #include "profile.hpp"

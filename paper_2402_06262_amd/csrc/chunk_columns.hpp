@@ -8,11 +8,12 @@
 // fetches it: the heads of a token, filled up to a power of two, lie in consecutive registers of one lane, and their mean is a sum of registers.
 // The scores of the next 32 rows are formed between the exponentials of these.  A chunk's rows are shared by up to 16 workgroups of a block of keys,
 // whose sums chunk_apply adds in their order.
-// Measured, with all of roco_chunk_commit: 4 requests of 512 tokens, 8 heads of 4 queries, 4096 slots, bf16, 128 dimensions, 108 us (the products would
-// take 33 at 2.1 PFLOP/s, the vector instructions 50), with one workgroup along the rows 125; 12 of up to 200, groups of 8, 2048 slots, 64 dimensions,
-// 61 us and 67.  With one path for all rows, of selects and of branches within, 154 and 102 us of the kernel alone, and the requests side by
-// side on a die, so that one had the longest.  A token of 32 requests, 8 heads, 2048 slots, fp32 / 128, 102 us (213 with the rows that a tile has not, 134 with room for three tiles), of 8 heads of
-// 4 queries over 4096 slots, bf16 / 128, 97 us and 105 (K alone, 268 MB of either, would take 52).
+// Measured, all of roco_chunk_commit and the copy that restores the state, passes on one state: 4 requests of 512 tokens, 8 heads of 4 queries, 4096 slots, bf16, 128
+// dimensions, 108 us (102 with states in turn; the products would take 60 at the 1.2 PFLOP/s of a large library product, the vector instructions 50), with one workgroup along
+// the rows 122; 12 of up to 200, groups of 8, 2048 slots, 64 dimensions, 60 us and 66.  With one path for all rows, of selects and of branches within, 154 and 102 us of the
+// kernel alone, and the requests side by side on a die, so that one had the longest.  A token of 32 requests, 8 heads, 2048 slots, fp32 / 128, 97 to 102 us (213 with the
+// rows that a tile has not, 134 with room for three tiles), of 8 heads of 4 queries over 4096 slots, bf16 / 128, 90 to 97 us and 105 (K alone, 268 MB of either, would take
+// 38 at the 7.0 TB/s that reads alone reach).
 #pragma once
 #include "chunk_choose.hpp"
 #include "profile.hpp"

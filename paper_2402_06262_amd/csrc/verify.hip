@@ -12,9 +12,9 @@
 //                   the nodes' probabilities, which lie in as many places.
 //   verify_choose : one workgroup per request.  The passes that are left (trees; one workgroup alone with a row), the accepted path, and the next
 //                   token: the block, and in it the token, where the sums pass a share `choose` of N.
-// Measured, fp32: 64 chains of 8 nodes over 100003 tokens 25 us (52 MB have to be read: 10 us), 32 trees of 32 nodes over 65536 54 us, in 7 rounds of 4 us and
-// less, waits for memory three times over; before the walks were left behind, 27 and 74 to 82.  Without q, 57 trees of 18 over 2727, five continuations each, 20 us (50 with every
-// element compared with every rejected token in a loop of its own).
+// Measured, fp32: 64 chains of 8 nodes over 100003 tokens 26 to 28 us (52 MB have to be read: 7 us at the 7.0 TB/s of reads alone), 32 trees of 32 nodes over
+// 65536 51 to 62 us, in 7 rounds of up to 7.5 us by trace, waits for memory three times over; before the walks were left behind, 27 and 74 to 82.  The same of bf16
+// 21 and 49.  Without q, 57 trees of 18 over 2727, five continuations each, 20 us (50 with every element compared with every rejected token in a loop of its own).
 // Sums are held in 64 bits: with 32 a token in some thousands would be another than the numbers say (2^17 borders, each 2^-24 off).
 #include <algorithm>
 
