@@ -601,6 +601,80 @@ def test_offsets_beyond_32_bits():
     assert (stats[u, 2, :n] == 10.0 + T).all() and stats[u, 2, n:n + T].tolist() == [3.0, 2.0, 1.0]
 
 
+@every_form
+@pytest.mark.parametrize("dtype,d,group", [("bf16", 128, 4), ("bf16", 64, 3), ("f32", 64, 2)])
+def test_rows_at_the_largest_distance(dtype, d, group):
+    """Tokens 2^24 bytes apart, the last of them behind 2^32; what lies between them is NaN."""
+    s = Step(d + group, dtype, d, [150, 20], [200, 65], heads=2, group=group, B=180).upload()
+    far = torch.full((s.total, (1 << 24) // s.dq.element_size()), math.nan, dtype=_DT[dtype], device="cuda")
+    assert (s.total - 1) * far.stride(0) * far.element_size() > 1 << 32
+    rows = far[:, 8:8 + 2 * (group + 2) * d].unflatten(1, (2 * (group + 2), d))
+    rows.copy_(torch.cat([s.dq, s.dk, s.dv], 1))
+    s.dq, s.dk, s.dv = rows[:, :2 * group], rows[:, 2 * group:2 * group + 2], rows[:, 2 * group + 2:]
+    s.check_attend(*s.attend())
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+
+
+@pytest.mark.parametrize("requests", [5000, 65535])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_as_many_requests_as_a_call_has(requests, dtype):
+    """One head each, up to four cached tokens and two new ones, against the same formulas side by side in 64 bits."""
+    d, B = 64, 6
+    rng = np.random.default_rng(requests)
+    used, tokens = rng.integers(0, 5, requests), rng.integers(0, 3, requests)
+    tokens[-1] = 2
+    start = np.concatenate([[0], np.cumsum(tokens)])
+    T = int(start[-1])
+    g = torch.Generator(device="cuda").manual_seed(requests)
+    randn = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(_DT[dtype])  # noqa: E731
+    K, V, q, k, v = randn(requests, B, d), randn(requests, B, d), randn(T, 1, d), randn(T, 1, d), randn(T, 1, d)
+    stats = torch.rand((requests, 3, B), generator=g, device="cuda") + 1.0
+    pos = dev(np.tile(np.arange(B), (requests, 1)))
+    p = roco.RocoParams(requests, d, B, 2, roco.ROCO_BF16 if dtype == "bf16" else roco.ROCO_F32)
+    n_used, dstart, qpos0 = dev(used), dev(start), dev(used + 10)
+    before = [x.clone() for x in (K, V, stats, pos)]
+    out, lse = torch.full((T, 1, d), 77.0, dtype=_DT[dtype], device="cuda"), torch.full((T, 1), 77.0, device="cuda")
+    ws = torch.empty(roco.chunk_workspace_bytes(p, 1, 1, T), dtype=torch.uint8, device="cuda")
+    roco.roco_chunk_attend(p, 1, 1, None, q, k, v, dstart, qpos0, K, V, pos, n_used, out, lse, ws)
+    roco.roco_chunk_commit(p, 1, 1, None, q, k, v, lse, dstart, qpos0, K, V, stats, pos, n_used, None, None, ws)
+    torch.cuda.synchronize()
+    of = torch.from_numpy(np.repeat(np.arange(requests), tokens)).cuda()           # request of a token, and which of its tokens it is
+    i = torch.arange(T, device="cuda") - torch.from_numpy(start).cuda()[of]
+    n = torch.from_numpy(used).cuda()[of]
+    first = torch.arange(T, device="cuda") - i
+    second = (first + 1).clamp(max=T - 1)
+    keys = torch.cat([before[0][of].double(), k[first].double(), k[second].double()], 1)     # six slots, the request's two tokens
+    values = torch.cat([before[1][of].double(), v[first].double(), v[second].double()], 1)
+    x = (q.double() * keys).sum(-1) / math.sqrt(d)
+    at = torch.arange(B + 2, device="cuda")
+    sees = torch.where(at < B, at < n[:, None], at - B <= i[:, None])
+    logit = float((q.double().abs() * keys.abs()).sum(-1).max()) / math.sqrt(d)
+    x = x.masked_fill(~sees, -math.inf)
+    want_lse = torch.logsumexp(x, 1)
+    prob = torch.exp(x - want_lse[:, None])
+    bound = (d + 8) * U * logit
+    rel = 2 * bound + (8 + 2 * math.sqrt(8)) * U + (0 if dtype == "f32" else 2.0 ** -8)
+    want, mass = (prob[..., None] * values).sum(1), (prob[..., None] * values.abs()).sum(1)
+    assert ((out[:, 0].double() - want).abs() <= rel * mass + (2.0 ** -8 if dtype == "bf16" else U) * want.abs()).all()
+    assert ((lse[:, 0].double() - want_lse).abs() <= bound + (8 + math.sqrt(8)) * U + 2.0 ** -22 * want_lse.abs()).all()
+    # nothing is evicted: slots used .. used + tokens - 1 take the tokens
+    assert n_used.tolist() == (used + tokens).tolist()
+    assert torch.equal(K[of, n + i], k[:, 0]) and torch.equal(V[of, n + i], v[:, 0]) and torch.equal(pos[of, n + i].long(), n + 10 + i)
+    prob = torch.exp(x - lse.double())
+    more = torch.zeros((requests, B + 2), dtype=torch.float64, device="cuda").index_add_(0, of, prob)
+    c = torch.from_numpy(tokens).cuda()
+    held = torch.arange(B, device="cuda") < torch.from_numpy(used).cuda()[:, None]
+    rel = 2 * bound + (8 + math.sqrt(2)) * U
+    wanted = before[2][:, 0].double() + torch.where(held, more[:, :B], 0.0)
+    new = (torch.arange(B, device="cuda") >= torch.from_numpy(used).cuda()[:, None]) & (torch.arange(B, device="cuda") < (torch.from_numpy(used).cuda() + c)[:, None])
+    assert ((stats[:, 0].double() - wanted).abs() <= rel * more[:, :B] + U * wanted)[~new].all()
+    token_sum = more[of, B + i]
+    assert ((stats[of, 0, n + i].double() - token_sum).abs() <= rel * token_sum).all()
+    assert torch.equal(stats[:, 2][~new], (before[2][:, 2] + torch.where(held, c[:, None], 0))[~new]) and torch.equal(stats[of, 2, n + i], (c[of] - i).float())
+
+
 # ---------------------------------------------------------------------------------------------------- streams, graphs, repetition
 def _step_of(s, ws=None):
     ws = s.ws if ws is None else ws
@@ -802,6 +876,51 @@ def test_a_chunk_is_a_drafted_chain(dtype, d, T, group, page, window):
     for i in (0, 1, 3, 4):
         assert torch.equal(mine[i].nan_to_num(7), state[i].nan_to_num(7))
     assert torch.equal(mine[2][:, 2], s.dstats[:, 2])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_a_compressed_prompt_then_chunks_then_decode_steps(dtype, d):
+    """On one dense cache: roco_prefill_compress, a chunk, roco_select_victims, roco_decode_step; the chunk and what the step evicts, appends and answers against
+    the oracle, from the state that the call before has left."""
+    heads, B, L, scope = 2, 96, 130, 12
+    s = Step(d, dtype, d, [B, B], [40, 3], heads=heads, B=B, scope=scope).upload()
+    rng = np.random.default_rng(d)
+    rnd = round_to_bf16 if dtype == "bf16" else (lambda x: x)
+    draw = lambda *shape: rnd(rng.standard_normal(shape).astype(np.float32))  # noqa: E731
+    next_slot = torch.full((s.U,), -1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(roco.prefill_workspace_bytes(s.p, L), roco.decode_workspace_bytes(s.p)), dtype=torch.uint8, device="cuda")
+    Q, K, V = (dev(draw(s.U, L, d), dtype) for _ in range(3))
+    s.dn_used.zero_()
+    roco.roco_prefill_compress(s.p, Q, K, V, dev(np.full(s.U, L)), L, s.dK, s.dV, s.dstats, s.dpos, s.dn_used, next_slot, None, ws)
+    torch.cuda.synchronize()
+    assert s.dn_used.tolist() == [B] * s.U
+
+    def read():
+        s.K, s.V, s.stats = s.dK.float().cpu().numpy(), s.dV.float().cpu().numpy(), s.dstats.cpu().numpy()
+        s.pos = s.dpos.cpu().numpy().astype(np.int64)
+
+    read()
+    s.qpos0 = np.array([L, L])
+    s.dqpos0 = dev(s.qpos0)
+    s.check_attend(*s.attend())
+    lse = s.exact_lse()
+    s.commit(lse)
+    s.check_commit(lse)
+    read()
+    roco.roco_select_victims(s.p, s.dstats, s.dpos, s.dn_used, next_slot, ws)
+    q, k, v, at = draw(s.U, d), draw(s.U, d), draw(s.U, d), np.repeat([L + 40, L + 3], heads)
+    out, ev_slot, ev_pos = torch.empty((s.U, d), dtype=_DT[dtype], device="cuda"), *(torch.full((s.U,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    roco.roco_decode_step(s.p, dev(q, dtype), dev(k, dtype), dev(v, dtype), dev(at), s.dK, s.dV, s.dstats, s.dpos, s.dn_used, next_slot, out, ev_slot, ev_pos, ws)
+    torch.cuda.synchronize()
+    for u in range(s.U):
+        st = orc.CacheState(s.K[u].astype(np.float64), s.V[u].astype(np.float64), *s.stats[u].astype(np.float64), s.pos[u].copy(), B)
+        slot = int(trees.choose_evictions(st, 1, scope, None)[0])
+        assert int(ev_slot[u]) == slot and int(ev_pos[u]) == s.pos[u, slot] and int(s.dpos[u, slot]) == at[u]
+        keep = np.arange(B) != slot
+        w = trees.tree_attend(s.K[u, keep], s.V[u, keep], s.pos[u, keep], q[u][None, None], k[u][None], v[u][None], [-1], int(at[u]), s.sc)
+        rel = 2 * (d + 8) * U * w.logit + (8 + 2 * math.sqrt(B)) * U + (0 if dtype == "f32" else 2.0 ** -8)
+        err = np.abs(out[u].float().cpu().numpy() - w.out[0, 0])
+        assert (err <= rel * w.mass[0, 0] + (2.0 ** -8 if dtype == "bf16" else U) * np.abs(w.out[0, 0]) + 1e-30).all()
 
 
 def test_prompts_in_chunks_then_drafts():

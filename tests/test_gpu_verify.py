@@ -151,6 +151,20 @@ def test_many_requests():
     b.check(*b.run())
 
 
+def test_as_many_requests_as_a_call_has():
+    b = Batch(20, 65535, 2, 5, 1)
+    b.check(*b.run())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 3])
+def test_the_largest_vocabulary(dtype, pad):
+    """2^22 tokens, the borders' last ones among those that are chosen."""
+    b = Batch(21, 3, 2, 1 << 22, 1, dtype=dtype, pad=pad, apart=3.0)
+    b.choose[:] = [1.0 - 2.0 ** -24, 0.0, 0.5]
+    b.check(*b.run())
+
+
 def test_captured_and_replayed_with_other_inputs():
     """Graphs of two shapes that share a workspace; a pass leaves nothing for the next."""
     batches = [Batch(17, 5, 12, 9000, 3, "distinct"), Batch(18, 9, 5, 3000, 1)]
